@@ -20,7 +20,9 @@
  *                            term: segment token i sees prefix + i + 1 keys)
  * and, fused from them, sa_kv_assemble_append (splice + append, one launch),
  * sa_segment_prefill_attn_append (append + attention, one launch) and the
- * copy-free splice sa_kv_splice_alias.
+ * copy-free splice sa_kv_splice_alias.  Several branches of one context are kept
+ * by sa_kv_fork, sa_kv_retain, sa_kv_release and sa_kv_compact, written by
+ * sa_kv_append_rope and attended by sa_shared_prefix_attn.
  *
  * Data layout (all device memory is owned by the caller):
  *   bf16 values are IEEE bfloat16 bit patterns (uint16).
@@ -463,6 +465,173 @@ sa_status sa_segment_prefill_attn_append(sa_ctx *ctx, const sa_layout *layout, i
                                          const int32_t *h_q_len, const int32_t *h_kv_len,
                                          sa_pages pages, float softmax_scale, void *o, float *lse,
                                          void *stream);
+
+/* ------------------------------------------------ branches of one context
+ *
+ * Several lookahead streams, or sub-agents isolated on one context (paper
+ * Sec. 3.2, Sec. 3.5), keep branches of a cached context alive side by side.
+ * The calls below fork a context without copying its full pages, write the
+ * branches' rows, attend over them with the common part read once, and give
+ * the pages of ended branches back.  They use the calling thread's device only
+ * within the call.  Calls that plan on the host (sa_kv_append_rope, sa_kv_fork,
+ * sa_shared_prefix_attn) return SA_ERR_UNSUPPORTED on a stream that is being
+ * captured into a graph, since a replay would find another call's plan in the
+ * context; sa_kv_retain, sa_kv_release and sa_kv_compact can be captured once
+ * a call of the same pool size has run on the context (they allocate nothing
+ * then), and their replays count as calls on it.
+ *
+ * A pool whose slots are shared by several tables keeps one count per slot,
+ * d_ref: device int32 [num_slots], the number of table entries that name the
+ * slot, owned by the caller and zero for a slot that is not in use.
+ * A count that does not fit its tables (a fork that takes a fresh slot with a
+ * count, or shares a page without one; a release that finds a count at zero; a
+ * compacted table that names a slot not in use) is latched like a bad page and
+ * reported by sa_sync_check as SA_ERR_RANGE.
+ */
+
+/* Norms and rotation of a segment's new rows (sa_kv_append_rope). */
+typedef struct sa_rope {
+    int32_t rot_dim;          /* leading dims of each head that are rotated: a multiple
+                                 of 16 from 0 to head_dim                               */
+    int32_t interleaved;      /* 0: dims d and d + rot_dim/2 are a pair; else 2d and 2d+1 */
+    const double *h_inv_freq; /* host [rot_dim / 2]: radians per position of each pair,
+                                 0 to 1024                                              */
+    const void *q_weight;     /* device bf16 [head_dim]; NULL: query heads are not normed */
+    const void *k_weight;     /* the same for key heads                                 */
+    float eps;                /* of the norms, > 0                                       */
+    float weight_offset;      /* added to every weight (1 where weights are stored less 1) */
+} sa_rope;
+
+/*
+ * sa_kv_append_rope — sa_kv_append for rows straight out of a projection: the
+ * norm of each query and key head, the rotation of both by position, and the
+ * key and value rows into the cache, in one pass.
+ *
+ * Token t of sequence b has cache position h_start[b] + t, where its rows go
+ * as by sa_kv_append, and rotation position h_pos[b] + t (h_pos NULL: h_start;
+ * they differ where a splice renumbered the pages of a context whose keys keep
+ * their angles).  Each query head row x, and each key head row, becomes
+ *   y = x / sqrt(mean_d x_d^2 + eps) * (weight_d + weight_offset)   (with weights)
+ *   (y_i, y_j) = (y_i cos a - y_j sin a, y_j cos a + y_i sin a),  a = position * inv_freq
+ * for its pairs (i, j), computed in fp32 (the angle exactly, modulo a turn) and
+ * rounded once to bf16; dims from rot_dim on are not rotated.  Query rows go to
+ * q_out, bf16 [sum new_len][num_q_heads][128]; value rows are copied bit for bit.
+ * q, k_new and v_new hold the rows of all sequences back to back; token t's
+ * heads start at element t * q_stride (k_stride, v_stride), so the three may be
+ * slices of one projection's output.  Strides are in elements, multiples of 8.
+ * q_out may be q itself with q_stride = num_q_heads * 128, and must not overlap
+ * it otherwise.
+ *
+ * Errors: those of sa_kv_append; SA_ERR_SHAPE for a negative position, a stride
+ * too small, an inv_freq out of range or a bad eps, SA_ERR_UNSUPPORTED for a bad
+ * rot_dim or a capturing stream, SA_ERR_ALIGN for a stride that is not a
+ * multiple of 8.  A missing or out-of-range page is latched for sa_sync_check;
+ * its rows are not written, q_out is.
+ */
+sa_status sa_kv_append_rope(sa_ctx *ctx, const sa_layout *layout, int32_t layer, const sa_rope *rope,
+                            const void *q, int64_t q_stride, const void *k_new, int64_t k_stride,
+                            const void *v_new, int64_t v_stride, void *q_out, void *k_pool, void *v_pool,
+                            int32_t batch, const int32_t *h_start, const int32_t *h_new_len,
+                            const int32_t *h_pos, sa_pages pages, void *stream);
+
+/*
+ * sa_kv_fork — open children of cached contexts.
+ *
+ * Child c continues sequence b = h_parent[c] of `src`, which holds h_src_len[b]
+ * tokens, and has room for h_reserve[c] more: its table lists the parent's full
+ * pages (the same slots), and fresh slots for the rest of its
+ *   pages_c = ceil((h_src_len[b] + h_reserve[c]) / page_size)
+ * pages, taken from the front of d_fresh, child after child.  Where the
+ * parent's last page is partial its valid rows are copied, in every layer, to
+ * the child's first fresh slot (whose other rows stay as they are), so the
+ * child's appends never touch a shared page.  A sequence may have any number of
+ * children; its own table stays as it is.  The children's table is written to
+ * d_dst_indptr[num_children + 1] and d_dst_indices (capacity dst_capacity).
+ * d_ref (nullable): the count of every listed slot is raised by one per entry.
+ * *h_fresh_used receives the number of fresh slots taken.  Fresh slots must not
+ * repeat nor be pages of a source context (SA_DEBUG=1 checks).
+ *
+ * Errors: SA_ERR_SHAPE, SA_ERR_RANGE (a parent out of range), SA_ERR_NO_PAGES,
+ * SA_ERR_UNSUPPORTED (capture), SA_ERR_NULL, SA_ERR_ALIGN, SA_ERR_HIP.
+ */
+sa_status sa_kv_fork(sa_ctx *ctx, const sa_layout *layout, void *k_pool, void *v_pool, int32_t batch,
+                     const int32_t *h_src_len, int32_t num_children, const int32_t *h_parent,
+                     const int32_t *h_reserve, sa_pages src, const int32_t *d_fresh, int32_t num_fresh,
+                     int32_t *d_dst_indptr, int32_t *d_dst_indices, int32_t dst_capacity, int32_t *d_ref,
+                     int32_t *h_fresh_used, void *stream);
+
+/*
+ * sa_kv_retain — raise the count of every slot that the batch's tables name, by
+ * one per entry indptr[0] .. indptr[batch] - 1 (tables made by sa_kv_assemble
+ * or sa_kv_splice_alias, which keep no counts).  max_entries: entries that
+ * pages.indices holds; a table that runs beyond them is latched as an error and
+ * nothing is counted.  Errors: SA_ERR_SHAPE, SA_ERR_NULL, SA_ERR_HIP.
+ */
+sa_status sa_kv_retain(sa_ctx *ctx, const sa_layout *layout, int32_t batch, sa_pages pages,
+                       int64_t max_entries, int32_t *d_ref, void *stream);
+
+/*
+ * sa_kv_release — the batch's tables end: lower the count of every slot they
+ * name, by one per entry (never below zero), and list the slots whose count is
+ * then zero: d_free[0 .. *d_num_free) holds them in ascending order and the
+ * rest of d_free (num_slots entries) is -1.  d_free and d_num_free may both be
+ * NULL (counts only).  max_entries as in sa_kv_retain.
+ * Errors: SA_ERR_SHAPE, SA_ERR_NULL, SA_ERR_HIP.
+ */
+sa_status sa_kv_release(sa_ctx *ctx, const sa_layout *layout, int32_t batch, sa_pages pages,
+                        int64_t max_entries, int32_t *d_ref, int32_t *d_free, int32_t *d_num_free,
+                        void *stream);
+
+/*
+ * sa_kv_compact — vacate the slots from `limit` on, so that the pool can shrink
+ * or its tail serve something else: the pages in use (count > 0) in slots
+ * >= limit move, in ascending order, to the slots < limit that are not in use,
+ * in ascending order, in every layer of both pools.  Where there are more such
+ * pages than free slots the last ones stay.
+ *   d_moved[0], [1]   pages moved, pages left in slots >= limit
+ *   d_slot_map[s]     (num_slots entries) where slot s's page is now; -1 if
+ *                     slot s was not in use
+ *   d_ref_out         the counts after the move (may be d_ref)
+ *   d_indices_out     the num_entries table entries d_indices through the map
+ *                     (may be d_indices); an entry outside the pool stays as it
+ *                     is and is latched
+ * Moved pages stay in their old slots too, as bits nobody names.
+ * Errors: SA_ERR_RANGE (limit outside [0, num_slots]), SA_ERR_SHAPE,
+ * SA_ERR_NULL, SA_ERR_ALIGN, SA_ERR_HIP.
+ */
+sa_status sa_kv_compact(sa_ctx *ctx, const sa_layout *layout, void *k_pool, void *v_pool, int32_t limit,
+                        const int32_t *d_ref, int32_t *d_ref_out, const int32_t *d_indices,
+                        int32_t *d_indices_out, int64_t num_entries, int32_t *d_slot_map, int32_t *d_moved,
+                        void *stream);
+
+/*
+ * sa_shared_prefix_attn — sa_segment_prefill_attn for a batch whose sequences
+ * share prefixes, each read and multiplied once for all of its sequences.
+ *
+ * The members of group g are sequences h_group_indptr[g] .. h_group_indptr[g+1]-1;
+ * every sequence is in one group (group_indptr runs from 0 to batch; a group
+ * may have one member or none).  The caches of a group's members hold the same
+ * keys and values for their first h_shared_len[g] tokens (the same pages, as
+ * sa_kv_fork leaves them, or equal copies): whole 64-key tiles of them are read
+ * through the page list of the group's first member that has query rows.  The
+ * result is that of sa_segment_prefill_attn over the same tables, held to the
+ * same tolerance.  shared_len may be anything from 0 to the smallest
+ * h_kv_len - h_q_len of the group.  Where the members' rows fill the kernel's
+ * row tiles anyway (long segments) the group is computed member by member.  The
+ * softmax scale is always applied exactly; the kernel variants and the block
+ * clock do not apply to this call, sa_set_kernel_events times its first kernel
+ * (SA_TIMED_ATTN), and its partial results (66 KB per key-range part) take the
+ * place of the split-KV partials that sa_reserve sizes.
+ *
+ * Errors: those of sa_segment_prefill_attn, SA_ERR_SHAPE for bad groups or
+ * shared lengths, SA_ERR_UNSUPPORTED for a capturing stream.
+ */
+sa_status sa_shared_prefix_attn(sa_ctx *ctx, const sa_layout *layout, int32_t layer, const void *q,
+                                const void *k_pool, const void *v_pool, int32_t batch,
+                                const int32_t *h_q_len, const int32_t *h_kv_len, sa_pages pages,
+                                int32_t num_groups, const int32_t *h_group_indptr,
+                                const int32_t *h_shared_len, float softmax_scale, void *o, float *lse,
+                                void *stream);
 
 #ifdef __cplusplus
 }

@@ -17,7 +17,8 @@ __all__ = [
     "sa_kv_append", "sa_kv_assemble", "sa_kv_assemble_append", "sa_kv_splice_alias",
     "sa_segment_prefill_attn", "sa_segment_prefill_attn_append", "sa_set_exact_scale", "sa_set_fused_append",
     "sa_set_kernel_events", "sa_set_block_clock", "sa_set_xcd_weights", "sa_sync_check", "sa_reserve",
-    "sa_segment_prefill_attn_noalloc", "sa_attn_plan_stats", "EXPORTED_SYMBOLS",
+    "sa_segment_prefill_attn_noalloc", "sa_attn_plan_stats", "Rope", "sa_kv_append_rope", "sa_kv_fork",
+    "sa_kv_retain", "sa_kv_release", "sa_kv_compact", "sa_shared_prefix_attn", "EXPORTED_SYMBOLS",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -29,7 +30,8 @@ EXPORTED_SYMBOLS = ("sa_create", "sa_destroy", "sa_status_string", "sa_last_erro
                     "sa_kv_splice_alias", "sa_segment_prefill_attn", "sa_segment_prefill_attn_append",
                     "sa_set_exact_scale", "sa_set_fused_append", "sa_set_kernel_events",
                     "sa_set_block_clock", "sa_set_xcd_weights", "sa_reserve",
-                    "sa_segment_prefill_attn_noalloc", "sa_attn_plan_stats")
+                    "sa_segment_prefill_attn_noalloc", "sa_attn_plan_stats", "sa_kv_append_rope",
+                    "sa_kv_fork", "sa_kv_retain", "sa_kv_release", "sa_kv_compact", "sa_shared_prefix_attn")
 
 STATUS = {0: "SA_OK", 1: "SA_ERR_NULL", 2: "SA_ERR_SHAPE", 3: "SA_ERR_UNSUPPORTED",
           4: "SA_ERR_ALIGN", 5: "SA_ERR_RANGE", 6: "SA_ERR_NO_PAGES", 7: "SA_ERR_HIP",
@@ -51,6 +53,12 @@ class Layout(ctypes.Structure):
 
 class _Pages(ctypes.Structure):
     _fields_ = [("indptr", ctypes.c_void_p), ("indices", ctypes.c_void_p)]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("h_inv_freq", ctypes.c_void_p),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("weight_offset", ctypes.c_float)]
 
 
 def library_path() -> str:
@@ -93,11 +101,19 @@ def load_library():
     lib.sa_reserve.argtypes = [P, I64, I64]
     lib.sa_segment_prefill_attn_noalloc.argtypes = lib.sa_segment_prefill_attn.argtypes
     lib.sa_attn_plan_stats.argtypes = [LP, I32, P, P, I32, P]
+    lib.sa_kv_append_rope.argtypes = [P, LP, I32, ctypes.POINTER(_Rope), P, I64, P, I64, P, I64, P, P, P, I32, P, P,
+                                      P, _Pages, P]
+    lib.sa_kv_fork.argtypes = [P, LP, P, P, I32, P, I32, P, P, _Pages, P, I32, P, P, I32, P, P, P]
+    lib.sa_kv_retain.argtypes = [P, LP, I32, _Pages, I64, P, P]
+    lib.sa_kv_release.argtypes = [P, LP, I32, _Pages, I64, P, P, P, P]
+    lib.sa_kv_compact.argtypes = [P, LP, P, P, I32, P, P, P, P, I64, P, P, P]
+    lib.sa_shared_prefix_attn.argtypes = [P, LP, I32, P, P, P, I32, P, P, _Pages, I32, P, P, ctypes.c_float, P, P, P]
     for name in ("sa_create", "sa_sync_check", "sa_kv_append", "sa_kv_assemble", "sa_kv_assemble_append",
                  "sa_kv_splice_alias", "sa_segment_prefill_attn", "sa_segment_prefill_attn_append",
                  "sa_set_exact_scale", "sa_set_fused_append", "sa_set_kernel_events", "sa_set_block_clock",
                  "sa_set_xcd_weights",
-                 "sa_reserve", "sa_segment_prefill_attn_noalloc", "sa_attn_plan_stats"):
+                 "sa_reserve", "sa_segment_prefill_attn_noalloc", "sa_attn_plan_stats", "sa_kv_append_rope",
+                 "sa_kv_fork", "sa_kv_retain", "sa_kv_release", "sa_kv_compact", "sa_shared_prefix_attn"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -455,3 +471,161 @@ def sa_segment_prefill_attn_append(ctx, layout: Layout, layer: int, q, k_pool, v
         _dev(v_pool, "v_pool", "b16", n), _dev(k_new, "k_new", "b16", rows, nullable=T == 0),
         _dev(v_new, "v_new", "b16", rows, nullable=T == 0), int(len(q_len)), _ptr(q_len), _ptr(kv_len),
         _pages(pages_indptr, pages_indices, len(q_len)), float(softmax_scale), op, lp, _stream(stream)))
+
+
+# ---------------------------------------------------------------- branches of one context
+
+def _same_device(ctx, *tensors):
+    """The branch calls run on ctx's device: a tensor elsewhere is refused rather than read there."""
+    if isinstance(ctx, Context):
+        for t in tensors:
+            if t is not None and hasattr(t, "device") and t.is_cuda and t.device.index != ctx.device:
+                raise ValueError(f"a tensor is on {t.device}, the context on device {ctx.device}")
+
+
+def _stream_of(ctx, stream):
+    """`stream`, or torch's current stream of ctx's device (not of the current device)."""
+    if stream is None and isinstance(ctx, Context):
+        torch = _torch or _load_torch()
+        if _raw_stream is not None:
+            return _raw_stream(ctx.device)
+        return torch.cuda.current_stream(ctx.device).cuda_stream
+    return _stream(stream)
+
+
+def _head_rows(t, what: str, tokens: int, heads: int, d: int):
+    """(address, token stride in elements) of a [tokens][heads][d] tensor whose heads are contiguous within a token."""
+    if tokens == 0:
+        return (None if t is None else t.data_ptr() or None), heads * d
+    torch = _torch or _load_torch()
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{what}: a device tensor is required")
+    if not t.is_cuda:
+        raise ValueError(f"{what}: tensor is not on a GPU")
+    if t.dtype not in _KINDS["b16"]:
+        raise ValueError(f"{what}: dtype {t.dtype}, expected a 2-byte dtype (bf16 bits)")
+    if t.dim() != 3 or t.shape[0] < tokens or t.shape[1] != heads or t.shape[2] != d:
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected ({tokens}, {heads}, {d})")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{what}: the heads of a token must be contiguous")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * d
+
+
+class Rope:
+    """Norms and rotation of sa_kv_append_rope (sa_rope): inv_freq, radians per position of each pair of dims
+    (float64, its length sets rot_dim); q_weight, k_weight, bf16 norm weights of one head (None: no norm)."""
+
+    def __init__(self, inv_freq=(), q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
+                 weight_offset: float = 0.0):
+        self.inv_freq = np.ascontiguousarray(inv_freq, dtype=np.float64).reshape(-1)
+        self.q_weight, self.k_weight = q_weight, k_weight
+        self.eps, self.interleaved, self.weight_offset = float(eps), bool(interleaved), float(weight_offset)
+
+    def _struct(self, d: int):
+        return _Rope(2 * len(self.inv_freq), int(self.interleaved), self.inv_freq.ctypes.data if len(self.inv_freq) else None,
+                     _dev(self.q_weight, "q_weight", "b16", d, nullable=True),
+                     _dev(self.k_weight, "k_weight", "b16", d, nullable=True), self.eps, self.weight_offset)
+
+
+def sa_kv_append_rope(ctx, layout: Layout, layer: int, rope: Rope, q, k_new, v_new, q_out, k_pool, v_pool, start,
+                      new_len, pages_indptr, pages_indices, pos=None, stream=None):
+    """Norms and rotates the query and key heads of new tokens; query rows go to q_out, key and value rows into
+    their pages.  q, k_new, v_new: [tokens][heads][128], possibly slices of one projection's output.  pos: rotation
+    position of each sequence's first new token (None: start)."""
+    start, new_len = _host_i32(start), _host_i32(new_len)
+    pos = None if pos is None else _host_i32(pos)
+    if start.shape != new_len.shape or (pos is not None and pos.shape != start.shape):
+        raise ValueError("start, new_len and pos differ in length")
+    B, T, D = len(new_len), max(0, _total(new_len)), int(layout.head_dim)
+    Hq, Hkv = int(layout.num_q_heads), int(layout.num_kv_heads)
+    _same_device(ctx, q, k_new, v_new, q_out, k_pool, v_pool, rope.q_weight, rope.k_weight, pages_indptr, pages_indices)
+    qp, qs = _head_rows(q, "q", T, Hq, D)
+    kp, ks = _head_rows(k_new, "k_new", T, Hkv, D)
+    vp, vs = _head_rows(v_new, "v_new", T, Hkv, D)
+    n = _pool_numel(layout)
+    r = rope._struct(D)
+    _check(load_library().sa_kv_append_rope(
+        _ctx_handle(ctx), ctypes.byref(layout), int(layer), ctypes.byref(r), qp, qs, kp, ks, vp, vs,
+        _dev(q_out, "q_out", "b16", T * Hq * D, nullable=T == 0), _dev(k_pool, "k_pool", "b16", n),
+        _dev(v_pool, "v_pool", "b16", n), int(B), _ptr(start), _ptr(new_len), _ptr(pos),
+        _pages(pages_indptr, pages_indices, B), _stream_of(ctx, stream)))
+
+
+def sa_kv_fork(ctx, layout: Layout, k_pool, v_pool, src_len, parent, reserve, src_indptr, src_indices, fresh,
+               dst_indptr, dst_indices, ref=None, stream=None) -> int:
+    """Opens children of cached contexts: shared full pages, a copy of the partial one, fresh pages for reserve.
+    parent: the sequence each child continues.  Returns the number of fresh slots taken."""
+    src_len, parent, reserve = _host_i32(src_len), _host_i32(parent), _host_i32(reserve)
+    if parent.shape != reserve.shape:
+        raise ValueError("parent and reserve differ in length")
+    B, C, n = len(src_len), len(parent), _pool_numel(layout)
+    _same_device(ctx, k_pool, v_pool, src_indptr, src_indices, fresh, dst_indptr, dst_indices, ref)
+    used = np.zeros(1, dtype=np.int32)
+    _check(load_library().sa_kv_fork(
+        _ctx_handle(ctx), ctypes.byref(layout), _dev(k_pool, "k_pool", "b16", n), _dev(v_pool, "v_pool", "b16", n),
+        int(B), _ptr(src_len), int(C), _ptr(parent), _ptr(reserve),
+        _Pages(_dev(src_indptr, "src indptr", "i32", B + 1), _dev(src_indices, "src indices", "i32", 0, nullable=True)),
+        _dev(fresh, "fresh", "i32", 0, nullable=True), 0 if fresh is None else int(fresh.numel()),
+        _dev(dst_indptr, "dst indptr", "i32", C + 1), _dev(dst_indices, "dst indices", "i32", 0, nullable=True),
+        0 if dst_indices is None else int(dst_indices.numel()),
+        _dev(ref, "ref", "i32", int(layout.num_slots), nullable=True), _ptr(used), _stream_of(ctx, stream)))
+    return int(used[0])
+
+
+def _count_args(ctx, layout, pages_indptr, pages_indices, ref):
+    _same_device(ctx, pages_indptr, pages_indices, ref)
+    ip = _dev(pages_indptr, "page table indptr", "i32", 2)
+    return (_ctx_handle(ctx), ctypes.byref(layout), int(pages_indptr.numel()) - 1,
+            _Pages(ip, _dev(pages_indices, "page table indices", "i32", 0)), int(pages_indices.numel()),
+            _dev(ref, "ref", "i32", int(layout.num_slots)))
+
+
+def sa_kv_retain(ctx, layout: Layout, pages_indptr, pages_indices, ref, stream=None):
+    """Raises the count of every slot that the tables name."""
+    _check(load_library().sa_kv_retain(*_count_args(ctx, layout, pages_indptr, pages_indices, ref),
+                                       _stream_of(ctx, stream)))
+
+
+def sa_kv_release(ctx, layout: Layout, pages_indptr, pages_indices, ref, free=None, num_free=None, stream=None):
+    """Lowers the count of every slot that the tables name; free [num_slots] then lists the slots without a count,
+    ascending, and num_free [1] says how many."""
+    _same_device(ctx, free, num_free)
+    _check(load_library().sa_kv_release(
+        *_count_args(ctx, layout, pages_indptr, pages_indices, ref),
+        _dev(free, "free", "i32", int(layout.num_slots), nullable=True), _dev(num_free, "num_free", "i32", 1, nullable=True),
+        _stream_of(ctx, stream)))
+
+
+def sa_kv_compact(ctx, layout: Layout, k_pool, v_pool, limit: int, ref, ref_out, indices, indices_out, slot_map, moved,
+                  stream=None):
+    """Moves the pages in use in slots >= limit into free slots below.  ref_out and indices_out may be ref and
+    indices; slot_map [num_slots] receives where each slot's page is, moved [2] the pages moved and left."""
+    _same_device(ctx, k_pool, v_pool, ref, ref_out, indices, indices_out, slot_map, moved)
+    n, slots = _pool_numel(layout), int(layout.num_slots)
+    entries = 0 if indices is None else int(indices.numel())
+    _check(load_library().sa_kv_compact(
+        _ctx_handle(ctx), ctypes.byref(layout), _dev(k_pool, "k_pool", "b16", n), _dev(v_pool, "v_pool", "b16", n),
+        int(limit), _dev(ref, "ref", "i32", slots), _dev(ref_out, "ref_out", "i32", slots),
+        _dev(indices, "indices", "i32", 0, nullable=entries == 0),
+        _dev(indices_out, "indices_out", "i32", entries, nullable=entries == 0), entries,
+        _dev(slot_map, "slot_map", "i32", slots), _dev(moved, "moved", "i32", 2), _stream_of(ctx, stream)))
+
+
+def sa_shared_prefix_attn(ctx, layout: Layout, layer: int, q, k_pool, v_pool, q_len, kv_len, pages_indptr,
+                          pages_indices, group_indptr, shared_len, softmax_scale: float, o, lse=None, stream=None):
+    """sa_segment_prefill_attn for groups of sequences (group_indptr) that share their first shared_len tokens, whose
+    keys and values are read once for the group."""
+    q_len, kv_len = _host_i32(q_len), _host_i32(kv_len)
+    groups, shared = _host_i32(group_indptr), _host_i32(shared_len)
+    if q_len.shape != kv_len.shape:
+        raise ValueError("q_len and kv_len differ in length")
+    if len(groups) != len(shared) + 1:
+        raise ValueError("group_indptr must have one entry more than shared_len")
+    _same_device(ctx, q, k_pool, v_pool, pages_indptr, pages_indices, o, lse)
+    qp, op, lp, _ = _attn_dev(layout, q_len, q, o, lse)
+    n = _pool_numel(layout)
+    _check(load_library().sa_shared_prefix_attn(
+        _ctx_handle(ctx), ctypes.byref(layout), int(layer), qp, _dev(k_pool, "k_pool", "b16", n),
+        _dev(v_pool, "v_pool", "b16", n), int(len(q_len)), _ptr(q_len), _ptr(kv_len),
+        _pages(pages_indptr, pages_indices, len(q_len)), int(len(shared)), _ptr(groups), _ptr(shared),
+        float(softmax_scale), op, lp, _stream_of(ctx, stream)))

@@ -234,7 +234,10 @@ __device__ __forceinline__ bool part_arrive(const AttnArgs& a, const PartInfo& p
 // source is chosen per group of four keys; a group holding keys of both kinds
 // (prefix lengths that are not a multiple of 4) takes the checked load, so the
 // steps that load its tile are plain steps.
-template <int P, bool kPoolRsrc, int kGroups, int GRP, bool kRead = false, bool kExact = false>
+//
+// kRowParts: the partials of parts go out as plain rows, for a merge launch
+// that finds each row of an item in several items' parts (attn_shared.h).
+template <int P, bool kPoolRsrc, int kGroups, int GRP, bool kRead = false, bool kExact = false, bool kRowParts = false>
 __device__ __attribute__((always_inline)) inline void pipe_group(const AttnArgs& a, const AttnItem& it,
                                                                  const SeqDesc& sd, const PipeLds& L) {
   static_assert(P == 16 || P == 32, "page size");
@@ -897,6 +900,8 @@ __device__ __attribute__((always_inline)) inline void pipe_group(const AttnArgs&
     m_used = m_new;
   }
 
+  // (plain rows) the tile buffers become the waves' transposition room
+  if constexpr (kRowParts) lds_barrier();
   if (!wave_active) return;
   const float l_tot = pair_sum(l);
   const float l_out = kExact ? pair_sum(l + corr) : l_tot;
@@ -923,6 +928,29 @@ __device__ __attribute__((always_inline)) inline void pipe_group(const AttnArgs&
         }
       if (a.lse != nullptr && hh_o == 0)
         a.lse[(int64_t)(sd.q_start + o_tok) * a.Hq + o_head] = lse2 * 0.69314718055994531f;
+    }
+  } else if constexpr (kRowParts) {
+    // This wave's 32 rows of fp32 turned to row order in 16 KB of LDS, so that
+    // every store is whole lines; chunk c of row r sits at c ^ r, which spreads
+    // both the writes and the reads over all banks.
+    lds_u8* const room = wave == 0 ? L.k0 : wave == 1 ? L.k1 : wave == 2 ? L.v0 : L.v1;
+    const int row_o = lane_o & 31;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const int dt = k >> 2, i = k & 3, c = 8 * dt + 2 * i + hh_o;
+      *(__attribute__((address_space(3))) f32x4*)(room + row_o * 512 + ((c ^ row_o) << 4)) =
+          f32x4{oacc[dt][4 * i] * inv, oacc[dt][4 * i + 1] * inv, oacc[dt][4 * i + 2] * inv, oacc[dt][4 * i + 3] * inv};
+    }
+    const int64_t prow = (int64_t)it.part * kRows + wave * 32;
+    if (hh_o == 0 && o_row < rows_total) a.part_lse[prow + row_o] = lse2;
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);                    // lgkmcnt(0): the wave's own rows are in LDS
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const int r = 2 * k + hh_o, c = row_o;
+      const f32x4 x = *(const __attribute__((address_space(3))) f32x4*)(room + r * 512 + ((c ^ r) << 4));
+      if (it.row0 + wave * 32 + r < rows_total) *(f32x4*)(a.part_o + (prow + r) * kHD + 4 * c) = x;
     }
   } else if constexpr (kGroups == 1) {
     // A part's partial: this wave's 32 rows in accumulator order (16-byte
@@ -1040,7 +1068,7 @@ __device__ __forceinline__ float quad_sum(float x) {
   return pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
-template <int P, bool kExact, int kNB>
+template <int P, bool kExact, int kNB, bool kRowParts = false>
 __device__ __attribute__((always_inline)) inline void decode_group(const AttnArgs& a, const AttnItem& it,
                                                                    lds_u8* k0, lds_u8* k1, lds_u8* v0, lds_u8* v1,
                                                                    lds_f32* stats) {
@@ -1336,12 +1364,15 @@ __device__ __attribute__((always_inline)) inline void decode_group(const AttnArg
       const int64_t orow = (int64_t)(it.q_start + tok) * a.Hq + it.kvh * G + (r - tok * G);
       st_bf16x4(a.o + orow * kHD + 4 * c, o[0], o[1], o[2], o[3]);
       if (a.lse != nullptr && c == 0) a.lse[orow] = lse2 * 0.69314718055994531f;
+    } else if constexpr (kRowParts) {
+      *(f32x4*)(a.part_o + ((int64_t)it.part * kPipeRows + row) * kHD + 4 * c) = o;
+      if (c == 0) a.part_lse[(int64_t)it.part * kPipeRows + row] = lse2;
     } else {
       part_st4(rp, (uint32_t)it.part * (kPipeRows * kHD * 4) + (uint32_t)e * 16, o);
       if (c == 0) part_st1(rp, l_base + (uint32_t)it.part * (kPipeRows * 4) + row * 4, 0, lse2);
     }
   }
-  if (whole) return;
+  if (kRowParts || whole) return;
   // A key-range part: counted once all of its stores are acknowledged; the
   // block of the last part merges the item's parts, its threads spread over
   // (row, four d, every nsub-th part).

@@ -1,0 +1,113 @@
+// Attention of a batch whose members share a prefix (sa_shared_prefix_attn).
+//
+// For one query row with key sets A (the shared prefix) and B (its sequence's
+// own keys), each again cut into parts p,
+//   L = log2 sum_p 2^(L_p),   O = sum_p 2^(L_p - L) O_p,
+// O_p and L_p the normalised output and log2-sum-exp over part p alone.  No row
+// of a group is masked inside the shared prefix, so the rows of all its members
+// pack into 128-row tiles over it: its keys and values are read once per tile
+// instead of once per member, and the matrix work of the padded rows goes.  One
+// launch makes all parts (the members' rows lie next to each other in Q, so a
+// prefix tile is an item of attn_pipe_kernel's body whose "sequence" is the
+// whole group), a second joins them row by row.
+#pragma once
+
+#include "attn_pipe.h"
+#include "branch_plan.h"
+
+namespace sa {
+
+template <int P, bool kPoolRsrc>
+__global__ __launch_bounds__(256, 2) void attn_shared_kernel(AttnArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t k_lds0[kTileBytes], k_lds1[kTileBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t v_lds0[kTileBytes], v_lds1[kTileBytes];
+  __shared__ float dec_stats[2 * 4 * kDecRows + 1];
+  const AttnItem it = ld_uniform(a.items + blockIdx.x);
+  if (it.kv_begin >= it.kv_end) return;                     // padding item
+  const SeqDesc sd{it.q_start, it.q_len, it.kv_len, 0};
+  const PipeLds L{(lds_u8*)k_lds0, (lds_u8*)k_lds1, (lds_u8*)v_lds0, (lds_u8*)v_lds1,
+                  nullptr, nullptr, nullptr, nullptr, nullptr};
+  const int rows = it.q_len * a.G;
+  if (rows <= 16)
+    decode_group<P, true, 1, true>(a, it, (lds_u8*)k_lds0, (lds_u8*)k_lds1, (lds_u8*)v_lds0, (lds_u8*)v_lds1,
+                                   (lds_f32*)dec_stats);
+  else if (rows <= kDecRows)
+    decode_group<P, true, 2, true>(a, it, (lds_u8*)k_lds0, (lds_u8*)k_lds1, (lds_u8*)v_lds0, (lds_u8*)v_lds1,
+                                   (lds_f32*)dec_stats);
+  else
+    pipe_group<P, kPoolRsrc, 1, 0, false, true, true>(a, it, sd, L);
+}
+
+struct MergeRowsArgs {
+  const float* part_o;       // [parts][kPipeRows][kHD]
+  const float* part_lse;     // [parts][kPipeRows], log2
+  const MergeUnit* units;
+  uint16_t* o;
+  float* lse;                // nullable
+  int32_t Hq, G;
+};
+
+// One block per unit: half a wave (32 threads, four d each) per row, and with
+// at most four rows several half waves share a row's parts and meet in LDS.
+__global__ __launch_bounds__(256) void merge_rows_kernel(MergeRowsArgs a) {
+  __shared__ f32x4 red[8][32];
+  __shared__ float red_m[8], red_den[8];
+  const MergeUnit u = ld_uniform(a.units + blockIdx.x);
+  const int hw = threadIdx.x >> 5, c = threadIdx.x & 31;
+  const int nsub = u.n >= 8 ? 1 : 8 / (u.n > 4 ? 8 : u.n > 2 ? 4 : u.n);   // half waves per row
+  const int sub = hw % nsub;
+  const int np = u.a_n + u.b_n;
+  for (int r0 = 0; r0 < u.n; r0 += 8 / nsub) {
+    const int r = r0 + hw / nsub;
+    const bool mine = r < u.n;
+    float mx = -INFINITY, den = 0.f;
+    f32x4 num = f32x4{};
+    auto row_of = [&](int s) {
+      return s < u.a_n ? (int64_t)(u.a_part + s) * kPipeRows + u.a_row + r
+                       : (int64_t)(u.b_part + s - u.a_n) * kPipeRows + u.b_row + r;
+    };
+    if (mine) {
+      for (int s = sub; s < np; s += nsub) mx = fmaxf(mx, a.part_lse[row_of(s)]);
+      const float off = mx == -INFINITY ? 0.f : mx;
+      for (int s = sub; s < np; s += nsub) {
+        const int64_t p = row_of(s);
+        const float w = exp2f_fast(a.part_lse[p] - off);
+        den += w;
+        num += w * *(const f32x4*)(a.part_o + p * kHD + 4 * c);
+      }
+    }
+    if (nsub > 1) {
+      red[hw][c] = num;
+      if (c == 0) {
+        red_m[hw] = mx;
+        red_den[hw] = den;
+      }
+      __syncthreads();
+      if (mine && sub == 0) {
+        float all = mx;
+        for (int k = 1; k < nsub; ++k) all = fmaxf(all, red_m[hw + k]);
+        const float off = all == -INFINITY ? 0.f : all;
+        float f = exp2f_fast(mx - off);
+        num *= f;
+        den *= f;
+        for (int k = 1; k < nsub; ++k) {
+          f = exp2f_fast(red_m[hw + k] - off);
+          num += f * red[hw + k][c];
+          den += f * red_den[hw + k];
+        }
+        mx = all;
+      }
+      __syncthreads();
+    }
+    if (mine && sub == 0) {
+      const float inv = den > 0.f ? 1.f / den : 0.f;
+      const int row = u.r0 + r, tok = row / a.G;
+      const int64_t orow = (int64_t)(u.q_start + tok) * a.Hq + u.kvh * a.G + (row - tok * a.G);
+      st_bf16x4(a.o + orow * kHD + 4 * c, num[0] * inv, num[1] * inv, num[2] * inv, num[3] * inv);
+      if (a.lse != nullptr && c == 0)
+        a.lse[orow] = den > 0.f ? (mx + __builtin_amdgcn_logf(den)) * 0.69314718055994531f : -INFINITY;
+    }
+  }
+}
+
+}  // namespace sa

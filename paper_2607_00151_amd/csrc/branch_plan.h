@@ -1,0 +1,294 @@
+// Host-side planning of the calls that keep several branches of one context
+// alive: the fork of cached contexts and the attention of a batch whose
+// members share a prefix.  Plain C++17 with no HIP dependency, like plan.h.
+//
+// The records defined here are also the device-side plan formats, so they are
+// plain int32 structs.
+#pragma once
+
+#include "plan.h"
+
+namespace sa {
+
+// ------------------------------------------------------------------ fork
+
+// One child of a fork: the first `full` pages of its table are its parent's,
+// the others fresh slots from position `fresh0` of the free list on, the first
+// of which takes `rows` rows of the parent's partial page (0: it has none).
+struct ForkChild {
+  int32_t parent, full, rows, fresh0, dst0;
+};
+
+struct ForkPlan {
+  std::vector<ForkChild> children;
+  std::vector<int32_t> dst_indptr;     // [children + 1]
+  std::vector<int32_t> copies;         // children with a partial page
+  int64_t n_dst = 0, fresh_used = 0;
+};
+
+inline sa_status plan_fork(const sa_layout* layout, int32_t batch, const int32_t* h_src_len, int32_t num_children,
+                           const int32_t* h_parent, const int32_t* h_reserve, int32_t num_fresh, int32_t dst_capacity,
+                           ForkPlan& out, std::string& err) {
+  sa_status s = check_layout(layout, err);
+  if (s != SA_OK) return s;
+  if (batch < 1) return plan_fail(err, SA_ERR_SHAPE, "batch %d < 1", batch);
+  if (num_children < 1) return plan_fail(err, SA_ERR_SHAPE, "num_children %d < 1", num_children);
+  if (!h_src_len || !h_parent || !h_reserve) return plan_fail(err, SA_ERR_NULL, "a host array is NULL");
+  if (num_fresh < 0 || dst_capacity < 0) return plan_fail(err, SA_ERR_SHAPE, "negative capacity");
+  for (int b = 0; b < batch; ++b)
+    if (h_src_len[b] < 0) return plan_fail(err, SA_ERR_SHAPE, "sequence %d: src_len %d", b, h_src_len[b]);
+  const int P = layout->page_size;
+  out = ForkPlan{};
+  out.dst_indptr.assign((size_t)num_children + 1, 0);
+  for (int c = 0; c < num_children; ++c) {
+    const int b = h_parent[c];
+    if (b < 0 || b >= batch) return plan_fail(err, SA_ERR_RANGE, "child %d: parent %d outside [0, %d)", c, b, batch);
+    if (h_reserve[c] < 0) return plan_fail(err, SA_ERR_SHAPE, "child %d: reserve %d", c, h_reserve[c]);
+    const int64_t len = h_src_len[b], full = len / P, rows = len % P;
+    const int64_t pages = (len + h_reserve[c] + P - 1) / P;
+    if (out.n_dst + pages > INT32_MAX) return plan_fail(err, SA_ERR_SHAPE, "destination table too large");
+    out.children.push_back({b, (int32_t)full, (int32_t)rows, (int32_t)out.fresh_used, (int32_t)out.n_dst});
+    if (rows > 0) out.copies.push_back(c);
+    out.n_dst += pages;
+    out.fresh_used += pages - full;
+    out.dst_indptr[c + 1] = (int32_t)out.n_dst;
+  }
+  if (out.fresh_used > num_fresh)
+    return plan_fail(err, SA_ERR_NO_PAGES, "need %lld fresh slots, %d given", (long long)out.fresh_used, num_fresh);
+  if (out.n_dst > dst_capacity)
+    return plan_fail(err, SA_ERR_NO_PAGES, "destination table needs %lld entries, capacity %d", (long long)out.n_dst,
+                     dst_capacity);
+  return SA_OK;
+}
+
+// SA_DEBUG check of a fork against host copies of the source table and of the
+// free list's first entries: every page in range, the fresh slots distinct and
+// none of them a page of a source context.
+inline sa_status debug_check_fork(const ForkPlan& plan, const int32_t* indptr, const int32_t* indices,
+                                  const int32_t* fresh, int64_t num_slots, std::string& err) {
+  std::vector<int32_t> used;
+  for (size_t c = 0; c < plan.children.size(); ++c) {
+    const ForkChild& ch = plan.children[c];
+    const int32_t pages = ch.full + (ch.rows > 0);
+    const int32_t have = indptr[ch.parent + 1] - indptr[ch.parent];
+    if (pages > have)
+      return plan_fail(err, SA_ERR_RANGE, "child %d: its parent's table has %d of %d pages", (int)c, have, pages);
+    for (int j = 0; j < pages; ++j) {
+      const int32_t slot = indices[indptr[ch.parent] + j];
+      if (slot < 0 || slot >= num_slots)
+        return plan_fail(err, SA_ERR_RANGE, "sequence %d: page %d has slot %d outside [0, %lld)", ch.parent, j, slot,
+                         (long long)num_slots);
+      used.push_back(slot);
+    }
+  }
+  std::sort(used.begin(), used.end());
+  std::vector<int32_t> taken(fresh, fresh + plan.fresh_used);
+  std::sort(taken.begin(), taken.end());
+  for (size_t i = 0; i < taken.size(); ++i) {
+    if (taken[i] < 0 || taken[i] >= num_slots)
+      return plan_fail(err, SA_ERR_RANGE, "a free-list entry is slot %d, outside [0, %lld)", taken[i],
+                       (long long)num_slots);
+    if (i > 0 && taken[i] == taken[i - 1])
+      return plan_fail(err, SA_ERR_OVERLAP, "slot %d appears twice in the free list", taken[i]);
+    if (std::binary_search(used.begin(), used.end(), taken[i]))
+      return plan_fail(err, SA_ERR_OVERLAP, "fresh slot %d is also a page of a source context", taken[i]);
+  }
+  return SA_OK;
+}
+
+// ------------------------------------------------------------------ shared prefix
+
+// Rows of one member and KV head whose parts the merge joins: packed rows
+// r0 .. r0 + n - 1 of the member whose first token is q_start, found in parts
+// a_part .. a_part + a_n - 1 from row a_row on (the shared prefix) and in
+// b_part .. from row b_row on (the member's own keys).
+struct MergeUnit {
+  int32_t q_start, r0, n, kvh;
+  int32_t a_part, a_n, a_row;
+  int32_t b_part, b_n, b_row;
+};
+constexpr int kMergeUnitRows = 32;     // most rows of a unit
+
+struct SharedPlan {
+  std::vector<AttnItem> items;         // one per workgroup, in launch order
+  std::vector<MergeUnit> units;
+  int32_t n_parts = 0;
+  int64_t total_q = 0;
+  bool any_shared = false;             // some group's prefix is computed once for its members
+};
+
+inline sa_status check_groups(int32_t batch, const int32_t* h_q_len, const int32_t* h_kv_len, int32_t num_groups,
+                              const int32_t* h_group_indptr, const int32_t* h_shared_len, std::string& err) {
+  if (num_groups < 1) return plan_fail(err, SA_ERR_SHAPE, "num_groups %d < 1", num_groups);
+  if (!h_group_indptr || !h_shared_len) return plan_fail(err, SA_ERR_NULL, "h_group_indptr / h_shared_len is NULL");
+  if (h_group_indptr[0] != 0 || h_group_indptr[num_groups] != batch)
+    return plan_fail(err, SA_ERR_SHAPE, "group_indptr must run from 0 to the batch size %d", batch);
+  for (int g = 0; g < num_groups; ++g)
+    if (h_group_indptr[g + 1] < h_group_indptr[g])
+      return plan_fail(err, SA_ERR_SHAPE, "group_indptr decreases at %d", g);
+  for (int g = 0; g < num_groups; ++g) {
+    if (h_shared_len[g] < 0) return plan_fail(err, SA_ERR_SHAPE, "group %d: shared_len %d", g, h_shared_len[g]);
+    for (int b = h_group_indptr[g]; b < h_group_indptr[g + 1]; ++b)
+      if (h_shared_len[g] > h_kv_len[b] - h_q_len[b])
+        return plan_fail(err, SA_ERR_SHAPE, "group %d: shared_len %d beyond the %d cached tokens of sequence %d", g,
+                         h_shared_len[g], h_kv_len[b] - h_q_len[b], b);
+  }
+  return SA_OK;
+}
+
+// The launch's work items.  A group whose prefix is computed once gives row
+// tiles of all its members' packed rows over the keys [0, S), S its shared
+// length rounded down to whole 64-key tiles, and row tiles of each member over
+// [S, kv_len); every other member gives row tiles over all of its keys.  Tiles
+// are split by key range into parts; a tile that is the only one to see its
+// rows and has one part writes the output itself.
+inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc>& seqs, int32_t num_groups,
+                              const int32_t* h_group_indptr, const int32_t* h_shared_len, int num_cu,
+                              SharedPlan& out) {
+  const int Hkv = layout->num_kv_heads, G = layout->num_q_heads / Hkv;
+  constexpr int kRows = 128;
+  out = SharedPlan{};
+  struct Tile {
+    int32_t seq, row0, rows, q_start, q_len, kv_len, k0, k1;   // rows: of this tile
+    bool prefix;
+    int32_t part0 = -1, parts = 1;                              // of KV head 0; head h's are part0 + h * parts on
+    int64_t tiles() const { return (k1 - k0 + kKT - 1) / kKT; }
+  };
+  std::vector<Tile> tiles;
+  struct Member {
+    int32_t seq, prefix0, row_in_group, own0;                  // first prefix tile of its group (-1), its first row there
+  };
+  std::vector<Member> members;
+  for (int g = 0; g < num_groups; ++g) {
+    const int b0 = h_group_indptr[g], b1 = h_group_indptr[g + 1];
+    int64_t rows = 0, apart = 0;
+    int first = -1;
+    for (int b = b0; b < b1; ++b) {
+      const int64_t r = (int64_t)seqs[b].q_len * G;
+      rows += r;
+      apart += (r + kRows - 1) / kRows;
+      if (first < 0 && r > 0) first = b;
+    }
+    if (first < 0) continue;
+    const int32_t S = h_shared_len[g] / kKT * kKT;
+    // worth it where packing the members' rows leaves clearly fewer row tiles over the prefix
+    const bool shared = S > 0 && rows <= INT32_MAX / 2 && 8 * ((rows + kRows - 1) / kRows) <= 7 * apart;
+    const int32_t prefix0 = shared ? (int32_t)tiles.size() : -1;
+    if (shared) {
+      out.any_shared = true;
+      const int32_t q_len = (int32_t)(rows / G);
+      for (int64_t r0 = 0; r0 < rows; r0 += kRows)
+        tiles.push_back({first, (int32_t)r0, (int32_t)std::min<int64_t>(kRows, rows - r0), seqs[first].q_start, q_len,
+                         S + q_len, 0, S, true});
+    }
+    int64_t at = 0;
+    for (int b = b0; b < b1; ++b) {
+      const SeqDesc& q = seqs[b];
+      const int32_t n = q.q_len * G;
+      if (n == 0) continue;
+      members.push_back({b, prefix0, (int32_t)at, (int32_t)tiles.size()});
+      for (int r0 = 0; r0 < n; r0 += kRows) {
+        const int last = std::min(r0 + kRows, n) - 1;
+        tiles.push_back({b, r0, last + 1 - r0, q.q_start, q.q_len, q.kv_len, shared ? S : 0,
+                         q.kv_len - q.q_len + last / G + 1, false});
+      }
+      at += n;
+    }
+  }
+  // key-range parts: the smallest chunk whose blocks are two per CU
+  int64_t longest = 1;
+  for (const Tile& t : tiles) longest = std::max(longest, t.tiles());
+  auto parts_of = [](const Tile& t, int64_t c) {
+    return std::max<int64_t>(1, std::min<int64_t>((t.tiles() + c - 1) / c, kMaxItemParts));
+  };
+  auto blocks = [&](int64_t c) {
+    int64_t n = 0;
+    for (const Tile& t : tiles) n += parts_of(t, c) * Hkv;
+    return n;
+  };
+  const int64_t slots = std::max<int64_t>(2 * num_cu, (int64_t)tiles.size() * Hkv + num_cu);
+  int64_t lo = std::min<int64_t>(4, longest), hi = longest;
+  while (lo < hi) {
+    const int64_t mid = lo + (hi - lo) / 2;
+    if (blocks(mid) <= slots) hi = mid; else lo = mid + 1;
+  }
+  const int64_t chunk = lo;
+  for (const Member& m : members) {
+    const int32_t n = seqs[m.seq].q_len * G;
+    for (int32_t r0 = 0, t = m.own0; r0 < n; r0 += kRows, ++t) {
+      tiles[t].parts = (int32_t)parts_of(tiles[t], chunk);
+      if (m.prefix0 >= 0 || tiles[t].parts > 1) {
+        tiles[t].part0 = out.n_parts;
+        out.n_parts += tiles[t].parts * Hkv;
+      }
+    }
+  }
+  for (Tile& t : tiles)
+    if (t.prefix) {
+      t.parts = (int32_t)parts_of(t, chunk);
+      t.part0 = out.n_parts;
+      out.n_parts += t.parts * Hkv;
+    }
+  // blocks: longest first, the row tiles of one key range next to each other on
+  // one XCD (block i runs on XCD i % 8), which reads it through its L2 once
+  struct Bundle {
+    int64_t tiles = 0;
+    std::vector<AttnItem> items;
+  };
+  std::vector<Bundle> bundles;
+  for (size_t i = 0; i < tiles.size();) {
+    size_t j = i + 1;
+    while (j < tiles.size() && tiles[j].seq == tiles[i].seq && tiles[j].prefix == tiles[i].prefix && tiles[i].prefix) ++j;
+    for (int h = 0; h < Hkv; ++h)
+      for (int k = 0; k < tiles[i].parts; ++k) {
+        Bundle bu;
+        for (size_t x = i; x < j; ++x) {
+          const Tile& t = tiles[x];
+          const int64_t n = t.tiles();
+          AttnItem it{t.seq, h, t.row0, 0, 0, -1, 0, t.q_start, t.q_len, t.kv_len};
+          it.kv_begin = (int32_t)(t.k0 + n * k / t.parts * kKT);
+          it.kv_end = (int32_t)std::min<int64_t>(t.k0 + n * (k + 1) / t.parts * kKT, t.k1);
+          if (t.part0 >= 0) it.part = t.part0 + h * t.parts + k;
+          bu.tiles += item_tiles(it);
+          bu.items.push_back(it);
+        }
+        bundles.push_back(std::move(bu));
+      }
+    i = j;
+  }
+  std::stable_sort(bundles.begin(), bundles.end(), [](const Bundle& x, const Bundle& y) { return x.tiles > y.tiles; });
+  std::vector<std::vector<AttnItem>> queue(kNumXcd);
+  int64_t load[kNumXcd] = {0};
+  for (const Bundle& b : bundles) {
+    const int x = (int)(std::min_element(load, load + kNumXcd) - load);
+    load[x] += b.tiles;
+    queue[x].insert(queue[x].end(), b.items.begin(), b.items.end());
+  }
+  size_t depth = 0;
+  for (const auto& q : queue) depth = std::max(depth, q.size());
+  out.items.assign(depth * kNumXcd, AttnItem{0, 0, 0, 0, 0, -1, 0, 0, 0, 0});
+  for (int x = 0; x < kNumXcd; ++x)
+    for (size_t i = 0; i < queue[x].size(); ++i) out.items[i * kNumXcd + x] = queue[x][i];
+  // merge units: rows of one member, one own tile and one prefix tile
+  for (const Member& m : members) {
+    const int32_t n = seqs[m.seq].q_len * G;
+    for (int h = 0; h < Hkv; ++h)
+      for (int32_t r = 0; r < n;) {
+        const Tile& own = tiles[m.own0 + r / kRows];
+        int32_t e = std::min(r + kMergeUnitRows, std::min(own.row0 + own.rows, n));
+        MergeUnit u{seqs[m.seq].q_start, r, 0, h, 0, 0, 0, own.part0 + h * own.parts, own.parts, r - own.row0};
+        if (m.prefix0 >= 0) {
+          const Tile& pre = tiles[m.prefix0 + (m.row_in_group + r) / kRows];
+          e = std::min(e, pre.row0 + kRows - m.row_in_group);
+          u.a_part = pre.part0 + h * pre.parts;
+          u.a_n = pre.parts;
+          u.a_row = m.row_in_group + r - pre.row0;
+        }
+        u.n = e - r;
+        r = e;
+        if (own.part0 >= 0) out.units.push_back(u);
+      }
+  }
+}
+
+}  // namespace sa

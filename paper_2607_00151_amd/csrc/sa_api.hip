@@ -20,6 +20,10 @@
 #include "attn_kernel.h"
 #include "attn_pipe.h"
 #include "kv_kernels.h"
+#include "attn_shared.h"
+#include "branch_kernels.h"
+#include "branch_plan.h"
+#include "rope_kernels.h"
 
 namespace {
 
@@ -97,7 +101,10 @@ class PlanKey {
   bool same_ = false;
 };
 
-enum PlanKind { kPlanAppend = 0, kPlanAssemble = 1, kPlanAttn = 2, kPlanAlias = 3, kPlanKinds = 4 };
+enum PlanKind {
+  kPlanAppend = 0, kPlanAssemble = 1, kPlanAttn = 2, kPlanAlias = 3, kPlanRope = 4, kPlanFork = 5, kPlanShared = 6,
+  kPlanKinds = 7
+};
 
 // Fixed device scratch of sa_segment_prefill_attn_noalloc: the launch's plan
 // (sequence records, work items, part records) in its first kNoAllocPlanBytes,
@@ -178,6 +185,21 @@ struct sa_ctx {
     int32_t n_parts = 0;
     int64_t total_q = 0;
   } attn_rec, na_rec;
+  struct RopeRec {
+    size_t o_tok = 0, o_start = 0, o_pos = 0;
+    int64_t total = 0;
+  } rope_rec;
+  struct ForkRec {
+    size_t o_ch = 0, o_ip = 0, o_cp = 0;
+    int64_t n_dst = 0, fresh_used = 0, n_copies = 0;
+  } fork_rec;
+  struct SharedRec {
+    size_t o_it = 0, o_un = 0, n_items = 0, n_units = 0;
+    int64_t total_q = 0, n_parts = 0;
+    bool any_shared = false;
+  } shared_rec;
+  uint8_t* work = nullptr;         // slot scans of sa_kv_release and sa_kv_compact
+  size_t work_cap = 0;
   PlanKey na_key;                  // sa_segment_prefill_attn_noalloc: the plan na_host holds
   bool na_valid = false;
   struct Stage {
@@ -459,6 +481,7 @@ void sa_destroy(sa_ctx* ctx) {
     if (s.ev) (void)hipEventDestroy(s.ev);
   }
   if (ctx->part) (void)hipFree(ctx->part);
+  if (ctx->work) (void)hipFree(ctx->work);
   for (void* p : ctx->retired_dev) (void)hipFree(p);
   for (void* p : ctx->retired_host) (void)hipHostFree(p);
   if (ctx->d_err) (void)hipFree(ctx->d_err);
@@ -875,6 +898,25 @@ sa_status sa_kv_splice_alias(sa_ctx* ctx, const sa_layout* layout, int32_t batch
 
 namespace {
 
+// Room for this many bytes of split-KV partials.
+sa_status reserve_parts(sa_ctx* ctx, size_t need) {
+  if (need <= ctx->part_cap) return SA_OK;
+  // at least doubled: part counts follow the lengths, and each growth is an
+  // allocation in the call whose outgrown buffer stays until sa_destroy
+  size_t cap = std::max(need, 2 * ctx->part_cap);
+  if (ctx->part) ctx->retired_dev.push_back(ctx->part);    // an enqueued launch may still use it
+  ctx->part = nullptr;
+  ctx->part_cap = 0;
+  if (cap > need && hipMalloc(&ctx->part, cap) != hipSuccess) {
+    (void)hipGetLastError();
+    ctx->part = nullptr;
+    cap = need;                                            // no room for twice as much: what the launch takes
+  }
+  if (ctx->part == nullptr) SA_HIP(hipMalloc(&ctx->part, cap));
+  ctx->part_cap = cap;
+  return SA_OK;
+}
+
 // The attention launch; with `append` each sequence's q_len new K/V rows
 // (k_new, v_new) also go to its positions kv_len - q_len .. kv_len - 1: by the
 // attention launch itself, which then reads the segment's keys from k_new /
@@ -983,22 +1025,8 @@ sa_status attn_launch(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   const int32_t n_parts = rec.n_parts;
 
   if (n_parts > 0 && !noalloc) {
-    const size_t need = (size_t)n_parts * rows_item * (sa::kHD + 1) * sizeof(float);
-    if (need > ctx->part_cap) {
-      // at least doubled: part counts follow the lengths, and each growth is an
-      // allocation in the call whose outgrown buffer stays until sa_destroy
-      size_t cap = std::max(need, 2 * ctx->part_cap);
-      if (ctx->part) ctx->retired_dev.push_back(ctx->part);    // an enqueued launch may still use it
-      ctx->part = nullptr;
-      ctx->part_cap = 0;
-      if (cap > need && hipMalloc(&ctx->part, cap) != hipSuccess) {
-        (void)hipGetLastError();
-        ctx->part = nullptr;
-        cap = need;                                            // no room for twice as much: what the launch takes
-      }
-      if (ctx->part == nullptr) SA_HIP(hipMalloc(&ctx->part, cap));
-      ctx->part_cap = cap;
-    }
+    s = reserve_parts(ctx, (size_t)n_parts * rows_item * (sa::kHD + 1) * sizeof(float));
+    if (s != SA_OK) return s;
   }
 
   uint8_t* dev = ctx->plans[kPlanAttn].dev;
@@ -1202,6 +1230,551 @@ sa_status sa_segment_prefill_attn_append(sa_ctx* ctx, const sa_layout* layout, i
                                          void* o, float* lse, void* stream) {
   return attn_launch(ctx, layout, layer, q, k_pool, v_pool, true, k_new, v_new, batch, h_q_len,
                      h_kv_len, pages, softmax_scale, o, lse, stream);
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------ branches of a context
+
+namespace {
+
+// The calling thread's device, put back when the call returns.
+struct DeviceGuard {
+  int before = -1;
+  DeviceGuard() {
+    if (hipGetDevice(&before) != hipSuccess) before = -1;
+  }
+  ~DeviceGuard() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+// A call whose plan lives in the context's buffers would be replayed with
+// whatever plan is there by then, so it is not captured into a graph.
+sa_status refuse_capture(hipStream_t stream, const char* call) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  SA_HIP(hipStreamIsCapturing(stream, &st));
+  if (st != hipStreamCaptureStatusNone)
+    return fail(SA_ERR_UNSUPPORTED, "%s keeps its plan in the context and cannot be captured into a graph", call);
+  return SA_OK;
+}
+
+// Nothing thrown by the host containers crosses the C entry points.
+template <typename F>
+sa_status no_throw(F&& body) {
+  try {
+    return body();
+  } catch (const std::exception& e) {
+    return fail(SA_ERR_HIP, "host: %s", e.what());
+  }
+}
+
+sa_status reserve_work(sa_ctx* ctx, size_t need) {
+  if (need <= ctx->work_cap) return SA_OK;
+  if (ctx->work) ctx->retired_dev.push_back(ctx->work);
+  ctx->work = nullptr;
+  ctx->work_cap = 0;
+  SA_HIP(hipMalloc(&ctx->work, need));
+  ctx->work_cap = need;
+  return SA_OK;
+}
+
+sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const sa_rope* rope, const void* q,
+                      int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                      void* q_out, void* k_pool, void* v_pool, int32_t batch, const int32_t* h_start,
+                      const int32_t* h_new_len, const int32_t* h_pos, sa_pages pages, void* stream) {
+  sa_status s = check_layout(layout);
+  if (s != SA_OK) return s;
+  if (layer < 0 || layer >= layout->num_layers)
+    return fail(SA_ERR_SHAPE, "layer %d outside [0, %d)", layer, layout->num_layers);
+  if (batch < 1) return fail(SA_ERR_SHAPE, "batch %d < 1", batch);
+  const int Hq = layout->num_q_heads, Hkv = layout->num_kv_heads;
+  if (!rope) return fail(SA_ERR_NULL, "rope is NULL");
+  if (rope->rot_dim < 0 || rope->rot_dim > sa::kHD || rope->rot_dim % 16 != 0)
+    return fail(SA_ERR_UNSUPPORTED, "rot_dim %d (a multiple of 16 up to 128)", rope->rot_dim);
+  if (rope->rot_dim > 0 && !rope->h_inv_freq) return fail(SA_ERR_NULL, "h_inv_freq is NULL");
+  if ((rope->q_weight || rope->k_weight) &&
+      (!std::isfinite(rope->eps) || rope->eps <= 0.f || !std::isfinite(rope->weight_offset)))
+    return fail(SA_ERR_SHAPE, "eps %g must be finite and positive, weight_offset %g finite", rope->eps,
+                rope->weight_offset);
+  for (int j = 0; j < rope->rot_dim / 2; ++j)
+    if (!std::isfinite(rope->h_inv_freq[j]) || rope->h_inv_freq[j] < 0. || rope->h_inv_freq[j] > 1024.)
+      return fail(SA_ERR_SHAPE, "inv_freq[%d] = %g outside [0, 1024]", j, rope->h_inv_freq[j]);
+  const int64_t widths[3] = {(int64_t)Hq * sa::kHD, (int64_t)Hkv * sa::kHD, (int64_t)Hkv * sa::kHD};
+  const int64_t strides[3] = {q_stride, k_stride, v_stride};
+  for (int i = 0; i < 3; ++i) {
+    if (strides[i] < widths[i] || strides[i] > INT32_MAX)
+      return fail(SA_ERR_SHAPE, "%c token stride %lld, at least %lld needed", "qkv"[i], (long long)strides[i],
+                  (long long)widths[i]);
+    if (strides[i] % 8 != 0) return fail(SA_ERR_ALIGN, "%c token stride %lld is not a multiple of 8", "qkv"[i],
+                                         (long long)strides[i]);
+  }
+  if (!h_start || !h_new_len) return fail(SA_ERR_NULL, "h_start / h_new_len is NULL");
+  const int32_t* const h_rot = h_pos ? h_pos : h_start;
+  bool same = false;
+  sa_ctx::RopeRec rec;
+  if (ctx) {
+    sa_ctx::DevPlan& dp = ctx->plans[kPlanRope];
+    dp.key.begin();
+    dp.key.add(h_start, (size_t)batch);
+    dp.key.add(h_new_len, (size_t)batch);
+    dp.key.add(h_rot, (size_t)batch);
+    same = dp.reusable(dp.key.end(), (hipStream_t)stream) && !debug_checks();
+    if (!same) dp.key_valid = false;
+    rec = ctx->rope_rec;
+  }
+  std::vector<int32_t> tok_begin;
+  if (!same) {
+    rec = sa_ctx::RopeRec{};
+    tok_begin.resize((size_t)batch + 1);
+    for (int b = 0; b < batch; ++b) {
+      if (h_start[b] < 0 || h_new_len[b] < 0 || (int64_t)h_start[b] + h_new_len[b] > INT32_MAX)
+        return fail(SA_ERR_SHAPE, "sequence %d: start %d, new_len %d", b, h_start[b], h_new_len[b]);
+      if (h_rot[b] < 0 || (int64_t)h_rot[b] + h_new_len[b] > INT32_MAX)
+        return fail(SA_ERR_SHAPE, "sequence %d: position %d, new_len %d", b, h_rot[b], h_new_len[b]);
+      tok_begin[b] = (int32_t)rec.total;
+      rec.total += h_new_len[b];
+      if (rec.total > INT32_MAX / 2) return fail(SA_ERR_SHAPE, "too many new tokens");
+    }
+    tok_begin[batch] = (int32_t)rec.total;
+  }
+  if (!k_pool || !v_pool || !pages.indptr || !pages.indices)
+    return fail(SA_ERR_NULL, "pool or page table pointer is NULL");
+  if (rec.total > 0 && (!q || !k_new || !v_new || !q_out)) return fail(SA_ERR_NULL, "a row pointer is NULL");
+  for (const void* p : {q, k_new, v_new, (const void*)q_out, (const void*)k_pool, (const void*)v_pool, rope->q_weight,
+                        rope->k_weight})
+    if (!aligned16(p)) return fail(SA_ERR_ALIGN, "a row, weight or pool pointer is not 16-byte aligned");
+  DeviceGuard guard;
+  s = check_ctx(ctx);
+  if (s != SA_OK) return s;
+  if (rec.total == 0) return SA_OK;
+  s = refuse_capture((hipStream_t)stream, "sa_kv_append_rope");
+  if (s != SA_OK) return s;
+  if (debug_checks()) {
+    std::vector<int32_t> ip, ix;
+    s = fetch_table(pages.indptr, pages.indices, batch, (hipStream_t)stream, ip, ix);
+    if (s != SA_OK) return s;
+    s = sa::debug_check_append(batch, h_start, h_new_len, ip.data(), ix.data(), layout->page_size, layout->num_slots,
+                               g_err);
+    if (s != SA_OK) return s;
+  }
+  uint8_t* dev = ctx->plans[kPlanRope].dev;
+  if (!same) {
+    PlanImage img;
+    rec.o_tok = img.add(tok_begin.data(), tok_begin.size());
+    rec.o_start = img.add(h_start, (size_t)batch);
+    rec.o_pos = img.add(h_rot, (size_t)batch);
+    s = upload_plan(ctx, kPlanRope, img, (hipStream_t)stream, &dev);
+    if (s != SA_OK) return s;
+    ctx->rope_rec = rec;
+    ctx->plans[kPlanRope].key_valid = true;
+  }
+  sa::RopeArgs a{};
+  const int64_t lo = (int64_t)layer * layer_elems(layout);
+  a.q = (const uint16_t*)q;
+  a.k = (const uint16_t*)k_new;
+  a.v = (const uint16_t*)v_new;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q_out = (uint16_t*)q_out;
+  a.k_pool = (uint16_t*)k_pool + lo;
+  a.v_pool = (uint16_t*)v_pool + lo;
+  a.q_weight = (const uint16_t*)rope->q_weight;
+  a.k_weight = (const uint16_t*)rope->k_weight;
+  a.tok_begin = (const int32_t*)(dev + rec.o_tok);
+  a.start = (const int32_t*)(dev + rec.o_start);
+  a.pos = (const int32_t*)(dev + rec.o_pos);
+  a.indptr = pages.indptr;
+  a.indices = pages.indices;
+  a.err = ctx->d_err;
+  a.num_slots = layout->num_slots;
+  a.T = (int32_t)rec.total;
+  a.B = batch;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.P = layout->page_size;
+  a.rot = rope->rot_dim;
+  a.half_lanes = rope->rot_dim / 16;
+  a.eps = rope->eps;
+  a.offset = rope->weight_offset;
+  for (int j = 0; j < rope->rot_dim / 2; ++j) {
+    // turns per position modulo 1, in units of 2^-64
+    const long double turns = (long double)rope->h_inv_freq[j] / 6.283185307179586476925286766559L;
+    const long double frac = std::ldexp(turns - std::floor(turns), 64);
+    a.freq[j] = frac >= 18446744073709551615.0L ? UINT64_MAX : (uint64_t)(frac + 0.5L);
+  }
+  const int64_t waves = rec.total * ((Hq + 2 * (int64_t)Hkv + sa::kRopeRows - 1) / sa::kRopeRows);
+  const int64_t blocks = (waves + 3) / 4;
+  if (blocks > INT32_MAX) return fail(SA_ERR_SHAPE, "too many new tokens for these heads");
+  if (rope->interleaved)
+    launch_timed(sa::rope_append_kernel<true>, dim3((unsigned)blocks), dim3(256), (hipStream_t)stream,
+                 ctx->kernel_ev[SA_TIMED_PAGES], a);
+  else
+    launch_timed(sa::rope_append_kernel<false>, dim3((unsigned)blocks), dim3(256), (hipStream_t)stream,
+                 ctx->kernel_ev[SA_TIMED_PAGES], a);
+  SA_HIP(hipGetLastError());
+  return SA_OK;
+}
+
+sa_status kv_fork(sa_ctx* ctx, const sa_layout* layout, void* k_pool, void* v_pool, int32_t batch,
+                  const int32_t* h_src_len, int32_t num_children, const int32_t* h_parent, const int32_t* h_reserve,
+                  sa_pages src, const int32_t* d_fresh, int32_t num_fresh, int32_t* d_dst_indptr,
+                  int32_t* d_dst_indices, int32_t dst_capacity, int32_t* d_ref, int32_t* h_fresh_used, void* stream) {
+  sa_status s = check_layout(layout);
+  if (s != SA_OK) return s;
+  sa_ctx::ForkRec rec;
+  sa::ForkPlan plan;
+  bool same = false;
+  if (ctx && batch >= 1 && num_children >= 1 && h_src_len && h_parent && h_reserve) {
+    sa_ctx::DevPlan& dp = ctx->plans[kPlanFork];
+    const int32_t head[5] = {layout->page_size, batch, num_children, num_fresh, dst_capacity};
+    dp.key.begin();
+    dp.key.add(head, 5);
+    dp.key.add(h_src_len, (size_t)batch);
+    dp.key.add(h_parent, (size_t)num_children);
+    dp.key.add(h_reserve, (size_t)num_children);
+    same = dp.reusable(dp.key.end(), (hipStream_t)stream) && !debug_checks();
+    if (!same) dp.key_valid = false;
+    rec = ctx->fork_rec;
+  }
+  if (!same) {
+    s = sa::plan_fork(layout, batch, h_src_len, num_children, h_parent, h_reserve, num_fresh, dst_capacity, plan,
+                      g_err);
+    if (s != SA_OK) return s;
+    rec = sa_ctx::ForkRec{};
+    rec.n_dst = plan.n_dst;
+    rec.fresh_used = plan.fresh_used;
+    rec.n_copies = (int64_t)plan.copies.size();
+  }
+  const int64_t copy_blocks = rec.n_copies * layout->num_layers * 2;
+  const int64_t table_blocks = (std::max<int64_t>(rec.n_dst, num_children + 1) + 255) / 256;
+  if (copy_blocks + table_blocks > INT32_MAX) return fail(SA_ERR_SHAPE, "too many partial pages for these layers");
+  if (!h_fresh_used || !k_pool || !v_pool || !src.indptr || !d_dst_indptr || (rec.n_dst > 0 && !d_dst_indices) ||
+      (rec.n_dst > rec.fresh_used && !src.indices) || (rec.n_copies > 0 && !src.indices) ||
+      (rec.fresh_used > 0 && !d_fresh))
+    return fail(SA_ERR_NULL, "a device pointer or h_fresh_used is NULL");
+  if (!aligned16(k_pool) || !aligned16(v_pool)) return fail(SA_ERR_ALIGN, "pool pointer not 16-byte aligned");
+  DeviceGuard guard;
+  s = check_ctx(ctx);
+  if (s != SA_OK) return s;
+  s = refuse_capture((hipStream_t)stream, "sa_kv_fork");
+  if (s != SA_OK) return s;
+  if (debug_checks()) {
+    std::vector<int32_t> ip, ix, fresh((size_t)rec.fresh_used);
+    s = fetch_table(src.indptr, src.indices, batch, (hipStream_t)stream, ip, ix);
+    if (s != SA_OK) return s;
+    if (rec.fresh_used > 0)
+      SA_HIP(hipMemcpy(fresh.data(), d_fresh, sizeof(int32_t) * rec.fresh_used, hipMemcpyDeviceToHost));
+    s = sa::debug_check_fork(plan, ip.data(), ix.data(), fresh.data(), layout->num_slots, g_err);
+    if (s != SA_OK) return s;
+  }
+  uint8_t* dev = ctx->plans[kPlanFork].dev;
+  if (!same) {
+    PlanImage img;
+    rec.o_ch = img.add(plan.children.data(), plan.children.size());
+    rec.o_ip = img.add(plan.dst_indptr.data(), plan.dst_indptr.size());
+    rec.o_cp = img.add(plan.copies.data(), plan.copies.size());
+    s = upload_plan(ctx, kPlanFork, img, (hipStream_t)stream, &dev);
+    if (s != SA_OK) return s;
+    ctx->fork_rec = rec;
+    ctx->plans[kPlanFork].key_valid = true;
+  }
+  sa::ForkArgs a{};
+  a.k_pool = (uint16_t*)k_pool;
+  a.v_pool = (uint16_t*)v_pool;
+  a.children = (const sa::ForkChild*)(dev + rec.o_ch);
+  a.dst_indptr = (const int32_t*)(dev + rec.o_ip);
+  a.copies = (const int32_t*)(dev + rec.o_cp);
+  a.src_indptr = src.indptr;
+  a.src_indices = src.indices;
+  a.fresh = d_fresh;
+  a.out_indptr = d_dst_indptr;
+  a.out_indices = d_dst_indices;
+  a.ref = d_ref;
+  a.err = ctx->d_err;
+  a.num_slots = layout->num_slots;
+  a.slot_elems = slot_elems(layout);
+  a.layer_elems = layer_elems(layout);
+  a.n_dst = (int32_t)rec.n_dst;
+  a.C = num_children;
+  a.n_copies = (int32_t)rec.n_copies;
+  a.table_blocks = (int32_t)table_blocks;
+  a.Hkv = layout->num_kv_heads;
+  a.P = layout->page_size;
+  launch_timed(sa::fork_kernel, dim3((unsigned)(copy_blocks + table_blocks)), dim3(256), (hipStream_t)stream,
+               ctx->kernel_ev[SA_TIMED_PAGES], a);
+  SA_HIP(hipGetLastError());
+  *h_fresh_used = (int32_t)rec.fresh_used;
+  return SA_OK;
+}
+
+// Checks that the calls over counts have in common.
+sa_status check_counts(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_pages pages, int64_t max_entries,
+                       const int32_t* d_ref) {
+  sa_status s = check_layout(layout);
+  if (s != SA_OK) return s;
+  if (batch < 1) return fail(SA_ERR_SHAPE, "batch %d < 1", batch);
+  if (max_entries < 0) return fail(SA_ERR_SHAPE, "max_entries %lld", (long long)max_entries);
+  if (!pages.indptr || (max_entries > 0 && !pages.indices) || !d_ref)
+    return fail(SA_ERR_NULL, "a page table pointer or d_ref is NULL");
+  return check_ctx(ctx);
+}
+
+template <bool kUp>
+void launch_count(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_pages pages, int64_t max_entries,
+                  int32_t* d_ref, hipStream_t st) {
+  sa::CountArgs a{};
+  a.indptr = pages.indptr;
+  a.indices = pages.indices;
+  a.ref = d_ref;
+  a.err = ctx->d_err;
+  a.num_slots = layout->num_slots;
+  a.max_entries = max_entries;
+  a.batch = batch;
+  const int64_t blocks = std::min<int64_t>(std::max<int64_t>(1, (max_entries + 255) / 256), 1024);
+  launch_timed(sa::count_kernel<kUp>, dim3((unsigned)blocks), dim3(256), st, ctx->kernel_ev[SA_TIMED_PAGES], a);
+}
+
+sa_status kv_release(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_pages pages, int64_t max_entries,
+                     int32_t* d_ref, int32_t* d_free, int32_t* d_num_free, void* stream) {
+  DeviceGuard guard;
+  sa_status s = check_layout(layout);
+  if (s != SA_OK) return s;
+  if ((d_free == nullptr) != (d_num_free == nullptr))
+    return fail(SA_ERR_NULL, "give both d_free and d_num_free or neither");
+  s = check_counts(ctx, layout, batch, pages, max_entries, d_ref);
+  if (s != SA_OK) return s;
+  const hipStream_t st = (hipStream_t)stream;
+  const int chunks = (int)((layout->num_slots + sa::kScanChunk - 1) / sa::kScanChunk);
+  s = reserve_work(ctx, (size_t)chunks * sizeof(int32_t));
+  if (s != SA_OK) return s;
+  launch_count<false>(ctx, layout, batch, pages, max_entries, d_ref, st);
+  SA_HIP(hipGetLastError());
+  if (d_free == nullptr) return SA_OK;
+  sa::FreeArgs f{d_ref, d_free, d_num_free, (int32_t*)ctx->work, (int32_t)layout->num_slots, chunks};
+  hipLaunchKernelGGL(sa::free_count_kernel, dim3((unsigned)chunks), dim3(sa::kScanThreads), 0, st, f);
+  SA_HIP(hipGetLastError());
+  hipLaunchKernelGGL(sa::free_list_kernel, dim3((unsigned)chunks), dim3(sa::kScanThreads), 0, st, f);
+  SA_HIP(hipGetLastError());
+  return SA_OK;
+}
+
+sa_status kv_compact(sa_ctx* ctx, const sa_layout* layout, void* k_pool, void* v_pool, int32_t limit,
+                     const int32_t* d_ref, int32_t* d_ref_out, const int32_t* d_indices, int32_t* d_indices_out,
+                     int64_t num_entries, int32_t* d_slot_map, int32_t* d_moved, void* stream) {
+  DeviceGuard guard;
+  sa_status s = check_layout(layout);
+  if (s != SA_OK) return s;
+  if (limit < 0 || limit > layout->num_slots)
+    return fail(SA_ERR_RANGE, "limit %d outside [0, %lld]", limit, (long long)layout->num_slots);
+  if (num_entries < 0) return fail(SA_ERR_SHAPE, "num_entries %lld", (long long)num_entries);
+  if (!k_pool || !v_pool || !d_ref || !d_ref_out || !d_slot_map || !d_moved ||
+      (num_entries > 0 && (!d_indices || !d_indices_out)))
+    return fail(SA_ERR_NULL, "a device pointer is NULL");
+  if (!aligned16(k_pool) || !aligned16(v_pool)) return fail(SA_ERR_ALIGN, "pool pointer not 16-byte aligned");
+  s = check_ctx(ctx);
+  if (s != SA_OK) return s;
+  const hipStream_t st = (hipStream_t)stream;
+  const size_t n = (size_t)layout->num_slots;
+  const int chunks = (int)((n + sa::kScanChunk - 1) / sa::kScanChunk);
+  s = reserve_work(ctx, (4 * n + 2 * (size_t)chunks) * sizeof(int32_t));
+  if (s != SA_OK) return s;
+  sa::CompactArgs a{};
+  a.k_pool = (uint16_t*)k_pool;
+  a.v_pool = (uint16_t*)v_pool;
+  a.ref = d_ref;
+  a.ref_out = d_ref_out;
+  a.indices = d_indices;
+  a.indices_out = d_indices_out;
+  a.slot_map = d_slot_map;
+  a.moved = d_moved;
+  a.err = ctx->d_err;
+  a.rank = (int32_t*)ctx->work;
+  a.hole = a.rank + n;
+  a.mover = a.hole + n;
+  a.mover_ref = a.mover + n;
+  a.counts = a.mover_ref + n;
+  a.slot_elems = slot_elems(layout);
+  a.layer_elems = layer_elems(layout);
+  a.num_entries = num_entries;
+  a.num_slots = (int32_t)n;
+  a.limit = limit;
+  a.chunks = chunks;
+  a.num_layers = layout->num_layers;
+  hipLaunchKernelGGL(sa::compact_count_kernel, dim3((unsigned)chunks), dim3(sa::kScanThreads), 0, st, a);
+  SA_HIP(hipGetLastError());
+  hipLaunchKernelGGL(sa::compact_rank_kernel, dim3((unsigned)chunks), dim3(sa::kScanThreads), 0, st, a);
+  SA_HIP(hipGetLastError());
+  hipLaunchKernelGGL(sa::compact_map_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, a);
+  SA_HIP(hipGetLastError());
+  const int64_t most = std::min<int64_t>(limit, (int64_t)n - limit) * layout->num_layers * 2;
+  const int64_t blocks = std::min<int64_t>(std::max<int64_t>(std::max<int64_t>(most, (num_entries + 255) / 256), 1),
+                                           16 * (int64_t)ctx->num_cu);
+  launch_timed(sa::compact_move_kernel, dim3((unsigned)blocks), dim3(256), st, ctx->kernel_ev[SA_TIMED_PAGES], a);
+  SA_HIP(hipGetLastError());
+  return SA_OK;
+}
+
+template <int P>
+void launch_shared(bool pool_rsrc, dim3 grid, hipStream_t st, const hipEvent_t* ev, const sa::AttnArgs& a) {
+  if (pool_rsrc) launch_timed(sa::attn_shared_kernel<P, true>, grid, dim3(256), st, ev, a);
+  else launch_timed(sa::attn_shared_kernel<P, false>, grid, dim3(256), st, ev, a);
+}
+
+sa_status shared_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const void* q, const void* k_pool,
+                      const void* v_pool, int32_t batch, const int32_t* h_q_len, const int32_t* h_kv_len,
+                      sa_pages pages, int32_t num_groups, const int32_t* h_group_indptr, const int32_t* h_shared_len,
+                      float softmax_scale, void* o, float* lse, void* stream) {
+  sa_ctx::SharedRec rec;
+  std::vector<sa::SeqDesc> seqs;
+  bool same = false;
+  sa_status s = sa::check_attn_call(layout, layer, batch, h_q_len, h_kv_len, softmax_scale, g_err);
+  if (s != SA_OK) return s;
+  if (ctx && num_groups >= 1 && h_group_indptr && h_shared_len) {
+    sa_ctx::DevPlan& dp = ctx->plans[kPlanShared];
+    const int32_t head[4] = {layout->num_q_heads, layout->num_kv_heads, batch, num_groups};
+    dp.key.begin();
+    dp.key.add(head, 4);
+    dp.key.add(h_q_len, (size_t)batch);
+    dp.key.add(h_kv_len, (size_t)batch);
+    dp.key.add(h_group_indptr, (size_t)num_groups + 1);
+    dp.key.add(h_shared_len, (size_t)num_groups);
+    same = dp.reusable(dp.key.end(), (hipStream_t)stream) && !debug_checks();
+    if (!same) dp.key_valid = false;
+    rec = ctx->shared_rec;
+  }
+  if (!same) {
+    rec = sa_ctx::SharedRec{};
+    s = sa::plan_attn_check(layout, layer, batch, h_q_len, h_kv_len, softmax_scale, seqs, rec.total_q, g_err);
+    if (s != SA_OK) return s;
+    s = sa::check_groups(batch, h_q_len, h_kv_len, num_groups, h_group_indptr, h_shared_len, g_err);
+    if (s != SA_OK) return s;
+  }
+  if (rec.total_q > 0 && (!q || !o)) return fail(SA_ERR_NULL, "q / o is NULL");
+  if (!k_pool || !v_pool || !pages.indptr || !pages.indices)
+    return fail(SA_ERR_NULL, "pool or page table pointer is NULL");
+  if (!aligned16(q) || !aligned16(o) || !aligned16(k_pool) || !aligned16(v_pool) ||
+      (reinterpret_cast<uintptr_t>(lse) & 3u))
+    return fail(SA_ERR_ALIGN, "q, o, pools must be 16-byte aligned (lse 4-byte)");
+  DeviceGuard guard;
+  s = check_ctx(ctx);
+  if (s != SA_OK) return s;
+  if (rec.total_q == 0) return SA_OK;
+  s = refuse_capture((hipStream_t)stream, "sa_shared_prefix_attn");
+  if (s != SA_OK) return s;
+  sa::SharedPlan plan;
+  uint8_t* dev = ctx->plans[kPlanShared].dev;
+  if (!same) {
+    sa::plan_shared_items(layout, seqs, num_groups, h_group_indptr, h_shared_len, ctx->num_cu, plan);
+    rec.n_items = plan.items.size();
+    rec.n_units = plan.units.size();
+    rec.n_parts = plan.n_parts;
+    PlanImage img;
+    rec.o_it = img.add(plan.items.data(), plan.items.size());
+    rec.o_un = img.add(plan.units.data(), plan.units.size());
+    s = upload_plan(ctx, kPlanShared, img, (hipStream_t)stream, &dev);
+    if (s != SA_OK) return s;
+    ctx->shared_rec = rec;
+    ctx->plans[kPlanShared].key_valid = true;
+  }
+  s = reserve_parts(ctx, (size_t)rec.n_parts * kPartBytes);
+  if (s != SA_OK) return s;
+
+  sa::AttnArgs a{};
+  const int64_t lo = (int64_t)layer * layer_elems(layout);
+  a.q = (const uint16_t*)q;
+  a.k = (const uint16_t*)k_pool + lo;
+  a.v = (const uint16_t*)v_pool + lo;
+  a.o = (uint16_t*)o;
+  a.lse = lse;
+  a.part_o = ctx->part;
+  a.part_lse = ctx->part + (size_t)rec.n_parts * sa::kPipeRows * sa::kHD;
+  a.items = (const sa::AttnItem*)(dev + rec.o_it);
+  a.indptr = pages.indptr;
+  a.indices = pages.indices;
+  a.err = ctx->d_err;
+  a.num_slots = (int32_t)layout->num_slots;
+  a.n_items = (int32_t)rec.n_items;
+  a.Hq = layout->num_q_heads;
+  a.Hkv = layout->num_kv_heads;
+  a.G = a.Hq / a.Hkv;
+  a.c = softmax_scale * 1.4426950408889634f;
+  const bool pool_rsrc = layer_elems(layout) * 2 < ((int64_t)1 << 31);
+  const dim3 grid((unsigned)rec.n_items);
+  if (layout->page_size == 16) launch_shared<16>(pool_rsrc, grid, (hipStream_t)stream, ctx->kernel_ev[SA_TIMED_ATTN], a);
+  else launch_shared<32>(pool_rsrc, grid, (hipStream_t)stream, ctx->kernel_ev[SA_TIMED_ATTN], a);
+  SA_HIP(hipGetLastError());
+  if (rec.n_units > 0) {
+    sa::MergeRowsArgs m{a.part_o, a.part_lse, (const sa::MergeUnit*)(dev + rec.o_un), a.o, lse, a.Hq, a.G};
+    hipLaunchKernelGGL(sa::merge_rows_kernel, dim3((unsigned)rec.n_units), dim3(256), 0, (hipStream_t)stream, m);
+    SA_HIP(hipGetLastError());
+  }
+  return SA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+sa_status sa_kv_append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const sa_rope* rope, const void* q,
+                            int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new,
+                            int64_t v_stride, void* q_out, void* k_pool, void* v_pool, int32_t batch,
+                            const int32_t* h_start, const int32_t* h_new_len, const int32_t* h_pos, sa_pages pages,
+                            void* stream) {
+  return no_throw([&] {
+    return append_rope(ctx, layout, layer, rope, q, q_stride, k_new, k_stride, v_new, v_stride, q_out, k_pool, v_pool,
+                       batch, h_start, h_new_len, h_pos, pages, stream);
+  });
+}
+
+sa_status sa_kv_fork(sa_ctx* ctx, const sa_layout* layout, void* k_pool, void* v_pool, int32_t batch,
+                     const int32_t* h_src_len, int32_t num_children, const int32_t* h_parent,
+                     const int32_t* h_reserve, sa_pages src, const int32_t* d_fresh, int32_t num_fresh,
+                     int32_t* d_dst_indptr, int32_t* d_dst_indices, int32_t dst_capacity, int32_t* d_ref,
+                     int32_t* h_fresh_used, void* stream) {
+  return no_throw([&] {
+    return kv_fork(ctx, layout, k_pool, v_pool, batch, h_src_len, num_children, h_parent, h_reserve, src, d_fresh,
+                   num_fresh, d_dst_indptr, d_dst_indices, dst_capacity, d_ref, h_fresh_used, stream);
+  });
+}
+
+sa_status sa_kv_retain(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_pages pages, int64_t max_entries,
+                       int32_t* d_ref, void* stream) {
+  return no_throw([&] {
+    DeviceGuard guard;
+    const sa_status s = check_counts(ctx, layout, batch, pages, max_entries, d_ref);
+    if (s != SA_OK) return s;
+    launch_count<true>(ctx, layout, batch, pages, max_entries, d_ref, (hipStream_t)stream);
+    SA_HIP(hipGetLastError());
+    return SA_OK;
+  });
+}
+
+sa_status sa_kv_release(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_pages pages, int64_t max_entries,
+                        int32_t* d_ref, int32_t* d_free, int32_t* d_num_free, void* stream) {
+  return no_throw(
+      [&] { return kv_release(ctx, layout, batch, pages, max_entries, d_ref, d_free, d_num_free, stream); });
+}
+
+sa_status sa_kv_compact(sa_ctx* ctx, const sa_layout* layout, void* k_pool, void* v_pool, int32_t limit,
+                        const int32_t* d_ref, int32_t* d_ref_out, const int32_t* d_indices, int32_t* d_indices_out,
+                        int64_t num_entries, int32_t* d_slot_map, int32_t* d_moved, void* stream) {
+  return no_throw([&] {
+    return kv_compact(ctx, layout, k_pool, v_pool, limit, d_ref, d_ref_out, d_indices, d_indices_out, num_entries,
+                      d_slot_map, d_moved, stream);
+  });
+}
+
+sa_status sa_shared_prefix_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const void* q,
+                                const void* k_pool, const void* v_pool, int32_t batch, const int32_t* h_q_len,
+                                const int32_t* h_kv_len, sa_pages pages, int32_t num_groups,
+                                const int32_t* h_group_indptr, const int32_t* h_shared_len, float softmax_scale,
+                                void* o, float* lse, void* stream) {
+  return no_throw([&] {
+    return shared_attn(ctx, layout, layer, q, k_pool, v_pool, batch, h_q_len, h_kv_len, pages, num_groups,
+                       h_group_indptr, h_shared_len, softmax_scale, o, lse, stream);
+  });
 }
 
 }  // extern "C"
