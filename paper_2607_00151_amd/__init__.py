@@ -475,12 +475,21 @@ def sa_segment_prefill_attn_append(ctx, layout: Layout, layer: int, q, k_pool, v
 
 # ---------------------------------------------------------------- branches of one context
 
-def _same_device(ctx, *tensors):
-    """The branch calls run on ctx's device: a tensor elsewhere is refused rather than read there."""
-    if isinstance(ctx, Context):
-        for t in tensors:
-            if t is not None and hasattr(t, "device") and t.is_cuda and t.device.index != ctx.device:
-                raise ValueError(f"a tensor is on {t.device}, the context on device {ctx.device}")
+def _device_of(ctx):
+    """ctx's device, or None where it is only a handle."""
+    return ctx.device if isinstance(ctx, Context) else None
+
+
+def _on(t, what: str, kind: str, min_numel: int, device, nullable: bool = False):
+    """_dev for the branch calls, which run on ctx's device: a tensor elsewhere is refused rather than read there.
+    One pass of the cheap tests for the usual case; _dev names what is wrong with any other."""
+    if t is not None and device is not None and _KINDS is not None and isinstance(t, _torch.Tensor):
+        at = t.get_device()
+        if at == device and t.dtype in _KINDS[kind] and t.is_contiguous() and t.numel() >= min_numel:
+            return t.data_ptr() or None
+        if at >= 0 and at != device:
+            raise ValueError(f"{what}: the tensor is on device {at}, the context on device {device}")
+    return _dev(t, what, kind, min_numel, nullable)
 
 
 def _stream_of(ctx, stream):
@@ -493,22 +502,26 @@ def _stream_of(ctx, stream):
     return _stream(stream)
 
 
-def _head_rows(t, what: str, tokens: int, heads: int, d: int):
+def _head_rows(t, what: str, tokens: int, heads: int, d: int, device):
     """(address, token stride in elements) of a [tokens][heads][d] tensor whose heads are contiguous within a token."""
     if tokens == 0:
         return (None if t is None else t.data_ptr() or None), heads * d
     torch = _torch or _load_torch()
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{what}: a device tensor is required")
-    if not t.is_cuda:
+    at = t.get_device()
+    if at < 0:
         raise ValueError(f"{what}: tensor is not on a GPU")
+    if device is not None and at != device:
+        raise ValueError(f"{what}: the tensor is on device {at}, the context on device {device}")
     if t.dtype not in _KINDS["b16"]:
         raise ValueError(f"{what}: dtype {t.dtype}, expected a 2-byte dtype (bf16 bits)")
-    if t.dim() != 3 or t.shape[0] < tokens or t.shape[1] != heads or t.shape[2] != d:
-        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected ({tokens}, {heads}, {d})")
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] < tokens or shape[1] != heads or shape[2] != d:
+        raise ValueError(f"{what}: shape {tuple(shape)}, expected ({tokens}, {heads}, {d})")
+    if stride[2] != 1 or (heads > 1 and stride[1] != d):
         raise ValueError(f"{what}: the heads of a token must be contiguous")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * d
+    return t.data_ptr(), stride[0] if shape[0] > 1 else heads * d
 
 
 class Rope:
@@ -521,10 +534,12 @@ class Rope:
         self.q_weight, self.k_weight = q_weight, k_weight
         self.eps, self.interleaved, self.weight_offset = float(eps), bool(interleaved), float(weight_offset)
 
-    def _struct(self, d: int):
-        return _Rope(2 * len(self.inv_freq), int(self.interleaved), self.inv_freq.ctypes.data if len(self.inv_freq) else None,
-                     _dev(self.q_weight, "q_weight", "b16", d, nullable=True),
-                     _dev(self.k_weight, "k_weight", "b16", d, nullable=True), self.eps, self.weight_offset)
+    def _struct(self, d: int, device):
+        n = len(self.inv_freq)
+        return _Rope(2 * n, self.interleaved, self.inv_freq.ctypes.data if n else None,
+                     None if self.q_weight is None else _on(self.q_weight, "q_weight", "b16", d, device),
+                     None if self.k_weight is None else _on(self.k_weight, "k_weight", "b16", d, device), self.eps,
+                     self.weight_offset)
 
 
 def sa_kv_append_rope(ctx, layout: Layout, layer: int, rope: Rope, q, k_new, v_new, q_out, k_pool, v_pool, start,
@@ -536,19 +551,22 @@ def sa_kv_append_rope(ctx, layout: Layout, layer: int, rope: Rope, q, k_new, v_n
     pos = None if pos is None else _host_i32(pos)
     if start.shape != new_len.shape or (pos is not None and pos.shape != start.shape):
         raise ValueError("start, new_len and pos differ in length")
-    B, T, D = len(new_len), max(0, _total(new_len)), int(layout.head_dim)
-    Hq, Hkv = int(layout.num_q_heads), int(layout.num_kv_heads)
-    _same_device(ctx, q, k_new, v_new, q_out, k_pool, v_pool, rope.q_weight, rope.k_weight, pages_indptr, pages_indices)
-    qp, qs = _head_rows(q, "q", T, Hq, D)
-    kp, ks = _head_rows(k_new, "k_new", T, Hkv, D)
-    vp, vs = _head_rows(v_new, "v_new", T, Hkv, D)
+    B, T, D, at = len(new_len), max(0, _total(new_len)), layout.head_dim, _device_of(ctx)
+    Hq, Hkv = layout.num_q_heads, layout.num_kv_heads
+    qp, qs = _head_rows(q, "q", T, Hq, D, at)
+    kp, ks = _head_rows(k_new, "k_new", T, Hkv, D, at)
+    vp, vs = _head_rows(v_new, "v_new", T, Hkv, D, at)
     n = _pool_numel(layout)
-    r = rope._struct(D)
     _check(load_library().sa_kv_append_rope(
-        _ctx_handle(ctx), ctypes.byref(layout), int(layer), ctypes.byref(r), qp, qs, kp, ks, vp, vs,
-        _dev(q_out, "q_out", "b16", T * Hq * D, nullable=T == 0), _dev(k_pool, "k_pool", "b16", n),
-        _dev(v_pool, "v_pool", "b16", n), int(B), _ptr(start), _ptr(new_len), _ptr(pos),
-        _pages(pages_indptr, pages_indices, B), _stream_of(ctx, stream)))
+        _ctx_handle(ctx), ctypes.byref(layout), int(layer), ctypes.byref(rope._struct(D, at)), qp, qs, kp, ks, vp, vs,
+        _on(q_out, "q_out", "b16", T * Hq * D, at, nullable=T == 0), _on(k_pool, "k_pool", "b16", n, at),
+        _on(v_pool, "v_pool", "b16", n, at), B, _ptr(start), _ptr(new_len), _ptr(pos),
+        _table_on(pages_indptr, pages_indices, B, at, "page table"), _stream_of(ctx, stream)))
+
+
+def _table_on(indptr, indices, batch: int, device, what: str, nullable: bool = False):
+    return _Pages(_on(indptr, f"{what} indptr", "i32", batch + 1, device),
+                  _on(indices, f"{what} indices", "i32", 0, device, nullable))
 
 
 def sa_kv_fork(ctx, layout: Layout, k_pool, v_pool, src_len, parent, reserve, src_indptr, src_indices, fresh,
@@ -558,26 +576,23 @@ def sa_kv_fork(ctx, layout: Layout, k_pool, v_pool, src_len, parent, reserve, sr
     src_len, parent, reserve = _host_i32(src_len), _host_i32(parent), _host_i32(reserve)
     if parent.shape != reserve.shape:
         raise ValueError("parent and reserve differ in length")
-    B, C, n = len(src_len), len(parent), _pool_numel(layout)
-    _same_device(ctx, k_pool, v_pool, src_indptr, src_indices, fresh, dst_indptr, dst_indices, ref)
-    used = np.zeros(1, dtype=np.int32)
+    B, C, n, at = len(src_len), len(parent), _pool_numel(layout), _device_of(ctx)
+    used = ctypes.c_int32(0)
     _check(load_library().sa_kv_fork(
-        _ctx_handle(ctx), ctypes.byref(layout), _dev(k_pool, "k_pool", "b16", n), _dev(v_pool, "v_pool", "b16", n),
-        int(B), _ptr(src_len), int(C), _ptr(parent), _ptr(reserve),
-        _Pages(_dev(src_indptr, "src indptr", "i32", B + 1), _dev(src_indices, "src indices", "i32", 0, nullable=True)),
-        _dev(fresh, "fresh", "i32", 0, nullable=True), 0 if fresh is None else int(fresh.numel()),
-        _dev(dst_indptr, "dst indptr", "i32", C + 1), _dev(dst_indices, "dst indices", "i32", 0, nullable=True),
-        0 if dst_indices is None else int(dst_indices.numel()),
-        _dev(ref, "ref", "i32", int(layout.num_slots), nullable=True), _ptr(used), _stream_of(ctx, stream)))
-    return int(used[0])
+        _ctx_handle(ctx), ctypes.byref(layout), _on(k_pool, "k_pool", "b16", n, at), _on(v_pool, "v_pool", "b16", n, at),
+        B, _ptr(src_len), C, _ptr(parent), _ptr(reserve), _table_on(src_indptr, src_indices, B, at, "src", True),
+        _on(fresh, "fresh", "i32", 0, at, nullable=True), 0 if fresh is None else fresh.numel(),
+        _on(dst_indptr, "dst indptr", "i32", C + 1, at), _on(dst_indices, "dst indices", "i32", 0, at, nullable=True),
+        0 if dst_indices is None else dst_indices.numel(),
+        _on(ref, "ref", "i32", layout.num_slots, at, nullable=True), ctypes.addressof(used), _stream_of(ctx, stream)))
+    return used.value
 
 
 def _count_args(ctx, layout, pages_indptr, pages_indices, ref):
-    _same_device(ctx, pages_indptr, pages_indices, ref)
-    ip = _dev(pages_indptr, "page table indptr", "i32", 2)
-    return (_ctx_handle(ctx), ctypes.byref(layout), int(pages_indptr.numel()) - 1,
-            _Pages(ip, _dev(pages_indices, "page table indices", "i32", 0)), int(pages_indices.numel()),
-            _dev(ref, "ref", "i32", int(layout.num_slots)))
+    at = _device_of(ctx)
+    table = _table_on(pages_indptr, pages_indices, 1, at, "page table")
+    return (_ctx_handle(ctx), ctypes.byref(layout), pages_indptr.numel() - 1, table, pages_indices.numel(),
+            _on(ref, "ref", "i32", layout.num_slots, at))
 
 
 def sa_kv_retain(ctx, layout: Layout, pages_indptr, pages_indices, ref, stream=None):
@@ -589,10 +604,10 @@ def sa_kv_retain(ctx, layout: Layout, pages_indptr, pages_indices, ref, stream=N
 def sa_kv_release(ctx, layout: Layout, pages_indptr, pages_indices, ref, free=None, num_free=None, stream=None):
     """Lowers the count of every slot that the tables name; free [num_slots] then lists the slots without a count,
     ascending, and num_free [1] says how many."""
-    _same_device(ctx, free, num_free)
+    at = _device_of(ctx)
     _check(load_library().sa_kv_release(
         *_count_args(ctx, layout, pages_indptr, pages_indices, ref),
-        _dev(free, "free", "i32", int(layout.num_slots), nullable=True), _dev(num_free, "num_free", "i32", 1, nullable=True),
+        _on(free, "free", "i32", layout.num_slots, at, nullable=True), _on(num_free, "num_free", "i32", 1, at, nullable=True),
         _stream_of(ctx, stream)))
 
 
@@ -600,15 +615,14 @@ def sa_kv_compact(ctx, layout: Layout, k_pool, v_pool, limit: int, ref, ref_out,
                   stream=None):
     """Moves the pages in use in slots >= limit into free slots below.  ref_out and indices_out may be ref and
     indices; slot_map [num_slots] receives where each slot's page is, moved [2] the pages moved and left."""
-    _same_device(ctx, k_pool, v_pool, ref, ref_out, indices, indices_out, slot_map, moved)
-    n, slots = _pool_numel(layout), int(layout.num_slots)
-    entries = 0 if indices is None else int(indices.numel())
+    n, slots, at = _pool_numel(layout), layout.num_slots, _device_of(ctx)
+    entries = 0 if indices is None else indices.numel()
     _check(load_library().sa_kv_compact(
-        _ctx_handle(ctx), ctypes.byref(layout), _dev(k_pool, "k_pool", "b16", n), _dev(v_pool, "v_pool", "b16", n),
-        int(limit), _dev(ref, "ref", "i32", slots), _dev(ref_out, "ref_out", "i32", slots),
-        _dev(indices, "indices", "i32", 0, nullable=entries == 0),
-        _dev(indices_out, "indices_out", "i32", entries, nullable=entries == 0), entries,
-        _dev(slot_map, "slot_map", "i32", slots), _dev(moved, "moved", "i32", 2), _stream_of(ctx, stream)))
+        _ctx_handle(ctx), ctypes.byref(layout), _on(k_pool, "k_pool", "b16", n, at), _on(v_pool, "v_pool", "b16", n, at),
+        int(limit), _on(ref, "ref", "i32", slots, at), _on(ref_out, "ref_out", "i32", slots, at),
+        _on(indices, "indices", "i32", 0, at, nullable=entries == 0),
+        _on(indices_out, "indices_out", "i32", entries, at, nullable=entries == 0), entries,
+        _on(slot_map, "slot_map", "i32", slots, at), _on(moved, "moved", "i32", 2, at), _stream_of(ctx, stream)))
 
 
 def sa_shared_prefix_attn(ctx, layout: Layout, layer: int, q, k_pool, v_pool, q_len, kv_len, pages_indptr,
@@ -621,11 +635,11 @@ def sa_shared_prefix_attn(ctx, layout: Layout, layer: int, q, k_pool, v_pool, q_
         raise ValueError("q_len and kv_len differ in length")
     if len(groups) != len(shared) + 1:
         raise ValueError("group_indptr must have one entry more than shared_len")
-    _same_device(ctx, q, k_pool, v_pool, pages_indptr, pages_indices, o, lse)
-    qp, op, lp, _ = _attn_dev(layout, q_len, q, o, lse)
-    n = _pool_numel(layout)
+    B, T, at, n = len(q_len), max(0, _total(q_len)), _device_of(ctx), _pool_numel(layout)
+    rows = T * layout.num_q_heads
     _check(load_library().sa_shared_prefix_attn(
-        _ctx_handle(ctx), ctypes.byref(layout), int(layer), qp, _dev(k_pool, "k_pool", "b16", n),
-        _dev(v_pool, "v_pool", "b16", n), int(len(q_len)), _ptr(q_len), _ptr(kv_len),
-        _pages(pages_indptr, pages_indices, len(q_len)), int(len(shared)), _ptr(groups), _ptr(shared),
-        float(softmax_scale), op, lp, _stream_of(ctx, stream)))
+        _ctx_handle(ctx), ctypes.byref(layout), int(layer), _on(q, "q", "b16", rows * layout.head_dim, at, T == 0),
+        _on(k_pool, "k_pool", "b16", n, at), _on(v_pool, "v_pool", "b16", n, at), B, _ptr(q_len), _ptr(kv_len),
+        _table_on(pages_indptr, pages_indices, B, at, "page table"), len(shared), _ptr(groups), _ptr(shared),
+        float(softmax_scale), _on(o, "o", "b16", rows * layout.head_dim, at, T == 0),
+        None if lse is None else _on(lse, "lse", "f32", rows, at), _stream_of(ctx, stream)))

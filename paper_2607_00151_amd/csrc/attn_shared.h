@@ -44,70 +44,97 @@ struct MergeRowsArgs {
   const MergeUnit* units;
   uint16_t* o;
   float* lse;                // nullable
-  int32_t Hq, G;
+  int32_t Hq, G, block_rows;
 };
 
-// One block per unit: half a wave (32 threads, four d each) per row, and with
-// at most four rows several half waves share a row's parts and meet in LDS.
+__device__ __forceinline__ float half_max(float x) {
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor(x, d));
+  return x;
+}
+__device__ __forceinline__ float half_sum(float x) {
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) x += __shfl_xor(x, d);
+  return x;
+}
+
+// Block (unit, y): rows block_rows y .. of the unit, 8 / block_rows half waves
+// (32 threads, four d each) per row, which share the row's parts and meet in LDS.
+// A half wave takes its parts 32 at a time: lane c has the c-th one's weight, and
+// the partial rows are loaded eight ahead of their use.  With block_rows = 1, 2,
+// 4 or 8 by the most parts of a row (merge_block_rows) a half wave has at most
+// about eight parts, whose loads are all in flight at once: the launch is bound
+// by that latency.  32 branches of 16K, 33 parts a row: TODO
 __global__ __launch_bounds__(256) void merge_rows_kernel(MergeRowsArgs a) {
   __shared__ f32x4 red[8][32];
   __shared__ float red_m[8], red_den[8];
   const MergeUnit u = ld_uniform(a.units + blockIdx.x);
-  const int hw = threadIdx.x >> 5, c = threadIdx.x & 31;
-  const int nsub = u.n >= 8 ? 1 : 8 / (u.n > 4 ? 8 : u.n > 2 ? 4 : u.n);   // half waves per row
+  const int r0 = blockIdx.y * a.block_rows;
+  if (r0 >= u.n) return;
+  const int lane = threadIdx.x & 63, hw = threadIdx.x >> 5, c = threadIdx.x & 31;
+  const int nsub = 8 / a.block_rows;
   const int sub = hw % nsub;
-  const int np = u.a_n + u.b_n;
-  for (int r0 = 0; r0 < u.n; r0 += 8 / nsub) {
-    const int r = r0 + hw / nsub;
-    const bool mine = r < u.n;
-    float mx = -INFINITY, den = 0.f;
-    f32x4 num = f32x4{};
-    auto row_of = [&](int s) {
-      return s < u.a_n ? (int64_t)(u.a_part + s) * kPipeRows + u.a_row + r
-                       : (int64_t)(u.b_part + s - u.a_n) * kPipeRows + u.b_row + r;
+  const int r = r0 + hw / nsub;
+  const bool mine = r < u.n;
+  const int np = mine ? u.a_n + u.b_n : 0;
+  auto row_of = [&](int s) {
+    return s < u.a_n ? (int64_t)(u.a_part + s) * kPipeRows + u.a_row + r
+                     : (int64_t)(u.b_part + s - u.a_n) * kPipeRows + u.b_row + r;
+  };
+  float mx = -INFINITY, den = 0.f;
+  f32x4 num = f32x4{};
+  constexpr int kAhead = 8;
+  for (int s0 = sub; s0 < np; s0 += 32 * nsub) {
+    const int n = min(32, (np - s0 + nsub - 1) / nsub);      // parts of this round
+    f32x4 x[kAhead];
+    auto load = [&](int k0) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (k0 + k < n) x[k] = *(const f32x4*)(a.part_o + row_of(s0 + (k0 + k) * nsub) * kHD + 4 * c);
     };
-    if (mine) {
-      for (int s = sub; s < np; s += nsub) mx = fmaxf(mx, a.part_lse[row_of(s)]);
-      const float off = mx == -INFINITY ? 0.f : mx;
-      for (int s = sub; s < np; s += nsub) {
-        const int64_t p = row_of(s);
-        const float w = exp2f_fast(a.part_lse[p] - off);
-        den += w;
-        num += w * *(const f32x4*)(a.part_o + p * kHD + 4 * c);
-      }
-    }
-    if (nsub > 1) {
-      red[hw][c] = num;
-      if (c == 0) {
-        red_m[hw] = mx;
-        red_den[hw] = den;
-      }
-      __syncthreads();
-      if (mine && sub == 0) {
-        float all = mx;
-        for (int k = 1; k < nsub; ++k) all = fmaxf(all, red_m[hw + k]);
-        const float off = all == -INFINITY ? 0.f : all;
-        float f = exp2f_fast(mx - off);
-        num *= f;
-        den *= f;
-        for (int k = 1; k < nsub; ++k) {
-          f = exp2f_fast(red_m[hw + k] - off);
-          num += f * red[hw + k][c];
-          den += f * red_den[hw + k];
-        }
-        mx = all;
-      }
-      __syncthreads();
-    }
-    if (mine && sub == 0) {
-      const float inv = den > 0.f ? 1.f / den : 0.f;
-      const int row = u.r0 + r, tok = row / a.G;
-      const int64_t orow = (int64_t)(u.q_start + tok) * a.Hq + u.kvh * a.G + (row - tok * a.G);
-      st_bf16x4(a.o + orow * kHD + 4 * c, num[0] * inv, num[1] * inv, num[2] * inv, num[3] * inv);
-      if (a.lse != nullptr && c == 0)
-        a.lse[orow] = den > 0.f ? (mx + __builtin_amdgcn_logf(den)) * 0.69314718055994531f : -INFINITY;
+    load(0);
+    const float l = c < n ? a.part_lse[row_of(s0 + c * nsub)] : -INFINITY;
+    const float m_new = fmaxf(mx, half_max(l));
+    const float off = m_new == -INFINITY ? 0.f : m_new;
+    const float f = exp2f_fast(mx - off), w = exp2f_fast(l - off);
+    num *= f;
+    den = den * f + half_sum(w);
+    mx = m_new;
+    for (int k0 = 0; k0 < n; k0 += kAhead) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (k0 + k < n) num += __shfl(w, (lane & 32) + k0 + k) * x[k];
+      load(k0 + kAhead);
     }
   }
+  if (nsub > 1) {
+    red[hw][c] = num;
+    if (c == 0) {
+      red_m[hw] = mx;
+      red_den[hw] = den;
+    }
+    __syncthreads();
+    if (!mine || sub != 0) return;
+    float all = mx;
+    for (int k = 1; k < nsub; ++k) all = fmaxf(all, red_m[hw + k]);
+    const float off = all == -INFINITY ? 0.f : all;
+    float f = exp2f_fast(mx - off);
+    num *= f;
+    den *= f;
+    for (int k = 1; k < nsub; ++k) {
+      f = exp2f_fast(red_m[hw + k] - off);
+      num += f * red[hw + k][c];
+      den += f * red_den[hw + k];
+    }
+    mx = all;
+  }
+  if (!mine) return;
+  const float inv = den > 0.f ? 1.f / den : 0.f;
+  const int row = u.r0 + r, tok = row / a.G;
+  const int64_t orow = (int64_t)(u.q_start + tok) * a.Hq + u.kvh * a.G + (row - tok * a.G);
+  st_bf16x4(a.o + orow * kHD + 4 * c, num[0] * inv, num[1] * inv, num[2] * inv, num[3] * inv);
+  if (a.lse != nullptr && c == 0)
+    a.lse[orow] = den > 0.f ? (mx + __builtin_amdgcn_logf(den)) * 0.69314718055994531f : -INFINITY;
 }
 
 }  // namespace sa

@@ -108,12 +108,14 @@ struct MergeUnit {
   int32_t b_part, b_n, b_row;
 };
 constexpr int kMergeUnitRows = 32;     // most rows of a unit
+// rows per block of the merge, for rows of at most so many parts
+inline int merge_block_rows(int most_parts) { return most_parts <= 8 ? 8 : most_parts <= 16 ? 4 : most_parts <= 32 ? 2 : 1; }
 
 struct SharedPlan {
   std::vector<AttnItem> items;         // one per workgroup, in launch order
   std::vector<MergeUnit> units;
   int32_t n_parts = 0;
-  int64_t total_q = 0;
+  int32_t most_rows = 0, most_parts = 0;   // of a unit
   bool any_shared = false;             // some group's prefix is computed once for its members
 };
 
@@ -134,6 +136,68 @@ inline sa_status check_groups(int32_t batch, const int32_t* h_q_len, const int32
                          h_shared_len[g], h_kv_len[b] - h_q_len[b], b);
   }
   return SA_OK;
+}
+
+// What the choice of a chunk needs of a row tile (of one KV head; the others are alike).
+struct SharedShape {
+  int64_t tiles;             // 64-key tiles
+  int32_t rows;
+  bool decode;               // takes the kernel's path for few rows
+  bool streams;              // reads its keys from memory (a group's other row tiles find them in L2)
+};
+
+// Time of the launches at a chunk size, in units of 10 ns.
+inline int64_t shared_chunk_cost(const std::vector<SharedShape>& shapes, int Hkv, int num_cu, int most_parts, int64_t c) {
+  struct Run {
+    int64_t time, blocks;
+  };
+  std::vector<Run> runs;
+  int64_t n = 0, streamed = 0, part_rows = 0;
+  for (const SharedShape& s : shapes) {
+    const int64_t k = std::max<int64_t>(1, std::min<int64_t>((s.tiles + c - 1) / c, most_parts));
+    n += k * Hkv;
+    part_rows += k * Hkv * s.rows;
+    if (s.streams) streamed += s.tiles * Hkv;
+  }
+  for (const SharedShape& s : shapes) {
+    const int64_t k = std::max<int64_t>(1, std::min<int64_t>((s.tiles + c - 1) / c, most_parts));
+    const int64_t t = s.decode ? 80 : n > num_cu ? 187 : 112;
+    runs.push_back({(s.tiles + k - 1) / k * t + 400, k * Hkv});
+  }
+  std::sort(runs.begin(), runs.end(), [](const Run& x, const Run& y) { return x.time > y.time; });
+  // the busiest of the slots: the mean, and of any k slots + 1 longest blocks some slot has k + 1
+  const int64_t slots = (n > num_cu ? 2 : 1) * (int64_t)num_cu;
+  int64_t sum = 0, before = 0, busy = 0;
+  for (const Run& r : runs) {
+    sum += r.time * r.blocks;
+    const int64_t last = before + r.blocks - 1;              // index of the run's last block
+    busy = std::max(busy, (last / slots + 1) * r.time);
+    before += r.blocks;
+  }
+  busy = std::max(busy, sum / slots);
+  const int64_t stream = streamed * 546 / 1000;
+  return std::max(busy, stream) + std::min(busy, stream) / 4 + 300 + part_rows * 1032 / 45000;
+}
+
+inline int64_t choose_shared_chunk(const std::vector<SharedShape>& shapes, int Hkv, int num_cu, int most_parts) {
+  int64_t longest = 1, total = 0;
+  for (const SharedShape& s : shapes) {
+    longest = std::max(longest, s.tiles);
+    total += s.tiles * Hkv;
+  }
+  int64_t best = INT64_MAX, chunk = longest;
+  auto consider = [&](int64_t c) {
+    c = std::min(std::max<int64_t>(c, 4), longest);
+    const int64_t t = shared_chunk_cost(shapes, Hkv, num_cu, most_parts, c);
+    if (t < best) {
+      best = t;
+      chunk = c;
+    }
+  };
+  // equal parts of the longest tile, as many as there is room for
+  const int64_t most = std::min<int64_t>(64, (longest + 3) / 4);
+  for (int64_t k = 1; k <= most; k += 1 + k / 8) consider((longest + k - 1) / k);
+  return chunk;
 }
 
 // The launch's work items.  A group whose prefix is computed once gives row
@@ -195,24 +259,14 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
       at += n;
     }
   }
-  // key-range parts: the smallest chunk whose blocks are two per CU
-  int64_t longest = 1;
-  for (const Tile& t : tiles) longest = std::max(longest, t.tiles());
+  // Key-range parts of one chunk size: of a few, the one that the model ends first.
   auto parts_of = [](const Tile& t, int64_t c) {
     return std::max<int64_t>(1, std::min<int64_t>((t.tiles() + c - 1) / c, kMaxItemParts));
   };
-  auto blocks = [&](int64_t c) {
-    int64_t n = 0;
-    for (const Tile& t : tiles) n += parts_of(t, c) * Hkv;
-    return n;
-  };
-  const int64_t slots = std::max<int64_t>(2 * num_cu, (int64_t)tiles.size() * Hkv + num_cu);
-  int64_t lo = std::min<int64_t>(4, longest), hi = longest;
-  while (lo < hi) {
-    const int64_t mid = lo + (hi - lo) / 2;
-    if (blocks(mid) <= slots) hi = mid; else lo = mid + 1;
-  }
-  const int64_t chunk = lo;
+  std::vector<SharedShape> shapes;
+  for (const Tile& t : tiles)
+    shapes.push_back({t.tiles(), t.rows, t.q_len * G <= kDecodeRows, !t.prefix || t.row0 == 0});
+  const int64_t chunk = choose_shared_chunk(shapes, Hkv, num_cu, kMaxItemParts);
   for (const Member& m : members) {
     const int32_t n = seqs[m.seq].q_len * G;
     for (int32_t r0 = 0, t = m.own0; r0 < n; r0 += kRows, ++t) {
@@ -286,7 +340,10 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
         }
         u.n = e - r;
         r = e;
-        if (own.part0 >= 0) out.units.push_back(u);
+        if (own.part0 < 0) continue;
+        out.units.push_back(u);
+        out.most_rows = std::max(out.most_rows, u.n);
+        out.most_parts = std::max(out.most_parts, u.a_n + u.b_n);
       }
   }
 }

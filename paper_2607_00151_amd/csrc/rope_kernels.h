@@ -13,11 +13,15 @@
 // phase (one integer multiply), of which the top 32 bits, signed, go to fp32 and
 // to v_sin / v_cos, whose arguments are turns.
 //
-// Bytes are all this does (2 * 256 per head row, read and written once): a row is
-// 16 lanes of 16 bytes, a wave takes 16 rows of one token, all its loads first.
-// The sum of squares is a 4-step DPP reduction within the 16 lanes, and the
-// sines and cosines, which depend only on token and dim, are made once per lane
-// for the wave's rows.
+// Bytes are the floor (2 * 256 per head row, read and written once), but at 16
+// lanes of 16 bytes a row the vector instructions per row come close behind, so
+// everything that depends only on token and dim is made once per wave: with
+// G = w + offset, r = rsqrt(...) and the partner's value p (of the same row)
+//   out = r * (x * (G cos) + p * (+-G' sin)),
+// the two products per dim of one token, for query and for key heads.  A wave
+// takes 16 head rows at a time of one token, the next 16 in flight, for as many
+// rounds as leave the chip enough waves; the sum of squares is a 4-step DPP
+// reduction within a row's 16 lanes.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -46,13 +50,13 @@ struct RopeArgs {
   int32_t* err;
   int64_t num_slots;
   int32_t T, B, Hq, Hkv, P;
-  int32_t half_lanes;        // pairs (d, d + rot/2): rot / 16; interleaved: unused
   int32_t rot;
+  int32_t rounds;            // rounds of kRopeRows head rows per wave
   float eps, offset;
   uint64_t freq[64];         // turns per position, as a fraction of 2^64
 };
 
-constexpr int kRopeRows = 16;        // head rows per wave: 4 loads of 16 bytes per lane
+constexpr int kRopeRows = 16;        // head rows of a round: 4 loads of 16 bytes per lane
 
 // Largest b with tok_begin[b] <= t, by the whole wave: 64 probes per round.
 __device__ __forceinline__ int wave_find_seq(const int32_t* tok_begin, int B, int t) {
@@ -90,33 +94,43 @@ __device__ __forceinline__ void unpack8(u32x4 w, float (&x)[8]) {
   }
 }
 
-template <bool kInterleaved>
+// kPair: where a dim's partner is -- in the same lane (dims 2d, 2d + 1), 8 lanes
+// on (d, d + 64: a DPP rotation), or in any lane of the row (a permute).
+enum RopePair { kPairInLane, kPairFull, kPairAny };
+
+template <RopePair kPair>
 __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
   const int lane = threadIdx.x & 63;
   const int c = lane & 15, sub = lane >> 4;                 // 16-byte chunk of the row, row within a load
-  const int n_rows = a.Hq + 2 * a.Hkv;
-  const int per_tok = (n_rows + kRopeRows - 1) / kRopeRows;
+  const int n_qk = a.Hq + a.Hkv, n_rows = n_qk + a.Hkv;
+  const int rows_wave = a.rounds * kRopeRows;
+  const int per_tok = (n_rows + rows_wave - 1) / rows_wave;
   const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (w >= (int64_t)a.T * per_tok) return;
   const int t = (int)(w / per_tok);
-  const int row0 = (int)(w - (int64_t)t * per_tok) * kRopeRows;
+  const int row_begin = (int)(w - (int64_t)t * per_tok) * rows_wave;
+  const int row_end = min(row_begin + rows_wave, n_rows);
 
-  u32x4 x[4];
+  const uint16_t* const qt = a.q + t * a.q_stride + c * 8;
+  const uint16_t* const kt = a.k + t * a.k_stride + c * 8 - a.Hq * kHD;
+  const uint16_t* const vt = a.v + t * a.v_stride + c * 8 - n_qk * kHD;
+  auto load = [&](int row0, u32x4 (&x)[4]) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = row0 + 4 * i + sub;
-    if (row < a.Hq) x[i] = ld_u32x4(a.q + t * a.q_stride + row * kHD + c * 8);
-    else if (row < a.Hq + a.Hkv) x[i] = ld_u32x4(a.k + t * a.k_stride + (row - a.Hq) * kHD + c * 8);
-    else if (row < n_rows) x[i] = ld_u32x4(a.v + t * a.v_stride + (row - a.Hq - a.Hkv) * kHD + c * 8);
-    else x[i] = u32x4{0u, 0u, 0u, 0u};
-  }
+    for (int i = 0; i < 4; ++i) {
+      const int row = row0 + 4 * i + sub;
+      if (row < row_end) x[i] = ld_u32x4((row < a.Hq ? qt : row < n_qk ? kt : vt) + row * kHD);
+    }
+  };
+  u32x4 x[4];
+  load(row_begin, x);
+
   const int b = __builtin_amdgcn_readfirstlane(wave_find_seq(a.tok_begin, a.B, t));
   const int step = t - a.tok_begin[b];
   // where the token's key and value rows go
   const int at = a.start[b] + step;
   const int page = at / a.P, prow = at - page * a.P;
   int32_t slot = -1;
-  if (row0 + kRopeRows > a.Hq) {
+  if (row_end > a.Hq) {
     const int32_t base = a.indptr[b];
     if (page < a.indptr[b + 1] - base) slot = a.indices[base + page];
     if (slot < 0 || (int64_t)slot >= a.num_slots) {
@@ -124,78 +138,114 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
       if (lane == 0) atomicOr(a.err, 2);
     }
   }
-  // cosines and sines of this lane's pairs
-  constexpr int kPairs = kInterleaved ? 4 : 8;
-  const int hl = a.half_lanes;
-  const bool rotates = kInterleaved ? true : c < 2 * hl;
-  const bool upper = !kInterleaved && c >= hl;
-  const uint32_t pos = (uint32_t)(a.pos[b] + step);
-  float cs[kPairs], sn[kPairs];
-#pragma unroll
-  for (int e = 0; e < kPairs; ++e) {
-    const int j = kInterleaved ? 4 * c + e : 8 * (upper ? c - hl : c) + e;
-    const bool on = kInterleaved ? 2 * j < a.rot : rotates;
-    const uint64_t phase = on ? a.freq[j] * pos : 0;
-    const float turns = (float)(int32_t)(phase >> 32) * 2.3283064365386963e-10f;   // 2^-32
-    cs[e] = __builtin_amdgcn_cosf(turns);
-    sn[e] = __builtin_amdgcn_sinf(turns);
-    if (upper) sn[e] = -sn[e];                              // own * cos - partner * sin, the sign of the upper half
-  }
-  const int partner = kInterleaved ? lane : (sub << 4) + (!rotates ? c : upper ? c - hl : c + hl);
 
+  // this lane's partner lane and its pairs' cosines and signed sines
+  const int hl = a.rot >> 4;                                // lanes of each half (pairs of halves)
+  const bool rotates = kPair == kPairFull ? true : kPair == kPairAny ? c < 2 * hl : 8 * c < a.rot;
+  const bool upper = kPair == kPairFull ? c >= 8 : kPair == kPairAny && c >= hl;
+  const int partner = kPair == kPairInLane || !rotates ? c : kPair == kPairFull ? c ^ 8 : upper ? c - hl : c + hl;
+  const uint32_t pos = (uint32_t)(a.pos[b] + step);
+  float cs[8], sn[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = row0 + 4 * i + sub;
-    const bool is_q = row < a.Hq, is_k = !is_q && row < a.Hq + a.Hkv;
-    u32x4 other;
-    if constexpr (!kInterleaved)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) other[e] = (uint32_t)__shfl((int)x[i][e], partner);
-    float y[8], z[8];
-    unpack8(x[i], y);
-    const uint16_t* wt = is_q ? a.q_weight : a.k_weight;
-    float ss = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(y[e], y[e], ss);
-    ss = row16_sum(ss);
-    const bool normed = (is_q || is_k) && wt != nullptr;
-    const float r = __builtin_amdgcn_rsqf(ss * (1.f / kHD) + a.eps);
-    if (normed) {
-      float g[8];
-      unpack8(ld_u32x4(wt + c * 8), g);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = y[e] * r * (g[e] + a.offset);
+  for (int e = 0; e < 8; ++e) {
+    if (kPair == kPairInLane && (e & 1)) {
+      cs[e] = cs[e - 1];
+      sn[e] = -sn[e - 1];
+      continue;
     }
-    if constexpr (kInterleaved) {
+    const int j = kPair == kPairInLane ? 4 * c + e / 2 : 8 * (upper ? partner : c) + e;
+    cs[e] = 1.f;
+    sn[e] = 0.f;
+    if (rotates) {
+      const uint64_t f = a.freq[j];
+      const uint32_t phase = __umulhi((uint32_t)f, pos) + (uint32_t)(f >> 32) * pos;
+      const float turns = (float)(int32_t)phase * 2.3283064365386963e-10f;   // 2^-32
+      cs[e] = __builtin_amdgcn_cosf(turns);
+      const float s = __builtin_amdgcn_sinf(turns);
+      sn[e] = upper ? s : -s;
+    }
+  }
+  // out = r * (x * own + p * other)
+  struct Coef {
+    float own[8], other[8];
+    bool normed;
+  };
+  auto coefs = [&](const uint16_t* wt) __attribute__((always_inline)) {
+    Coef k;
+    k.normed = wt != nullptr;
+    float g[8], h[8];
+    if (k.normed) {
+      unpack8(ld_u32x4(wt + c * 8), g);
+      unpack8(ld_u32x4(wt + partner * 8), h);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float own = k.normed ? g[e] + a.offset : 1.f;
+      const float other = k.normed ? h[kPair == kPairInLane ? e ^ 1 : e] + a.offset : 1.f;
+      k.own[e] = own * cs[e];
+      k.other[e] = other * sn[e];
+    }
+    return k;
+  };
+  auto turn = [&](u32x4 raw, const Coef& k) __attribute__((always_inline)) {
+    float y[8], p[8];
+    unpack8(raw, y);
+    if constexpr (kPair == kPairInLane) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = rotates ? y[e ^ 1] : 0.f;
+    } else {
+      u32x4 o;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        z[2 * e] = y[2 * e] * cs[e] - y[2 * e + 1] * sn[e];
-        z[2 * e + 1] = y[2 * e + 1] * cs[e] + y[2 * e] * sn[e];
+        if constexpr (kPair == kPairFull)
+          o[e] = (uint32_t)__builtin_amdgcn_mov_dpp((int)raw[e], 0x128, 0xF, 0xF, true);   // 8 lanes on
+        else
+          o[e] = rotates ? (uint32_t)__shfl((int)raw[e], (lane & 48) + partner) : 0u;
       }
-    } else {
-      float p[8];
-      unpack8(other, p);
-      if (normed) {
-        float g[8];
-        unpack8(ld_u32x4(wt + (partner & 15) * 8), g);
+      unpack8(o, p);
+    }
+    float r = 1.f;
+    if (k.normed) {
+      float ss[2] = {0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = p[e] * r * (g[e] + a.offset);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = rotates ? y[e] * cs[e] - p[e] * sn[e] : y[e];
+      for (int e = 0; e < 8; ++e) ss[e & 1] = __builtin_fmaf(y[e], y[e], ss[e & 1]);
+      r = __builtin_amdgcn_rsqf(row16_sum(ss[0] + ss[1]) * (1.f / kHD) + a.eps);
     }
     typedef __bf16 b8 __attribute__((ext_vector_type(8)));
     b8 out;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) out[e] = (__bf16)z[e];
-    const u32x4 turned = __builtin_bit_cast(u32x4, out);
-    if (is_q)
-      st_u32x4(a.q_out + ((int64_t)t * a.Hq + row) * kHD + c * 8, turned);
-    else if (row < n_rows && slot >= 0) {
-      const int head = row - a.Hq - (is_k ? 0 : a.Hkv);
-      const int64_t dst = (((int64_t)slot * a.Hkv + head) * a.P + prow) * kHD + c * 8;
-      st_u32x4((is_k ? a.k_pool : a.v_pool) + dst, is_k ? turned : x[i]);
+    for (int e = 0; e < 8; ++e) {
+      const float z = __builtin_fmaf(y[e], k.own[e], p[e] * k.other[e]);
+      out[e] = (__bf16)(k.normed ? r * z : z);
     }
+    return __builtin_bit_cast(u32x4, out);
+  };
+
+  uint16_t* const q_out = a.q_out + (int64_t)t * a.Hq * kHD + c * 8;
+  const int64_t page_at = ((int64_t)slot * a.Hkv * a.P + prow) * kHD + c * 8;
+  Coef cq, ck;
+  if (row_begin < a.Hq) cq = coefs(a.q_weight);
+  if (row_end > a.Hq && row_begin < n_qk) ck = coefs(a.k_weight);
+  for (int row0 = row_begin; row0 < row_end; row0 += kRopeRows) {
+    u32x4 next[4];
+    load(row0 + kRopeRows, next);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int first = row0 + 4 * i, row = first + sub;    // first: the same for the whole wave
+      if (first < a.Hq) {
+        const u32x4 out = turn(x[i], cq);
+        if (row < a.Hq) st_u32x4(q_out + row * kHD, out);
+      }
+      if (first + 3 >= a.Hq && first < n_qk) {
+        const u32x4 out = turn(x[i], ck);
+        if (row >= a.Hq && row < n_qk && slot >= 0)
+          st_u32x4(a.k_pool + page_at + (int64_t)(row - a.Hq) * a.P * kHD, out);
+      }
+      if (first + 3 >= n_qk && row >= n_qk && row < row_end && slot >= 0)
+        st_u32x4(a.v_pool + page_at + (int64_t)(row - n_qk) * a.P * kHD, x[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = next[i];
   }
 }
 

@@ -189,6 +189,9 @@ struct sa_ctx {
     size_t o_tok = 0, o_start = 0, o_pos = 0;
     int64_t total = 0;
   } rope_rec;
+  // inv_freq values and what they are in turns: 64 long double divisions took 2 us of every call
+  double rope_freq[sa::kHD / 2] = {};
+  uint64_t rope_turns[sa::kHD / 2] = {};
   struct ForkRec {
     size_t o_ch = 0, o_ip = 0, o_cp = 0;
     int64_t n_dst = 0, fresh_used = 0, n_copies = 0;
@@ -196,6 +199,7 @@ struct sa_ctx {
   struct SharedRec {
     size_t o_it = 0, o_un = 0, n_items = 0, n_units = 0;
     int64_t total_q = 0, n_parts = 0;
+    int most_rows = 0, block_rows = 8;
     bool any_shared = false;
   } shared_rec;
   uint8_t* work = nullptr;         // slot scans of sa_kv_release and sa_kv_compact
@@ -1297,7 +1301,8 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
       (!std::isfinite(rope->eps) || rope->eps <= 0.f || !std::isfinite(rope->weight_offset)))
     return fail(SA_ERR_SHAPE, "eps %g must be finite and positive, weight_offset %g finite", rope->eps,
                 rope->weight_offset);
-  for (int j = 0; j < rope->rot_dim / 2; ++j)
+  const int n_freq = rope->rot_dim / 2;
+  for (int j = 0; j < n_freq; ++j)
     if (!std::isfinite(rope->h_inv_freq[j]) || rope->h_inv_freq[j] < 0. || rope->h_inv_freq[j] > 1024.)
       return fail(SA_ERR_SHAPE, "inv_freq[%d] = %g outside [0, 1024]", j, rope->h_inv_freq[j]);
   const int64_t widths[3] = {(int64_t)Hq * sa::kHD, (int64_t)Hkv * sa::kHD, (int64_t)Hkv * sa::kHD};
@@ -1395,24 +1400,32 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   a.Hkv = Hkv;
   a.P = layout->page_size;
   a.rot = rope->rot_dim;
-  a.half_lanes = rope->rot_dim / 16;
   a.eps = rope->eps;
   a.offset = rope->weight_offset;
-  for (int j = 0; j < rope->rot_dim / 2; ++j) {
-    // turns per position modulo 1, in units of 2^-64
-    const long double turns = (long double)rope->h_inv_freq[j] / 6.283185307179586476925286766559L;
-    const long double frac = std::ldexp(turns - std::floor(turns), 64);
-    a.freq[j] = frac >= 18446744073709551615.0L ? UINT64_MAX : (uint64_t)(frac + 0.5L);
+  if (n_freq > 0 && memcmp(ctx->rope_freq, rope->h_inv_freq, n_freq * sizeof(double)) != 0) {
+    for (int j = 0; j < n_freq; ++j) {
+      // turns per position modulo 1, in units of 2^-64
+      const long double turns = (long double)rope->h_inv_freq[j] / 6.283185307179586476925286766559L;
+      const long double frac = std::ldexp(turns - std::floor(turns), 64) + 0.5L;
+      ctx->rope_turns[j] = frac >= 18446744073709551616.0L ? 0 : (uint64_t)frac;
+    }
+    memcpy(ctx->rope_freq, rope->h_inv_freq, n_freq * sizeof(double));
   }
-  const int64_t waves = rec.total * ((Hq + 2 * (int64_t)Hkv + sa::kRopeRows - 1) / sa::kRopeRows);
-  const int64_t blocks = (waves + 3) / 4;
+  memcpy(a.freq, ctx->rope_turns, n_freq * sizeof(uint64_t));
+  const int n_rows = Hq + 2 * Hkv;
+  a.rounds = (n_rows + sa::kRopeRows - 1) / sa::kRopeRows;
+  a.rounds = std::max(1, std::min<int>(a.rounds, (int)(rec.total * a.rounds / (16 * (int64_t)ctx->num_cu))));
+  const int rows_wave = a.rounds * sa::kRopeRows;
+  const int64_t blocks = (rec.total * ((n_rows + rows_wave - 1) / rows_wave) + 3) / 4;
   if (blocks > INT32_MAX) return fail(SA_ERR_SHAPE, "too many new tokens for these heads");
+  const hipEvent_t* const ev = ctx->kernel_ev[SA_TIMED_PAGES];
+  const dim3 grid((unsigned)blocks), threads(256);
   if (rope->interleaved)
-    launch_timed(sa::rope_append_kernel<true>, dim3((unsigned)blocks), dim3(256), (hipStream_t)stream,
-                 ctx->kernel_ev[SA_TIMED_PAGES], a);
+    launch_timed(sa::rope_append_kernel<sa::kPairInLane>, grid, threads, (hipStream_t)stream, ev, a);
+  else if (rope->rot_dim == sa::kHD)
+    launch_timed(sa::rope_append_kernel<sa::kPairFull>, grid, threads, (hipStream_t)stream, ev, a);
   else
-    launch_timed(sa::rope_append_kernel<false>, dim3((unsigned)blocks), dim3(256), (hipStream_t)stream,
-                 ctx->kernel_ev[SA_TIMED_PAGES], a);
+    launch_timed(sa::rope_append_kernel<sa::kPairAny>, grid, threads, (hipStream_t)stream, ev, a);
   SA_HIP(hipGetLastError());
   return SA_OK;
 }
@@ -1547,14 +1560,19 @@ sa_status kv_release(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_pag
   if (s != SA_OK) return s;
   const hipStream_t st = (hipStream_t)stream;
   const int chunks = (int)((layout->num_slots + sa::kScanChunk - 1) / sa::kScanChunk);
-  s = reserve_work(ctx, (size_t)chunks * sizeof(int32_t));
-  if (s != SA_OK) return s;
+  const bool counted = chunks > 1;
+  if (counted && d_free != nullptr) {
+    s = reserve_work(ctx, (size_t)chunks * sizeof(int32_t));
+    if (s != SA_OK) return s;
+  }
   launch_count<false>(ctx, layout, batch, pages, max_entries, d_ref, st);
   SA_HIP(hipGetLastError());
   if (d_free == nullptr) return SA_OK;
-  sa::FreeArgs f{d_ref, d_free, d_num_free, (int32_t*)ctx->work, (int32_t)layout->num_slots, chunks};
-  hipLaunchKernelGGL(sa::free_count_kernel, dim3((unsigned)chunks), dim3(sa::kScanThreads), 0, st, f);
-  SA_HIP(hipGetLastError());
+  sa::FreeArgs f{d_ref, d_free, d_num_free, counted ? (int32_t*)ctx->work : nullptr, (int32_t)layout->num_slots, chunks};
+  if (counted) {
+    hipLaunchKernelGGL(sa::free_count_kernel, dim3((unsigned)chunks), dim3(sa::kScanThreads), 0, st, f);
+    SA_HIP(hipGetLastError());
+  }
   hipLaunchKernelGGL(sa::free_list_kernel, dim3((unsigned)chunks), dim3(sa::kScanThreads), 0, st, f);
   SA_HIP(hipGetLastError());
   return SA_OK;
@@ -1594,7 +1612,8 @@ sa_status kv_compact(sa_ctx* ctx, const sa_layout* layout, void* k_pool, void* v
   a.hole = a.rank + n;
   a.mover = a.hole + n;
   a.mover_ref = a.mover + n;
-  a.counts = a.mover_ref + n;
+  const bool counted = chunks > 1;
+  a.counts = counted ? a.mover_ref + n : nullptr;
   a.slot_elems = slot_elems(layout);
   a.layer_elems = layer_elems(layout);
   a.num_entries = num_entries;
@@ -1602,14 +1621,14 @@ sa_status kv_compact(sa_ctx* ctx, const sa_layout* layout, void* k_pool, void* v
   a.limit = limit;
   a.chunks = chunks;
   a.num_layers = layout->num_layers;
-  hipLaunchKernelGGL(sa::compact_count_kernel, dim3((unsigned)chunks), dim3(sa::kScanThreads), 0, st, a);
-  SA_HIP(hipGetLastError());
+  if (counted) {
+    hipLaunchKernelGGL(sa::compact_count_kernel, dim3((unsigned)chunks), dim3(sa::kScanThreads), 0, st, a);
+    SA_HIP(hipGetLastError());
+  }
   hipLaunchKernelGGL(sa::compact_rank_kernel, dim3((unsigned)chunks), dim3(sa::kScanThreads), 0, st, a);
   SA_HIP(hipGetLastError());
-  hipLaunchKernelGGL(sa::compact_map_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, a);
-  SA_HIP(hipGetLastError());
   const int64_t most = std::min<int64_t>(limit, (int64_t)n - limit) * layout->num_layers * 2;
-  const int64_t blocks = std::min<int64_t>(std::max<int64_t>(std::max<int64_t>(most, (num_entries + 255) / 256), 1),
+  const int64_t blocks = std::min<int64_t>(std::max<int64_t>(most, (std::max<int64_t>(num_entries, (int64_t)n) + 255) / 256),
                                            16 * (int64_t)ctx->num_cu);
   launch_timed(sa::compact_move_kernel, dim3((unsigned)blocks), dim3(256), st, ctx->kernel_ev[SA_TIMED_PAGES], a);
   SA_HIP(hipGetLastError());
@@ -1670,6 +1689,9 @@ sa_status shared_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
     rec.n_items = plan.items.size();
     rec.n_units = plan.units.size();
     rec.n_parts = plan.n_parts;
+    rec.most_rows = plan.most_rows;
+    rec.block_rows = sa::merge_block_rows(plan.most_parts);
+    rec.any_shared = plan.any_shared;
     PlanImage img;
     rec.o_it = img.add(plan.items.data(), plan.items.size());
     rec.o_un = img.add(plan.units.data(), plan.units.size());
@@ -1706,8 +1728,9 @@ sa_status shared_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   else launch_shared<32>(pool_rsrc, grid, (hipStream_t)stream, ctx->kernel_ev[SA_TIMED_ATTN], a);
   SA_HIP(hipGetLastError());
   if (rec.n_units > 0) {
-    sa::MergeRowsArgs m{a.part_o, a.part_lse, (const sa::MergeUnit*)(dev + rec.o_un), a.o, lse, a.Hq, a.G};
-    hipLaunchKernelGGL(sa::merge_rows_kernel, dim3((unsigned)rec.n_units), dim3(256), 0, (hipStream_t)stream, m);
+    sa::MergeRowsArgs m{a.part_o, a.part_lse, (const sa::MergeUnit*)(dev + rec.o_un), a.o, lse, a.Hq, a.G, rec.block_rows};
+    const dim3 blocks((unsigned)rec.n_units, (unsigned)((rec.most_rows + rec.block_rows - 1) / rec.block_rows));
+    hipLaunchKernelGGL(sa::merge_rows_kernel, blocks, dim3(256), 0, (hipStream_t)stream, m);
     SA_HIP(hipGetLastError());
   }
   return SA_OK;
