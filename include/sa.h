@@ -617,11 +617,12 @@ sa_status sa_kv_compact(sa_ctx *ctx, const sa_layout *layout, void *k_pool, void
  * result is that of sa_segment_prefill_attn over the same tables, held to the
  * same tolerance.  shared_len may be anything from 0 to the smallest
  * h_kv_len - h_q_len of the group.  Where the members' rows fill the kernel's
- * row tiles anyway (long segments) the group is computed member by member.  The
- * softmax scale is always applied exactly; the kernel variants and the block
- * clock do not apply to this call, sa_set_kernel_events times its first kernel
- * (SA_TIMED_ATTN), and its partial results (66 KB per key-range part) take the
- * place of the split-KV partials that sa_reserve sizes.
+ * row tiles anyway (long segments) the group is computed member by member, and a
+ * batch that would gain nothing goes to the segment attention's launch.  The
+ * softmax scale is always applied exactly; SA_ATTN_VARIANT and the block clock
+ * apply only to such batches.  sa_set_kernel_events times the first kernel
+ * (SA_TIMED_ATTN), and the partial results (516 bytes per query row, head and
+ * key-range part) take the place of the split-KV partials that sa_reserve sizes.
  *
  * Errors: those of sa_segment_prefill_attn, SA_ERR_SHAPE for bad groups or
  * shared lengths, SA_ERR_UNSUPPORTED for a capturing stream.

@@ -235,8 +235,9 @@ __device__ __forceinline__ bool part_arrive(const AttnArgs& a, const PartInfo& p
 // (prefix lengths that are not a multiple of 4) takes the checked load, so the
 // steps that load its tile are plain steps.
 //
-// kRowParts: the partials of parts go out as plain rows, for a merge launch
-// that finds each row of an item in several items' parts (attn_shared.h).
+// kRowParts: the partials of parts go out as plain rows, from row it.part of
+// part_o on, for a merge launch that finds each row of an item in several items'
+// parts (attn_shared.h).
 template <int P, bool kPoolRsrc, int kGroups, int GRP, bool kRead = false, bool kExact = false, bool kRowParts = false>
 __device__ __attribute__((always_inline)) inline void pipe_group(const AttnArgs& a, const AttnItem& it,
                                                                  const SeqDesc& sd, const PipeLds& L) {
@@ -941,7 +942,7 @@ __device__ __attribute__((always_inline)) inline void pipe_group(const AttnArgs&
       *(__attribute__((address_space(3))) f32x4*)(room + row_o * 512 + ((c ^ row_o) << 4)) =
           f32x4{oacc[dt][4 * i] * inv, oacc[dt][4 * i + 1] * inv, oacc[dt][4 * i + 2] * inv, oacc[dt][4 * i + 3] * inv};
     }
-    const int64_t prow = (int64_t)it.part * kRows + wave * 32;
+    const int64_t prow = (int64_t)it.part + wave * 32;
     if (hh_o == 0 && o_row < rows_total) a.part_lse[prow + row_o] = lse2;
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0xC07F);                    // lgkmcnt(0): the wave's own rows are in LDS
@@ -1365,8 +1366,8 @@ __device__ __attribute__((always_inline)) inline void decode_group(const AttnArg
       st_bf16x4(a.o + orow * kHD + 4 * c, o[0], o[1], o[2], o[3]);
       if (a.lse != nullptr && c == 0) a.lse[orow] = lse2 * 0.69314718055994531f;
     } else if constexpr (kRowParts) {
-      *(f32x4*)(a.part_o + ((int64_t)it.part * kPipeRows + row) * kHD + 4 * c) = o;
-      if (c == 0) a.part_lse[(int64_t)it.part * kPipeRows + row] = lse2;
+      *(f32x4*)(a.part_o + ((int64_t)it.part + row) * kHD + 4 * c) = o;
+      if (c == 0) a.part_lse[(int64_t)it.part + row] = lse2;
     } else {
       part_st4(rp, (uint32_t)it.part * (kPipeRows * kHD * 4) + (uint32_t)e * 16, o);
       if (c == 0) part_st1(rp, l_base + (uint32_t)it.part * (kPipeRows * 4) + row * 4, 0, lse2);

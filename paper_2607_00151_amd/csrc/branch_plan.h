@@ -6,6 +6,8 @@
 // plain int32 structs.
 #pragma once
 
+#include <tuple>
+
 #include "plan.h"
 
 namespace sa {
@@ -99,24 +101,26 @@ inline sa_status debug_check_fork(const ForkPlan& plan, const int32_t* indptr, c
 // ------------------------------------------------------------------ shared prefix
 
 // Rows of one member and KV head whose parts the merge joins: packed rows
-// r0 .. r0 + n - 1 of the member whose first token is q_start, found in parts
-// a_part .. a_part + a_n - 1 from row a_row on (the shared prefix) and in
-// b_part .. from row b_row on (the member's own keys).
+// r0 .. r0 + n - 1 of the member whose first token is q_start.  Of the rows that
+// partials are kept by, row r0's are a_row, a_row + a_stride, ... (a_n of them: the
+// shared prefix) and b_row, b_row + b_stride, ... (b_n: the member's own keys), and
+// the next rows' follow each.
 struct MergeUnit {
   int32_t q_start, r0, n, kvh;
-  int32_t a_part, a_n, a_row;
-  int32_t b_part, b_n, b_row;
+  int32_t a_row, a_n, a_stride;
+  int32_t b_row, b_n, b_stride;
 };
 constexpr int kMergeUnitRows = 32;     // most rows of a unit
 // rows per block of the merge, for rows of at most so many parts
 inline int merge_block_rows(int most_parts) { return most_parts <= 8 ? 8 : most_parts <= 16 ? 4 : most_parts <= 32 ? 2 : 1; }
 
+// part of an item: the row its partial starts at among all partials (-1: none)
 struct SharedPlan {
+  bool shared = false;                 // some group's prefix is computed once for its members
   std::vector<AttnItem> items;         // one per workgroup, in launch order
   std::vector<MergeUnit> units;
-  int32_t n_parts = 0;
+  int64_t part_rows = 0;               // rows of all partials
   int32_t most_rows = 0, most_parts = 0;   // of a unit
-  bool any_shared = false;             // some group's prefix is computed once for its members
 };
 
 inline sa_status check_groups(int32_t batch, const int32_t* h_q_len, const int32_t* h_kv_len, int32_t num_groups,
@@ -138,31 +142,47 @@ inline sa_status check_groups(int32_t batch, const int32_t* h_q_len, const int32
   return SA_OK;
 }
 
-// What the choice of a chunk needs of a row tile (of one KV head; the others are alike).
+// Row tiles of one KV head that the choice of a chunk need not tell apart.
 struct SharedShape {
-  int64_t tiles;             // 64-key tiles
-  int32_t rows;
+  int64_t tiles;             // 64-key tiles of each
   bool decode;               // takes the kernel's path for few rows
   bool streams;              // reads its keys from memory (a group's other row tiles find them in L2)
+  int64_t count, rows;       // how many, and their packed rows in all
 };
 
-// Time of the launches at a chunk size, in units of 10 ns.
-inline int64_t shared_chunk_cost(const std::vector<SharedShape>& shapes, int Hkv, int num_cu, int most_parts, int64_t c) {
+struct SharedCost {
+  int64_t total;             // units of 10 ns
+  bool compute;              // bound by the blocks' work, not by the stream of keys
+};
+
+inline int64_t shared_parts(int64_t tiles, int64_t chunk) {
+  return std::max<int64_t>(1, std::min<int64_t>((tiles + chunk - 1) / chunk, kMaxItemParts));
+}
+
+// Time of the two launches at a chunk size, in units of 10 ns.  Measured
+// (MI355X): a prefill tile 127 alone on its CU and 180 where two blocks share
+// one, a decode tile 80, 300 for a block's start and end; the keys stream at 54.6
+// per tile and 100 blocks (6 TB/s), with a quarter of the shorter of work and
+// stream not overlapping; the merge 700, and 1032 bytes written and read per row
+// and part at 9 TB/s.  Model and measurement, us: 32 branches of 16K, 34 and 31;
+// 64 of 64K, 64/8 heads, 162 and 167; 4 of 4K 14 and 15; 16 of 16K with 16 to 64
+// query tokens each 181 and 184.
+inline SharedCost shared_chunk_cost(const std::vector<SharedShape>& shapes, int Hkv, int num_cu, int64_t chunk) {
   struct Run {
     int64_t time, blocks;
   };
   std::vector<Run> runs;
   int64_t n = 0, streamed = 0, part_rows = 0;
   for (const SharedShape& s : shapes) {
-    const int64_t k = std::max<int64_t>(1, std::min<int64_t>((s.tiles + c - 1) / c, most_parts));
-    n += k * Hkv;
+    const int64_t k = shared_parts(s.tiles, chunk);
+    n += k * Hkv * s.count;
     part_rows += k * Hkv * s.rows;
-    if (s.streams) streamed += s.tiles * Hkv;
+    if (s.streams) streamed += s.tiles * Hkv * s.count;
   }
   for (const SharedShape& s : shapes) {
-    const int64_t k = std::max<int64_t>(1, std::min<int64_t>((s.tiles + c - 1) / c, most_parts));
-    const int64_t t = s.decode ? 80 : n > num_cu ? 187 : 112;
-    runs.push_back({(s.tiles + k - 1) / k * t + 400, k * Hkv});
+    const int64_t k = shared_parts(s.tiles, chunk);
+    const int64_t t = s.decode ? 80 : n > num_cu ? 180 : 127;
+    runs.push_back({(s.tiles + k - 1) / k * t + 300, k * Hkv * s.count});
   }
   std::sort(runs.begin(), runs.end(), [](const Run& x, const Run& y) { return x.time > y.time; });
   // the busiest of the slots: the mean, and of any k slots + 1 longest blocks some slot has k + 1
@@ -170,34 +190,29 @@ inline int64_t shared_chunk_cost(const std::vector<SharedShape>& shapes, int Hkv
   int64_t sum = 0, before = 0, busy = 0;
   for (const Run& r : runs) {
     sum += r.time * r.blocks;
-    const int64_t last = before + r.blocks - 1;              // index of the run's last block
-    busy = std::max(busy, (last / slots + 1) * r.time);
     before += r.blocks;
+    busy = std::max(busy, ((before - 1) / slots + 1) * r.time);
   }
   busy = std::max(busy, sum / slots);
   const int64_t stream = streamed * 546 / 1000;
-  return std::max(busy, stream) + std::min(busy, stream) / 4 + 300 + part_rows * 1032 / 45000;
+  return {std::max(busy, stream) + std::min(busy, stream) / 4 + 700 + part_rows * 1032 / 90000, busy > stream};
 }
 
-inline int64_t choose_shared_chunk(const std::vector<SharedShape>& shapes, int Hkv, int num_cu, int most_parts) {
-  int64_t longest = 1, total = 0;
-  for (const SharedShape& s : shapes) {
-    longest = std::max(longest, s.tiles);
-    total += s.tiles * Hkv;
+// The same work by sa_segment_prefill_attn, every member over all of its keys:
+// members' repeated reads of the shared keys come out of the caches, 14 TB/s over
+// all (measured over 2 to 64 members), 700 for the launch.  Of 25 batches of 1 to
+// 12 groups measured both ways the model passes on those that end sooner so (12.7
+// against 16.6 us: 2 + 9 members on 5.4K, 8/2 heads) and shares the others (31
+// against 154: 32 on 16K).
+inline int64_t segment_cost(const std::vector<SeqDesc>& seqs, int G, int Hkv, int num_cu) {
+  int64_t stream = 0, compute = 0;
+  for (const SeqDesc& s : seqs) {
+    const int64_t rows = (int64_t)s.q_len * G, tiles = (s.kv_len + kKT - 1) / kKT * Hkv;
+    if (rows == 0) continue;
+    if (rows <= kDecodeRows) stream += tiles;
+    else compute += tiles * ((rows + 127) / 128);
   }
-  int64_t best = INT64_MAX, chunk = longest;
-  auto consider = [&](int64_t c) {
-    c = std::min(std::max<int64_t>(c, 4), longest);
-    const int64_t t = shared_chunk_cost(shapes, Hkv, num_cu, most_parts, c);
-    if (t < best) {
-      best = t;
-      chunk = c;
-    }
-  };
-  // equal parts of the longest tile, as many as there is room for
-  const int64_t most = std::min<int64_t>(64, (longest + 3) / 4);
-  for (int64_t k = 1; k <= most; k += 1 + k / 8) consider((longest + k - 1) / k);
-  return chunk;
+  return 700 + std::max(stream * 234 / 1000, compute * 210 / (2 * num_cu)) + stream * 80 / (2 * num_cu) / 4;
 }
 
 // The launch's work items.  A group whose prefix is computed once gives row
@@ -205,7 +220,8 @@ inline int64_t choose_shared_chunk(const std::vector<SharedShape>& shapes, int H
 // length rounded down to whole 64-key tiles, and row tiles of each member over
 // [S, kv_len); every other member gives row tiles over all of its keys.  Tiles
 // are split by key range into parts; a tile that is the only one to see its
-// rows and has one part writes the output itself.
+// rows and has one part writes the output itself.  Where no group's prefix is
+// worth it, out.shared is false and there are no items.
 inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc>& seqs, int32_t num_groups,
                               const int32_t* h_group_indptr, const int32_t* h_shared_len, int num_cu,
                               SharedPlan& out) {
@@ -215,7 +231,8 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
   struct Tile {
     int32_t seq, row0, rows, q_start, q_len, kv_len, k0, k1;   // rows: of this tile
     bool prefix;
-    int32_t part0 = -1, parts = 1;                              // of KV head 0; head h's are part0 + h * parts on
+    int32_t parts = 1;
+    int64_t place = -1;                                         // row of its first part, KV head 0, among the partials
     int64_t tiles() const { return (k1 - k0 + kKT - 1) / kKT; }
   };
   std::vector<Tile> tiles;
@@ -223,6 +240,7 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
     int32_t seq, prefix0, row_in_group, own0;                  // first prefix tile of its group (-1), its first row there
   };
   std::vector<Member> members;
+  bool any = false;
   for (int g = 0; g < num_groups; ++g) {
     const int b0 = h_group_indptr[g], b1 = h_group_indptr[g + 1];
     int64_t rows = 0, apart = 0;
@@ -236,10 +254,10 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
     if (first < 0) continue;
     const int32_t S = h_shared_len[g] / kKT * kKT;
     // worth it where packing the members' rows leaves clearly fewer row tiles over the prefix
-    const bool shared = S > 0 && rows <= INT32_MAX / 2 && 8 * ((rows + kRows - 1) / kRows) <= 7 * apart;
+    const bool shared = S > 0 && rows + S <= INT32_MAX / 2 && 8 * ((rows + kRows - 1) / kRows) <= 7 * apart;
     const int32_t prefix0 = shared ? (int32_t)tiles.size() : -1;
     if (shared) {
-      out.any_shared = true;
+      any = true;
       const int32_t q_len = (int32_t)(rows / G);
       for (int64_t r0 = 0; r0 < rows; r0 += kRows)
         tiles.push_back({first, (int32_t)r0, (int32_t)std::min<int64_t>(kRows, rows - r0), seqs[first].q_start, q_len,
@@ -259,34 +277,74 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
       at += n;
     }
   }
-  // Key-range parts of one chunk size: of a few, the one that the model ends first.
-  auto parts_of = [](const Tile& t, int64_t c) {
-    return std::max<int64_t>(1, std::min<int64_t>((t.tiles() + c - 1) / c, kMaxItemParts));
-  };
+  if (!any) return;
+
+  // Key-range parts of one chunk size, the one that the model ends first.
+  std::map<std::tuple<int64_t, bool, bool>, std::pair<int64_t, int64_t>> classes;
+  int64_t longest = 1;
+  for (const Tile& t : tiles) {
+    auto& c = classes[{t.tiles(), (int64_t)t.q_len * G <= kDecodeRows, !t.prefix || t.row0 == 0}];
+    ++c.first;
+    c.second += t.rows;
+    longest = std::max(longest, t.tiles());
+  }
   std::vector<SharedShape> shapes;
-  for (const Tile& t : tiles)
-    shapes.push_back({t.tiles(), t.rows, t.q_len * G <= kDecodeRows, !t.prefix || t.row0 == 0});
-  const int64_t chunk = choose_shared_chunk(shapes, Hkv, num_cu, kMaxItemParts);
-  for (const Member& m : members) {
-    const int32_t n = seqs[m.seq].q_len * G;
-    for (int32_t r0 = 0, t = m.own0; r0 < n; r0 += kRows, ++t) {
-      tiles[t].parts = (int32_t)parts_of(tiles[t], chunk);
-      if (m.prefix0 >= 0 || tiles[t].parts > 1) {
-        tiles[t].part0 = out.n_parts;
-        out.n_parts += tiles[t].parts * Hkv;
-      }
+  for (const auto& c : classes)
+    shapes.push_back({std::get<0>(c.first), std::get<1>(c.first), std::get<2>(c.first), c.second.first, c.second.second});
+  SharedCost best{INT64_MAX, false};
+  int64_t chunk = longest;
+  const int64_t most = std::min<int64_t>(64, (longest + 3) / 4);
+  for (int64_t k = 1; k <= most; k += 1 + k / 8) {
+    const int64_t c = std::min(std::max<int64_t>((longest + k - 1) / k, 4), longest);
+    const SharedCost t = shared_chunk_cost(shapes, Hkv, num_cu, c);
+    if (t.total < best.total) {
+      best = t;
+      chunk = c;
     }
   }
+  if (best.total >= segment_cost(seqs, G, Hkv, num_cu)) return;
+  out.shared = true;
+
+  int64_t rows_used = 0, prefix_blocks = 0, fill = 0;           // fill: time of the other blocks, 10 ns
+  for (Tile& t : tiles) {
+    t.parts = (int32_t)shared_parts(t.tiles(), chunk);
+    if (t.prefix) prefix_blocks += (int64_t)t.parts * Hkv;
+    else fill += (t.tiles() * 120 + 300 * t.parts) * Hkv;
+  }
+  auto place = [&](Tile& t) {
+    t.place = rows_used;
+    rows_used += (int64_t)t.parts * Hkv * t.rows;
+  };
+  for (const Member& m : members) {
+    const int32_t n = seqs[m.seq].q_len * G;
+    for (int32_t r0 = 0, t = m.own0; r0 < n; r0 += kRows, ++t)
+      if (m.prefix0 >= 0 || tiles[t].parts > 1) place(tiles[t]);
+  }
   for (Tile& t : tiles)
-    if (t.prefix) {
-      t.parts = (int32_t)parts_of(t, chunk);
-      t.part0 = out.n_parts;
-      out.n_parts += t.parts * Hkv;
-    }
+    if (t.prefix) place(t);
+  out.part_rows = rows_used;
+
+  // Bound by work, with more prefix parts than CUs but at most two for each: every
+  // CU starts with one part, the members' own blocks fill its other slot, and the
+  // CU's second part follows them.  The parts of the first kind are then longer
+  // than those of the second by the tiles they are ahead, so that both end
+  // together.  64 branches of 64K, 64/8 heads, us of the first launch: all parts
+  // alike in order of length 158, this 150 (the call 178 and 167).
+  const bool fit = best.compute && prefix_blocks > num_cu && prefix_blocks <= 2 * num_cu && fill > 0;
+  const double ahead = fit ? fill / 127.0 / num_cu : 0.0;
+  auto part_begin = [&](const Tile& t, int k) {                 // in tiles from t.k0
+    const int64_t n = t.tiles();
+    const int n_long = t.prefix && fit ? (int)((int64_t)t.parts * num_cu / prefix_blocks) : 0;
+    if (n_long == 0 || n_long == t.parts) return n * k / t.parts;
+    const double a = std::min(ahead, std::max(0.0, (double)(n - 4 * t.parts) / n_long));
+    const double shrt = (n - a * n_long) / t.parts;
+    return std::min<int64_t>(n, std::llround(k * shrt + std::min(k, n_long) * a));
+  };
   // blocks: longest first, the row tiles of one key range next to each other on
   // one XCD (block i runs on XCD i % 8), which reads it through its L2 once
   struct Bundle {
     int64_t tiles = 0;
+    bool prefix;
     std::vector<AttnItem> items;
   };
   std::vector<Bundle> bundles;
@@ -296,13 +354,13 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
     for (int h = 0; h < Hkv; ++h)
       for (int k = 0; k < tiles[i].parts; ++k) {
         Bundle bu;
+        bu.prefix = tiles[i].prefix;
         for (size_t x = i; x < j; ++x) {
           const Tile& t = tiles[x];
-          const int64_t n = t.tiles();
           AttnItem it{t.seq, h, t.row0, 0, 0, -1, 0, t.q_start, t.q_len, t.kv_len};
-          it.kv_begin = (int32_t)(t.k0 + n * k / t.parts * kKT);
-          it.kv_end = (int32_t)std::min<int64_t>(t.k0 + n * (k + 1) / t.parts * kKT, t.k1);
-          if (t.part0 >= 0) it.part = t.part0 + h * t.parts + k;
+          it.kv_begin = (int32_t)(t.k0 + part_begin(t, k) * kKT);
+          it.kv_end = (int32_t)std::min<int64_t>(t.k0 + part_begin(t, k + 1) * kKT, t.k1);
+          if (t.place >= 0) it.part = (int32_t)(t.place + ((int64_t)h * t.parts + k) * t.rows);
           bu.tiles += item_tiles(it);
           bu.items.push_back(it);
         }
@@ -310,19 +368,28 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
       }
     i = j;
   }
-  std::stable_sort(bundles.begin(), bundles.end(), [](const Bundle& x, const Bundle& y) { return x.tiles > y.tiles; });
-  std::vector<std::vector<AttnItem>> queue(kNumXcd);
+  std::stable_sort(bundles.begin(), bundles.end(), [](const Bundle& x, const Bundle& y) {
+    return x.tiles * (int64_t)y.items.size() > y.tiles * (int64_t)x.items.size();
+  });
+  std::vector<std::vector<AttnItem>> queue(kNumXcd), fillers(kNumXcd);
   int64_t load[kNumXcd] = {0};
   for (const Bundle& b : bundles) {
     const int x = (int)(std::min_element(load, load + kNumXcd) - load);
     load[x] += b.tiles;
-    queue[x].insert(queue[x].end(), b.items.begin(), b.items.end());
+    auto& q = fit && !b.prefix ? fillers[x] : queue[x];
+    q.insert(q.end(), b.items.begin(), b.items.end());
   }
+  const size_t round = (size_t)std::max(1, num_cu / kNumXcd);
   size_t depth = 0;
-  for (const auto& q : queue) depth = std::max(depth, q.size());
+  for (int x = 0; x < kNumXcd; ++x) {
+    auto& q = queue[x];
+    q.insert(q.begin() + std::min(round, q.size()), fillers[x].begin(), fillers[x].end());
+    depth = std::max(depth, q.size());
+  }
   out.items.assign(depth * kNumXcd, AttnItem{0, 0, 0, 0, 0, -1, 0, 0, 0, 0});
   for (int x = 0; x < kNumXcd; ++x)
     for (size_t i = 0; i < queue[x].size(); ++i) out.items[i * kNumXcd + x] = queue[x][i];
+
   // merge units: rows of one member, one own tile and one prefix tile
   for (const Member& m : members) {
     const int32_t n = seqs[m.seq].q_len * G;
@@ -330,17 +397,18 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
       for (int32_t r = 0; r < n;) {
         const Tile& own = tiles[m.own0 + r / kRows];
         int32_t e = std::min(r + kMergeUnitRows, std::min(own.row0 + own.rows, n));
-        MergeUnit u{seqs[m.seq].q_start, r, 0, h, 0, 0, 0, own.part0 + h * own.parts, own.parts, r - own.row0};
+        MergeUnit u{seqs[m.seq].q_start, r, 0, h, 0, 0, 0, 0, own.parts, own.rows};
+        u.b_row = (int32_t)(own.place + (int64_t)h * own.parts * own.rows + r - own.row0);
         if (m.prefix0 >= 0) {
           const Tile& pre = tiles[m.prefix0 + (m.row_in_group + r) / kRows];
           e = std::min(e, pre.row0 + kRows - m.row_in_group);
-          u.a_part = pre.part0 + h * pre.parts;
+          u.a_row = (int32_t)(pre.place + (int64_t)h * pre.parts * pre.rows + m.row_in_group + r - pre.row0);
           u.a_n = pre.parts;
-          u.a_row = m.row_in_group + r - pre.row0;
+          u.a_stride = pre.rows;
         }
         u.n = e - r;
         r = e;
-        if (own.part0 < 0) continue;
+        if (own.place < 0) continue;
         out.units.push_back(u);
         out.most_rows = std::max(out.most_rows, u.n);
         out.most_parts = std::max(out.most_parts, u.a_n + u.b_n);

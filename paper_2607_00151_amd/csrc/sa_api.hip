@@ -198,9 +198,9 @@ struct sa_ctx {
   } fork_rec;
   struct SharedRec {
     size_t o_it = 0, o_un = 0, n_items = 0, n_units = 0;
-    int64_t total_q = 0, n_parts = 0;
+    int64_t total_q = 0, part_rows = 0;
     int most_rows = 0, block_rows = 8;
-    bool any_shared = false;
+    bool shared = false;           // else the batch goes to the segment attention
   } shared_rec;
   uint8_t* work = nullptr;         // slot scans of sa_kv_release and sa_kv_compact
   size_t work_cap = 0;
@@ -1659,9 +1659,10 @@ sa_status shared_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
     dp.key.add(h_kv_len, (size_t)batch);
     dp.key.add(h_group_indptr, (size_t)num_groups + 1);
     dp.key.add(h_shared_len, (size_t)num_groups);
-    same = dp.reusable(dp.key.end(), (hipStream_t)stream) && !debug_checks();
-    if (!same) dp.key_valid = false;
+    const bool equal = dp.key.end();
     rec = ctx->shared_rec;
+    same = rec.shared ? dp.reusable(equal, (hipStream_t)stream) : equal && dp.key_valid;
+    if (!same) dp.key_valid = false;
   }
   if (!same) {
     rec = sa_ctx::SharedRec{};
@@ -1686,21 +1687,32 @@ sa_status shared_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   uint8_t* dev = ctx->plans[kPlanShared].dev;
   if (!same) {
     sa::plan_shared_items(layout, seqs, num_groups, h_group_indptr, h_shared_len, ctx->num_cu, plan);
+    if (plan.part_rows > INT32_MAX) return fail(SA_ERR_SHAPE, "too many partial rows (%lld)", (long long)plan.part_rows);
+    rec.shared = plan.shared;
     rec.n_items = plan.items.size();
     rec.n_units = plan.units.size();
-    rec.n_parts = plan.n_parts;
+    rec.part_rows = plan.part_rows;
     rec.most_rows = plan.most_rows;
     rec.block_rows = sa::merge_block_rows(plan.most_parts);
-    rec.any_shared = plan.any_shared;
-    PlanImage img;
-    rec.o_it = img.add(plan.items.data(), plan.items.size());
-    rec.o_un = img.add(plan.units.data(), plan.units.size());
-    s = upload_plan(ctx, kPlanShared, img, (hipStream_t)stream, &dev);
-    if (s != SA_OK) return s;
+    if (plan.shared) {
+      PlanImage img;
+      rec.o_it = img.add(plan.items.data(), plan.items.size());
+      rec.o_un = img.add(plan.units.data(), plan.units.size());
+      s = upload_plan(ctx, kPlanShared, img, (hipStream_t)stream, &dev);
+      if (s != SA_OK) return s;
+    }
     ctx->shared_rec = rec;
     ctx->plans[kPlanShared].key_valid = true;
   }
-  s = reserve_parts(ctx, (size_t)rec.n_parts * kPartBytes);
+  if (!rec.shared) {
+    const bool exact = ctx->exact_scale;
+    ctx->exact_scale = true;
+    s = attn_launch(ctx, layout, layer, q, k_pool, v_pool, false, nullptr, nullptr, batch, h_q_len, h_kv_len, pages,
+                    softmax_scale, o, lse, stream);
+    ctx->exact_scale = exact;
+    return s;
+  }
+  s = reserve_parts(ctx, (size_t)rec.part_rows * (sa::kHD + 1) * sizeof(float));
   if (s != SA_OK) return s;
 
   sa::AttnArgs a{};
@@ -1711,7 +1723,7 @@ sa_status shared_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   a.o = (uint16_t*)o;
   a.lse = lse;
   a.part_o = ctx->part;
-  a.part_lse = ctx->part + (size_t)rec.n_parts * sa::kPipeRows * sa::kHD;
+  a.part_lse = ctx->part + (size_t)rec.part_rows * sa::kHD;
   a.items = (const sa::AttnItem*)(dev + rec.o_it);
   a.indptr = pages.indptr;
   a.indices = pages.indices;

@@ -4,9 +4,10 @@
 // Over seeded random shapes it checks that
 //   * a fork plan matches a direct page-by-page count, and refuses bad arguments;
 //   * the shared-prefix work list sees every (query row, visible key) pair
-//     exactly once, each item's pages are its group's or its member's, parts are
-//     numbered once each, and every row split over parts is in one merge unit
-//     that names exactly the parts that hold it.
+//     exactly once, each item's pages are its group's or its member's, partials
+//     do not overlap, and every row split over parts is in one merge unit
+//     that names exactly the rows of the partials that hold it; a batch that is
+//     passed on has no items.
 // Prints "ALL OK" and exits 0 on success.
 #include <cstdio>
 #include <cstdlib>
@@ -18,7 +19,7 @@
 
 #include "branch_plan.h"
 
-static int g_fail = 0;
+static int g_fail = 0, g_shared = 0, g_passed_on = 0;
 #define CHECK(cond, ...)                                                   \
   do {                                                                     \
     if (!(cond)) {                                                         \
@@ -98,7 +99,7 @@ static void shared_case(std::mt19937_64& r, int id) {
   std::vector<int32_t> indptr{0}, shared, q, kv;
   for (int g = 0; g < groups; ++g) {
     const int n = r() % 5 == 0 ? (int)(r() % 2) : (int)(r() % 20);
-    const int S = r() % 4 == 0 ? (int)(r() % 70) : (int)(r() % 3000);
+    const int S = r() % 4 == 0 ? (int)(r() % 70) : (int)(r() % (r() % 3 ? 3000 : 30000));
     shared.push_back(S);
     for (int i = 0; i < n; ++i) {
       const int ql = r() % 6 == 0 ? 0 : r() % 3 == 0 ? (int)(1 + r() % 90) : 1;
@@ -118,20 +119,26 @@ static void shared_case(std::mt19937_64& r, int id) {
   sa::SharedPlan plan;
   const int cus[] = {1, 8, 64, 256};
   sa::plan_shared_items(&L, seqs, groups, indptr.data(), shared.data(), cus[r() % 4], plan);
+  if (!plan.shared) {
+    CHECK(plan.items.empty() && plan.units.empty(), "case %d", id);
+    ++g_passed_on;
+    return;
+  }
+  ++g_shared;
   std::vector<int> seq_of(total), group_of(B);
   for (int b = 0; b < B; ++b)
     for (int t = 0; t < q[b]; ++t) seq_of[seqs[b].q_start + t] = b;
   for (int g = 0; g < groups; ++g)
     for (int b = indptr[g]; b < indptr[g + 1]; ++b) group_of[b] = g;
-  // (token, packed head) -> keys seen, and the (part, row in part) places of its partials
+  // (token, head) -> keys seen, and the rows of its partials
   typedef std::tuple<int, int> Row;                  // token, query head
-  std::map<Row, std::vector<std::pair<int, int>>> keys, places;
+  std::map<Row, std::vector<std::pair<int, int>>> keys;
+  std::map<Row, std::vector<int>> places;
   std::map<Row, int> whole;
   std::set<int> parts;
   for (const sa::AttnItem& it : plan.items) {
     if (it.kv_end <= it.kv_begin) continue;
     CHECK(it.kv_begin % sa::kKT == 0, "case %d", id);
-    if (it.part >= 0) CHECK(parts.insert(it.part).second && it.part < plan.n_parts, "case %d: part %d", id, it.part);
     const int pre = it.kv_len - it.q_len;
     for (int x = 0; x < 128; ++x) {
       const int row = it.row0 + x;
@@ -143,20 +150,23 @@ static void shared_case(std::mt19937_64& r, int id) {
       CHECK(it.seq == b || (group_of[it.seq] == group_of[b] && it.kv_end <= shared[group_of[b]] / 64 * 64),
             "case %d: pages of another sequence", id);
       if (end > it.kv_begin) keys[Row(it.q_start + tok, head)].push_back({it.kv_begin, end});
-      if (it.part >= 0) places[Row(it.q_start + tok, head)].push_back({it.part, x});
+      if (it.part >= 0) {
+        CHECK(parts.insert(it.part + x).second && it.part + x < plan.part_rows, "case %d: partial row %d", id, it.part + x);
+        places[Row(it.q_start + tok, head)].push_back(it.part + x);
+      }
       else whole[Row(it.q_start + tok, head)]++;
     }
   }
-  CHECK((int)parts.size() == plan.n_parts, "case %d", id);
-  std::map<Row, std::vector<std::pair<int, int>>> merged;
+  CHECK((int64_t)parts.size() == plan.part_rows, "case %d", id);
+  std::map<Row, std::vector<int>> merged;
   for (const sa::MergeUnit& u : plan.units) {
     CHECK(u.n >= 1 && u.n <= sa::kMergeUnitRows, "case %d: %d rows", id, u.n);
     for (int x = 0; x < u.n; ++x) {
       const int row = u.r0 + x;
       auto& m = merged[Row(u.q_start + row / G, u.kvh * G + row % G)];
       CHECK(m.empty(), "case %d: a row in two units", id);
-      for (int k = 0; k < u.a_n; ++k) m.push_back({u.a_part + k, u.a_row + x});
-      for (int k = 0; k < u.b_n; ++k) m.push_back({u.b_part + k, u.b_row + x});
+      for (int k = 0; k < u.a_n; ++k) m.push_back(u.a_row + k * u.a_stride + x);
+      for (int k = 0; k < u.b_n; ++k) m.push_back(u.b_row + k * u.b_stride + x);
     }
   }
   for (int b = 0; b < B; ++b)
@@ -182,7 +192,8 @@ static void shared_case(std::mt19937_64& r, int id) {
 int main() {
   std::mt19937_64 r(11);
   for (int i = 0; i < 2000; ++i) fork_case(r, i);
-  for (int i = 0; i < 400; ++i) shared_case(r, i);
+  for (int i = 0; i < 1500; ++i) shared_case(r, i);
+  CHECK(g_shared > 100 && g_passed_on > 100, "%d shared, %d passed on", g_shared, g_passed_on);
   // refusals
   sa_layout L = layout(8, 2, 16);
   std::string err;
