@@ -44,7 +44,7 @@ struct MergeRowsArgs {
   const MergeUnit* units;
   uint16_t* o;
   float* lse;                // nullable
-  int32_t Hq, G, block_rows;
+  int32_t Hq, Hkv, G, block_rows;
 };
 
 __device__ __forceinline__ float half_max(float x) {
@@ -58,7 +58,7 @@ __device__ __forceinline__ float half_sum(float x) {
   return x;
 }
 
-// Block (unit, y): rows block_rows y .. of the unit, 8 / block_rows half waves
+// Block ((unit, KV head), y): rows block_rows y .. of the unit, 8 / block_rows half waves
 // (32 threads, four d each) per row, which share the row's parts and meet in LDS.
 // A half wave takes its parts 32 at a time: lane c has the c-th one's weight, and
 // the partial rows are loaded eight ahead of their use.  With block_rows = 1, 2,
@@ -69,7 +69,8 @@ __device__ __forceinline__ float half_sum(float x) {
 __global__ __launch_bounds__(256) void merge_rows_kernel(MergeRowsArgs a) {
   __shared__ f32x4 red[8][32];
   __shared__ float red_m[8], red_den[8];
-  const MergeUnit u = ld_uniform(a.units + blockIdx.x);
+  const int unit = blockIdx.x / a.Hkv, kvh = blockIdx.x - unit * a.Hkv;
+  const MergeUnit u = ld_uniform(a.units + unit);
   const int r0 = blockIdx.y * a.block_rows;
   if (r0 >= u.n) return;
   const int lane = threadIdx.x & 63, hw = threadIdx.x >> 5, c = threadIdx.x & 31;
@@ -79,7 +80,8 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(MergeRowsArgs a) {
   const bool mine = r < u.n;
   const int np = mine ? u.a_n + u.b_n : 0;
   auto row_of = [&](int s) {
-    return (s < u.a_n ? (int64_t)u.a_row + (int64_t)s * u.a_stride : (int64_t)u.b_row + (int64_t)(s - u.a_n) * u.b_stride) + r;
+    return r + (s < u.a_n ? (int64_t)u.a_row + ((int64_t)kvh * u.a_n + s) * u.a_stride
+                          : (int64_t)u.b_row + ((int64_t)kvh * u.b_n + s - u.a_n) * u.b_stride);
   };
   float mx = -INFINITY, den = 0.f;
   f32x4 num = f32x4{};
@@ -131,7 +133,7 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(MergeRowsArgs a) {
   if (!mine) return;
   const float inv = den > 0.f ? 1.f / den : 0.f;
   const int row = u.r0 + r, tok = row / a.G;
-  const int64_t orow = (int64_t)(u.q_start + tok) * a.Hq + u.kvh * a.G + (row - tok * a.G);
+  const int64_t orow = (int64_t)(u.q_start + tok) * a.Hq + kvh * a.G + (row - tok * a.G);
   st_bf16x4(a.o + orow * kHD + 4 * c, num[0] * inv, num[1] * inv, num[2] * inv, num[3] * inv);
   if (a.lse != nullptr && c == 0)
     a.lse[orow] = den > 0.f ? (mx + __builtin_amdgcn_logf(den)) * 0.69314718055994531f : -INFINITY;

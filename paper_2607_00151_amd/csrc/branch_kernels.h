@@ -11,6 +11,7 @@
 #include "branch_plan.h"
 #include "common.h"
 #include "kv_kernels.h"
+#include "rope_kernels.h"
 
 namespace sa {
 
@@ -45,8 +46,13 @@ __global__ __launch_bounds__(256) void fork_kernel(ForkArgs a) {
   if ((int)blockIdx.x < a.table_blocks) {
     const int e = blockIdx.x * 256 + tid;
     if (e <= a.C) a.out_indptr[e] = a.dst_indptr[e];
+    // the child of the wave's first entry, and of each lane's from there on
+    const int first = __builtin_amdgcn_readfirstlane(e);
+    if (first >= a.n_dst) return;
+    int c = __builtin_amdgcn_readfirstlane(wave_find_seq(a.dst_indptr, a.C, first));
     if (e >= a.n_dst) return;
-    const ForkChild ch = a.children[find_seq(a.dst_indptr, a.C, e)];
+    if (a.dst_indptr[c + 1] <= min(first + 63, a.n_dst - 1)) c += find_seq(a.dst_indptr + c, a.C - c, e);
+    const ForkChild ch = a.children[c];
     const int j = e - ch.dst0;
     int32_t slot = -1;
     if (j < ch.full) {
@@ -60,8 +66,11 @@ __global__ __launch_bounds__(256) void fork_kernel(ForkArgs a) {
       atomicOr(a.err, 4);
     } else if (a.ref != nullptr) {
       // a shared page is in use already, a fresh slot is not
-      const int old = atomicAdd(a.ref + slot, 1);
-      if (j < ch.full ? old < 1 : old != 0) atomicOr(a.err, kCountError);
+      if (j >= ch.full) {
+        if (atomicAdd(a.ref + slot, 1) != 0) atomicOr(a.err, kCountError);
+      } else if (ch.raise > 0 && atomicAdd(a.ref + slot, ch.raise) < 1) {
+        atomicOr(a.err, kCountError);
+      }
     }
     return;
   }
@@ -142,57 +151,75 @@ __global__ __launch_bounds__(256) void count_kernel(CountArgs a) {
 
 constexpr int kScanThreads = 512;
 constexpr int kScanPer = 8;                                 // slots per thread
+constexpr int kScanWaves = kScanThreads / 64;
 constexpr int kScanChunk = kScanThreads * kScanPer;
 
-// Sums of two numbers over the block; every thread gets them.
-__device__ __forceinline__ int2 block_sum(int2 x, int2* room) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    x.x += __shfl_xor(x.x, d);
-    x.y += __shfl_xor(x.y, d);
-  }
-  __syncthreads();
-  if (lane == 0) room[wave] = x;
-  __syncthreads();
-  int2 s = {0, 0};
-#pragma unroll
-  for (int k = 0; k < kScanThreads / 64; ++k) {
-    s.x += room[k].x;
-    s.y += room[k].y;
-  }
-  return s;
+// A wave has 512 slots in a row, lane l slots l, 64 + l, ...: loads and stores of
+// whole lines, and a slot's place among the wave's listed ones by ballots.
+__device__ __forceinline__ int scan_slot(int i) {
+  return blockIdx.x * kScanChunk + (threadIdx.x >> 6) * (64 * kScanPer) + i * 64 + (threadIdx.x & 63);
+}
+__device__ __forceinline__ int lanes_before(uint64_t mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
 }
 
-// Sum over the threads before this one.
-__device__ __forceinline__ int block_before(int x, int2* room) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int inc = x;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(inc, d);
-    if (lane >= d) inc += y;
-  }
-  __syncthreads();
-  if (lane == 63) room[wave].x = inc;
-  __syncthreads();
-  int s = inc - x;
-  for (int k = 0; k < wave; ++k) s += room[k].x;
-  return s;
-}
+struct ScanRoom {
+  int own[kScanWaves], before[kScanWaves], all[kScanWaves];
+};
 
-// Listed slots before this block's chunk (x) and in all (y), from the chunks'
-// numbers or, with one chunk, from the thread's own.
-__device__ __forceinline__ int2 count_listed(const int32_t* counts, int chunks, int own, int2* room) {
-  int2 n = {0, 0};
-  if (counts == nullptr) n.y = own;
-  else
+// Of the listed slots (mask[i]: lanes whose i-th slot is): those before this
+// wave's (x) and all of the pool's (y).  counts: the chunks' numbers, or null with
+// one chunk.  Every thread of the block takes part.
+__device__ __forceinline__ int2 scan_block(const uint64_t (&mask)[kScanPer], const int32_t* counts, int chunks,
+                                           ScanRoom& room) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int own = 0;
+#pragma unroll
+  for (int i = 0; i < kScanPer; ++i) own += __popcll(mask[i]);
+  int before = 0, all = 0;
+  if (counts != nullptr) {
     for (int k = threadIdx.x; k < chunks; k += kScanThreads) {
       const int x = counts[k];
-      n.y += x;
-      if (k < (int)blockIdx.x) n.x += x;
+      all += x;
+      if (k < (int)blockIdx.x) before += x;
     }
-  return block_sum(n, room);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+      before += __shfl_xor(before, d);
+      all += __shfl_xor(all, d);
+    }
+  } else {
+    all = own;
+  }
+  if (lane == 0) {
+    room.own[wave] = own;
+    room.before[wave] = before;
+    room.all[wave] = all;
+  }
+  __syncthreads();
+  int2 n = {0, 0};
+#pragma unroll
+  for (int k = 0; k < kScanWaves; ++k) {
+    n.x += room.before[k] + (k < wave ? room.own[k] : 0);
+    n.y += room.all[k];
+  }
+  __syncthreads();                                          // the room may be used again
+  return n;
+}
+
+// A chunk's number of listed slots.
+__device__ __forceinline__ void count_block(const uint64_t (&mask)[kScanPer], int32_t* count, ScanRoom& room) {
+  int own = 0;
+#pragma unroll
+  for (int i = 0; i < kScanPer; ++i) own += __popcll(mask[i]);
+  if ((threadIdx.x & 63) == 0) room.own[threadIdx.x >> 6] = own;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    int n = 0;
+    for (int k = 0; k < kScanWaves; ++k) n += room.own[k];
+    *count = n;
+  }
+  __syncthreads();
 }
 
 struct FreeArgs {
@@ -203,32 +230,37 @@ struct FreeArgs {
   int32_t num_slots, chunks;
 };
 
-__global__ __launch_bounds__(kScanThreads) void free_count_kernel(FreeArgs a) {
-  __shared__ int2 room[kScanThreads / 64];
-  const int s0 = blockIdx.x * kScanChunk + threadIdx.x;
-  int2 n = {0, 0};
+__device__ __forceinline__ void idle_slots(const FreeArgs& a, uint64_t (&mask)[kScanPer]) {
+  bool idle[kScanPer];
 #pragma unroll
   for (int i = 0; i < kScanPer; ++i) {
-    const int s = s0 + i * kScanThreads;
-    n.x += s < a.num_slots && a.ref[s] == 0;
+    const int s = scan_slot(i);
+    idle[i] = s < a.num_slots && a.ref[s] == 0;
   }
-  n = block_sum(n, room);
-  if (threadIdx.x == 0) a.counts[blockIdx.x] = n.x;
+#pragma unroll
+  for (int i = 0; i < kScanPer; ++i) mask[i] = __ballot(idle[i]);
+}
+
+__global__ __launch_bounds__(kScanThreads) void free_count_kernel(FreeArgs a) {
+  __shared__ ScanRoom room;
+  uint64_t mask[kScanPer];
+  idle_slots(a, mask);
+  count_block(mask, a.counts + blockIdx.x, room);
 }
 
 // The slots without a count, ascending, then -1 up to num_slots.
 __global__ __launch_bounds__(kScanThreads) void free_list_kernel(FreeArgs a) {
-  __shared__ int2 room[kScanThreads / 64];
-  const int s0 = blockIdx.x * kScanChunk + threadIdx.x * kScanPer;
-  unsigned idle = 0;
-#pragma unroll
-  for (int i = 0; i < kScanPer; ++i) idle |= (unsigned)(s0 + i < a.num_slots && a.ref[s0 + i] == 0) << i;
-  const int2 n = count_listed(a.counts, a.chunks, __popc(idle), room);
-  int at = n.x + block_before(__popc(idle), room);
+  __shared__ ScanRoom room;
+  uint64_t mask[kScanPer];
+  idle_slots(a, mask);
+  const int2 n = scan_block(mask, a.counts, a.chunks, room);
+  int at = n.x;
 #pragma unroll
   for (int i = 0; i < kScanPer; ++i) {
-    if ((idle >> i) & 1) a.free_list[at++] = s0 + i;
-    if (s0 + i < a.num_slots && s0 + i >= n.y) a.free_list[s0 + i] = -1;
+    const int s = scan_slot(i);
+    if ((mask[i] >> (threadIdx.x & 63)) & 1) a.free_list[at + lanes_before(mask[i])] = s;
+    at += __popcll(mask[i]);
+    if (s < a.num_slots && s >= n.y) a.free_list[s] = -1;
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.num_free = n.y;
 }
@@ -257,25 +289,28 @@ struct CompactArgs {
 };
 
 // Holes are the free slots below the limit, movers the slots in use from it on.
-__device__ __forceinline__ bool is_hole(const CompactArgs& a, int s) { return s < a.limit && a.ref[s] <= 0; }
-__device__ __forceinline__ bool is_mover(const CompactArgs& a, int s) {
-  return s >= a.limit && s < a.num_slots && a.ref[s] > 0;
+__device__ __forceinline__ void holes_and_movers(const CompactArgs& a, int (&count)[kScanPer], uint64_t (&hole)[kScanPer],
+                                                 uint64_t (&mover)[kScanPer]) {
+#pragma unroll
+  for (int i = 0; i < kScanPer; ++i) {
+    const int s = scan_slot(i);
+    count[i] = s < a.num_slots ? a.ref[s] : 0;
+  }
+#pragma unroll
+  for (int i = 0; i < kScanPer; ++i) {
+    const int s = scan_slot(i);
+    hole[i] = __ballot(s < a.limit && count[i] <= 0);
+    mover[i] = __ballot(s >= a.limit && count[i] > 0);
+  }
 }
 
 __global__ __launch_bounds__(kScanThreads) void compact_count_kernel(CompactArgs a) {
-  __shared__ int2 room[kScanThreads / 64];
-  const int s0 = blockIdx.x * kScanChunk + threadIdx.x;
-  int2 n = {0, 0};
-#pragma unroll
-  for (int i = 0; i < kScanPer; ++i) {
-    n.x += is_hole(a, s0 + i * kScanThreads);
-    n.y += is_mover(a, s0 + i * kScanThreads);
-  }
-  n = block_sum(n, room);
-  if (threadIdx.x == 0) {
-    a.counts[blockIdx.x] = n.x;
-    a.counts[a.chunks + blockIdx.x] = n.y;
-  }
+  __shared__ ScanRoom room;
+  int count[kScanPer];
+  uint64_t hole[kScanPer], mover[kScanPer];
+  holes_and_movers(a, count, hole, mover);
+  count_block(hole, a.counts + blockIdx.x, room);
+  count_block(mover, a.counts + a.chunks + blockIdx.x, room);
 }
 
 // Ranks of holes and movers, of which the first min(holes, movers) take part.
@@ -284,41 +319,35 @@ __global__ __launch_bounds__(kScanThreads) void compact_count_kernel(CompactArgs
 constexpr int kStays = -1, kIdle = -2;
 
 __global__ __launch_bounds__(kScanThreads) void compact_rank_kernel(CompactArgs a) {
-  __shared__ int2 room[kScanThreads / 64];
-  const int s0 = blockIdx.x * kScanChunk + threadIdx.x * kScanPer;
+  __shared__ ScanRoom room;
   int count[kScanPer];
-  unsigned hole = 0, mover = 0;
-#pragma unroll
-  for (int i = 0; i < kScanPer; ++i) {
-    count[i] = s0 + i < a.num_slots ? a.ref[s0 + i] : 0;
-    hole |= (unsigned)(s0 + i < a.limit && count[i] <= 0) << i;
-    mover |= (unsigned)(s0 + i >= a.limit && count[i] > 0) << i;
-  }
-  const int2 hs = count_listed(a.counts, a.chunks, __popc(hole), room);
-  const int2 ms = count_listed(a.counts == nullptr ? nullptr : a.counts + a.chunks, a.chunks, __popc(mover), room);
+  uint64_t hole[kScanPer], mover[kScanPer];
+  holes_and_movers(a, count, hole, mover);
+  const int2 hs = scan_block(hole, a.counts, a.chunks, room);
+  const int2 ms = scan_block(mover, a.counts == nullptr ? nullptr : a.counts + a.chunks, a.chunks, room);
   const int n = min(hs.y, ms.y);
-  int h = hs.x + block_before(__popc(hole), room);
-  int m = ms.x + block_before(__popc(mover), room);
+  int h = hs.x, m = ms.x;
 #pragma unroll
   for (int i = 0; i < kScanPer; ++i) {
-    const int s = s0 + i;
-    if (s >= a.num_slots) break;
+    const int s = scan_slot(i);
     int rank = count[i] > 0 ? kStays : kIdle;
-    if ((hole >> i) & 1) {
-      if (h < n) {
-        rank = h;
-        a.hole[h] = s;
+    if ((hole[i] >> (threadIdx.x & 63)) & 1) {
+      const int at = h + lanes_before(hole[i]);
+      if (at < n) {
+        rank = at;
+        a.hole[at] = s;
       }
-      ++h;
-    } else if ((mover >> i) & 1) {
-      if (m < n) {
-        rank = m;
-        a.mover[m] = s;
-        a.mover_ref[m] = count[i];
+    } else if ((mover[i] >> (threadIdx.x & 63)) & 1) {
+      const int at = m + lanes_before(mover[i]);
+      if (at < n) {
+        rank = at;
+        a.mover[at] = s;
+        a.mover_ref[at] = count[i];
       }
-      ++m;
     }
-    a.rank[s] = rank;
+    h += __popcll(hole[i]);
+    m += __popcll(mover[i]);
+    if (s < a.num_slots) a.rank[s] = rank;
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     a.moved[0] = n;

@@ -16,9 +16,11 @@ namespace sa {
 
 // One child of a fork: the first `full` pages of its table are its parent's,
 // the others fresh slots from position `fresh0` of the free list on, the first
-// of which takes `rows` rows of the parent's partial page (0: it has none).
+// of which takes `rows` rows of the parent's partial page (0: it has none).  raise:
+// what the shared pages' counts rise by with this child's entries -- the number of
+// the parent's children for the first of them, 0 for the others.
 struct ForkChild {
-  int32_t parent, full, rows, fresh0, dst0;
+  int32_t parent, full, rows, fresh0, dst0, raise;
 };
 
 struct ForkPlan {
@@ -42,6 +44,7 @@ inline sa_status plan_fork(const sa_layout* layout, int32_t batch, const int32_t
   const int P = layout->page_size;
   out = ForkPlan{};
   out.dst_indptr.assign((size_t)num_children + 1, 0);
+  std::vector<int32_t> first((size_t)batch, -1);               // first child of each sequence
   for (int c = 0; c < num_children; ++c) {
     const int b = h_parent[c];
     if (b < 0 || b >= batch) return plan_fail(err, SA_ERR_RANGE, "child %d: parent %d outside [0, %d)", c, b, batch);
@@ -49,7 +52,9 @@ inline sa_status plan_fork(const sa_layout* layout, int32_t batch, const int32_t
     const int64_t len = h_src_len[b], full = len / P, rows = len % P;
     const int64_t pages = (len + h_reserve[c] + P - 1) / P;
     if (out.n_dst + pages > INT32_MAX) return plan_fail(err, SA_ERR_SHAPE, "destination table too large");
-    out.children.push_back({b, (int32_t)full, (int32_t)rows, (int32_t)out.fresh_used, (int32_t)out.n_dst});
+    if (first[b] < 0) first[b] = c;
+    out.children.push_back({b, (int32_t)full, (int32_t)rows, (int32_t)out.fresh_used, (int32_t)out.n_dst, 0});
+    ++out.children[first[b]].raise;
     if (rows > 0) out.copies.push_back(c);
     out.n_dst += pages;
     out.fresh_used += pages - full;
@@ -100,16 +105,18 @@ inline sa_status debug_check_fork(const ForkPlan& plan, const int32_t* indptr, c
 
 // ------------------------------------------------------------------ shared prefix
 
-// Rows of one member and KV head whose parts the merge joins: packed rows
+// Rows of one member whose parts the merge joins, of every KV head: packed rows
 // r0 .. r0 + n - 1 of the member whose first token is q_start.  Of the rows that
-// partials are kept by, row r0's are a_row, a_row + a_stride, ... (a_n of them: the
-// shared prefix) and b_row, b_row + b_stride, ... (b_n: the member's own keys), and
-// the next rows' follow each.
+// partials are kept by, row r0's of KV head 0 are a_row, a_row + a_stride, ... (a_n
+// of them: the shared prefix) and b_row, b_row + b_stride, ... (b_n: the member's
+// own keys), the next rows' follow each, and the next KV head's are a_n * a_stride
+// and b_n * b_stride further.
 struct MergeUnit {
-  int32_t q_start, r0, n, kvh;
+  int32_t q_start, r0, n;
   int32_t a_row, a_n, a_stride;
   int32_t b_row, b_n, b_stride;
 };
+constexpr int64_t kMaxPartRows = INT32_MAX - 1024;   // rows of all partials: places are int32
 constexpr int kMergeUnitRows = 32;     // most rows of a unit
 // rows per block of the merge, for rows of at most so many parts
 inline int merge_block_rows(int most_parts) { return most_parts <= 8 ? 8 : most_parts <= 16 ? 4 : most_parts <= 32 ? 2 : 1; }
@@ -323,6 +330,7 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
   for (Tile& t : tiles)
     if (t.prefix) place(t);
   out.part_rows = rows_used;
+  if (rows_used > kMaxPartRows) return;                         // refused by the caller
 
   // Bound by work, with more prefix parts than CUs but at most two for each: every
   // CU starts with one part, the members' own blocks fill its other slot, and the
@@ -343,76 +351,74 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
   // blocks: longest first, the row tiles of one key range next to each other on
   // one XCD (block i runs on XCD i % 8), which reads it through its L2 once
   struct Bundle {
-    int64_t tiles = 0;
-    bool prefix;
-    std::vector<AttnItem> items;
+    int64_t length;                                              // tiles of each of its items
+    int32_t tile, count, kvh, part;                              // row tiles tile .. tile + count - 1
   };
   std::vector<Bundle> bundles;
   for (size_t i = 0; i < tiles.size();) {
     size_t j = i + 1;
-    while (j < tiles.size() && tiles[j].seq == tiles[i].seq && tiles[j].prefix == tiles[i].prefix && tiles[i].prefix) ++j;
-    for (int h = 0; h < Hkv; ++h)
-      for (int k = 0; k < tiles[i].parts; ++k) {
-        Bundle bu;
-        bu.prefix = tiles[i].prefix;
-        for (size_t x = i; x < j; ++x) {
-          const Tile& t = tiles[x];
-          AttnItem it{t.seq, h, t.row0, 0, 0, -1, 0, t.q_start, t.q_len, t.kv_len};
-          it.kv_begin = (int32_t)(t.k0 + part_begin(t, k) * kKT);
-          it.kv_end = (int32_t)std::min<int64_t>(t.k0 + part_begin(t, k + 1) * kKT, t.k1);
-          if (t.place >= 0) it.part = (int32_t)(t.place + ((int64_t)h * t.parts + k) * t.rows);
-          bu.tiles += item_tiles(it);
-          bu.items.push_back(it);
-        }
-        bundles.push_back(std::move(bu));
-      }
+    while (j < tiles.size() && tiles[i].prefix && tiles[j].prefix && tiles[j].seq == tiles[i].seq) ++j;
+    for (int k = 0; k < tiles[i].parts; ++k) {
+      const int64_t length = part_begin(tiles[i], k + 1) - part_begin(tiles[i], k);
+      for (int h = 0; h < Hkv; ++h) bundles.push_back({length, (int32_t)i, (int32_t)(j - i), h, k});
+    }
     i = j;
   }
-  std::stable_sort(bundles.begin(), bundles.end(), [](const Bundle& x, const Bundle& y) {
-    return x.tiles * (int64_t)y.items.size() > y.tiles * (int64_t)x.items.size();
-  });
-  std::vector<std::vector<AttnItem>> queue(kNumXcd), fillers(kNumXcd);
+  std::stable_sort(bundles.begin(), bundles.end(), [](const Bundle& x, const Bundle& y) { return x.length > y.length; });
+  std::vector<int32_t> queue[kNumXcd], fillers[kNumXcd];        // bundles
   int64_t load[kNumXcd] = {0};
-  for (const Bundle& b : bundles) {
+  size_t n_queue[kNumXcd] = {0}, n_fill[kNumXcd] = {0}, depth = 0;
+  for (size_t i = 0; i < bundles.size(); ++i) {
+    const Bundle& b = bundles[i];
     const int x = (int)(std::min_element(load, load + kNumXcd) - load);
-    load[x] += b.tiles;
-    auto& q = fit && !b.prefix ? fillers[x] : queue[x];
-    q.insert(q.end(), b.items.begin(), b.items.end());
-  }
-  const size_t round = (size_t)std::max(1, num_cu / kNumXcd);
-  size_t depth = 0;
-  for (int x = 0; x < kNumXcd; ++x) {
-    auto& q = queue[x];
-    q.insert(q.begin() + std::min(round, q.size()), fillers[x].begin(), fillers[x].end());
-    depth = std::max(depth, q.size());
+    load[x] += b.length * b.count;
+    const bool filler = fit && !tiles[b.tile].prefix;
+    (filler ? fillers : queue)[x].push_back((int32_t)i);
+    (filler ? n_fill : n_queue)[x] += b.count;
+    depth = std::max(depth, n_fill[x] + n_queue[x]);
   }
   out.items.assign(depth * kNumXcd, AttnItem{0, 0, 0, 0, 0, -1, 0, 0, 0, 0});
-  for (int x = 0; x < kNumXcd; ++x)
-    for (size_t i = 0; i < queue[x].size(); ++i) out.items[i * kNumXcd + x] = queue[x][i];
+  const size_t round = (size_t)std::max(1, num_cu / kNumXcd);
+  for (int x = 0; x < kNumXcd; ++x) {
+    size_t at = 0, gap = std::min(round, n_queue[x]);           // the fillers' place
+    auto emit = [&](const Bundle& b) {
+      for (int32_t y = b.tile; y < b.tile + b.count; ++y) {
+        if (at == gap) at += n_fill[x];
+        const Tile& t = tiles[y];
+        AttnItem it{t.seq, b.kvh, t.row0, 0, 0, -1, 0, t.q_start, t.q_len, t.kv_len};
+        it.kv_begin = (int32_t)(t.k0 + part_begin(t, b.part) * kKT);
+        it.kv_end = (int32_t)std::min<int64_t>(t.k0 + part_begin(t, b.part + 1) * kKT, t.k1);
+        if (t.place >= 0) it.part = (int32_t)(t.place + ((int64_t)b.kvh * t.parts + b.part) * t.rows);
+        out.items[at++ * kNumXcd + x] = it;
+      }
+    };
+    for (int32_t i : queue[x]) emit(bundles[i]);
+    at = gap;
+    gap = SIZE_MAX;
+    for (int32_t i : fillers[x]) emit(bundles[i]);
+  }
 
   // merge units: rows of one member, one own tile and one prefix tile
   for (const Member& m : members) {
     const int32_t n = seqs[m.seq].q_len * G;
-    for (int h = 0; h < Hkv; ++h)
-      for (int32_t r = 0; r < n;) {
-        const Tile& own = tiles[m.own0 + r / kRows];
-        int32_t e = std::min(r + kMergeUnitRows, std::min(own.row0 + own.rows, n));
-        MergeUnit u{seqs[m.seq].q_start, r, 0, h, 0, 0, 0, 0, own.parts, own.rows};
-        u.b_row = (int32_t)(own.place + (int64_t)h * own.parts * own.rows + r - own.row0);
-        if (m.prefix0 >= 0) {
-          const Tile& pre = tiles[m.prefix0 + (m.row_in_group + r) / kRows];
-          e = std::min(e, pre.row0 + kRows - m.row_in_group);
-          u.a_row = (int32_t)(pre.place + (int64_t)h * pre.parts * pre.rows + m.row_in_group + r - pre.row0);
-          u.a_n = pre.parts;
-          u.a_stride = pre.rows;
-        }
-        u.n = e - r;
-        r = e;
-        if (own.place < 0) continue;
-        out.units.push_back(u);
-        out.most_rows = std::max(out.most_rows, u.n);
-        out.most_parts = std::max(out.most_parts, u.a_n + u.b_n);
+    for (int32_t r = 0; r < n;) {
+      const Tile& own = tiles[m.own0 + r / kRows];
+      int32_t e = std::min(r + kMergeUnitRows, std::min(own.row0 + own.rows, n));
+      MergeUnit u{seqs[m.seq].q_start, r, 0, 0, 0, 0, (int32_t)own.place + r - own.row0, own.parts, own.rows};
+      if (m.prefix0 >= 0) {
+        const Tile& pre = tiles[m.prefix0 + (m.row_in_group + r) / kRows];
+        e = std::min(e, pre.row0 + kRows - m.row_in_group);
+        u.a_row = (int32_t)pre.place + m.row_in_group + r - pre.row0;
+        u.a_n = pre.parts;
+        u.a_stride = pre.rows;
       }
+      u.n = e - r;
+      r = e;
+      if (own.place < 0) continue;
+      out.units.push_back(u);
+      out.most_rows = std::max(out.most_rows, u.n);
+      out.most_parts = std::max(out.most_parts, u.a_n + u.b_n);
+    }
   }
 }
 

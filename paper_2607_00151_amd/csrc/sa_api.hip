@@ -1687,7 +1687,8 @@ sa_status shared_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   uint8_t* dev = ctx->plans[kPlanShared].dev;
   if (!same) {
     sa::plan_shared_items(layout, seqs, num_groups, h_group_indptr, h_shared_len, ctx->num_cu, plan);
-    if (plan.part_rows > INT32_MAX) return fail(SA_ERR_SHAPE, "too many partial rows (%lld)", (long long)plan.part_rows);
+    if (plan.part_rows > sa::kMaxPartRows)
+      return fail(SA_ERR_SHAPE, "too many partial rows (%lld)", (long long)plan.part_rows);
     rec.shared = plan.shared;
     rec.n_items = plan.items.size();
     rec.n_units = plan.units.size();
@@ -1740,8 +1741,8 @@ sa_status shared_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   else launch_shared<32>(pool_rsrc, grid, (hipStream_t)stream, ctx->kernel_ev[SA_TIMED_ATTN], a);
   SA_HIP(hipGetLastError());
   if (rec.n_units > 0) {
-    sa::MergeRowsArgs m{a.part_o, a.part_lse, (const sa::MergeUnit*)(dev + rec.o_un), a.o, lse, a.Hq, a.G, rec.block_rows};
-    const dim3 blocks((unsigned)rec.n_units, (unsigned)((rec.most_rows + rec.block_rows - 1) / rec.block_rows));
+    sa::MergeRowsArgs m{a.part_o, a.part_lse, (const sa::MergeUnit*)(dev + rec.o_un), a.o, lse, a.Hq, a.Hkv, a.G, rec.block_rows};
+    const dim3 blocks((unsigned)(rec.n_units * a.Hkv), (unsigned)((rec.most_rows + rec.block_rows - 1) / rec.block_rows));
     hipLaunchKernelGGL(sa::merge_rows_kernel, blocks, dim3(256), 0, (hipStream_t)stream, m);
     SA_HIP(hipGetLastError());
   }
