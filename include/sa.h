@@ -546,7 +546,8 @@ sa_status sa_kv_append_rope(sa_ctx *ctx, const sa_layout *layout, int32_t layer,
  * the child's first fresh slot (whose other rows stay as they are), so the
  * child's appends never touch a shared page.  A sequence may have any number of
  * children; its own table stays as it is.  The children's table is written to
- * d_dst_indptr[num_children + 1] and d_dst_indices (capacity dst_capacity).
+ * d_dst_indptr[num_children + 1] and d_dst_indices (capacity dst_capacity),
+ * which must not be the source table.
  * d_ref (nullable): the count of every listed slot is raised by one per entry.
  * *h_fresh_used receives the number of fresh slots taken.  Fresh slots must not
  * repeat nor be pages of a source context (SA_DEBUG=1 checks).
@@ -595,7 +596,8 @@ sa_status sa_kv_release(sa_ctx *ctx, const sa_layout *layout, int32_t batch, sa_
  *   d_indices_out     the num_entries table entries d_indices through the map
  *                     (may be d_indices); an entry outside the pool stays as it
  *                     is and is latched
- * Moved pages stay in their old slots too, as bits nobody names.
+ * Moved pages stay in their old slots too, as bits nobody names.  The outputs
+ * other than d_ref_out and d_indices_out must not overlap the inputs.
  * Errors: SA_ERR_RANGE (limit outside [0, num_slots]), SA_ERR_SHAPE,
  * SA_ERR_NULL, SA_ERR_ALIGN, SA_ERR_HIP.
  */
@@ -615,7 +617,8 @@ sa_status sa_kv_compact(sa_ctx *ctx, const sa_layout *layout, void *k_pool, void
  * sa_kv_fork leaves them, or equal copies): whole 64-key tiles of them are read
  * through the page list of the group's first member that has query rows.  The
  * result is that of sa_segment_prefill_attn over the same tables, held to the
- * same tolerance.  shared_len may be anything from 0 to the smallest
+ * same tolerance (and, as there, an infinite or NaN value row of the segment
+ * reaches the earlier rows of its own 64-key tile).  shared_len may be anything from 0 to the smallest
  * h_kv_len - h_q_len of the group.  Where the members' rows fill the kernel's
  * row tiles anyway (long segments) the group is computed member by member, and a
  * batch that would gain nothing goes to the segment attention's launch.  The

@@ -148,7 +148,7 @@ def _load_torch():
     global _torch, _KINDS, _raw_stream
     import torch
     two = {d for d in (getattr(torch, n, None) for n in ("bfloat16", "float16", "int16", "uint16")) if d is not None}
-    _KINDS = {"i32": {torch.int32}, "b16": two, "f32": {torch.float32}}
+    _KINDS = {"i32": {torch.int32}, "b16": two, "f32": {torch.float32}, "bf16": two - {torch.float16}}
     # the current stream's handle without a Stream object around it, where torch has it
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     _torch = torch
@@ -158,7 +158,8 @@ def _load_torch():
 def _dev(t, what: str, kind: str, min_numel: int = 0, nullable: bool = False):
     """Device address of a caller tensor after checking what the C ABI will assume
     of it: a contiguous CUDA tensor whose element type matches `kind` ("i32": int32
-    table entries, "b16": 2-byte bf16 bit patterns, "f32": float32) and that holds at
+    table entries, "b16": 2-byte bf16 bit patterns, "bf16": the same, but not
+    float16, "f32": float32) and that holds at
     least min_numel elements.  Raises ValueError otherwise; None passes only when
     nullable."""
     if t is None:
@@ -174,7 +175,8 @@ def _dev(t, what: str, kind: str, min_numel: int = 0, nullable: bool = False):
         raise ValueError(f"{what}: tensor is not contiguous")
     # the types in everyday use by a table; any other 2-byte type that is not bool by its size
     if t.dtype not in _KINDS[kind] and not (kind == "b16" and t.element_size() == 2 and t.dtype != torch.bool):
-        want = {"i32": "torch.int32", "b16": "a 2-byte dtype (bf16 bits)", "f32": "torch.float32"}[kind]
+        want = {"i32": "torch.int32", "b16": "a 2-byte dtype (bf16 bits)", "f32": "torch.float32",
+                "bf16": "torch.bfloat16 (or its bits in a 2-byte integer)"}[kind]
         raise ValueError(f"{what}: dtype {t.dtype}, expected {want}")
     if t.numel() < min_numel:
         raise ValueError(f"{what}: {t.numel()} elements, at least {min_numel} needed")
@@ -523,8 +525,8 @@ def _head_rows(t, what: str, tokens: int, heads: int, d: int, device):
         raise ValueError(f"{what}: tensor is not on a GPU")
     if device is not None and at != device:
         raise ValueError(f"{what}: the tensor is on device {at}, the context on device {device}")
-    if t.dtype not in _KINDS["b16"]:
-        raise ValueError(f"{what}: dtype {t.dtype}, expected a 2-byte dtype (bf16 bits)")
+    if t.dtype not in _KINDS["bf16"]:
+        raise ValueError(f"{what}: dtype {t.dtype}, expected torch.bfloat16 (or its bits in a 2-byte integer)")
     shape, stride = t.shape, t.stride()
     if len(shape) != 3 or shape[0] < tokens or shape[1] != heads or shape[2] != d:
         raise ValueError(f"{what}: shape {tuple(shape)}, expected ({tokens}, {heads}, {d})")
@@ -546,8 +548,8 @@ class Rope:
     def _struct(self, d: int, device):
         n = len(self.inv_freq)
         return _Rope(2 * n, self.interleaved, _ptr(self.inv_freq) if n else None,
-                     None if self.q_weight is None else _on(self.q_weight, "q_weight", "b16", d, device),
-                     None if self.k_weight is None else _on(self.k_weight, "k_weight", "b16", d, device), self.eps,
+                     None if self.q_weight is None else _on(self.q_weight, "q_weight", "bf16", d, device),
+                     None if self.k_weight is None else _on(self.k_weight, "k_weight", "bf16", d, device), self.eps,
                      self.weight_offset)
 
 
@@ -568,8 +570,8 @@ def sa_kv_append_rope(ctx, layout: Layout, layer: int, rope: Rope, q, k_new, v_n
     n = _pool_numel(layout)
     _check(load_library().sa_kv_append_rope(
         _ctx_handle(ctx), ctypes.byref(layout), int(layer), ctypes.byref(rope._struct(D, at)), qp, qs, kp, ks, vp, vs,
-        _on(q_out, "q_out", "b16", T * Hq * D, at, nullable=T == 0), _on(k_pool, "k_pool", "b16", n, at),
-        _on(v_pool, "v_pool", "b16", n, at), B, _ptr(start), _ptr(new_len), _ptr(pos),
+        _on(q_out, "q_out", "bf16", T * Hq * D, at, nullable=T == 0), _on(k_pool, "k_pool", "bf16", n, at),
+        _on(v_pool, "v_pool", "bf16", n, at), B, _ptr(start), _ptr(new_len), _ptr(pos),
         _table_on(pages_indptr, pages_indices, B, at, "page table"), _stream_of(ctx, stream)))
 
 
@@ -588,7 +590,7 @@ def sa_kv_fork(ctx, layout: Layout, k_pool, v_pool, src_len, parent, reserve, sr
     B, C, n, at = len(src_len), len(parent), _pool_numel(layout), _device_of(ctx)
     used = ctypes.c_int32(0)
     _check(load_library().sa_kv_fork(
-        _ctx_handle(ctx), ctypes.byref(layout), _on(k_pool, "k_pool", "b16", n, at), _on(v_pool, "v_pool", "b16", n, at),
+        _ctx_handle(ctx), ctypes.byref(layout), _on(k_pool, "k_pool", "bf16", n, at), _on(v_pool, "v_pool", "bf16", n, at),
         B, _ptr(src_len), C, _ptr(parent), _ptr(reserve), _table_on(src_indptr, src_indices, B, at, "src", True),
         _on(fresh, "fresh", "i32", 0, at, nullable=True), 0 if fresh is None else fresh.numel(),
         _on(dst_indptr, "dst indptr", "i32", C + 1, at), _on(dst_indices, "dst indices", "i32", 0, at, nullable=True),
@@ -627,7 +629,7 @@ def sa_kv_compact(ctx, layout: Layout, k_pool, v_pool, limit: int, ref, ref_out,
     n, slots, at = _pool_numel(layout), layout.num_slots, _device_of(ctx)
     entries = 0 if indices is None else indices.numel()
     _check(load_library().sa_kv_compact(
-        _ctx_handle(ctx), ctypes.byref(layout), _on(k_pool, "k_pool", "b16", n, at), _on(v_pool, "v_pool", "b16", n, at),
+        _ctx_handle(ctx), ctypes.byref(layout), _on(k_pool, "k_pool", "bf16", n, at), _on(v_pool, "v_pool", "bf16", n, at),
         int(limit), _on(ref, "ref", "i32", slots, at), _on(ref_out, "ref_out", "i32", slots, at),
         _on(indices, "indices", "i32", 0, at, nullable=entries == 0),
         _on(indices_out, "indices_out", "i32", entries, at, nullable=entries == 0), entries,
@@ -647,8 +649,8 @@ def sa_shared_prefix_attn(ctx, layout: Layout, layer: int, q, k_pool, v_pool, q_
     B, T, at, n = len(q_len), max(0, _total(q_len)), _device_of(ctx), _pool_numel(layout)
     rows = T * layout.num_q_heads
     _check(load_library().sa_shared_prefix_attn(
-        _ctx_handle(ctx), ctypes.byref(layout), int(layer), _on(q, "q", "b16", rows * layout.head_dim, at, T == 0),
-        _on(k_pool, "k_pool", "b16", n, at), _on(v_pool, "v_pool", "b16", n, at), B, _ptr(q_len), _ptr(kv_len),
+        _ctx_handle(ctx), ctypes.byref(layout), int(layer), _on(q, "q", "bf16", rows * layout.head_dim, at, T == 0),
+        _on(k_pool, "k_pool", "bf16", n, at), _on(v_pool, "v_pool", "bf16", n, at), B, _ptr(q_len), _ptr(kv_len),
         _table_on(pages_indptr, pages_indices, B, at, "page table"), len(shared), _ptr(groups), _ptr(shared),
-        float(softmax_scale), _on(o, "o", "b16", rows * layout.head_dim, at, T == 0),
+        float(softmax_scale), _on(o, "o", "bf16", rows * layout.head_dim, at, T == 0),
         None if lse is None else _on(lse, "lse", "f32", rows, at), _stream_of(ctx, stream)))

@@ -235,7 +235,7 @@ __device__ __forceinline__ void idle_slots(const FreeArgs& a, uint64_t (&mask)[k
 #pragma unroll
   for (int i = 0; i < kScanPer; ++i) {
     const int s = scan_slot(i);
-    idle[i] = s < a.num_slots && a.ref[s] == 0;
+    idle[i] = s < a.num_slots && a.ref[s] <= 0;
   }
 #pragma unroll
   for (int i = 0; i < kScanPer; ++i) mask[i] = __ballot(idle[i]);

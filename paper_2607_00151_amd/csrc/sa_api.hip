@@ -1257,9 +1257,13 @@ struct DeviceGuard {
 // whatever plan is there by then, so it is not captured into a graph.
 sa_status refuse_capture(hipStream_t stream, const char* call) {
   hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
-  SA_HIP(hipStreamIsCapturing(stream, &st));
+  const hipError_t e = hipStreamIsCapturing(stream, &st);
+  if (e != hipSuccess) {
+    (void)hipGetLastError();         // not left for a later call's check
+    return fail(SA_ERR_HIP, "hipStreamIsCapturing failed: %s", hipGetErrorString(e));
+  }
   if (st != hipStreamCaptureStatusNone)
-    return fail(SA_ERR_UNSUPPORTED, "%s keeps its plan in the context and cannot be captured into a graph", call);
+    return fail(SA_ERR_UNSUPPORTED, "%s cannot be captured into a graph", call);
   return SA_OK;
 }
 
@@ -1273,8 +1277,10 @@ sa_status no_throw(F&& body) {
   }
 }
 
-sa_status reserve_work(sa_ctx* ctx, size_t need) {
+sa_status reserve_work(sa_ctx* ctx, size_t need, hipStream_t stream) {
   if (need <= ctx->work_cap) return SA_OK;
+  const sa_status s = refuse_capture(stream, "a call that has to allocate for a pool of this size");
+  if (s != SA_OK) return s;
   if (ctx->work) ctx->retired_dev.push_back(ctx->work);
   ctx->work = nullptr;
   ctx->work_cap = 0;
@@ -1293,6 +1299,8 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
     return fail(SA_ERR_SHAPE, "layer %d outside [0, %d)", layer, layout->num_layers);
   if (batch < 1) return fail(SA_ERR_SHAPE, "batch %d < 1", batch);
   const int Hq = layout->num_q_heads, Hkv = layout->num_kv_heads;
+  if ((int64_t)Hq + 2 * (int64_t)Hkv > (1 << 16))
+    return fail(SA_ERR_UNSUPPORTED, "%d + 2 * %d heads (at most 65536)", Hq, Hkv);
   if (!rope) return fail(SA_ERR_NULL, "rope is NULL");
   if (rope->rot_dim < 0 || rope->rot_dim > sa::kHD || rope->rot_dim % 16 != 0)
     return fail(SA_ERR_UNSUPPORTED, "rot_dim %d (a multiple of 16 up to 128)", rope->rot_dim);
@@ -1353,7 +1361,7 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   s = check_ctx(ctx);
   if (s != SA_OK) return s;
   if (rec.total == 0) return SA_OK;
-  s = refuse_capture((hipStream_t)stream, "sa_kv_append_rope");
+  s = refuse_capture((hipStream_t)stream, "sa_kv_append_rope keeps its plan in the context and");
   if (s != SA_OK) return s;
   if (debug_checks()) {
     std::vector<int32_t> ip, ix;
@@ -1471,7 +1479,7 @@ sa_status kv_fork(sa_ctx* ctx, const sa_layout* layout, void* k_pool, void* v_po
   DeviceGuard guard;
   s = check_ctx(ctx);
   if (s != SA_OK) return s;
-  s = refuse_capture((hipStream_t)stream, "sa_kv_fork");
+  s = refuse_capture((hipStream_t)stream, "sa_kv_fork keeps its plan in the context and");
   if (s != SA_OK) return s;
   if (debug_checks()) {
     std::vector<int32_t> ip, ix, fresh((size_t)rec.fresh_used);
@@ -1562,7 +1570,7 @@ sa_status kv_release(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_pag
   const int chunks = (int)((layout->num_slots + sa::kScanChunk - 1) / sa::kScanChunk);
   const bool counted = chunks > 1;
   if (counted && d_free != nullptr) {
-    s = reserve_work(ctx, (size_t)chunks * sizeof(int32_t));
+    s = reserve_work(ctx, (size_t)chunks * sizeof(int32_t), st);
     if (s != SA_OK) return s;
   }
   launch_count<false>(ctx, layout, batch, pages, max_entries, d_ref, st);
@@ -1596,7 +1604,7 @@ sa_status kv_compact(sa_ctx* ctx, const sa_layout* layout, void* k_pool, void* v
   const hipStream_t st = (hipStream_t)stream;
   const size_t n = (size_t)layout->num_slots;
   const int chunks = (int)((n + sa::kScanChunk - 1) / sa::kScanChunk);
-  s = reserve_work(ctx, (4 * n + 2 * (size_t)chunks) * sizeof(int32_t));
+  s = reserve_work(ctx, (4 * n + 2 * (size_t)chunks) * sizeof(int32_t), st);
   if (s != SA_OK) return s;
   sa::CompactArgs a{};
   a.k_pool = (uint16_t*)k_pool;
@@ -1681,7 +1689,7 @@ sa_status shared_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   s = check_ctx(ctx);
   if (s != SA_OK) return s;
   if (rec.total_q == 0) return SA_OK;
-  s = refuse_capture((hipStream_t)stream, "sa_shared_prefix_attn");
+  s = refuse_capture((hipStream_t)stream, "sa_shared_prefix_attn keeps its plan in the context and");
   if (s != SA_OK) return s;
   sa::SharedPlan plan;
   uint8_t* dev = ctx->plans[kPlanShared].dev;
@@ -1706,12 +1714,14 @@ sa_status shared_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
     ctx->plans[kPlanShared].key_valid = true;
   }
   if (!rec.shared) {
-    const bool exact = ctx->exact_scale;
+    struct Exact {
+      bool& now;
+      const bool before;
+      ~Exact() { now = before; }
+    } scale{ctx->exact_scale, ctx->exact_scale};
     ctx->exact_scale = true;
-    s = attn_launch(ctx, layout, layer, q, k_pool, v_pool, false, nullptr, nullptr, batch, h_q_len, h_kv_len, pages,
-                    softmax_scale, o, lse, stream);
-    ctx->exact_scale = exact;
-    return s;
+    return attn_launch(ctx, layout, layer, q, k_pool, v_pool, false, nullptr, nullptr, batch, h_q_len, h_kv_len, pages,
+                       softmax_scale, o, lse, stream);
   }
   s = reserve_parts(ctx, (size_t)rec.part_rows * (sa::kHD + 1) * sizeof(float));
   if (s != SA_OK) return s;

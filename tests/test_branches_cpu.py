@@ -66,7 +66,7 @@ def rope(lib, L=None, freq=None, rot=128, eps=1e-6, w=FAKE, off=0.0, interleaved
     (CTX, {}), (CTX, dict(rot=0, freq=[])), (CTX, dict(w=None, eps=0.0)), (CTX, dict(interleaved=1)),
     (CTX, dict(pos=[2**31 - 3])), (CTX, dict(new=[0], q=None, k=None, q_out=None)), (CTX, dict(qs=1536)),
     (UNSUPPORTED, dict(L=layout(head_dim=64))), (UNSUPPORTED, dict(rot=24)), (UNSUPPORTED, dict(rot=144)),
-    (UNSUPPORTED, dict(rot=-16)), (NULL, dict(no_struct=True)), (NULL, dict(freq=[])), (SHAPE, dict(eps=0.0)),
+    (UNSUPPORTED, dict(rot=-16)), (UNSUPPORTED, dict(L=layout(num_q_heads=65536, num_kv_heads=1), qs=65536 * 128)), (NULL, dict(no_struct=True)), (NULL, dict(freq=[])), (SHAPE, dict(eps=0.0)),
     (SHAPE, dict(eps=float("nan"))), (SHAPE, dict(off=float("inf"))), (SHAPE, dict(freq=[-1.0] + [1.0] * 63)),
     (SHAPE, dict(freq=[float("nan")] * 64)), (SHAPE, dict(freq=[2000.0] * 64)), (SHAPE, dict(qs=1016)),
     (SHAPE, dict(ks=128)), (SHAPE, dict(vs=0)), (SHAPE, dict(qs=1 << 40)), (ALIGN, dict(qs=1028)), (SHAPE, dict(layer=2)),

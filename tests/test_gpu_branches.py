@@ -592,6 +592,89 @@ def test_planned_calls_refuse_capture():
             sa.sa_kv_fork(ctx, w["L"], w["kp"], w["vp"], [16], [0], [0], w["indptr"], w["indices"], t, t, t)
 
 
+def test_counts_refuse_to_allocate_in_a_capture():
+    L = lay((2, 2), 16, 10000)
+    ctx = sa.Context(0)
+    ref, free = torch.zeros(10000, dtype=torch.int32, device="cuda"), torch.zeros(10000, dtype=torch.int32, device="cuda")
+    n, ip, ix = torch.zeros(1, dtype=torch.int32, device="cuda"), dev([0, 1]), dev([3])
+    sa.sa_kv_retain(ctx, L, ip, ix, ref)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        with pytest.raises(sa.SaError, match="SA_ERR_UNSUPPORTED"):
+            sa.sa_kv_release(ctx, L, ip, ix, ref, free, n)
+    sa.sa_kv_release(ctx, L, ip, ix, ref, free, n)
+    sa.sa_sync_check(ctx)
+    assert int(n) == 10000 and torch.equal(free.cpu(), torch.arange(10000, dtype=torch.int32))
+
+
+def test_binding_refuses_other_types_and_layouts():
+    L = lay((4, 2), 16, 8)
+    ctx = sa.Context(0)
+    q, k = torch.zeros((2, 4, D), dtype=torch.bfloat16, device="cuda"), torch.zeros((2, 2, D), dtype=torch.bfloat16, device="cuda")
+    pool = torch.zeros((1, 8, 2, 16, D), dtype=torch.bfloat16, device="cuda")
+    ip, ix = dev([0, 1]), dev([3])
+
+    def rope(q=q, k=k, out=q, pool=pool, r=sa.Rope(), ip=ip):
+        sa.sa_kv_append_rope(ctx, L, 0, r, q, k, k, out, pool, pool.clone(), [0], [2], ip, ix)
+
+    rope()
+    for bad in (dict(q=q.half()), dict(out=q.half()), dict(q=q.float()), dict(k=k.transpose(0, 1)), dict(q=q[:, :3]),
+                dict(q=q.flatten(1)), dict(q=q[:1]), dict(out=q[:1]), dict(pool=pool.half()), dict(pool=pool[:, :7]),
+                dict(r=sa.Rope(q_weight=q[0, 0].half())), dict(r=sa.Rope(q_weight=q[0, 0, :64])), dict(ip=ip.long()),
+                dict(q=torch.zeros((2, 4, 2 * D), dtype=torch.bfloat16, device="cuda")[:, :, ::2]), dict(q=None)):
+        with pytest.raises(ValueError):
+            rope(**bad)
+    for stride_ok in (torch.zeros((2, 9, D), dtype=torch.bfloat16, device="cuda")[:, 1:5],):
+        rope(q=stride_ok)
+    with pytest.raises(sa.SaError, match="SA_ERR_SHAPE"):
+        rope(q=q[:1].expand(2, 4, D))
+    with pytest.raises(ValueError):
+        sa.sa_kv_release(ctx, L, ip, ix, torch.zeros(7, dtype=torch.int32, device="cuda"))
+    with pytest.raises(ValueError):
+        sa.sa_kv_compact(ctx, L, pool, pool, 4, ix, ix, ix, ix, ix, ix)
+    sa.sa_sync_check(ctx)
+
+
+def test_pools_beyond_4_gib_of_a_layer():
+    """Slots whose rows lie past 2^32 bytes of their pool: every call reaches them."""
+    r = np.random.default_rng(31)
+    heads, page, far = (32, 8), 16, 139000
+    w = branch_batch(r, heads, page, [(1500, [(90, 1)] * 20)])
+    small, big = w["L"], lay(heads, page, far + w["L"].num_slots)
+    pools = []
+    for name in ("kp", "vp"):
+        p = torch.empty((1, big.num_slots, 8, page, D), dtype=torch.int16, device="cuda")
+        p[:, far:] = w[name]
+        pools.append(p)
+    w.update(L=big, kp=pools[0], vp=pools[1], indices=w["indices"] + far)
+    ctx = sa.Context(0)
+    o, lse = run_shared(ctx, w)
+    check_attention(w, o, lse, D ** -0.5)
+    # new rows onto the first member's last page, through a fork of it
+    ref = torch.zeros(big.num_slots, dtype=torch.int32, device="cuda")
+    one_ip, one_ix = w["indptr"][:2].contiguous(), w["indices"][:int(w["indptr"][1])].contiguous()
+    sa.sa_kv_retain(ctx, big, one_ip, one_ix, ref)
+    fresh = dev([far + small.num_slots - 1])
+    dip, dix = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(100, dtype=torch.int32, device="cuda")
+    assert sa.sa_kv_fork(ctx, big, *pools, [1590], [0], [1], one_ip, one_ix, fresh, dip, dix, ref=ref) == 1
+    q, k, v = rows(r, (1, 32, D)).cuda(), rows(r, (1, 8, D)).cuda(), rows(r, (1, 8, D)).cuda()
+    out = torch.empty_like(q)
+    sa.sa_kv_append_rope(ctx, big, 0, sa.Rope(), q, k, v, out, *pools, [1590], [1], dip, dix)
+    sa.sa_sync_check(ctx)
+    last = pools[0][0, int(fresh[0])]
+    assert torch.equal(last[:, :6], pools[0][0, int(one_ix[-1])][:, :6])
+    assert torch.equal(last[:, 6], k[0].view(torch.int16)) and torch.equal(out, q)
+    # and down into the first slots
+    smap, mv = torch.zeros_like(ref), torch.zeros(2, dtype=torch.int32, device="cuda")
+    kept = dix[:100].contiguous()
+    before = pools[1][0, kept.long()].clone()
+    sa.sa_kv_compact(ctx, big, *pools, far, ref, ref, kept, kept, smap, mv)
+    sa.sa_sync_check(ctx)
+    assert mv.tolist() == [101, 0] and int(kept.max()) <= 100
+    assert torch.equal(pools[1][0, kept.long()], before)
+
+
 # ------------------------------------------------------------------------- together
 
 def test_branches_from_fork_to_compaction():
