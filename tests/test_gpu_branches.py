@@ -413,8 +413,15 @@ def test_counts_and_compaction_replay_from_a_graph():
 
 # ------------------------------------------------------------------------- sa_shared_prefix_attn
 
+def anchor(heads):
+    """A group whose prefix is worth reading once: with it in the batch the call shares every group's prefix it can,
+    however small, instead of passing the batch on to the segment attention."""
+    return (28000 // heads[1], [(3, 1)] * 32)
+
+
 def branch_batch(r, heads, page, groups, layers=1, layer=0, spare=2):
-    """Caches of groups [(shared, [(own, q), ...])], pages shared as a fork leaves them: the partial one copied."""
+    """Caches of groups [(shared, [(own, q), ...])], pages shared as a fork leaves them: the partial one copied.
+    K, V: each sequence's rows as (shared part, own part)."""
     Hq, Hkv = heads
     lists, at, q_len, kv_len, gp, need = [], 0, [], [], [0], 0
     for s, members in groups:
@@ -423,29 +430,37 @@ def branch_batch(r, heads, page, groups, layers=1, layer=0, spare=2):
     perm = r.permutation(L.num_slots).astype(np.int32)
     kp, vp = pool_bits(r, L, FILL), pool_bits(r, L, FILL)
     K, V = [], []
-    host = [torch.full(kp.shape[1:], float("nan"), dtype=torch.bfloat16) for _ in range(2)]
+    g = torch.Generator(device="cuda").manual_seed(int(r.integers(1 << 30)))
+
+    def gpu_rows(n):
+        return (torch.randn((n, Hkv, D), generator=g, device="cuda") * 0.5).to(torch.bfloat16)
+
+    def put(pool, pages, first, x):
+        pos = first + torch.arange(len(x), device="cuda")
+        slot = torch.from_numpy(np.array(pages, dtype=np.int64)).cuda()[pos // page]
+        pool[layer].permute(0, 2, 1, 3)[slot, pos % page] = x.view(torch.int16)
+
     for s, members in groups:
         common = list(perm[at:at + s // page])
         at += s // page
-        ks, vs = rows(r, (s, Hkv, D)), rows(r, (s, Hkv, D))
+        ks, vs = gpu_rows(s), gpu_rows(s)
+        cut = s // page * page
+        if cut:
+            put(kp, common, 0, ks[:cut])
+            put(vp, common, 0, vs[:cut])
         for own, q in members:
             n = -(-(s + own) // page) - s // page
             pages = common + list(perm[at:at + n])
             at += n
             lists.append(pages)
-            k, v = torch.cat([ks, rows(r, (own, Hkv, D))]), torch.cat([vs, rows(r, (own, Hkv, D))])
-            for pool, x in zip(host, (k, v)):
-                pos = np.arange(s + own)
-                pool.permute(0, 2, 1, 3)[torch.from_numpy(np.array(pages, dtype=np.int64)[pos // page]),
-                                         torch.from_numpy(pos % page)] = x
-            K.append(k)
-            V.append(v)
+            k, v = gpu_rows(own), gpu_rows(own)
+            put(kp, pages, cut, torch.cat([ks[cut:], k]))
+            put(vp, pages, cut, torch.cat([vs[cut:], v]))
+            K.append((ks, k))
+            V.append((vs, v))
             q_len.append(q)
             kv_len.append(s + own)
         gp.append(len(lists))
-    for pool, h in zip((kp, vp), host):
-        keep = torch.isnan(h)
-        pool[layer] = torch.where(keep.cuda(), pool[layer], h.cuda().view(torch.int16))
     indptr = np.concatenate([[0], np.cumsum([len(x) for x in lists])]).astype(np.int32)
     indices = np.concatenate([np.array(x, np.int32) for x in lists])
     q = rows(r, (sum(q_len), Hq, D))
@@ -461,7 +476,7 @@ def check_attention(w, o, lse, scale):
         if n == 0:
             continue
         q = w["q"][t0:t0 + n].cuda().double().view(n, Hkv, G, D).permute(1, 0, 2, 3).reshape(Hkv, n * G, D)
-        k, v = (x[b].cuda().double().permute(1, 0, 2).contiguous() for x in (w["K"], w["V"]))
+        k, v = (torch.cat([y.cuda() for y in x[b]]).double().permute(1, 0, 2).contiguous() for x in (w["K"], w["V"]))
         kt = k.transpose(1, 2).contiguous()
         s = torch.matmul(q, kt) * scale
         hide = torch.arange(kv, device="cuda")[None, :] > (kv - n + torch.arange(n, device="cuda").repeat_interleave(G))[:, None]
@@ -497,7 +512,7 @@ def run_shared(ctx, w, with_lse=True, scale=D ** -0.5, stream=None):
 
 
 SHARED = [
-    # heads, page, groups of (shared, [(own tokens, of them new), ...])
+    # heads, page, groups of (shared, [(own tokens, of them new), ...]); an anchor group comes with each
     ((32, 8), 16, [(200, [(1, 1), (20, 1), (64, 1), (7, 1)])]),
     ((8, 2), 16, [(64, [(1, 1), (1, 1)])]),
     ((8, 2), 16, [(63, [(1, 1), (3, 1)]), (65, [(1, 1), (2, 1), (90, 1)]), (0, [(5, 1), (6, 2)])]),
@@ -511,6 +526,7 @@ SHARED = [
     ((4, 1), 16, [(256, [(200, 150), (300, 200)])]),           # long segments: member by member
     ((4, 1), 16, [(3000, [(1, 1)] * 3), (100, [(2000, 1), (1, 1), (700, 3)]), (0, [(1, 1)])]),
     ((8, 2), 32, [(5000, [(129, 2)] * 17)]),
+    ((16, 2), 32, [(2000, [(30, 1)]), (1500, [(900, 1)] * 2), (0, [(4000, 1)]), (70, [(5000, 300)])]),
 ]
 
 
@@ -518,7 +534,8 @@ SHARED = [
 def test_shared_prefix_attention(i):
     heads, page, groups = SHARED[i]
     r = np.random.default_rng(100 + i)
-    w = branch_batch(r, heads, page, groups, layers=1 + i % 2, layer=i % 2)
+    at = i % (len(groups) + 1)
+    w = branch_batch(r, heads, page, groups[:at] + [anchor(heads)] + groups[at:], layers=1 + i % 2, layer=i % 2)
     ctx = sa.Context(0)
     o, lse = run_shared(ctx, w)
     check_attention(w, o, lse, D ** -0.5)
@@ -527,12 +544,23 @@ def test_shared_prefix_attention(i):
     assert torch.equal(o, o2)
 
 
+@pytest.mark.parametrize("i", range(len(SHARED)))
+def test_shared_prefix_attention_of_small_batches(i):
+    """The same groups by themselves: most are passed on to the segment attention."""
+    heads, page, groups = SHARED[i]
+    w = branch_batch(np.random.default_rng(200 + i), heads, page, groups)
+    ctx = sa.Context(0)
+    sa.sa_set_exact_scale(ctx, False)                        # the call's own scale is exact all the same
+    for _ in range(2):
+        o, lse = run_shared(ctx, w)
+        check_attention(w, o, lse, D ** -0.5)
+
+
 def test_shared_prefix_attention_with_large_scores():
     r = np.random.default_rng(7)
-    w = branch_batch(r, (32, 8), 16, [(900, [(50, 1)] * 12), (300, [(10, 1)] * 5)])
-    kf = w["kp"].view(torch.bfloat16)
-    kf *= 8                                                  # exact: a power of two (and NaN stays NaN)
-    w["K"] = [k * 8 for k in w["K"]]
+    w = branch_batch(r, (32, 8), 16, [(900, [(50, 1)] * 12), anchor((32, 8)), (300, [(10, 1)] * 5)])
+    w["kp"].view(torch.bfloat16).mul_(8)                     # exact: a power of two (and NaN stays NaN)
+    w["K"] = [(a * 8, b * 8) for a, b in w["K"]]
     ctx = sa.Context(0)
     o, lse = run_shared(ctx, w, scale=1.0)
     check_attention(w, o, lse, 1.0)
@@ -540,7 +568,7 @@ def test_shared_prefix_attention_with_large_scores():
 
 def test_shared_prefix_attention_agrees_with_the_segment_attention():
     r = np.random.default_rng(8)
-    w = branch_batch(r, (32, 8), 16, [(2000, [(30, 1)] * 10), (100, [(30, 4)] * 3)])
+    w = branch_batch(r, (32, 8), 16, [(6000, [(30, 1)] * 20), (100, [(30, 4)] * 3)])
     ctx = sa.Context(0)
     o, lse = run_shared(ctx, w)
     o2, lse2 = torch.empty_like(o), torch.empty_like(lse)
@@ -553,8 +581,9 @@ def test_shared_prefix_attention_agrees_with_the_segment_attention():
 def test_shared_prefix_attention_plans_follow_the_lengths():
     ctx = sa.Context(0)
     side = torch.cuda.Stream()
-    for i, n in enumerate([1, 5, 12, 5]):
-        w = branch_batch(np.random.default_rng(40 + i), (8, 2), 16, [(400 + 64 * i, [(9, 1)] * n)])
+    for i, n in enumerate([1, 5, 12, 5, 1, 12]):             # shared, but the fifth
+        groups = [(400 + 64 * i, [(9, 1)] * n)] + ([anchor((8, 2))] if i != 4 else [])
+        w = branch_batch(np.random.default_rng(40 + i), (8, 2), 16, groups)
         torch.cuda.synchronize()
         o, lse = run_shared(ctx, w, stream=side if i == 2 else None)
         torch.cuda.synchronize()
@@ -562,7 +591,7 @@ def test_shared_prefix_attention_plans_follow_the_lengths():
 
 
 def test_shared_prefix_attention_reports_bad_pages():
-    w = branch_batch(np.random.default_rng(12), (8, 2), 16, [(256, [(9, 1)] * 6)])
+    w = branch_batch(np.random.default_rng(12), (8, 2), 16, [(256, [(9, 1)] * 6), anchor((8, 2))])
     ctx = sa.Context(0)
     w["indices"][3] = w["L"].num_slots                       # a shared page of the first member
     with pytest.raises(sa.SaError, match="SA_ERR_RANGE"):
@@ -640,7 +669,7 @@ def test_pools_beyond_4_gib_of_a_layer():
     """Slots whose rows lie past 2^32 bytes of their pool: every call reaches them."""
     r = np.random.default_rng(31)
     heads, page, far = (32, 8), 16, 139000
-    w = branch_batch(r, heads, page, [(1500, [(90, 1)] * 20)])
+    w = branch_batch(r, heads, page, [(1500, [(90, 1)] * 20), anchor(heads)])
     small, big = w["L"], lay(heads, page, far + w["L"].num_slots)
     pools = []
     for name in ("kp", "vp"):
@@ -678,73 +707,65 @@ def test_pools_beyond_4_gib_of_a_layer():
 # ------------------------------------------------------------------------- together
 
 def test_branches_from_fork_to_compaction():
-    """A context is forked, its branches grow by rotated rows and attend; two end, the pool is compacted, and the
-    others go on: every step's attention against float64 over rows kept on the host."""
+    """A context is forked, its branches grow by rotated rows and attend (the prefix computed once); all but two end,
+    the pool is compacted, and the two go on: every step's attention against float64 over the rows in the cache."""
     r = np.random.default_rng(21)
-    heads, page, layers, n0 = (8, 2), 16, 2, 203
+    heads, page, layers, n0, n = (8, 2), 16, 2, 14003, 24
     Hq, Hkv = heads
-    L = lay(heads, page, 64, layers)
-    inv = 10000.0 ** (-np.arange(64) / 64)
-    rope = sa.Rope(inv, rows(r, (D,), 1.0).cuda(), rows(r, (D,), 1.0).cuda(), 1e-6)
+    first = -(-n0 // page)
+    L = lay(heads, page, first + 5 * n, layers)
+    rope = sa.Rope(10000.0 ** (-np.arange(64) / 64), rows(r, (D,), 1.0).cuda(), rows(r, (D,), 1.0).cuda(), 1e-6)
     ctx = sa.Context(0)
     kp, vp = pool_bits(r, L, FILL), pool_bits(r, L, FILL)
-    ref = torch.zeros(64, dtype=torch.int32, device="cuda")
-    fresh = r.permutation(64).astype(np.int32)
-    sip, six = dev([0, 13]), dev(fresh[:13])
+    ref = torch.zeros(L.num_slots, dtype=torch.int32, device="cuda")
+    fresh = r.permutation(L.num_slots).astype(np.int32)
+    sip, six = dev([0, first]), dev(fresh[:first])
     sa.sa_kv_retain(ctx, L, sip, six, ref)
-    pools = (kp.view(torch.bfloat16), vp.view(torch.bfloat16))
 
     def append(start, new, ip, ix):
         q, k, v = (rows(r, (sum(new), h, D)).cuda() for h in (Hq, Hkv, Hkv))
+        out = torch.empty_like(q)
         for layer in range(layers):
-            out = torch.empty_like(q)
             sa.sa_kv_append_rope(ctx, L, layer, rope, q, k, v, out, kp, vp, start, new, ip, ix)
         return out
 
-    def cached(ip, ix, lens, layer):
-        ipn, ixn = ip.cpu().numpy(), ix.cpu().numpy()
-        res = []
-        for pool in pools:
-            res.append([pool[layer][torch.from_numpy(ixn[ipn[b]:ipn[b + 1]].astype(np.int64)).cuda()]
-                        .permute(0, 2, 1, 3).reshape(-1, Hkv, D)[:n].cpu() for b, n in enumerate(lens)])
-        return res
+    def cached(ip, ix, lens, layer=1):
+        ipn = ip.tolist()
+        return [[(pool.view(torch.bfloat16)[layer][ix[ipn[b]:ipn[b + 1]].long()].permute(0, 2, 1, 3)
+                  .reshape(-1, Hkv, D)[:m].clone(),) for b, m in enumerate(lens)] for pool in (kp, vp)]
+
+    def attend(new, lens, ip, ix, q):
+        K, V = cached(ip, ix, lens)
+        w = dict(L=L, kp=kp, vp=vp, indptr=ip, indices=ix, q=q.cpu(), K=K, V=V, q_len=new, kv_len=lens,
+                 groups=[0, len(new)], shared=[n0], heads=heads, layer=1)
+        check_attention(w, *run_shared(ctx, w), D ** -0.5)
+        return K, V
 
     append([0], [n0], sip, six)
-    base = cached(sip, six, [n0], 1)
-    dip, dix = torch.zeros(5, dtype=torch.int32, device="cuda"), torch.zeros(4 * 16, dtype=torch.int32, device="cuda")
-    used = sa.sa_kv_fork(ctx, L, kp, vp, [n0], [0] * 4, [40] * 4, sip, six, dev(fresh[13:]), dip, dix, ref=ref)
-    assert used == 4 * 4
-    lens = [n0] * 4
-    for new in ([5, 1, 9, 2], [1, 1, 1, 1], [20, 3, 1, 0]):
+    base = cached(sip, six, [n0])
+    dip = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+    dix = torch.zeros(n * (first + 4), dtype=torch.int32, device="cuda")
+    used = sa.sa_kv_fork(ctx, L, kp, vp, [n0], [0] * n, [40] * n, sip, six, dev(fresh[first:]), dip, dix, ref=ref)
+    assert used == n * (-(-(n0 + 40) // page) - n0 // page)
+    lens = [n0] * n
+    for new in ([5, 1, 9, 2] * 6, [1] * n, [20, 3, 1, 0] * 6):
         q = append(lens, new, dip, dix)
-        lens = [a + n for a, n in zip(lens, new)]
-        K, V = cached(dip, dix, lens, 1)
-        for b in range(4):
-            assert torch.equal(K[b][:n0], base[0][0]) and torch.equal(V[b][:n0], base[1][0])
-        w = dict(L=L, kp=kp, vp=vp, indptr=dip, indices=dix, q=q.cpu(), K=K, V=V, q_len=new, kv_len=lens,
-                 groups=[0, 4], shared=[n0], heads=heads, layer=1)
-        o, lse = run_shared(ctx, w)
-        check_attention(w, o, lse, D ** -0.5)
-    # branches 2 and 3 and the parent's own table end; branches 0 and 1 move together
-    K, V = cached(dip, dix, lens, 1)
-    free, nfree = torch.zeros(64, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
-    two = dip[2:].contiguous()
-    sa.sa_kv_release(ctx, L, two, dix, ref)
+        lens = [a + m for a, m in zip(lens, new)]
+        K, V = attend(new, lens, dip, dix, q)
+        for b in range(n):
+            assert torch.equal(K[b][0][:n0], base[0][0][0]) and torch.equal(V[b][0][:n0], base[1][0][0])
+    # all branches but 0 and 1 and the context's own table end; the two that go on move together
+    free, nfree = torch.zeros_like(ref), torch.zeros(1, dtype=torch.int32, device="cuda")
+    sa.sa_kv_release(ctx, L, dip[2:].contiguous(), dix, ref)
     sa.sa_kv_release(ctx, L, sip, six, ref, free, nfree)
     live = sorted(set(dix[:int(dip[2])].tolist()))
-    assert free[:int(nfree)].tolist() == [s for s in range(64) if s not in live]
-    kept = dix[:int(dip[2])].contiguous()
+    assert free[:int(nfree)].tolist() == sorted(set(range(L.num_slots)) - set(live))
+    kept, ip2 = dix[:int(dip[2])].contiguous(), dip[:3].contiguous()
     smap, mv = torch.zeros_like(ref), torch.zeros(2, dtype=torch.int32, device="cuda")
     sa.sa_kv_compact(ctx, L, kp, vp, len(live), ref, ref, kept, kept, smap, mv)
     sa.sa_sync_check(ctx)
     assert mv[1] == 0 and sorted(set(kept.tolist())) == list(range(len(live)))
-    ip2 = dip[:3].contiguous()
-    K2, V2 = cached(ip2, kept, lens[:2], 1)
-    assert all(torch.equal(a, b) for a, b in zip(K[:2] + V[:2], K2 + V2))
+    K2, V2 = cached(ip2, kept, lens[:2])
+    assert all(torch.equal(a[0], b[0]) for a, b in zip(K[:2] + V[:2], K2 + V2))
     q = append(lens[:2], [1, 2], ip2, kept)
-    lens = [lens[0] + 1, lens[1] + 2]
-    K, V = cached(ip2, kept, lens, 1)
-    w = dict(L=L, kp=kp, vp=vp, indptr=ip2, indices=kept, q=q.cpu(), K=K, V=V, q_len=[1, 2], kv_len=lens,
-             groups=[0, 2], shared=[n0], heads=heads, layer=1)
-    o, lse = run_shared(ctx, w)
-    check_attention(w, o, lse, D ** -0.5)
+    attend([1, 2], [lens[0] + 1, lens[1] + 2], ip2, kept, q)
