@@ -6,12 +6,17 @@ Tolerances.  A bf16 rounding is off by at most 2^-8 of the value.
   and 128 dims add n 2^-23 A, and a score's error e moves its weight by 2 e at most: e = 128 2^-24 max_k sum|q k| scale.
 * Rotation: one rounding of each output, 2^-8; fp32 norm and rotation are below 2^-16 of the pair's size.
 """
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
 
 import paper_2607_00151_amd as sa
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 pytestmark = pytest.mark.gpu
 D = 128
 FILL = 0x7FC1          # a bf16 NaN pattern: any stray read or write shows up
@@ -640,7 +645,7 @@ def test_counts_refuse_to_allocate_in_a_capture():
 def test_binding_refuses_other_types_and_layouts():
     L = lay((4, 2), 16, 8)
     ctx = sa.Context(0)
-    q, k = torch.zeros((2, 4, D), dtype=torch.bfloat16, device="cuda"), torch.zeros((2, 2, D), dtype=torch.bfloat16, device="cuda")
+    q, k = (torch.zeros((2, h, D), dtype=torch.bfloat16, device="cuda") for h in (4, 2))
     pool = torch.zeros((1, 8, 2, 16, D), dtype=torch.bfloat16, device="cuda")
     ip, ix = dev([0, 1]), dev([3])
 
@@ -702,6 +707,86 @@ def test_pools_beyond_4_gib_of_a_layer():
     sa.sa_sync_check(ctx)
     assert mv.tolist() == [101, 0] and int(kept.max()) <= 100
     assert torch.equal(pools[1][0, kept.long()], before)
+
+
+DEBUG = r"""
+import sys
+sys.path.insert(0, {root!r}); sys.path.insert(0, {tests!r})
+import numpy as np, torch
+import paper_2607_00151_amd as sa
+from test_gpu_branches import D, bits, dev, lay, pool_bits, rows
+r = np.random.default_rng(1)
+L, ctx = lay((4, 2), 16, 16), sa.Context(0)
+kp, vp = pool_bits(r, L), pool_bits(r, L)
+before = bits(kp).copy(), bits(vp).copy()
+dip, dix = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros(8, dtype=torch.int32, device="cuda")
+
+def name(f):
+    try:
+        f()
+    except sa.SaError as e:
+        torch.cuda.synchronize()
+        assert np.array_equal(bits(kp), before[0]) and np.array_equal(bits(vp), before[1])
+        return e.name
+    sa.sa_sync_check(ctx)
+
+def fork(table=(3, 4), fresh=(7, 8, 9)):
+    sa.sa_kv_fork(ctx, L, kp, vp, [20], [0, 0], [4, 16], dev([0, len(table)]), dev(table), dev(fresh), dip, dix)
+
+def rope(table):
+    T = 2
+    q, k = rows(r, (T, 4, D)).cuda(), rows(r, (T, 2, D)).cuda()
+    sa.sa_kv_append_rope(ctx, L, 0, sa.Rope(), q, k, k, q, kp, vp, [5, 5], [1, 1], dev([0, 1, 2]), dev(table))
+
+assert name(lambda: fork(fresh=(7, 8, 7))) == "SA_ERR_OVERLAP"
+assert name(lambda: fork(fresh=(7, 4, 9))) == "SA_ERR_OVERLAP"
+assert name(lambda: fork(fresh=(7, 16, 9))) == "SA_ERR_RANGE"
+assert name(lambda: fork(table=(3, 16))) == "SA_ERR_RANGE"
+assert name(lambda: fork(table=(3,))) == "SA_ERR_RANGE"
+assert name(lambda: rope((6, 6))) == "SA_ERR_OVERLAP"
+assert name(lambda: rope((6, -1))) == "SA_ERR_RANGE"
+assert name(fork) is None and dix[:5].tolist() == [3, 7, 3, 8, 9]
+assert name(lambda: rope((6, 11))) is None
+print("debug branch checks ok", flush=True)
+"""
+
+
+@pytest.mark.timeout(300)
+def test_debug_checks():
+    code = DEBUG.format(root=ROOT, tests=os.path.join(ROOT, "tests"))
+    r = subprocess.run([sys.executable, "-u", "-c", code], env=dict(os.environ, SA_DEBUG="1"), capture_output=True,
+                       text=True, timeout=240)
+    print(r.stdout[-2000:], r.stderr[-3000:])
+    assert r.returncode == 0 and "debug branch checks ok" in r.stdout
+
+
+def test_reserved_contexts_give_the_same_bits():
+    w = branch_batch(np.random.default_rng(51), (8, 2), 16, [(700, [(9, 1)] * 6), anchor((8, 2))])
+    o, lse = run_shared(sa.Context(0), w)
+    ctx = sa.Context(0)
+    sa.sa_reserve(ctx, 1 << 20, 64 << 20)
+    for _ in range(2):
+        o2, lse2 = run_shared(ctx, w)
+        assert torch.equal(o, o2) and torch.equal(lse, lse2)
+        sa.sa_reserve(ctx, 4 << 20, 128 << 20)              # the plan on the device goes: made again
+
+
+def test_timing_events_bind_to_the_branch_kernels():
+    w = branch_batch(np.random.default_rng(52), (8, 2), 16, [anchor((8, 2))])
+    ctx = sa.Context(0)
+    run_shared(ctx, w)
+    ev = [torch.cuda.Event(enable_timing=True) for _ in range(4)]
+    for e in ev:
+        e.record()
+    sa.sa_set_kernel_events(ctx, sa.TIMED_ATTN, ev[0].cuda_event, ev[1].cuda_event)
+    sa.sa_set_kernel_events(ctx, sa.TIMED_PAGES, ev[2].cuda_event, ev[3].cuda_event)
+    run_shared(ctx, w)
+    ref = torch.zeros(w["L"].num_slots, dtype=torch.int32, device="cuda")
+    sa.sa_kv_retain(ctx, w["L"], w["indptr"], w["indices"], ref)
+    sa.sa_set_kernel_events(ctx, sa.TIMED_ATTN)
+    sa.sa_set_kernel_events(ctx, sa.TIMED_PAGES)
+    torch.cuda.synchronize()
+    assert 0 < ev[0].elapsed_time(ev[1]) < 10 and 0 < ev[2].elapsed_time(ev[3]) < 10
 
 
 # ------------------------------------------------------------------------- together
