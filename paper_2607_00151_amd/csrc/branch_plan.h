@@ -316,7 +316,8 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
   for (Tile& t : tiles) {
     t.parts = (int32_t)shared_parts(t.tiles(), chunk);
     if (t.prefix) prefix_blocks += (int64_t)t.parts * Hkv;
-    else fill += (t.tiles() * 120 + 300 * t.parts) * Hkv;
+    else if ((int64_t)t.q_len * G <= kDecodeRows) fill += (t.tiles() * 220 + 100 * t.parts) * Hkv;
+    else fill += (t.tiles() * 200 + 400 * t.parts) * Hkv;
   }
   auto place = [&](Tile& t) {
     t.place = rows_used;
@@ -336,8 +337,10 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
   // CU starts with one part, the members' own blocks fill its other slot, and the
   // CU's second part follows them.  The parts of the first kind are then longer
   // than those of the second by the tiles they are ahead, so that both end
-  // together.  64 branches of 64K, 64/8 heads, us of the first launch: all parts
-  // alike in order of length 158, this 150 (the call 178 and 167).
+  // together.  (Beside a prefix part a block of few rows takes 2.2 us a tile,
+  // another own block 2.)  64 branches of 64K, 64/8 heads, the call in us: all
+  // blocks by length 178, in this order with equal parts 181, this 163; 16 segments
+  // of 16 to 64 tokens on 16K 184, 193, 183.
   const bool fit = best.compute && prefix_blocks > num_cu && prefix_blocks <= 2 * num_cu && fill > 0;
   const double ahead = fit ? fill / 127.0 / num_cu : 0.0;
   auto part_begin = [&](const Tile& t, int k) {                 // in tiles from t.k0

@@ -53,7 +53,7 @@ struct RopeArgs {
   int32_t rot;
   int32_t rounds;            // rounds of kRopeRows head rows per wave
   float eps, offset;
-  uint64_t freq[64];         // turns per position, as a fraction of 2^64
+  const uint64_t* freq;      // [rot / 2] turns per position, as fractions of 2^64
 };
 
 constexpr int kRopeRows = 16;        // head rows of a round: 4 loads of 16 bytes per lane

@@ -186,12 +186,9 @@ struct sa_ctx {
     int64_t total_q = 0;
   } attn_rec, na_rec;
   struct RopeRec {
-    size_t o_tok = 0, o_start = 0, o_pos = 0;
+    size_t o_tok = 0, o_start = 0, o_pos = 0, o_freq = 0;
     int64_t total = 0;
   } rope_rec;
-  // inv_freq values and what they are in turns: 64 long double divisions took 2 us of every call
-  double rope_freq[sa::kHD / 2] = {};
-  uint64_t rope_turns[sa::kHD / 2] = {};
   struct ForkRec {
     size_t o_ch = 0, o_ip = 0, o_cp = 0;
     int64_t n_dst = 0, fresh_used = 0, n_copies = 0;
@@ -1332,6 +1329,9 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
     dp.key.add(h_start, (size_t)batch);
     dp.key.add(h_new_len, (size_t)batch);
     dp.key.add(h_rot, (size_t)batch);
+    int32_t words[sa::kHD];
+    if (n_freq > 0) memcpy(words, rope->h_inv_freq, n_freq * sizeof(double));
+    dp.key.add(words, 2 * (size_t)n_freq);
     same = dp.reusable(dp.key.end(), (hipStream_t)stream) && !debug_checks();
     if (!same) dp.key_valid = false;
     rec = ctx->rope_rec;
@@ -1377,6 +1377,13 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
     rec.o_tok = img.add(tok_begin.data(), tok_begin.size());
     rec.o_start = img.add(h_start, (size_t)batch);
     rec.o_pos = img.add(h_rot, (size_t)batch);
+    uint64_t turns[sa::kHD / 2];                   // per position, modulo 1, in units of 2^-64
+    for (int j = 0; j < n_freq; ++j) {
+      const long double x = (long double)rope->h_inv_freq[j] / 6.283185307179586476925286766559L;
+      const long double frac = std::ldexp(x - std::floor(x), 64) + 0.5L;
+      turns[j] = frac >= 18446744073709551616.0L ? 0 : (uint64_t)frac;
+    }
+    rec.o_freq = img.add(turns, (size_t)n_freq);
     s = upload_plan(ctx, kPlanRope, img, (hipStream_t)stream, &dev);
     if (s != SA_OK) return s;
     ctx->rope_rec = rec;
@@ -1398,6 +1405,7 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   a.tok_begin = (const int32_t*)(dev + rec.o_tok);
   a.start = (const int32_t*)(dev + rec.o_start);
   a.pos = (const int32_t*)(dev + rec.o_pos);
+  a.freq = (const uint64_t*)(dev + rec.o_freq);
   a.indptr = pages.indptr;
   a.indices = pages.indices;
   a.err = ctx->d_err;
@@ -1410,16 +1418,6 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   a.rot = rope->rot_dim;
   a.eps = rope->eps;
   a.offset = rope->weight_offset;
-  if (n_freq > 0 && memcmp(ctx->rope_freq, rope->h_inv_freq, n_freq * sizeof(double)) != 0) {
-    for (int j = 0; j < n_freq; ++j) {
-      // turns per position modulo 1, in units of 2^-64
-      const long double turns = (long double)rope->h_inv_freq[j] / 6.283185307179586476925286766559L;
-      const long double frac = std::ldexp(turns - std::floor(turns), 64) + 0.5L;
-      ctx->rope_turns[j] = frac >= 18446744073709551616.0L ? 0 : (uint64_t)frac;
-    }
-    memcpy(ctx->rope_freq, rope->h_inv_freq, n_freq * sizeof(double));
-  }
-  memcpy(a.freq, ctx->rope_turns, n_freq * sizeof(uint64_t));
   const int n_rows = Hq + 2 * Hkv;
   a.rounds = (n_rows + sa::kRopeRows - 1) / sa::kRopeRows;
   a.rounds = std::max(1, std::min<int>(a.rounds, (int)(rec.total * a.rounds / (16 * (int64_t)ctx->num_cu))));
