@@ -28,6 +28,7 @@
 #include <stdint.h>
 
 #include "common.h"
+#include "kv_kernels.h"
 #include "plan.h"
 
 namespace sa {
@@ -98,7 +99,14 @@ __device__ __forceinline__ void unpack8(u32x4 w, float (&x)[8]) {
 // on (d, d + 64: a DPP rotation), or in any lane of the row (a permute).
 enum RopePair { kPairInLane, kPairFull, kPairAny };
 
-template <RopePair kPair>
+// kStream: rows read and written past the caches' use of them (non-temporal), for
+// calls that move more than the Infinity Cache holds.  With and without, us:
+// 40.7K tokens of 48 head rows (1.0 GB) 174, 190; 16384 (0.4 GB) 72, 79; below it
+// the rows a call leaves in the cache are worth more -- 8192 tokens (0.2 GB) 37,
+// 33.5; 4096 with the segment's attention behind them 197.5, 193.8.
+constexpr int64_t kRopeStreamBytes = int64_t(256) << 20;
+
+template <RopePair kPair, bool kStream>
 __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
   const int lane = threadIdx.x & 63;
   const int c = lane & 15, sub = lane >> 4;                 // 16-byte chunk of the row, row within a load
@@ -118,8 +126,14 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int row = row0 + 4 * i + sub;
-      if (row < row_end) x[i] = ld_u32x4((row < a.Hq ? qt : row < n_qk ? kt : vt) + row * kHD);
+      if (row >= row_end) continue;
+      const uint16_t* const p = (row < a.Hq ? qt : row < n_qk ? kt : vt) + row * kHD;
+      x[i] = kStream ? ld_stream(p) : ld_u32x4(p);
     }
+  };
+  auto store = [&](uint16_t* p, u32x4 v) __attribute__((always_inline)) {
+    if constexpr (kStream) st_stream(p, v);
+    else st_u32x4(p, v);
   };
   u32x4 x[4];
   load(row_begin, x);
@@ -234,15 +248,15 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
       const int first = row0 + 4 * i, row = first + sub;    // first: the same for the whole wave
       if (first < a.Hq) {
         const u32x4 out = turn(x[i], cq);
-        if (row < a.Hq) st_u32x4(q_out + row * kHD, out);
+        if (row < a.Hq) store(q_out + row * kHD, out);
       }
       if (first + 3 >= a.Hq && first < n_qk) {
         const u32x4 out = turn(x[i], ck);
         if (row >= a.Hq && row < n_qk && slot >= 0)
-          st_u32x4(a.k_pool + page_at + (int64_t)(row - a.Hq) * a.P * kHD, out);
+          store(a.k_pool + page_at + (int64_t)(row - a.Hq) * a.P * kHD, out);
       }
       if (first + 3 >= n_qk && row >= n_qk && row < row_end && slot >= 0)
-        st_u32x4(a.v_pool + page_at + (int64_t)(row - n_qk) * a.P * kHD, x[i]);
+        store(a.v_pool + page_at + (int64_t)(row - n_qk) * a.P * kHD, x[i]);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = next[i];

@@ -1424,14 +1424,15 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   const int rows_wave = a.rounds * sa::kRopeRows;
   const int64_t blocks = (rec.total * ((n_rows + rows_wave - 1) / rows_wave) + 3) / 4;
   if (blocks > INT32_MAX) return fail(SA_ERR_SHAPE, "too many new tokens for these heads");
-  const hipEvent_t* const ev = ctx->kernel_ev[SA_TIMED_PAGES];
-  const dim3 grid((unsigned)blocks), threads(256);
-  if (rope->interleaved)
-    launch_timed(sa::rope_append_kernel<sa::kPairInLane>, grid, threads, (hipStream_t)stream, ev, a);
-  else if (rope->rot_dim == sa::kHD)
-    launch_timed(sa::rope_append_kernel<sa::kPairFull>, grid, threads, (hipStream_t)stream, ev, a);
-  else
-    launch_timed(sa::rope_append_kernel<sa::kPairAny>, grid, threads, (hipStream_t)stream, ev, a);
+  const bool streams = rec.total * n_rows * sa::kHD * 4 > sa::kRopeStreamBytes;
+  const sa::RopePair pair = rope->interleaved ? sa::kPairInLane : rope->rot_dim == sa::kHD ? sa::kPairFull : sa::kPairAny;
+  auto kernel = pair == sa::kPairInLane ? (streams ? sa::rope_append_kernel<sa::kPairInLane, true>
+                                                   : sa::rope_append_kernel<sa::kPairInLane, false>)
+              : pair == sa::kPairFull   ? (streams ? sa::rope_append_kernel<sa::kPairFull, true>
+                                                   : sa::rope_append_kernel<sa::kPairFull, false>)
+                                        : (streams ? sa::rope_append_kernel<sa::kPairAny, true>
+                                                   : sa::rope_append_kernel<sa::kPairAny, false>);
+  launch_timed(kernel, dim3((unsigned)blocks), dim3(256), (hipStream_t)stream, ctx->kernel_ev[SA_TIMED_PAGES], a);
   SA_HIP(hipGetLastError());
   return SA_OK;
 }

@@ -163,6 +163,30 @@ def test_append_rope_in_place_and_on_another_stream():
         np.testing.assert_array_equal(a, bits(b))
 
 
+@pytest.mark.parametrize("rot,inter", [(128, False), (64, False), (128, True)])
+def test_append_rope_of_many_tokens(rot, inter):
+    """More bytes than the Infinity Cache: checked against the same rows in pieces, and some rows in float64."""
+    heads, page, T = (32, 8), 16, 14001
+    L = lay(heads, page, -(-T // page) + 1)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    both = (torch.randn((T, 48, D), generator=g, device="cuda") * 0.5).to(torch.bfloat16)
+    q, k, v = both.split([32, 8, 8], dim=1)
+    ip, ix = dev([0, L.num_slots]), dev(np.random.default_rng(3).permutation(L.num_slots))
+    inv = 10000.0 ** (-2.0 * np.arange(rot // 2) / rot)
+    w = (1 + 0.1 * torch.randn(D, generator=g, device="cuda")).to(torch.bfloat16)
+    rope, ctx = sa.Rope(inv, w, w, 1e-6, inter), sa.Context(0)
+    pools = [pool_bits(None, L, FILL) for _ in range(4)]
+    q_out, q2 = (torch.empty((T, 32, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    sa.sa_kv_append_rope(ctx, L, 0, rope, q, k, v, q_out, pools[0], pools[1], [0], [T], ip, ix)
+    for a in range(0, T, 3500):
+        n = min(3500, T - a)
+        sa.sa_kv_append_rope(ctx, L, 0, rope, q[a:], k[a:], v[a:], q2[a:], pools[2], pools[3], [a], [n], ip, ix)
+    sa.sa_sync_check(ctx)
+    assert torch.equal(q_out, q2) and torch.equal(pools[0], pools[2]) and torch.equal(pools[1], pools[3])
+    pick = [0, 1, 6999, T - 1]
+    close_bf16(q_out[pick], *rope_reference(q[pick].cpu(), w.cpu(), pick, inv, 1e-6, inter, 0.0))
+
+
 def test_append_rope_reports_bad_pages_and_writes_the_rest():
     r = np.random.default_rng(6)
     L = lay((4, 2), 16, 8)
