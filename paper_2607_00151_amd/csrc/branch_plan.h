@@ -167,29 +167,31 @@ inline int64_t shared_parts(int64_t tiles, int64_t chunk) {
 }
 
 // Time of the two launches at a chunk size, in units of 10 ns.  Measured
-// (MI355X): a prefill tile 127 alone on its CU and 180 where two blocks share
-// one, a decode tile 80, 300 for a block's start and end; the keys stream at 54.6
-// per tile and 100 blocks (6 TB/s), with a quarter of the shorter of work and
-// stream not overlapping; the merge 700, and 1032 bytes written and read per row
-// and part at 9 TB/s.  Model and measurement, us: 32 branches of 16K, 34 and 31;
-// 64 of 64K, 64/8 heads, 162 and 167; 4 of 4K 14 and 15; 16 of 16K with 16 to 64
-// query tokens each 181 and 184.
+// (MI355X): a prefill tile 120 and a block's start and end 400 where at most one
+// long prefill block has each CU, 185 and 900 where two share one; a decode tile 80 and
+// its block 300; the keys stream at 54.6 per tile and 100 blocks (6 TB/s), with a
+// quarter of the shorter of work and stream not overlapping; the merge 700, and
+// 1032 bytes written and read per row and part at 9 TB/s.
 inline SharedCost shared_chunk_cost(const std::vector<SharedShape>& shapes, int Hkv, int num_cu, int64_t chunk) {
   struct Run {
     int64_t time, blocks;
   };
   std::vector<Run> runs;
-  int64_t n = 0, streamed = 0, part_rows = 0;
+  int64_t n = 0, n_long = 0, longest = 0, streamed = 0, part_rows = 0;
+  auto length = [&](const SharedShape& s) { return (s.tiles + shared_parts(s.tiles, chunk) - 1) / shared_parts(s.tiles, chunk); };
+  for (const SharedShape& s : shapes)
+    if (!s.decode) longest = std::max(longest, length(s));
   for (const SharedShape& s : shapes) {
     const int64_t k = shared_parts(s.tiles, chunk);
     n += k * Hkv * s.count;
+    if (!s.decode && 2 * length(s) > longest) n_long += k * Hkv * s.count;
     part_rows += k * Hkv * s.rows;
     if (s.streams) streamed += s.tiles * Hkv * s.count;
   }
+  const bool pairs = n_long > num_cu;
   for (const SharedShape& s : shapes) {
-    const int64_t k = shared_parts(s.tiles, chunk);
-    const int64_t t = s.decode ? 80 : n > num_cu ? 180 : 127;
-    runs.push_back({(s.tiles + k - 1) / k * t + 300, k * Hkv * s.count});
+    const int64_t k = shared_parts(s.tiles, chunk), t = length(s);
+    runs.push_back({s.decode ? t * 80 + 300 : pairs ? t * 185 + 900 : t * 120 + 400, k * Hkv * s.count});
   }
   std::sort(runs.begin(), runs.end(), [](const Run& x, const Run& y) { return x.time > y.time; });
   // the busiest of the slots: the mean, and of any k slots + 1 longest blocks some slot has k + 1
@@ -206,20 +208,35 @@ inline SharedCost shared_chunk_cost(const std::vector<SharedShape>& shapes, int 
 }
 
 // The same work by sa_segment_prefill_attn, every member over all of its keys:
-// members' repeated reads of the shared keys come out of the caches, 14 TB/s over
-// all (measured over 2 to 64 members), 700 for the launch.  Of 25 batches of 1 to
-// 12 groups measured both ways the model passes on those that end sooner so (12.7
-// against 16.6 us: 2 + 9 members on 5.4K, 8/2 heads) and shares the others (31
-// against 154: 32 on 16K).
+// the larger of its throughput (members' repeated reads of the shared keys come
+// out of the caches, 14 TB/s over all; row tiles at two blocks per CU) and of the
+// slowest item's way through its parts and their merge, whose costs are those that
+// plan_attn_items splits by; 700 for the launch, 1400 for the partials of 512
+// prefill parts.
 inline int64_t segment_cost(const std::vector<SeqDesc>& seqs, int G, int Hkv, int num_cu) {
-  int64_t stream = 0, compute = 0;
+  int64_t stream = 0, compute = 0, items = 0;
   for (const SeqDesc& s : seqs) {
     const int64_t rows = (int64_t)s.q_len * G, tiles = (s.kv_len + kKT - 1) / kKT * Hkv;
     if (rows == 0) continue;
+    items += (rows + 127) / 128 * Hkv;
     if (rows <= kDecodeRows) stream += tiles;
     else compute += tiles * ((rows + 127) / 128);
   }
-  return 700 + std::max(stream * 234 / 1000, compute * 210 / (2 * num_cu)) + stream * 80 / (2 * num_cu) / 4;
+  const int64_t slots = 2 * (int64_t)num_cu;
+  const double least = (double)(stream + compute) / slots;    // tiles of a part where the slots are shared evenly
+  double slowest = 0, parts = 0;
+  for (const SeqDesc& s : seqs) {
+    const double rows = (double)s.q_len * G, t = (s.kv_len + kKT - 1) / kKT;
+    if (rows == 0) continue;
+    const bool decode = rows <= kDecodeRows;
+    const double finest = decode ? std::sqrt(rows * t / 64) : std::sqrt(t / 2);
+    const double c = items >= slots ? t : std::min(t, std::max({4.0, finest, least}));
+    const double k = t / c;
+    slowest = std::max(slowest, decode ? 60 * c + (k > 1 ? 1.25 * rows * k : 0) : 93 * c + (k > 1 ? 60 * k : 0));
+    if (!decode && k > 1) parts += k * Hkv * std::ceil(rows / 128);
+  }
+  const int64_t flow = std::max(stream * 234 / 1000, compute * 210 / slots) + stream * 80 / slots / 4;
+  return 700 + std::max(flow, (int64_t)slowest) + (int64_t)(1400 * parts / 512);
 }
 
 // The launch's work items.  A group whose prefix is computed once gives row
