@@ -235,7 +235,7 @@ inline int64_t segment_cost(const std::vector<SeqDesc>& seqs, int G, int Hkv, in
     slowest = std::max(slowest, decode ? 60 * c + (k > 1 ? 1.25 * rows * k : 0) : 93 * c + (k > 1 ? 60 * k : 0));
     if (!decode && k > 1) parts += k * Hkv * std::ceil(rows / 128);
   }
-  const int64_t flow = std::max(stream * 234 / 1000, compute * 210 / slots) + stream * 80 / slots / 4;
+  const int64_t flow = std::max(stream * 234 / 1000, compute * 180 / slots) + stream * 80 / slots / 4;
   return 700 + std::max(flow, (int64_t)slowest) + (int64_t)(1400 * parts / 512);
 }
 
@@ -277,8 +277,11 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
     }
     if (first < 0) continue;
     const int32_t S = h_shared_len[g] / kKT * kKT;
-    // worth it where packing the members' rows leaves clearly fewer row tiles over the prefix
-    const bool shared = S > 0 && rows + S <= INT32_MAX / 2 && 8 * ((rows + kRows - 1) / kRows) <= 7 * apart;
+    // Worth it where packing the members' rows leaves clearly fewer row tiles over
+    // the prefix: every row then goes through partials.  8 segments of 45 to 64 tokens
+    // on 16K, us with the prefix computed once and member by member: 12 row tiles of
+    // 16 112 and 116, 13 of 16 125 and 125, 14 of 16 132 and 125, 16 of 16 145 and 137.
+    const bool shared = S > 0 && rows + S <= INT32_MAX / 2 && 5 * ((rows + kRows - 1) / kRows) <= 4 * apart;
     const int32_t prefix0 = shared ? (int32_t)tiles.size() : -1;
     if (shared) {
       any = true;
