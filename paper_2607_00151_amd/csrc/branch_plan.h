@@ -216,7 +216,7 @@ inline SharedCost shared_chunk_cost(const std::vector<SharedShape>& shapes, int 
 inline int64_t segment_cost(const std::vector<SeqDesc>& seqs, int G, int Hkv, int num_cu) {
   int64_t stream = 0, compute = 0, items = 0;
   for (const SeqDesc& s : seqs) {
-    const int64_t rows = (int64_t)s.q_len * G, tiles = (s.kv_len + kKT - 1) / kKT * Hkv;
+    const int64_t rows = (int64_t)s.q_len * G, tiles = ((int64_t)s.kv_len + kKT - 1) / kKT * Hkv;
     if (rows == 0) continue;
     items += (rows + 127) / 128 * Hkv;
     if (rows <= kDecodeRows) stream += tiles;
@@ -226,7 +226,7 @@ inline int64_t segment_cost(const std::vector<SeqDesc>& seqs, int G, int Hkv, in
   const double least = (double)(stream + compute) / slots;    // tiles of a part where the slots are shared evenly
   double slowest = 0, parts = 0;
   for (const SeqDesc& s : seqs) {
-    const double rows = (double)s.q_len * G, t = (s.kv_len + kKT - 1) / kKT;
+    const double rows = (double)s.q_len * G, t = (double)(((int64_t)s.kv_len + kKT - 1) / kKT);
     if (rows == 0) continue;
     const bool decode = rows <= kDecodeRows;
     const double finest = decode ? std::sqrt(rows * t / 64) : std::sqrt(t / 2);
@@ -257,7 +257,7 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
     bool prefix;
     int32_t parts = 1;
     int64_t place = -1;                                         // row of its first part, KV head 0, among the partials
-    int64_t tiles() const { return (k1 - k0 + kKT - 1) / kKT; }
+    int64_t tiles() const { return ((int64_t)k1 - k0 + kKT - 1) / kKT; }
   };
   std::vector<Tile> tiles;
   struct Member {

@@ -1239,6 +1239,9 @@ sa_status sa_segment_prefill_attn_append(sa_ctx* ctx, const sa_layout* layout, i
 
 namespace {
 
+// Blocks of 256 threads of one launch: its work items are counted in 32 bits.
+constexpr int64_t kMaxBlocks = (int64_t(1) << 24) - 1;
+
 // The calling thread's device, put back when the call returns.
 struct DeviceGuard {
   int before = -1;
@@ -1325,7 +1328,9 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   sa_ctx::RopeRec rec;
   if (ctx) {
     sa_ctx::DevPlan& dp = ctx->plans[kPlanRope];
+    const int32_t head[2] = {batch, n_freq};
     dp.key.begin();
+    dp.key.add(head, 2);
     dp.key.add(h_start, (size_t)batch);
     dp.key.add(h_new_len, (size_t)batch);
     dp.key.add(h_rot, (size_t)batch);
@@ -1371,6 +1376,14 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
                                g_err);
     if (s != SA_OK) return s;
   }
+  // as many rounds per wave as leave each CU 16 waves
+  const int n_rows = Hq + 2 * Hkv;
+  const int all_rounds = (n_rows + sa::kRopeRows - 1) / sa::kRopeRows;
+  const int rounds =
+      (int)std::max<int64_t>(1, std::min<int64_t>(all_rounds, rec.total * all_rounds / (16 * (int64_t)ctx->num_cu)));
+  const int rows_wave = rounds * sa::kRopeRows;
+  const int64_t blocks = (rec.total * ((n_rows + rows_wave - 1) / rows_wave) + 3) / 4;
+  if (blocks > kMaxBlocks) return fail(SA_ERR_SHAPE, "too many new tokens for one launch");
   uint8_t* dev = ctx->plans[kPlanRope].dev;
   if (!same) {
     PlanImage img;
@@ -1418,12 +1431,7 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   a.rot = rope->rot_dim;
   a.eps = rope->eps;
   a.offset = rope->weight_offset;
-  const int n_rows = Hq + 2 * Hkv;
-  a.rounds = (n_rows + sa::kRopeRows - 1) / sa::kRopeRows;
-  a.rounds = std::max(1, std::min<int>(a.rounds, (int)(rec.total * a.rounds / (16 * (int64_t)ctx->num_cu))));
-  const int rows_wave = a.rounds * sa::kRopeRows;
-  const int64_t blocks = (rec.total * ((n_rows + rows_wave - 1) / rows_wave) + 3) / 4;
-  if (blocks > INT32_MAX) return fail(SA_ERR_SHAPE, "too many new tokens for these heads");
+  a.rounds = rounds;
   const bool streams = rec.total * n_rows * sa::kHD * 4 > sa::kRopeStreamBytes;
   const sa::RopePair pair = rope->interleaved ? sa::kPairInLane : rope->rot_dim == sa::kHD ? sa::kPairFull : sa::kPairAny;
   auto kernel = pair == sa::kPairInLane ? (streams ? sa::rope_append_kernel<sa::kPairInLane, true>
@@ -1469,7 +1477,7 @@ sa_status kv_fork(sa_ctx* ctx, const sa_layout* layout, void* k_pool, void* v_po
   }
   const int64_t copy_blocks = rec.n_copies * layout->num_layers * 2;
   const int64_t table_blocks = (std::max<int64_t>(rec.n_dst, num_children + 1) + 255) / 256;
-  if (copy_blocks + table_blocks > INT32_MAX) return fail(SA_ERR_SHAPE, "too many partial pages for these layers");
+  if (copy_blocks + table_blocks > kMaxBlocks) return fail(SA_ERR_SHAPE, "too many partial pages for these layers");
   if (!h_fresh_used || !k_pool || !v_pool || !src.indptr || !d_dst_indptr || (rec.n_dst > 0 && !d_dst_indices) ||
       (rec.n_dst > rec.fresh_used && !src.indices) || (rec.n_copies > 0 && !src.indices) ||
       (rec.fresh_used > 0 && !d_fresh))
@@ -1530,7 +1538,7 @@ sa_status kv_fork(sa_ctx* ctx, const sa_layout* layout, void* k_pool, void* v_po
 }
 
 // Checks that the calls over counts have in common.
-sa_status check_counts(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_pages pages, int64_t max_entries,
+sa_status check_counts(const sa_layout* layout, int32_t batch, sa_pages pages, int64_t max_entries,
                        const int32_t* d_ref) {
   sa_status s = check_layout(layout);
   if (s != SA_OK) return s;
@@ -1538,7 +1546,7 @@ sa_status check_counts(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_p
   if (max_entries < 0) return fail(SA_ERR_SHAPE, "max_entries %lld", (long long)max_entries);
   if (!pages.indptr || (max_entries > 0 && !pages.indices) || !d_ref)
     return fail(SA_ERR_NULL, "a page table pointer or d_ref is NULL");
-  return check_ctx(ctx);
+  return SA_OK;
 }
 
 template <bool kUp>
@@ -1558,12 +1566,12 @@ void launch_count(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_pages 
 
 sa_status kv_release(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_pages pages, int64_t max_entries,
                      int32_t* d_ref, int32_t* d_free, int32_t* d_num_free, void* stream) {
-  DeviceGuard guard;
-  sa_status s = check_layout(layout);
+  sa_status s = check_counts(layout, batch, pages, max_entries, d_ref);
   if (s != SA_OK) return s;
   if ((d_free == nullptr) != (d_num_free == nullptr))
     return fail(SA_ERR_NULL, "give both d_free and d_num_free or neither");
-  s = check_counts(ctx, layout, batch, pages, max_entries, d_ref);
+  DeviceGuard guard;
+  s = check_ctx(ctx);
   if (s != SA_OK) return s;
   const hipStream_t st = (hipStream_t)stream;
   const int chunks = (int)((layout->num_slots + sa::kScanChunk - 1) / sa::kScanChunk);
@@ -1588,7 +1596,6 @@ sa_status kv_release(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_pag
 sa_status kv_compact(sa_ctx* ctx, const sa_layout* layout, void* k_pool, void* v_pool, int32_t limit,
                      const int32_t* d_ref, int32_t* d_ref_out, const int32_t* d_indices, int32_t* d_indices_out,
                      int64_t num_entries, int32_t* d_slot_map, int32_t* d_moved, void* stream) {
-  DeviceGuard guard;
   sa_status s = check_layout(layout);
   if (s != SA_OK) return s;
   if (limit < 0 || limit > layout->num_slots)
@@ -1598,6 +1605,7 @@ sa_status kv_compact(sa_ctx* ctx, const sa_layout* layout, void* k_pool, void* v
       (num_entries > 0 && (!d_indices || !d_indices_out)))
     return fail(SA_ERR_NULL, "a device pointer is NULL");
   if (!aligned16(k_pool) || !aligned16(v_pool)) return fail(SA_ERR_ALIGN, "pool pointer not 16-byte aligned");
+  DeviceGuard guard;
   s = check_ctx(ctx);
   if (s != SA_OK) return s;
   const hipStream_t st = (hipStream_t)stream;
@@ -1694,8 +1702,9 @@ sa_status shared_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   uint8_t* dev = ctx->plans[kPlanShared].dev;
   if (!same) {
     sa::plan_shared_items(layout, seqs, num_groups, h_group_indptr, h_shared_len, ctx->num_cu, plan);
-    if (plan.part_rows > sa::kMaxPartRows)
-      return fail(SA_ERR_SHAPE, "too many partial rows (%lld)", (long long)plan.part_rows);
+    if (plan.part_rows > sa::kMaxPartRows || (int64_t)plan.items.size() > kMaxBlocks ||
+        (int64_t)plan.units.size() * layout->num_kv_heads > kMaxBlocks)
+      return fail(SA_ERR_SHAPE, "the batch is too large for one launch (%lld partial rows)", (long long)plan.part_rows);
     rec.shared = plan.shared;
     rec.n_items = plan.items.size();
     rec.n_units = plan.units.size();
@@ -1787,8 +1796,10 @@ sa_status sa_kv_fork(sa_ctx* ctx, const sa_layout* layout, void* k_pool, void* v
 sa_status sa_kv_retain(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_pages pages, int64_t max_entries,
                        int32_t* d_ref, void* stream) {
   return no_throw([&] {
+    sa_status s = check_counts(layout, batch, pages, max_entries, d_ref);
+    if (s != SA_OK) return s;
     DeviceGuard guard;
-    const sa_status s = check_counts(ctx, layout, batch, pages, max_entries, d_ref);
+    s = check_ctx(ctx);
     if (s != SA_OK) return s;
     launch_count<true>(ctx, layout, batch, pages, max_entries, d_ref, (hipStream_t)stream);
     SA_HIP(hipGetLastError());

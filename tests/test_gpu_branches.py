@@ -163,6 +163,22 @@ def test_append_rope_in_place_and_on_another_stream():
         np.testing.assert_array_equal(a, bits(b))
 
 
+def test_append_rope_tells_batches_of_equal_words_apart():
+    """One sequence and 64 frequencies, then 17 sequences and 40, whose arrays are the same words one after another."""
+    r = np.random.default_rng(7)
+    L, ctx = lay((4, 2), 16, 8), sa.Context(0)
+    q, k = rows(r, (5, 4, D)).cuda(), rows(r, (5, 2, D)).cuda()
+    kp, vp = pool_bits(r, L, FILL), pool_bits(r, L, FILL)
+    out = torch.empty_like(q)
+    sa.sa_kv_append_rope(ctx, L, 0, sa.Rope(np.zeros(64)), q, k, k, out, kp, vp, [0], [5], dev([0, 1]), dev([3]))
+    sa.sa_sync_check(ctx)
+    before = bits(kp).copy()
+    sa.sa_kv_append_rope(ctx, L, 0, sa.Rope(np.zeros(40)), None, None, None, None, kp, vp, [0, 5] + [0] * 15, [0] * 17,
+                         dev([0] * 18), dev([3]))
+    sa.sa_sync_check(ctx)
+    np.testing.assert_array_equal(bits(kp), before)
+
+
 @pytest.mark.parametrize("rot,inter", [(128, False), (64, False), (128, True)])
 def test_append_rope_of_many_tokens(rot, inter):
     """More bytes than the Infinity Cache: checked against the same rows in pieces, and some rows in float64."""
