@@ -478,7 +478,8 @@ sa_status sa_segment_prefill_attn_append(sa_ctx *ctx, const sa_layout *layout, i
  * captured into a graph, since a replay would find another call's plan in the
  * context; sa_kv_retain, sa_kv_release and sa_kv_compact can be captured once
  * a call of the same pool size has run on the context (they allocate nothing
- * then), and their replays count as calls on it.
+ * then), and their replays count as calls on it.  Slots of more than 2^30
+ * elements and pools of 2^31 - 4096 slots or more are refused (SA_ERR_UNSUPPORTED).
  *
  * A pool whose slots are shared by several tables keeps one count per slot,
  * d_ref: device int32 [num_slots], the number of table entries that name the

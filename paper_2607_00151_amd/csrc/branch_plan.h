@@ -51,7 +51,7 @@ inline sa_status plan_fork(const sa_layout* layout, int32_t batch, const int32_t
     if (h_reserve[c] < 0) return plan_fail(err, SA_ERR_SHAPE, "child %d: reserve %d", c, h_reserve[c]);
     const int64_t len = h_src_len[b], full = len / P, rows = len % P;
     const int64_t pages = (len + h_reserve[c] + P - 1) / P;
-    if (out.n_dst + pages > INT32_MAX) return plan_fail(err, SA_ERR_SHAPE, "destination table too large");
+    if (out.n_dst + pages > INT32_MAX - 1024) return plan_fail(err, SA_ERR_SHAPE, "destination table too large");
     if (first[b] < 0) first[b] = c;
     out.children.push_back({b, (int32_t)full, (int32_t)rows, (int32_t)out.fresh_used, (int32_t)out.n_dst, 0});
     ++out.children[first[b]].raise;

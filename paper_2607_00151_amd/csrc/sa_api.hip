@@ -1242,6 +1242,17 @@ namespace {
 // Blocks of 256 threads of one launch: its work items are counted in 32 bits.
 constexpr int64_t kMaxBlocks = (int64_t(1) << 24) - 1;
 
+// The branch kernels index within a slot, and over the slots by whole chunks, in 32 bits.
+sa_status check_sizes(const sa_layout* layout) {
+  const sa_status s = check_layout(layout);
+  if (s != SA_OK) return s;
+  if (slot_elems(layout) > INT32_MAX / 2)
+    return fail(SA_ERR_UNSUPPORTED, "a slot of %lld elements", (long long)slot_elems(layout));
+  if (layout->num_slots > INT32_MAX - sa::kScanChunk)
+    return fail(SA_ERR_UNSUPPORTED, "a pool of %lld slots", (long long)layout->num_slots);
+  return SA_OK;
+}
+
 // The calling thread's device, put back when the call returns.
 struct DeviceGuard {
   int before = -1;
@@ -1293,7 +1304,7 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
                       int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
                       void* q_out, void* k_pool, void* v_pool, int32_t batch, const int32_t* h_start,
                       const int32_t* h_new_len, const int32_t* h_pos, sa_pages pages, void* stream) {
-  sa_status s = check_layout(layout);
+  sa_status s = check_sizes(layout);
   if (s != SA_OK) return s;
   if (layer < 0 || layer >= layout->num_layers)
     return fail(SA_ERR_SHAPE, "layer %d outside [0, %d)", layer, layout->num_layers);
@@ -1449,7 +1460,7 @@ sa_status kv_fork(sa_ctx* ctx, const sa_layout* layout, void* k_pool, void* v_po
                   const int32_t* h_src_len, int32_t num_children, const int32_t* h_parent, const int32_t* h_reserve,
                   sa_pages src, const int32_t* d_fresh, int32_t num_fresh, int32_t* d_dst_indptr,
                   int32_t* d_dst_indices, int32_t dst_capacity, int32_t* d_ref, int32_t* h_fresh_used, void* stream) {
-  sa_status s = check_layout(layout);
+  sa_status s = check_sizes(layout);
   if (s != SA_OK) return s;
   sa_ctx::ForkRec rec;
   sa::ForkPlan plan;
@@ -1540,7 +1551,7 @@ sa_status kv_fork(sa_ctx* ctx, const sa_layout* layout, void* k_pool, void* v_po
 // Checks that the calls over counts have in common.
 sa_status check_counts(const sa_layout* layout, int32_t batch, sa_pages pages, int64_t max_entries,
                        const int32_t* d_ref) {
-  sa_status s = check_layout(layout);
+  sa_status s = check_sizes(layout);
   if (s != SA_OK) return s;
   if (batch < 1) return fail(SA_ERR_SHAPE, "batch %d < 1", batch);
   if (max_entries < 0) return fail(SA_ERR_SHAPE, "max_entries %lld", (long long)max_entries);
@@ -1596,7 +1607,7 @@ sa_status kv_release(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_pag
 sa_status kv_compact(sa_ctx* ctx, const sa_layout* layout, void* k_pool, void* v_pool, int32_t limit,
                      const int32_t* d_ref, int32_t* d_ref_out, const int32_t* d_indices, int32_t* d_indices_out,
                      int64_t num_entries, int32_t* d_slot_map, int32_t* d_moved, void* stream) {
-  sa_status s = check_layout(layout);
+  sa_status s = check_sizes(layout);
   if (s != SA_OK) return s;
   if (limit < 0 || limit > layout->num_slots)
     return fail(SA_ERR_RANGE, "limit %d outside [0, %lld]", limit, (long long)layout->num_slots);
@@ -1663,7 +1674,9 @@ sa_status shared_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   sa_ctx::SharedRec rec;
   std::vector<sa::SeqDesc> seqs;
   bool same = false;
-  sa_status s = sa::check_attn_call(layout, layer, batch, h_q_len, h_kv_len, softmax_scale, g_err);
+  sa_status s = check_sizes(layout);
+  if (s != SA_OK) return s;
+  s = sa::check_attn_call(layout, layer, batch, h_q_len, h_kv_len, softmax_scale, g_err);
   if (s != SA_OK) return s;
   if (ctx && num_groups >= 1 && h_group_indptr && h_shared_len) {
     sa_ctx::DevPlan& dp = ctx->plans[kPlanShared];

@@ -133,6 +133,19 @@ def test_compact_refusals(lib):
     assert go(L=layout(head_dim=96)) == UNSUPPORTED
 
 
+def test_sizes_beyond_32_bits_are_refused(lib):
+    wide, deep = layout(num_q_heads=1 << 20, num_kv_heads=1 << 20, num_slots=1), layout(num_slots=2**31 - 1, num_layers=1)
+    assert fork(lib, L=wide) == UNSUPPORTED and fork(lib, L=deep) == UNSUPPORTED
+    assert rope(lib, L=wide) == UNSUPPORTED
+    P = sa._Pages(FAKE, FAKE)
+    for L in (wide, deep):
+        assert lib.sa_kv_release(None, ctypes.byref(L), 1, P, 4, FAKE, FAKE, FAKE, None) == UNSUPPORTED
+        assert lib.sa_kv_compact(None, ctypes.byref(L), FAKE, FAKE, 0, FAKE, FAKE, FAKE, FAKE, 4, FAKE, FAKE,
+                                 None) == UNSUPPORTED
+    # a destination table past 2^31 entries
+    assert fork(lib, src=[2**31 - 1] * 20, parent=range(20), reserve=[0] * 20, nfresh=2**31 - 1, cap=2**31 - 1) == SHAPE
+
+
 def test_shared_refusals(lib):
     def go(L=layout(), q_len=(1, 1), kv=(10, 9), groups=(0, 2), shared=(8,), q=FAKE, o=FAKE, lse=None, scale=0.1, layer=0):
         a, b, g, s = i32(q_len), i32(kv), i32(groups), i32(shared)
