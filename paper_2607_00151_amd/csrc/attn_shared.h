@@ -10,6 +10,11 @@
 // launch makes all parts (the members' rows lie next to each other in Q, so a
 // prefix tile is an item of attn_pipe_kernel's body whose "sequence" is the
 // whole group), a second joins them row by row.
+//
+// Bound by HBM for one token per member (32 of 16K keys, 32/8 heads: 110 MB in 24
+// us and the merge's 6.7, against 154 by the segment attention), by the matrix
+// cores and the softmax beside them from some 200 rows on (64 of 64K, 64/8 heads: 139
+// GFLOP in 150 us and 12, against 1155).
 #pragma once
 
 #include "attn_pipe.h"

@@ -21,7 +21,8 @@
 // the two products per dim of one token, for query and for key heads.  A wave
 // takes 16 head rows at a time of one token, the next 16 in flight, for as many
 // rounds as leave the chip enough waves; the sum of squares is a 4-step DPP
-// reduction within a row's 16 lanes.
+// reduction within a row's 16 lanes.  40.7K tokens of 48 head rows (1.0 GB): 237 us
+// with everything per row, 190 so, 175 (5.7 TB/s) with kStream; 64 tokens 5 us.
 #pragma once
 
 #include <hip/hip_runtime.h>
