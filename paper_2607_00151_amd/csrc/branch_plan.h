@@ -170,7 +170,7 @@ inline int64_t shared_parts(int64_t tiles, int64_t chunk) {
 // (MI355X): a prefill tile 120 and a block's start and end 400 where at most one
 // long prefill block has each CU, 185 and 900 where two share one; a decode tile 80 and
 // its block 300; the keys stream at 54.6 per tile and 100 blocks (6 TB/s), with a
-// quarter of the shorter of work and stream not overlapping; the merge 700, and
+// quarter of the shorter of work and stream not overlapping; the merge 530, and
 // 1032 bytes written and read per row and part at 9 TB/s.
 inline SharedCost shared_chunk_cost(const std::vector<SharedShape>& shapes, int Hkv, int num_cu, int64_t chunk) {
   struct Run {
@@ -204,7 +204,7 @@ inline SharedCost shared_chunk_cost(const std::vector<SharedShape>& shapes, int 
   }
   busy = std::max(busy, sum / slots);
   const int64_t stream = streamed * 546 / 1000;
-  return {std::max(busy, stream) + std::min(busy, stream) / 4 + 700 + part_rows * 1032 / 90000, busy > stream};
+  return {std::max(busy, stream) + std::min(busy, stream) / 4 + 530 + part_rows * 1032 / 90000, busy > stream};
 }
 
 // The same work by sa_segment_prefill_attn, every member over all of its keys:
@@ -267,11 +267,12 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
   bool any = false;
   for (int g = 0; g < num_groups; ++g) {
     const int b0 = h_group_indptr[g], b1 = h_group_indptr[g + 1];
-    int64_t rows = 0, apart = 0;
+    int64_t rows = 0, apart = 0, active = 0;
     int first = -1;
     for (int b = b0; b < b1; ++b) {
       const int64_t r = (int64_t)seqs[b].q_len * G;
       rows += r;
+      active += r > 0;
       apart += (r + kRows - 1) / kRows;
       if (first < 0 && r > 0) first = b;
     }
@@ -281,7 +282,13 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
     // the prefix: every row then goes through partials.  8 segments of 45 to 64 tokens
     // on 16K, us with the prefix computed once and member by member: 12 row tiles of
     // 16 112 and 116, 13 of 16 125 and 125, 14 of 16 132 and 125, 16 of 16 145 and 137.
-    const bool shared = S > 0 && rows + S <= INT32_MAX / 2 && 5 * ((rows + kRows - 1) / kRows) <= 4 * apart;
+    // With more than kDecodeRows rows a member the two partials of a row tile cost
+    // about as much as 20 key tiles, which the tiles saved have to outweigh: 16
+    // segments of 36 tokens on 4K (18 tiles of 32, 64 key tiles) 63 and 68, of 45
+    // (23 of 32) 74 and 67; 51 of 4 to 26 on 130, 32/4 heads, 30 and 20.
+    const int64_t packed = (rows + kRows - 1) / kRows;
+    const bool shared = S > 0 && rows + S <= INT32_MAX / 2 && 5 * packed <= 4 * apart &&
+                        (rows <= (int64_t)kDecodeRows * active || (apart - packed) * (S / kKT) >= 20 * apart);
     const int32_t prefix0 = shared ? (int32_t)tiles.size() : -1;
     if (shared) {
       any = true;

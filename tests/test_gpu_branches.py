@@ -572,6 +572,9 @@ SHARED = [
     ((4, 1), 16, [(3000, [(1, 1)] * 3), (100, [(2000, 1), (1, 1), (700, 3)]), (0, [(1, 1)])]),
     ((8, 2), 32, [(5000, [(129, 2)] * 17)]),
     ((16, 2), 32, [(2000, [(30, 1)]), (1500, [(900, 1)] * 2), (0, [(4000, 1)]), (70, [(5000, 300)])]),
+    ((32, 8), 16, [(3009, [(30, 13)] * 9), (70, [(9, 9)] * 3)]),  # several tokens each: tiles of many members
+    ((10, 2), 32, [(2650, [(20 + 7 * i, 9 + i) for i in range(14)])]),
+    ((12, 2), 16, [(6001, [(100, 30 + i) for i in range(7)])]),
 ]
 
 
