@@ -124,13 +124,14 @@ struct CountArgs {
 // never falls below zero: an entry that finds none left puts it back and raises
 // the error flag.
 template <bool kUp>
-__global__ __launch_bounds__(256) void count_kernel(CountArgs a) {
+__device__ __forceinline__ void count_entries(const CountArgs& a) {
   const int64_t lo = a.indptr[0], hi = a.indptr[a.batch];
   if (lo < 0 || hi < lo || hi > a.max_entries) {
     if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.err, 4);
     return;
   }
-  for (int64_t e = lo + (int64_t)blockIdx.x * 256 + threadIdx.x; e < hi; e += (int64_t)gridDim.x * 256) {
+  const int64_t stride = (int64_t)gridDim.x * blockDim.x;
+  for (int64_t e = lo + (int64_t)blockIdx.x * blockDim.x + threadIdx.x; e < hi; e += stride) {
     const int32_t slot = a.indices[e];
     if (slot < 0 || (int64_t)slot >= a.num_slots) {
       atomicOr(a.err, 4);
@@ -141,6 +142,11 @@ __global__ __launch_bounds__(256) void count_kernel(CountArgs a) {
       atomicOr(a.err, kCountError);
     }
   }
+}
+
+template <bool kUp>
+__global__ __launch_bounds__(256) void count_kernel(CountArgs a) {
+  count_entries<kUp>(a);
 }
 
 // ---------------------------------------------------------------- scans over the slots
@@ -237,7 +243,8 @@ __device__ __forceinline__ void idle_slots(const FreeArgs& a, uint64_t (&mask)[k
 #pragma unroll
   for (int i = 0; i < kScanPer; ++i) {
     const int s = scan_slot(i);
-    idle[i] = s < a.num_slots && a.ref[s] <= 0;
+    // at device scope: where the counts were lowered by this same launch
+    idle[i] = s < a.num_slots && __hip_atomic_load(a.ref + s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) <= 0;
   }
 #pragma unroll
   for (int i = 0; i < kScanPer; ++i) mask[i] = __ballot(idle[i]);
@@ -251,8 +258,7 @@ __global__ __launch_bounds__(kScanThreads) void free_count_kernel(FreeArgs a) {
 }
 
 // The slots without a count, ascending, then -1 up to num_slots.
-__global__ __launch_bounds__(kScanThreads) void free_list_kernel(FreeArgs a) {
-  __shared__ ScanRoom room;
+__device__ __forceinline__ void list_idle(const FreeArgs& a, ScanRoom& room) {
   uint64_t mask[kScanPer];
   idle_slots(a, mask);
   const int2 n = scan_block(mask, a.counts, a.chunks, room);
@@ -265,6 +271,25 @@ __global__ __launch_bounds__(kScanThreads) void free_list_kernel(FreeArgs a) {
     if (s < a.num_slots && s >= n.y) a.free_list[s] = -1;
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.num_free = n.y;
+}
+
+__global__ __launch_bounds__(kScanThreads) void free_list_kernel(FreeArgs a) {
+  __shared__ ScanRoom room;
+  list_idle(a, room);
+}
+
+// A small pool's whole release in one block: its entries lower the counts, and
+// once the atomics have returned the block lists the slots.  1020 entries and 1295
+// slots: 6.6 us against 2.1 and 3.6 in two launches, and a fork with its release
+// 13.8 against 15.7, the host's work of a launch less.
+constexpr int64_t kOneBlockEntries = 4096;
+
+__global__ __launch_bounds__(kScanThreads) void release_small_kernel(CountArgs c, FreeArgs a) {
+  __shared__ ScanRoom room;
+  count_entries<false>(c);
+  __threadfence();
+  __syncthreads();
+  list_idle(a, room);
 }
 
 // ---------------------------------------------------------------- compaction

@@ -1560,9 +1560,8 @@ sa_status check_counts(const sa_layout* layout, int32_t batch, sa_pages pages, i
   return SA_OK;
 }
 
-template <bool kUp>
-void launch_count(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_pages pages, int64_t max_entries,
-                  int32_t* d_ref, hipStream_t st) {
+sa::CountArgs count_args(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_pages pages, int64_t max_entries,
+                         int32_t* d_ref) {
   sa::CountArgs a{};
   a.indptr = pages.indptr;
   a.indices = pages.indices;
@@ -1571,7 +1570,12 @@ void launch_count(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_pages 
   a.num_slots = layout->num_slots;
   a.max_entries = max_entries;
   a.batch = batch;
-  const int64_t blocks = std::min<int64_t>(std::max<int64_t>(1, (max_entries + 255) / 256), 1024);
+  return a;
+}
+
+template <bool kUp>
+void launch_count(sa_ctx* ctx, const sa::CountArgs& a, hipStream_t st) {
+  const int64_t blocks = std::min<int64_t>(std::max<int64_t>(1, (a.max_entries + 255) / 256), 1024);
   launch_timed(sa::count_kernel<kUp>, dim3((unsigned)blocks), dim3(256), st, ctx->kernel_ev[SA_TIMED_PAGES], a);
 }
 
@@ -1591,10 +1595,20 @@ sa_status kv_release(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_pag
     s = reserve_work(ctx, (size_t)chunks * sizeof(int32_t), st);
     if (s != SA_OK) return s;
   }
-  launch_count<false>(ctx, layout, batch, pages, max_entries, d_ref, st);
+  const sa::CountArgs c = count_args(ctx, layout, batch, pages, max_entries, d_ref);
+  sa::FreeArgs f{d_ref, d_free, d_num_free, counted ? (int32_t*)ctx->work : nullptr, (int32_t)layout->num_slots, chunks};
+  if (d_free != nullptr && !counted && max_entries <= sa::kOneBlockEntries) {
+    const hipEvent_t* const ev = ctx->kernel_ev[SA_TIMED_PAGES];
+    if (ev[0] != nullptr)
+      hipExtLaunchKernelGGL(sa::release_small_kernel, dim3(1), dim3(sa::kScanThreads), 0, st, ev[0], ev[1], 0, c, f);
+    else
+      hipLaunchKernelGGL(sa::release_small_kernel, dim3(1), dim3(sa::kScanThreads), 0, st, c, f);
+    SA_HIP(hipGetLastError());
+    return SA_OK;
+  }
+  launch_count<false>(ctx, c, st);
   SA_HIP(hipGetLastError());
   if (d_free == nullptr) return SA_OK;
-  sa::FreeArgs f{d_ref, d_free, d_num_free, counted ? (int32_t*)ctx->work : nullptr, (int32_t)layout->num_slots, chunks};
   if (counted) {
     hipLaunchKernelGGL(sa::free_count_kernel, dim3((unsigned)chunks), dim3(sa::kScanThreads), 0, st, f);
     SA_HIP(hipGetLastError());
@@ -1814,7 +1828,7 @@ sa_status sa_kv_retain(sa_ctx* ctx, const sa_layout* layout, int32_t batch, sa_p
     DeviceGuard guard;
     s = check_ctx(ctx);
     if (s != SA_OK) return s;
-    launch_count<true>(ctx, layout, batch, pages, max_entries, d_ref, (hipStream_t)stream);
+    launch_count<true>(ctx, count_args(ctx, layout, batch, pages, max_entries, d_ref), (hipStream_t)stream);
     SA_HIP(hipGetLastError());
     return SA_OK;
   });
