@@ -297,7 +297,8 @@ sa_status sa_kv_splice_alias(sa_ctx *ctx, const sa_layout *layout, int32_t batch
  * exact share.  After sa_set_exact_scale(ctx, 0) the kernel instead
  * multiplies each query row by softmax_scale * log2(e) once and rounds it to
  * bf16 (faster; moves a row's scaled scores by up to
- * 2^-8 * sum_d |scale log2(e) q_d k_d| in log2 units).
+ * 2^-8 * sum_d |scale log2(e) q_d k_d| in log2 units).  A row that meets a
+ * score of +infinity or NaN has a NaN output and a NaN LSE.
  *
  * Errors: SA_ERR_SHAPE (0 <= q_len <= kv_len violated, bad batch or layer,
  * softmax_scale not finite and positive),

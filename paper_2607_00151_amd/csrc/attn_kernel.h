@@ -362,7 +362,7 @@ __global__ __launch_bounds__(64 * WAVES, (QT == 1 ? 2 : 1)) void attn_kernel(Att
   for (int qt = 0; qt < QT; ++qt) {
     const float l_tot = pair_sum(l[qt]);
     const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
-    const float lse2 = l_tot > 0.f ? m_used[qt] + __builtin_amdgcn_logf(l_tot) : -INFINITY;
+    const float lse2 = l_tot == 0.f ? -INFINITY : m_used[qt] + __builtin_amdgcn_logf(l_tot);
     if (it.part < 0) {
       if (row_valid[qt]) {
         uint16_t* orow = a.o + ((int64_t)(sd.q_start + tok[qt]) * a.Hq + head[qt]) * kHD;
@@ -423,16 +423,15 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a) {
   for (int s = 0; s < g.nsplit; ++s) mx = fmaxf(mx, a.part_lse[(int64_t)(g.part0 + s) * a.rows + lrow]);
   f32x4 num[4] = {};
   float den = 0.f;
-  if (mx != -INFINITY) {
+  const float sub = mx == -INFINITY ? 0.f : mx;             // also where every part is NaN
 #pragma unroll 2
-    for (int s = 0; s < g.nsplit; ++s) {
-      const int64_t p = (int64_t)(g.part0 + s) * a.rows + lrow;
-      const float w = exp2f_fast(a.part_lse[p] - mx);
-      const f32x4* src = (const f32x4*)(a.part_o + p * kHD + d0);
-      den += w;
+  for (int s = 0; s < g.nsplit; ++s) {
+    const int64_t p = (int64_t)(g.part0 + s) * a.rows + lrow;
+    const float w = exp2f_fast(a.part_lse[p] - sub);
+    const f32x4* src = (const f32x4*)(a.part_o + p * kHD + d0);
+    den += w;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) num[c] += w * src[c];
-    }
+    for (int c = 0; c < 4; ++c) num[c] += w * src[c];
   }
   const float inv = den > 0.f ? 1.f / den : 0.f;
   const int tok = r / a.G;
@@ -442,7 +441,7 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a) {
   for (int c = 0; c < 4; ++c)
     st_bf16x4(a.o + orow * kHD + d0 + 4 * c, num[c][0] * inv, num[c][1] * inv, num[c][2] * inv, num[c][3] * inv);
   if (a.lse != nullptr && d0 == 0)
-    a.lse[orow] = den > 0.f ? (mx + __builtin_amdgcn_logf(den)) * 0.69314718055994531f : -INFINITY;
+    a.lse[orow] = den == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(den)) * 0.69314718055994531f;
 }
 
 }  // namespace sa

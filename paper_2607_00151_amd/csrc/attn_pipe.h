@@ -907,7 +907,8 @@ __device__ __attribute__((always_inline)) inline void pipe_group(const AttnArgs&
   const float l_tot = pair_sum(l);
   const float l_out = kExact ? pair_sum(l + corr) : l_tot;
   const float inv = l_out > 0.f ? 1.f / l_out : 0.f;
-  const float lse2 = l_tot > 0.f ? m_used + __builtin_amdgcn_logf(l_tot) : -INFINITY;
+  // a row with an infinite or NaN score has a NaN sum: its part says so, and the merge's result is NaN
+  const float lse2 = l_tot == 0.f ? -INFINITY : m_used + __builtin_amdgcn_logf(l_tot);
   // The output row is worked out again from the lane index here rather than
   // kept from the start: values live across the loops beyond its registers
   // are spilled to scratch memory.
@@ -1001,7 +1002,7 @@ __device__ __attribute__((always_inline)) inline void pipe_group(const AttnArgs&
                   num[k][2] * dinv, num[k][3] * dinv);
       if (a.lse != nullptr && hh_o == 0)
         a.lse[(int64_t)(sd.q_start + o_tok) * a.Hq + o_head] =
-            den > 0.f ? (mx + __builtin_amdgcn_logf(den)) * 0.69314718055994531f : -INFINITY;
+            den == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(den)) * 0.69314718055994531f;
     }
   } else {
     // two groups: plain rows, merged by merge_kernel
@@ -1358,7 +1359,7 @@ __device__ __attribute__((always_inline)) inline void decode_group(const AttnArg
       o += f * *piece(w, row, c);
     }
     const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
-    const float lse2 = lsum > 0.f ? m + __builtin_amdgcn_logf(lsum) : -INFINITY;
+    const float lse2 = lsum == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(lsum);
     o *= inv;
     if (whole) {
       const int r = it.row0 + row, tok = r / G;
@@ -1445,7 +1446,7 @@ __device__ __attribute__((always_inline)) inline void decode_group(const AttnArg
       const int64_t orow = (int64_t)(it.q_start + tok) * a.Hq + it.kvh * G + (r - tok * G);
       st_bf16x4(a.o + orow * kHD + 4 * c, num[0] * dinv, num[1] * dinv, num[2] * dinv, num[3] * dinv);
       if (a.lse != nullptr && c == 0)
-        a.lse[orow] = den > 0.f ? (mx + __builtin_amdgcn_logf(den)) * 0.69314718055994531f : -INFINITY;
+        a.lse[orow] = den == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(den)) * 0.69314718055994531f;
     }
   }
 }

@@ -141,7 +141,7 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(MergeRowsArgs a) {
   const int64_t orow = (int64_t)(u.q_start + tok) * a.Hq + kvh * a.G + (row - tok * a.G);
   st_bf16x4(a.o + orow * kHD + 4 * c, num[0] * inv, num[1] * inv, num[2] * inv, num[3] * inv);
   if (a.lse != nullptr && c == 0)
-    a.lse[orow] = den > 0.f ? (mx + __builtin_amdgcn_logf(den)) * 0.69314718055994531f : -INFINITY;
+    a.lse[orow] = den == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(den)) * 0.69314718055994531f;
 }
 
 }  // namespace sa

@@ -1,0 +1,122 @@
+"""Calls for branches of one context where they can go wrong: values that are not finite, the edges of the slot scans,
+contexts after a failed call, groups that take every path of the shared-prefix attention's planner."""
+import os
+import subprocess
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_00151_amd as sa
+from test_gpu_branches import D, anchor, branch_batch, check_attention, run_shared
+
+pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+# ------------------------------------------------------------------------- values that are not finite
+
+NONFINITE = [
+    # heads, page, groups; with the anchor: the shared-prefix kernel, else the segment attention
+    ((8, 2), 16, [(900, [(5, 1), (40, 1), (7, 1)])], True),              # one token each
+    ((32, 8), 16, [(3009, [(30, 13)] * 9)], True),                       # tiles of many members' rows
+    ((8, 2), 16, [(900, [(5, 1), (40, 1), (7, 1)])], False),
+    ((8, 1), 16, [(9000, [(5, 1), (40, 1)])], False),                    # split by key range
+    ((4, 1), 16, [(256, [(200, 150), (300, 200)])], False),
+]
+
+
+def nonfinite_batch(i):
+    heads, page, groups, anchored = NONFINITE[i]
+    r = np.random.default_rng(300 + i)
+    return branch_batch(r, heads, page, groups + ([anchor(heads)] if anchored else []))
+
+
+def same_bits(a, b):
+    return (a.contiguous().view(torch.uint8) == b.contiguous().view(torch.uint8)).all().item()
+
+
+@pytest.mark.parametrize("i", range(len(NONFINITE)))
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_query_that_is_not_finite_stays_in_its_row(i, value):
+    w = nonfinite_batch(i)
+    ctx = sa.Context(0)
+    o, lse = (x.clone() for x in run_shared(ctx, w))
+    t, h = w["q_len"][0] + w["q_len"][1] - 1, w["heads"][0] - 1          # the second member's last row
+    clean = w["q"].clone()
+    w["q"][t, h, 17] = value                                             # scores of both infinities, or NaN
+    o2, lse2 = run_shared(ctx, w)
+    assert o2[t, h].isnan().all() and lse2[t, h].isnan()
+    o2[t, h], lse2[t, h] = o[t, h], lse[t, h]
+    check_attention(dict(w, q=clean), o2, lse2, D ** -0.5)                     # the rows beside it
+
+
+@pytest.mark.parametrize("i", range(len(NONFINITE)))
+def test_a_key_that_is_nan_reaches_the_rows_that_see_it(i):
+    """A shared key: every member's rows of its KV head; the last key of a member: that member's last token."""
+    w = nonfinite_batch(i)
+    Hq, Hkv = w["heads"]
+    G, page = Hq // Hkv, w["L"].page_size
+    ctx = sa.Context(0)
+    o, lse = (x.clone() for x in run_shared(ctx, w))
+    ip, ix = w["indptr"].tolist(), w["indices"].tolist()
+    pool = w["kp"].view(torch.bfloat16)
+    n = w["groups"][1]                                                   # members of the first group
+    last = sum(w["q_len"][:2]) - 1
+    cases = [(ix[ip[0] + 3 * 16 // page], 5, range(sum(w["q_len"][:n]))),
+             (ix[ip[1] + (w["kv_len"][1] - 1) // page], (w["kv_len"][1] - 1) % page, [last])]
+    for slot, row, tokens in cases:
+        keep = pool[0, slot, Hkv - 1, row].clone()
+        pool[0, slot, Hkv - 1, row, 100] = float("nan")
+        o2, lse2 = run_shared(ctx, w)
+        pool[0, slot, Hkv - 1, row] = keep
+        hit = torch.zeros(lse.shape, dtype=torch.bool, device="cuda")
+        hit[list(tokens), (Hkv - 1) * G:] = True
+        assert o2[hit].isnan().all() and lse2[hit].isnan().all()
+        check_attention(w, torch.where(hit[..., None], o, o2), torch.where(hit, lse, lse2), D ** -0.5)
+
+
+@pytest.mark.parametrize("i", range(len(NONFINITE)))
+def test_a_value_that_is_not_finite_leaves_the_other_members_alone(i):
+    w = nonfinite_batch(i)
+    Hq, Hkv = w["heads"]
+    G, page = Hq // Hkv, w["L"].page_size
+    ctx = sa.Context(0)
+    o, lse = (x.clone() for x in run_shared(ctx, w))
+    ip, ix = w["indptr"].tolist(), w["indices"].tolist()
+    at = w["kv_len"][1] - 1
+    w["vp"].view(torch.bfloat16)[0, ix[ip[1] + at // page], 0, at % page, 9] = float("inf")
+    o2, lse2 = run_shared(ctx, w)
+    t0, t1 = w["q_len"][0], sum(w["q_len"][:2])
+    assert not o2[t1 - 1, :G, 9].isfinite().any()
+    hit = torch.zeros(o.shape, dtype=torch.bool, device="cuda")
+    hit[t0:t1, :G, 9] = True                                             # the member's rows may see it, no other does
+    assert same_bits(o[~hit], o2[~hit]) and same_bits(lse, lse2)
+
+
+VARIANT = r"""
+import sys
+sys.path.insert(0, {root!r}); sys.path.insert(0, {tests!r})
+import numpy as np, torch
+import paper_2607_00151_amd as sa
+from test_gpu_branches import D, branch_batch, run_shared
+for heads, groups in (((8, 1), [(9000, [(5, 1), (40, 1)])]), ((4, 1), [(256, [(200, 150)])])):
+    w = branch_batch(np.random.default_rng(5), heads, 16, groups)
+    w["q"][0, 3, 17] = float("nan")
+    print("variant {variant}", groups, flush=True)
+    o, lse = run_shared(sa.Context(0), w)
+    assert o[0, 3].isnan().all() and lse[0, 3].isnan()
+    assert o[0, :3].isfinite().all() and lse[0, :3].isfinite().all()
+print("variant ok", flush=True)
+"""
+
+
+@pytest.mark.timeout(200)
+@pytest.mark.parametrize("variant", [1, 2])
+def test_other_attention_kernels_keep_nan_rows(variant):
+    code = VARIANT.format(root=ROOT, tests=os.path.join(ROOT, "tests"), variant=variant)
+    r = subprocess.run([sys.executable, "-u", "-c", code], env=dict(os.environ, SA_ATTN_VARIANT=str(variant)),
+                       capture_output=True, text=True, timeout=150)
+    print(r.stdout[-2000:], r.stderr[-3000:])
+    assert r.returncode == 0 and "variant ok" in r.stdout
