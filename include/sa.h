@@ -500,7 +500,7 @@ typedef struct sa_rope {
                                  0 to 1024                                              */
     const void *q_weight;     /* device bf16 [head_dim]; NULL: query heads are not normed */
     const void *k_weight;     /* the same for key heads                                 */
-    float eps;                /* of the norms, > 0                                       */
+    float eps;                /* of the norms, at least 2^-126                           */
     float weight_offset;      /* added to every weight (1 where weights are stored less 1) */
 } sa_rope;
 

@@ -5,6 +5,7 @@
 #include <hip/hip_ext.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -1317,8 +1318,9 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
     return fail(SA_ERR_UNSUPPORTED, "rot_dim %d (a multiple of 16 up to 128)", rope->rot_dim);
   if (rope->rot_dim > 0 && !rope->h_inv_freq) return fail(SA_ERR_NULL, "h_inv_freq is NULL");
   if ((rope->q_weight || rope->k_weight) &&
-      (!std::isfinite(rope->eps) || rope->eps <= 0.f || !std::isfinite(rope->weight_offset)))
-    return fail(SA_ERR_SHAPE, "eps %g must be finite and positive, weight_offset %g finite", rope->eps,
+      (!std::isfinite(rope->eps) || rope->eps < FLT_MIN || !std::isfinite(rope->weight_offset)))
+    // v_rsq takes a denormal for zero: a row of zeros would come out as 0 * inf
+    return fail(SA_ERR_SHAPE, "eps %g must be finite and at least 2^-126, weight_offset %g finite", rope->eps,
                 rope->weight_offset);
   const int n_freq = rope->rot_dim / 2;
   for (int j = 0; j < n_freq; ++j)
