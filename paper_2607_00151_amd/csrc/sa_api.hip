@@ -40,11 +40,15 @@ sa_status fail(sa_status s, const char* fmt, ...) {
   return s;
 }
 
+// A failure is this call's: it is reported here and not left for the next check
+// of the runtime's last error, the caller's own or that of a later launch.
 #define SA_HIP(call)                                                                 \
   do {                                                                               \
     hipError_t e_ = (call);                                                          \
-    if (e_ != hipSuccess)                                                            \
+    if (e_ != hipSuccess) {                                                          \
+      (void)hipGetLastError();                                                       \
       return fail(SA_ERR_HIP, "%s failed: %s", #call, hipGetErrorString(e_));        \
+    }                                                                                \
   } while (0)
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -445,7 +449,8 @@ sa_status sa_create(int device, sa_ctx** out) {
   if (!out) return fail(SA_ERR_NULL, "out is NULL");
   *out = nullptr;
   int n = 0;
-  if (hipGetDeviceCount(&n) != hipSuccess || device < 0 || device >= n)
+  if (hipGetDeviceCount(&n) != hipSuccess) (void)hipGetLastError();
+  if (device < 0 || device >= n)
     return fail(SA_ERR_DEVICE, "HIP device %d not present (%d visible)", device, n);
   hipDeviceProp_t prop;
   SA_HIP(hipGetDeviceProperties(&prop, device));
@@ -465,6 +470,7 @@ sa_status sa_create(int device, sa_ctx** out) {
   if (e == hipSuccess) e = hipHostMalloc(&c->na_host, kNoAllocPlanBytes, hipHostMallocDefault);
   if (e == hipSuccess) e = hipEventCreateWithFlags(&c->na_ev, hipEventDisableTiming);
   if (e != hipSuccess) {
+    (void)hipGetLastError();
     sa_destroy(c);
     return fail(SA_ERR_HIP, "context setup failed: %s", hipGetErrorString(e));
   }
@@ -1258,7 +1264,9 @@ sa_status check_sizes(const sa_layout* layout) {
 struct DeviceGuard {
   int before = -1;
   DeviceGuard() {
-    if (hipGetDevice(&before) != hipSuccess) before = -1;
+    if (hipGetDevice(&before) == hipSuccess) return;
+    (void)hipGetLastError();
+    before = -1;
   }
   ~DeviceGuard() {
     if (before >= 0) (void)hipSetDevice(before);

@@ -120,3 +120,21 @@ def test_other_attention_kernels_keep_nan_rows(variant):
                        capture_output=True, text=True, timeout=150)
     print(r.stdout[-2000:], r.stderr[-3000:])
     assert r.returncode == 0 and "variant ok" in r.stdout
+
+
+# ------------------------------------------------------------------------- contexts
+
+def test_a_call_that_failed_is_not_blamed_on_the_next():
+    """An allocation beyond the card's memory is refused; torch and later calls of the context go on."""
+    w = branch_batch(np.random.default_rng(9), (8, 2), 16, [(300, [(9, 1)] * 3), anchor((8, 2))])
+    ctx = sa.Context(0)
+    want, _ = run_shared(ctx, w)
+    with pytest.raises(sa.SaError, match="SA_ERR_HIP"):
+        sa.sa_reserve(ctx, 0, 1 << 45)
+    ref = torch.zeros(w["L"].num_slots, dtype=torch.int32, device="cuda")
+    with pytest.raises(sa.SaError, match="SA_ERR_HIP"):
+        sa.sa_reserve(ctx, 0, 1 << 45)
+    sa.sa_kv_retain(ctx, w["L"], w["indptr"], w["indices"], ref)
+    assert int(ref.sum()) == len(w["indices"])
+    got, _ = run_shared(ctx, w)
+    assert torch.equal(got, want)
