@@ -135,8 +135,14 @@ const char *sa_last_error(void);
  * call's plan takes about 40 bytes per work item (one per sequence, KV head
  * and 128 packed query rows, and per key-range part of a split item) plus
  * 16 bytes per sequence, 8 per key-range part and 768 of alignment; a splice's
- * about 24 bytes per surviving page plus 16 per sequence.  split_bytes:
- * capacity of the split-KV partials, 128 * 129 * 4 bytes per key-range part.
+ * about 24 bytes per surviving page plus 16 per sequence; a shared-prefix
+ * attention's 40 bytes per work item and 36 per up to 32 query rows of a
+ * sequence that are split, a rotated append's 12 bytes per sequence and 512 for
+ * the frequencies, a fork's 32 bytes per child, each with 768 of alignment.  It
+ * is also the capacity of the buffer in which sa_kv_release and sa_kv_compact
+ * scan the slots: 4 bytes per 4096 slots, and 16 per slot and 8 per 4096.
+ * split_bytes: capacity of the split-KV partials, 128 * 129 * 4 bytes per
+ * key-range part (sa_shared_prefix_attn: 516 bytes per query row, head and part).
  * Buffers only grow; outgrown ones are kept until sa_destroy.
  * Errors: SA_ERR_NULL (context), SA_ERR_SHAPE (negative size), SA_ERR_HIP.
  */
@@ -478,8 +484,8 @@ sa_status sa_segment_prefill_attn_append(sa_ctx *ctx, const sa_layout *layout, i
  * sa_shared_prefix_attn) return SA_ERR_UNSUPPORTED on a stream that is being
  * captured into a graph, since a replay would find another call's plan in the
  * context; sa_kv_retain, sa_kv_release and sa_kv_compact can be captured once
- * a call of the same pool size has run on the context (they allocate nothing
- * then), and their replays count as calls on it.  Slots of more than 2^30
+ * a call of the same pool size has run on the context or sa_reserve has made
+ * room for it (they allocate nothing then), and their replays count as calls on it.  Slots of more than 2^30
  * elements and pools of 2^31 - 4096 slots or more are refused (SA_ERR_UNSUPPORTED).
  *
  * A pool whose slots are shared by several tables keeps one count per slot,

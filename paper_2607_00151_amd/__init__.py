@@ -261,8 +261,8 @@ def _ctx_handle(ctx):
 
 
 def sa_reserve(ctx, plan_bytes: int, split_bytes: int = 0):
-    """Size ctx's plan buffers (each call kind's, and the pinned staging) to plan_bytes and
-    its split-KV partials to split_bytes, so later calls that fit allocate nothing."""
+    """Size ctx's plan buffers (each call kind's, the pinned staging and the slot scans' buffer) to
+    plan_bytes and its split-KV partials to split_bytes, so later calls that fit allocate nothing."""
     _check(load_library().sa_reserve(_ctx_handle(ctx), int(plan_bytes), int(split_bytes)))
 
 

@@ -524,6 +524,13 @@ sa_status sa_reserve(sa_ctx* ctx, int64_t plan_bytes, int64_t split_bytes) {
       SA_HIP(hipHostMalloc(&st.host, pb, hipHostMallocDefault));
       st.cap = pb;
     }
+  if (ctx->work_cap < pb) {
+    if (ctx->work) ctx->retired_dev.push_back(ctx->work);
+    ctx->work = nullptr;
+    ctx->work_cap = 0;
+    SA_HIP(hipMalloc(&ctx->work, pb));
+    ctx->work_cap = pb;
+  }
   if (ctx->part_cap < (size_t)split_bytes) {
     if (ctx->part) ctx->retired_dev.push_back(ctx->part);
     ctx->part = nullptr;

@@ -9,7 +9,7 @@ import pytest
 import torch
 
 import paper_2607_00151_amd as sa
-from test_gpu_branches import D, anchor, branch_batch, check_attention, run_shared
+from test_gpu_branches import D, anchor, branch_batch, check_attention, dev, lay, pool_bits, run_shared
 
 pytestmark = pytest.mark.gpu
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -100,7 +100,7 @@ import sys
 sys.path.insert(0, {root!r}); sys.path.insert(0, {tests!r})
 import numpy as np, torch
 import paper_2607_00151_amd as sa
-from test_gpu_branches import D, branch_batch, run_shared
+from test_gpu_branches import D, anchor, branch_batch, check_attention, dev, lay, pool_bits, run_shared
 for heads, groups in (((8, 1), [(9000, [(5, 1), (40, 1)])]), ((4, 1), [(256, [(200, 150)])])):
     w = branch_batch(np.random.default_rng(5), heads, 16, groups)
     w["q"][0, 3, 17] = float("nan")
@@ -138,3 +138,39 @@ def test_a_call_that_failed_is_not_blamed_on_the_next():
     assert int(ref.sum()) == len(w["indices"])
     got, _ = run_shared(ctx, w)
     assert torch.equal(got, want)
+
+
+def test_reserved_contexts_scan_slots_without_allocating():
+    """After sa_reserve the first release and the first compaction of a pool can be captured; replays follow the counts."""
+    slots, r = 9000, np.random.default_rng(10)
+    L = lay((1, 1), 16, slots)
+    kp, vp = pool_bits(r, L), pool_bits(r, L)
+    ctx = sa.Context(0)
+    sa.sa_reserve(ctx, 16 * slots + 8 * (slots // 4096 + 1))
+    ref, ix, ip = dev(np.zeros(slots)), dev([3, 4500]), dev([0, 2])
+    ref_out, ix_out, smap, free = (torch.zeros_like(x) for x in (ref, ix, ref, ref))
+    mv, nfree = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        sa.sa_kv_compact(ctx, L, kp, vp, 4200, ref, ref_out, ix, ix_out, smap, mv)
+        sa.sa_kv_release(ctx, L, ip, ix_out, ref_out, free, nfree)
+    for i in range(3):
+        count = (r.random(slots) < 0.3 + 0.1 * i).astype(np.int64)
+        count[[3, 4500]] = 1
+        ref.copy_(dev(count))
+        before = kp.cpu()
+        g.replay()
+        sa.sa_sync_check(ctx)
+        hole, high = np.flatnonzero(count[:4200] == 0), 4200 + np.flatnonzero(count[4200:])
+        n = min(len(hole), len(high))
+        assert mv.tolist() == [n, len(high) - n]
+        after = count.copy()
+        after[hole[:n]], after[high[:n]] = 1, 0
+        to = np.arange(slots)
+        to[high[:n]] = hole[:n]
+        np.testing.assert_array_equal(ix_out.cpu(), to[[3, 4500]])
+        after[to[[3, 4500]]] = 0
+        np.testing.assert_array_equal(ref_out.cpu(), after)
+        np.testing.assert_array_equal(free.cpu()[:int(nfree)], np.flatnonzero(after == 0))
+        assert torch.equal(kp.cpu()[:, hole[:n]], before[:, high[:n]])
