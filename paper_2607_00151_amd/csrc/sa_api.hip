@@ -1308,11 +1308,13 @@ sa_status reserve_work(sa_ctx* ctx, size_t need, hipStream_t stream) {
   if (need <= ctx->work_cap) return SA_OK;
   const sa_status s = refuse_capture(stream, "a call that has to allocate for a pool of this size");
   if (s != SA_OK) return s;
+  // at least doubled, as reserve_parts: a pool that grows by steps does not leave a buffer behind at each
+  const size_t cap = std::max(need, 2 * ctx->work_cap);
   if (ctx->work) ctx->retired_dev.push_back(ctx->work);
   ctx->work = nullptr;
   ctx->work_cap = 0;
-  SA_HIP(hipMalloc(&ctx->work, need));
-  ctx->work_cap = need;
+  SA_HIP(hipMalloc(&ctx->work, cap));
+  ctx->work_cap = cap;
   return SA_OK;
 }
 

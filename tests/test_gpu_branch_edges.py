@@ -174,3 +174,19 @@ def test_reserved_contexts_scan_slots_without_allocating():
         np.testing.assert_array_equal(ref_out.cpu(), after)
         np.testing.assert_array_equal(free.cpu()[:int(nfree)], np.flatnonzero(after == 0))
         assert torch.equal(kp.cpu()[:, hole[:n]], before[:, high[:n]])
+
+
+def test_a_growing_pool_leaves_few_scan_buffers_behind():
+    """40 compactions of 200K to 400K slots need up to 6.5 MB of scan room each, 196 MB if each growth kept its own."""
+    top = 400000
+    pool = torch.zeros((1, top, 1, 16, D), dtype=torch.bfloat16, device="cuda")
+    ref, out, smap = (torch.zeros(top, dtype=torch.int32, device="cuda") for _ in range(3))
+    mv = torch.zeros(2, dtype=torch.int32, device="cuda")
+    ctx = sa.Context(0)
+    sa.sa_kv_compact(ctx, lay((1, 1), 16, 1000), pool, pool, 500, ref, out, None, None, smap, mv)
+    torch.cuda.synchronize()
+    free = torch.cuda.mem_get_info()[0]
+    for slots in range(200000, top, 5000):
+        sa.sa_kv_compact(ctx, lay((1, 1), 16, slots), pool, pool, slots // 2, ref, out, None, None, smap, mv)
+    sa.sa_sync_check(ctx)
+    assert free - torch.cuda.mem_get_info()[0] < 32 << 20
