@@ -165,7 +165,10 @@ sa_status sa_attn_plan_stats(const sa_layout *layout, int32_t batch, const int32
                              const int32_t *h_kv_len, int32_t num_cu, int64_t *out);
 
 /* Wait for `stream`, then report SA_ERR_RANGE if any kernel of this context
- * met an out-of-range page id or slot since the last check (and clear it), or
+ * met an out-of-range page id or slot, or a slot's count that does not fit the
+ * tables, since the last check (and clear it; the message says which and ends
+ * with the flags: 1 an attention, 2 an append, 4 a splice, fork, count or
+ * compaction, 8 a count), or
  * SA_ERR_OVERLAP if launches split by key range overlapped against the rules
  * above and left the context's arrival counters off (and clear them; only then,
  * or while a launch of the context still runs on another stream, it also waits

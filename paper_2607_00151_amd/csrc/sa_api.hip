@@ -564,11 +564,14 @@ sa_status sa_sync_check(sa_ctx* ctx, void* stream) {
     }
   }
   if (w[0]) SA_HIP(hipMemset(ctx->d_err, 0, sizeof(int32_t)));
+  const bool pages = w[0] & ~sa::kCountError, counts = w[0] & sa::kCountError;
+  const std::string met = std::string(pages ? "an out-of-range page id or slot" : "") + (pages && counts ? " and " : "") +
+                          (counts ? "a slot's count that does not fit the tables" : "");
   if (off)
     return fail(SA_ERR_OVERLAP, "launches split by key range overlapped on this context (or in the allocation-free "
-                "call's scratch): outputs since the last check may be wrong; its arrival counters are cleared%s",
-                w[0] ? "; a kernel also met an out-of-range page id or slot" : "");
-  if (w[0]) return fail(SA_ERR_RANGE, "a kernel met an out-of-range page id or slot (flags 0x%x)", w[0]);
+                "call's scratch): outputs since the last check may be wrong; its arrival counters are cleared%s%s",
+                w[0] ? "; a kernel also met " : "", met.c_str());
+  if (w[0]) return fail(SA_ERR_RANGE, "a kernel met %s (flags 0x%x)", met.c_str(), w[0]);
   return SA_OK;
 }
 

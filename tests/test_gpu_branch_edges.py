@@ -190,3 +190,15 @@ def test_a_growing_pool_leaves_few_scan_buffers_behind():
         sa.sa_kv_compact(ctx, lay((1, 1), 16, slots), pool, pool, slots // 2, ref, out, None, None, smap, mv)
     sa.sa_sync_check(ctx)
     assert free - torch.cuda.mem_get_info()[0] < 32 << 20
+
+
+def test_the_check_says_what_a_kernel_met():
+    L, ctx = lay((2, 2), 16, 8), sa.Context(0)
+    ref = torch.zeros(8, dtype=torch.int32, device="cuda")
+    page, count = "an out-of-range page id or slot", "a slot's count that does not fit the tables"
+    for slots, met in (([2], count), ([8], page), ([8, 2], f"{page} and {count}")):
+        sa.sa_kv_release(ctx, L, dev([0, len(slots)]), dev(slots), ref)
+        with pytest.raises(sa.SaError, match=rf"SA_ERR_RANGE: a kernel met {met} \(flags"):
+            sa.sa_sync_check(ctx)
+        sa.sa_sync_check(ctx)
+    assert not ref.any()
