@@ -279,10 +279,13 @@ __global__ __launch_bounds__(kScanThreads) void free_list_kernel(FreeArgs a) {
 }
 
 // A small pool's whole release in one block: its entries lower the counts, and
-// once the atomics have returned the block lists the slots.  1020 entries and 1295
-// slots: 6.6 us against 2.1 and 3.6 in two launches, and a fork with its release
-// 13.8 against 15.7, the host's work of a launch less.
-constexpr int64_t kOneBlockEntries = 4096;
+// once the atomics have returned the block lists the slots.  What it saves is the
+// host's work of a launch; each thread's atomics follow one another, so it is for
+// few entries.  A call of it and of the two launches, us, 1295 slots: 16 entries
+// 6.5 and 8.9, 1020 7.7 and 9.1, 2048 8.9 and 9.1, 4096 11.8 and 9.2; 4096 slots:
+// 6.4 and 9.0, 8.3 and 9.2, 9.7 and 9.1, 13.0 and 9.1.  (Replayed from a graph, which
+// has no host's work to save, it takes 5.6 and 5.3, 7.5 and 6.1 at 1295 slots.)
+constexpr int64_t kOneBlockEntries = 1536;
 
 __global__ __launch_bounds__(kScanThreads) void release_small_kernel(CountArgs c, FreeArgs a) {
   __shared__ ScanRoom room;

@@ -9,7 +9,8 @@ import pytest
 import torch
 
 import paper_2607_00151_amd as sa
-from test_gpu_branches import D, anchor, branch_batch, check_attention, dev, lay, pool_bits, run_shared
+from test_gpu_branches import (D, anchor, bits, branch_batch, check_attention, compact_reference, dev, lay, pool_bits,
+                               run_shared)
 
 pytestmark = pytest.mark.gpu
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -100,7 +101,8 @@ import sys
 sys.path.insert(0, {root!r}); sys.path.insert(0, {tests!r})
 import numpy as np, torch
 import paper_2607_00151_amd as sa
-from test_gpu_branches import D, anchor, branch_batch, check_attention, dev, lay, pool_bits, run_shared
+from test_gpu_branches import (D, anchor, bits, branch_batch, check_attention, compact_reference, dev, lay, pool_bits,
+                               run_shared)
 for heads, groups in (((8, 1), [(9000, [(5, 1), (40, 1)])]), ((4, 1), [(256, [(200, 150)])])):
     w = branch_batch(np.random.default_rng(5), heads, 16, groups)
     w["q"][0, 3, 17] = float("nan")
@@ -202,3 +204,47 @@ def test_the_check_says_what_a_kernel_met():
             sa.sa_sync_check(ctx)
         sa.sa_sync_check(ctx)
     assert not ref.any()
+
+
+# ------------------------------------------------------------------------- the edges of the slot scans
+
+@pytest.mark.parametrize("slots,entries", [(4095, 0), (4096, 1), (4097, 3), (8192, 5000), (8193, 700), (4096, 1535),
+                                           (4096, 1536), (4096, 1537), (4095, 4096), (4096, 4097), (4097, 1536),
+                                           (70000, 30000), (1, 2), (513, 1536)])
+def test_release_at_the_edges_of_the_scans(slots, entries):
+    """Counts lowered and listed in one launch or several, chunks of 4096 slots: twice, the second one to nothing."""
+    r = np.random.default_rng(slots + entries)
+    L, ctx = lay((1, 1), 16, slots), sa.Context(0)
+    table = r.integers(0, slots, entries)
+    table[:entries // 2] = np.sort(table[:entries // 2])                 # neighbours and strangers
+    count = 2 * np.bincount(table, minlength=slots) + (r.random(slots) < 0.2)
+    ref, free = dev(count), torch.full((slots,), -7, dtype=torch.int32, device="cuda")
+    nfree = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ip, ix = dev([0, entries // 3, entries]), dev(table)
+    for _ in range(2):
+        count = count - np.bincount(table, minlength=slots)
+        sa.sa_kv_release(ctx, L, ip, ix, ref, free, nfree)
+        sa.sa_sync_check(ctx)
+        np.testing.assert_array_equal(ref.cpu(), count)
+        idle = np.flatnonzero(count == 0)
+        assert int(nfree) == len(idle)
+        np.testing.assert_array_equal(free.cpu(), np.concatenate([idle, np.full(slots - len(idle), -1)]))
+
+
+@pytest.mark.parametrize("slots,limit", [(4095, 2000), (4096, 4095), (4097, 4096), (4097, 1), (8192, 4096), (8193, 4097),
+                                         (12289, 8192)])
+def test_compaction_at_the_edges_of_the_scans(slots, limit):
+    r = np.random.default_rng(slots + limit)
+    L, ctx = lay((1, 1), 16, slots), sa.Context(0)
+    count = (r.random(slots) < 0.6) * r.integers(1, 4, slots)
+    table = np.repeat(np.arange(slots), count).astype(np.int32)
+    kp, vp = pool_bits(r, L), pool_bits(r, L)
+    to, after, wix, wk, moved = compact_reference(count, limit, table, bits(kp))
+    ref, ix = dev(count), dev(table)
+    smap, mv = torch.full_like(ref, -7), torch.full((2,), -7, dtype=torch.int32, device="cuda")
+    sa.sa_kv_compact(ctx, L, kp, vp, limit, ref, ref, ix, ix, smap, mv)
+    sa.sa_sync_check(ctx)
+    assert mv.tolist() == moved
+    for got, want in ((smap, to), (ref, after), (ix, wix)):
+        np.testing.assert_array_equal(got.cpu(), want)
+    np.testing.assert_array_equal(bits(kp), wk)
