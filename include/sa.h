@@ -66,7 +66,7 @@
  *     refuses, before launching, slots outside the pool or pages a sequence
  *     lacks (SA_ERR_RANGE), a free list that repeats a slot or hands out a
  *     surviving source slot, and two sequences writing the same row of a slot
- *     (SA_ERR_OVERLAP).
+ *     (SA_ERR_OVERLAP); every fork and shared-prefix attention likewise (see there).
  *   - Plan buffers grow on demand (hipMalloc) and an outgrown one is kept
  *     until sa_destroy, since kernels already enqueued may still read it; no
  *     call synchronises the device.  sa_reserve sizes them ahead of time.
@@ -630,7 +630,11 @@ sa_status sa_kv_compact(sa_ctx *ctx, const sa_layout *layout, void *k_pool, void
  * result is that of sa_segment_prefill_attn over the same tables, held to the
  * same tolerance (and, as there, an infinite or NaN value row of the segment
  * reaches the earlier rows of its own 64-key tile).  shared_len may be anything from 0 to the smallest
- * h_kv_len - h_q_len of the group.  Where the members' rows fill the kernel's
+ * h_kv_len - h_q_len of the group.  A shared_len beyond what the members have in
+ * common gives the later members wrong results; with SA_DEBUG=1 the call refuses it
+ * (SA_ERR_SHAPE), comparing the pages that are not the same slots bit for bit, and
+ * pages of the shared part that a table lacks or that lie outside the pool
+ * (SA_ERR_RANGE).  Where the members' rows fill the kernel's
  * row tiles anyway (long segments) the group is computed member by member, and a
  * batch that would gain nothing goes to the segment attention's launch.  The
  * softmax scale is always applied exactly; SA_ATTN_VARIANT and the block clock

@@ -149,6 +149,40 @@ inline sa_status check_groups(int32_t batch, const int32_t* h_q_len, const int32
   return SA_OK;
 }
 
+// SA_DEBUG check of the groups against a host copy of the page table: every page
+// of a shared prefix in range in the tables of all members with query rows.  Where
+// a member lists another slot than the member whose pages are read, `differ` names
+// both, whose first `rows` rows have to be equal copies.
+struct SharedCopy {
+  int32_t group, seq, of, page, slot, of_slot, rows;     // page of sequence seq, and of sequence `of`
+};
+
+inline sa_status debug_check_shared(int32_t num_groups, const int32_t* h_group_indptr, const int32_t* h_shared_len,
+                                    const int32_t* h_q_len, const int32_t* indptr, const int32_t* indices, int P,
+                                    int64_t num_slots, std::vector<SharedCopy>& differ, std::string& err) {
+  differ.clear();
+  for (int g = 0; g < num_groups; ++g) {
+    const int32_t S = h_shared_len[g];
+    const int64_t pages = ((int64_t)S + P - 1) / P;
+    int first = -1;
+    for (int b = h_group_indptr[g]; b < h_group_indptr[g + 1]; ++b) {
+      if (h_q_len[b] == 0) continue;
+      if (first < 0) first = b;
+      if (pages > indptr[b + 1] - indptr[b])
+        return plan_fail(err, SA_ERR_RANGE, "sequence %d: its table has %d of the %lld pages that group %d shares", b,
+                         indptr[b + 1] - indptr[b], (long long)pages, g);
+      for (int32_t j = 0; j < pages; ++j) {
+        const int32_t slot = indices[indptr[b] + j], of = indices[indptr[first] + j];
+        if (slot < 0 || slot >= num_slots)
+          return plan_fail(err, SA_ERR_RANGE, "sequence %d: page %d has slot %d outside [0, %lld)", b, j, slot,
+                           (long long)num_slots);
+        if (slot != of) differ.push_back({g, b, first, j, slot, of, std::min<int32_t>(P, S - j * P)});
+      }
+    }
+  }
+  return SA_OK;
+}
+
 // Row tiles of one KV head that the choice of a chunk need not tell apart.
 struct SharedShape {
   int64_t tiles;             // 64-key tiles of each

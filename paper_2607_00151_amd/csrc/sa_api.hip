@@ -1703,6 +1703,32 @@ void launch_shared(bool pool_rsrc, dim3 grid, hipStream_t st, const hipEvent_t* 
   else launch_timed(sa::attn_shared_kernel<P, false>, grid, dim3(256), st, ev, a);
 }
 
+// SA_DEBUG: what a group is said to share is the same in all of its members' caches, bit for bit.
+sa_status debug_shared(const sa_layout* layout, int32_t layer, const void* k_pool, const void* v_pool, int32_t batch,
+                       const int32_t* h_q_len, sa_pages pages, int32_t num_groups, const int32_t* h_group_indptr,
+                       const int32_t* h_shared_len, hipStream_t stream) {
+  std::vector<int32_t> ip, ix;
+  sa_status s = fetch_table(pages.indptr, pages.indices, batch, stream, ip, ix);
+  if (s != SA_OK) return s;
+  std::vector<sa::SharedCopy> differ;
+  s = sa::debug_check_shared(num_groups, h_group_indptr, h_shared_len, h_q_len, ip.data(), ix.data(), layout->page_size,
+                             layout->num_slots, differ, g_err);
+  if (s != SA_OK) return s;
+  const size_t n = (size_t)slot_elems(layout), head = (size_t)layout->page_size * sa::kHD;
+  std::vector<uint16_t> a(n), b(n);
+  for (const sa::SharedCopy& c : differ)
+    for (const void* pool : {k_pool, v_pool}) {
+      const uint16_t* const base = (const uint16_t*)pool + (int64_t)layer * layer_elems(layout);
+      SA_HIP(hipMemcpy(a.data(), base + c.slot * (int64_t)n, 2 * n, hipMemcpyDeviceToHost));
+      SA_HIP(hipMemcpy(b.data(), base + c.of_slot * (int64_t)n, 2 * n, hipMemcpyDeviceToHost));
+      for (int h = 0; h < layout->num_kv_heads; ++h)
+        if (memcmp(a.data() + h * head, b.data() + h * head, (size_t)c.rows * sa::kHD * 2) != 0)
+          return fail(SA_ERR_SHAPE, "group %d: shared_len %d, but sequences %d and %d differ on page %d", c.group,
+                      h_shared_len[c.group], c.of, c.seq, c.page);
+    }
+  return SA_OK;
+}
+
 sa_status shared_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const void* q, const void* k_pool,
                       const void* v_pool, int32_t batch, const int32_t* h_q_len, const int32_t* h_kv_len,
                       sa_pages pages, int32_t num_groups, const int32_t* h_group_indptr, const int32_t* h_shared_len,
@@ -1747,6 +1773,11 @@ sa_status shared_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   if (rec.total_q == 0) return SA_OK;
   s = refuse_capture((hipStream_t)stream, "sa_shared_prefix_attn keeps its plan in the context and");
   if (s != SA_OK) return s;
+  if (debug_checks()) {
+    s = debug_shared(layout, layer, k_pool, v_pool, batch, h_q_len, pages, num_groups, h_group_indptr, h_shared_len,
+                     (hipStream_t)stream);
+    if (s != SA_OK) return s;
+  }
   sa::SharedPlan plan;
   uint8_t* dev = ctx->plans[kPlanShared].dev;
   if (!same) {

@@ -248,3 +248,49 @@ def test_compaction_at_the_edges_of_the_scans(slots, limit):
     for got, want in ((smap, to), (ref, after), (ix, wix)):
         np.testing.assert_array_equal(got.cpu(), want)
     np.testing.assert_array_equal(bits(kp), wk)
+
+
+DEBUG = r"""
+import sys
+sys.path.insert(0, {root!r}); sys.path.insert(0, {tests!r})
+import numpy as np, torch
+import paper_2607_00151_amd as sa
+from test_gpu_branches import D, anchor, branch_batch, check_attention, run_shared
+w = branch_batch(np.random.default_rng(1), (8, 2), 16, [(203, [(9, 1), (30, 1), (12, 0), (40, 2)]), anchor((8, 2))], layers=2, layer=1)
+ctx = sa.Context(0)
+for _ in range(2):                                                 # the copied partial pages are equal
+    check_attention(w, *run_shared(ctx, w), D ** -0.5)
+
+def refused(w, status, text):
+    try:
+        run_shared(ctx, w)
+    except sa.SaError as e:
+        assert e.name == status and text in str(e), e
+        return
+    raise AssertionError("not refused: " + text)
+
+g = w["shared"]
+refused(dict(w, shared=[204] + g[1:]), "SA_ERR_SHAPE", "sequences 0 and 1 differ on page 12")    # one token too far
+run_shared(ctx, dict(w, shared=[192] + g[1:]))
+at = int(w["indptr"][1]) + 12
+keep, n = int(w["indices"][at]), w["L"].num_slots
+w["indices"][at] = n
+refused(w, "SA_ERR_RANGE", "outside [0, %d)" % n)
+w["indices"][at] = keep
+bits = w["vp"][1, keep, 1, 10]
+bits[127] ^= 1                                                    # the last shared row of a copy, one bit of one value
+refused(w, "SA_ERR_SHAPE", "sequences 0 and 1 differ on page 12")
+bits[127] ^= 1
+w["vp"][1, keep, 1, 11, 127] ^= 1                                   # the row behind it is the member's own
+run_shared(ctx, w)
+print("debug shared checks ok", flush=True)
+"""
+
+
+@pytest.mark.timeout(200)
+def test_debug_checks_of_shared_prefixes():
+    code = DEBUG.format(root=ROOT, tests=os.path.join(ROOT, "tests"))
+    r = subprocess.run([sys.executable, "-u", "-c", code], env=dict(os.environ, SA_DEBUG="1"), capture_output=True,
+                       text=True, timeout=150)
+    print(r.stdout[-2000:], r.stderr[-3000:])
+    assert r.returncode == 0 and "debug shared checks ok" in r.stdout
