@@ -652,6 +652,23 @@ sa_status sa_shared_prefix_attn(sa_ctx *ctx, const sa_layout *layout, int32_t la
                                 const int32_t *h_shared_len, float softmax_scale, void *o, float *lse,
                                 void *stream);
 
+/*
+ * sa_shared_plan_stats — what sa_shared_prefix_attn would make of these lengths
+ * on a GPU with num_cu compute units (host only: no context, no GPU).  out[0]:
+ * groups whose prefix is computed once for their members (0: the batch goes to
+ * the segment attention's launch, and the other numbers are 0); out[1]:
+ * workgroups; out[2]: rows of partial results, 516 bytes each; out[3]: the most
+ * parts that a row is joined from; out[4]: 1 if the prefix parts are of two
+ * lengths with the members' own workgroups between them.  h_once (nullable,
+ * [num_groups]): 1 for each group whose prefix is computed once, else 0.
+ * Errors: those of sa_shared_prefix_attn's shape checks; SA_ERR_NULL for a NULL
+ * out; SA_ERR_SHAPE for num_cu < 1.
+ */
+sa_status sa_shared_plan_stats(const sa_layout *layout, int32_t batch, const int32_t *h_q_len,
+                               const int32_t *h_kv_len, int32_t num_groups,
+                               const int32_t *h_group_indptr, const int32_t *h_shared_len,
+                               int32_t num_cu, int64_t *out, int32_t *h_once);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,7 +18,7 @@ __all__ = [
     "sa_segment_prefill_attn", "sa_segment_prefill_attn_append", "sa_set_exact_scale", "sa_set_fused_append",
     "sa_set_kernel_events", "sa_set_block_clock", "sa_set_xcd_weights", "sa_sync_check", "sa_reserve",
     "sa_segment_prefill_attn_noalloc", "sa_attn_plan_stats", "Rope", "sa_kv_append_rope", "sa_kv_fork",
-    "sa_kv_retain", "sa_kv_release", "sa_kv_compact", "sa_shared_prefix_attn", "EXPORTED_SYMBOLS",
+    "sa_kv_retain", "sa_kv_release", "sa_kv_compact", "sa_shared_prefix_attn", "sa_shared_plan_stats", "EXPORTED_SYMBOLS",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -31,7 +31,8 @@ EXPORTED_SYMBOLS = ("sa_create", "sa_destroy", "sa_status_string", "sa_last_erro
                     "sa_set_exact_scale", "sa_set_fused_append", "sa_set_kernel_events",
                     "sa_set_block_clock", "sa_set_xcd_weights", "sa_reserve",
                     "sa_segment_prefill_attn_noalloc", "sa_attn_plan_stats", "sa_kv_append_rope",
-                    "sa_kv_fork", "sa_kv_retain", "sa_kv_release", "sa_kv_compact", "sa_shared_prefix_attn")
+                    "sa_kv_fork", "sa_kv_retain", "sa_kv_release", "sa_kv_compact", "sa_shared_prefix_attn",
+                    "sa_shared_plan_stats")
 
 STATUS = {0: "SA_OK", 1: "SA_ERR_NULL", 2: "SA_ERR_SHAPE", 3: "SA_ERR_UNSUPPORTED",
           4: "SA_ERR_ALIGN", 5: "SA_ERR_RANGE", 6: "SA_ERR_NO_PAGES", 7: "SA_ERR_HIP",
@@ -108,12 +109,14 @@ def load_library():
     lib.sa_kv_release.argtypes = [P, LP, I32, _Pages, I64, P, P, P, P]
     lib.sa_kv_compact.argtypes = [P, LP, P, P, I32, P, P, P, P, I64, P, P, P]
     lib.sa_shared_prefix_attn.argtypes = [P, LP, I32, P, P, P, I32, P, P, _Pages, I32, P, P, ctypes.c_float, P, P, P]
+    lib.sa_shared_plan_stats.argtypes = [LP, I32, P, P, I32, P, P, I32, P, P]
     for name in ("sa_create", "sa_sync_check", "sa_kv_append", "sa_kv_assemble", "sa_kv_assemble_append",
                  "sa_kv_splice_alias", "sa_segment_prefill_attn", "sa_segment_prefill_attn_append",
                  "sa_set_exact_scale", "sa_set_fused_append", "sa_set_kernel_events", "sa_set_block_clock",
                  "sa_set_xcd_weights",
                  "sa_reserve", "sa_segment_prefill_attn_noalloc", "sa_attn_plan_stats", "sa_kv_append_rope",
-                 "sa_kv_fork", "sa_kv_retain", "sa_kv_release", "sa_kv_compact", "sa_shared_prefix_attn"):
+                 "sa_kv_fork", "sa_kv_retain", "sa_kv_release", "sa_kv_compact", "sa_shared_prefix_attn",
+                 "sa_shared_plan_stats"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -654,3 +657,21 @@ def sa_shared_prefix_attn(ctx, layout: Layout, layer: int, q, k_pool, v_pool, q_
         _table_on(pages_indptr, pages_indices, B, at, "page table"), len(shared), _ptr(groups), _ptr(shared),
         float(softmax_scale), _on(o, "o", "bf16", rows * layout.head_dim, at, T == 0),
         None if lse is None else _on(lse, "lse", "f32", rows, at), _stream_of(ctx, stream)))
+
+
+def sa_shared_plan_stats(layout: Layout, q_len, kv_len, group_indptr, shared_len, num_cu: int = 256) -> dict:
+    """What sa_shared_prefix_attn would make of these lengths (host only, no GPU): which groups' prefixes are computed
+    once (none: the batch goes to the segment attention), workgroups, rows of partial results, most parts of a row, and
+    whether prefix parts of two lengths enclose the members' own workgroups."""
+    q_len, kv_len = _host_i32(q_len), _host_i32(kv_len)
+    groups, shared = _host_i32(group_indptr), _host_i32(shared_len)
+    if q_len.shape != kv_len.shape:
+        raise ValueError("q_len and kv_len differ in length")
+    if len(groups) != len(shared) + 1:
+        raise ValueError("group_indptr must have one entry more than shared_len")
+    out, once = np.zeros(5, dtype=np.int64), np.zeros(len(shared), dtype=np.int32)
+    _check(load_library().sa_shared_plan_stats(
+        ctypes.byref(layout), len(q_len), _ptr(q_len), _ptr(kv_len), len(shared), _ptr(groups), _ptr(shared),
+        int(num_cu), out.ctypes.data, once.ctypes.data))
+    return {"once": [bool(x) for x in once], "items": int(out[1]), "part_rows": int(out[2]), "most_parts": int(out[3]),
+            "ahead": bool(out[4])}

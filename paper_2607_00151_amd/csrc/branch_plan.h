@@ -124,6 +124,8 @@ inline int merge_block_rows(int most_parts) { return most_parts <= 8 ? 8 : most_
 // part of an item: the row its partial starts at among all partials (-1: none)
 struct SharedPlan {
   bool shared = false;                 // some group's prefix is computed once for its members
+  bool ahead = false;                  // prefix parts of two lengths, the members' own blocks between them
+  std::vector<uint8_t> once;           // per group: its prefix is computed once (where shared)
   std::vector<AttnItem> items;         // one per workgroup, in launch order
   std::vector<MergeUnit> units;
   int64_t part_rows = 0;               // rows of all partials
@@ -299,6 +301,7 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
   };
   std::vector<Member> members;
   bool any = false;
+  out.once.assign((size_t)num_groups, 0);
   for (int g = 0; g < num_groups; ++g) {
     const int b0 = h_group_indptr[g], b1 = h_group_indptr[g + 1];
     int64_t rows = 0, apart = 0, active = 0;
@@ -326,6 +329,7 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
     const int32_t prefix0 = shared ? (int32_t)tiles.size() : -1;
     if (shared) {
       any = true;
+      out.once[g] = 1;
       const int32_t q_len = (int32_t)(rows / G);
       for (int64_t r0 = 0; r0 < rows; r0 += kRows)
         tiles.push_back({first, (int32_t)r0, (int32_t)std::min<int64_t>(kRows, rows - r0), seqs[first].q_start, q_len,
@@ -404,6 +408,7 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
   // of 16 to 64 tokens on 16K 184, 193, 183.
   const bool fit = best.compute && prefix_blocks > num_cu && prefix_blocks <= 2 * num_cu && fill > 0;
   const double ahead = fit ? fill / 127.0 / num_cu : 0.0;
+  out.ahead = fit;
   auto part_begin = [&](const Tile& t, int k) {                 // in tiles from t.k0
     const int64_t n = t.tiles();
     const int n_long = t.prefix && fit ? (int)((int64_t)t.parts * num_cu / prefix_blocks) : 0;

@@ -1913,4 +1913,32 @@ sa_status sa_shared_prefix_attn(sa_ctx* ctx, const sa_layout* layout, int32_t la
   });
 }
 
+sa_status sa_shared_plan_stats(const sa_layout* layout, int32_t batch, const int32_t* h_q_len, const int32_t* h_kv_len,
+                               int32_t num_groups, const int32_t* h_group_indptr, const int32_t* h_shared_len,
+                               int32_t num_cu, int64_t* out, int32_t* h_once) {
+  return no_throw([&] {
+    std::vector<sa::SeqDesc> seqs;
+    int64_t total_q = 0;
+    sa_status s = check_sizes(layout);
+    if (s != SA_OK) return s;
+    s = sa::plan_attn_check(layout, 0, batch, h_q_len, h_kv_len, 1.f, seqs, total_q, g_err);
+    if (s != SA_OK) return s;
+    s = sa::check_groups(batch, h_q_len, h_kv_len, num_groups, h_group_indptr, h_shared_len, g_err);
+    if (s != SA_OK) return s;
+    if (!out) return fail(SA_ERR_NULL, "out is NULL");
+    if (num_cu < 1) return fail(SA_ERR_SHAPE, "num_cu %d < 1", num_cu);
+    sa::SharedPlan plan;
+    sa::plan_shared_items(layout, seqs, num_groups, h_group_indptr, h_shared_len, num_cu, plan);
+    out[0] = plan.shared ? std::count(plan.once.begin(), plan.once.end(), 1) : 0;
+    out[1] = std::count_if(plan.items.begin(), plan.items.end(),
+                           [](const sa::AttnItem& it) { return it.kv_begin < it.kv_end; });
+    out[2] = plan.part_rows;
+    out[3] = plan.most_parts;
+    out[4] = plan.ahead;
+    if (h_once != nullptr)
+      for (int g = 0; g < num_groups; ++g) h_once[g] = plan.shared && plan.once[g];
+    return SA_OK;
+  });
+}
+
 }  // extern "C"
