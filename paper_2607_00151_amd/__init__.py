@@ -544,13 +544,21 @@ class Rope:
 
     def __init__(self, inv_freq=(), q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
                  weight_offset: float = 0.0):
-        self.inv_freq = np.ascontiguousarray(inv_freq, dtype=np.float64).reshape(-1)
+        self.inv_freq = inv_freq
         self.q_weight, self.k_weight = q_weight, k_weight
         self.eps, self.interleaved, self.weight_offset = float(eps), bool(interleaved), float(weight_offset)
 
+    @property
+    def inv_freq(self):
+        return self._inv_freq
+
+    @inv_freq.setter
+    def inv_freq(self, value):                 # read as doubles by every call, whatever it is set from
+        self._inv_freq = np.ascontiguousarray(value, dtype=np.float64).reshape(-1)
+
     def _struct(self, d: int, device):
-        n = len(self.inv_freq)
-        return _Rope(2 * n, self.interleaved, _ptr(self.inv_freq) if n else None,
+        n = len(self._inv_freq)
+        return _Rope(2 * n, self.interleaved, _ptr(self._inv_freq) if n else None,
                      None if self.q_weight is None else _on(self.q_weight, "q_weight", "bf16", d, device),
                      None if self.k_weight is None else _on(self.k_weight, "k_weight", "bf16", d, device), self.eps,
                      self.weight_offset)

@@ -36,3 +36,12 @@ def test_plan_stats_refusals(lib):  # noqa: F811
     assert go(q=[11, 1]) == SHAPE and go(L=layout(head_dim=64)) == UNSUPPORTED
     with pytest.raises(ValueError, match="one entry more"):
         sa.sa_shared_plan_stats(layout(), [1], [4], [0, 1], [0, 0])
+
+
+@pytest.mark.parametrize("value", [np.float32([1, 0.5, 0.25] * 8), [1.0] * 16, np.arange(32.0)[::2], np.float32(1)])
+def test_rope_frequencies_may_be_set_from_any_array(value):
+    rope = sa.Rope(np.ones(64))
+    rope.inv_freq = value
+    s, want = rope._struct(128, None), np.float64(value).reshape(-1)
+    assert s.rot_dim == 2 * len(want)
+    np.testing.assert_array_equal((ctypes.c_double * len(want)).from_address(s.h_inv_freq), want)
