@@ -307,7 +307,11 @@ sa_status sa_kv_splice_alias(sa_ctx *ctx, const sa_layout *layout, int32_t batch
  * multiplies each query row by softmax_scale * log2(e) once and rounds it to
  * bf16 (faster; moves a row's scaled scores by up to
  * 2^-8 * sum_d |scale log2(e) q_d k_d| in log2 units).  A row that meets a
- * score of +infinity or NaN has a NaN output and a NaN LSE.
+ * score of +infinity or NaN has a NaN output and a NaN LSE.  A masked key's
+ * probability is 0 and its value is multiplied by that: an infinite or NaN value
+ * of a segment's token reaches, besides the rows that see it, the earlier rows of
+ * the segment in its work item (128 packed rows, num_q_heads / num_kv_heads to a
+ * token), and no others.
  *
  * Errors: SA_ERR_SHAPE (0 <= q_len <= kv_len violated, bad batch or layer,
  * softmax_scale not finite and positive),
@@ -626,17 +630,20 @@ sa_status sa_kv_compact(sa_ctx *ctx, const sa_layout *layout, void *k_pool, void
  * may have one member or none).  The caches of a group's members hold the same
  * keys and values for their first h_shared_len[g] tokens (the same pages, as
  * sa_kv_fork leaves them, or equal copies): whole 64-key tiles of them are read
- * through the page list of the group's first member that has query rows.  The
- * result is that of sa_segment_prefill_attn over the same tables, held to the
- * same tolerance (and, as there, an infinite or NaN value row of the segment
- * reaches the earlier rows of its own 64-key tile).  shared_len may be anything from 0 to the smallest
- * h_kv_len - h_q_len of the group.  A shared_len beyond what the members have in
- * common gives the later members wrong results; with SA_DEBUG=1 the call refuses it
- * (SA_ERR_SHAPE), comparing the pages that are not the same slots bit for bit, and
- * pages of the shared part that a table lacks or that lie outside the pool
- * (SA_ERR_RANGE).  Where the members' rows fill the kernel's
- * row tiles anyway (long segments) the group is computed member by member, and a
- * batch that would gain nothing goes to the segment attention's launch.  The
+ * through the page list of the group's first member that has query rows.
+ * shared_len may be anything from 0 to the smallest h_kv_len - h_q_len of the
+ * group.  One beyond what the members have in common gives the later members
+ * wrong results; with SA_DEBUG=1 the call refuses it (SA_ERR_SHAPE), comparing
+ * the pages that are not the same slots bit for bit, and pages of the shared
+ * part that a table lacks or that lie outside the pool (SA_ERR_RANGE).
+ *
+ * The result is that of sa_segment_prefill_attn over the same tables, held to
+ * the same tolerance: probabilities are rounded to bf16 before the PV product,
+ * and parts are joined in fp32.  Scores and values that are not finite do what
+ * they do there; those of one member's own tokens do not reach the others.
+ * Where the members' rows fill the kernel's row tiles anyway (long segments)
+ * the group is computed member by member, and a batch that would gain nothing
+ * goes to the segment attention's launch (sa_shared_plan_stats tells).  The
  * softmax scale is always applied exactly; SA_ATTN_VARIANT and the block clock
  * apply only to such batches.  sa_set_kernel_events times the first kernel
  * (SA_TIMED_ATTN), and the partial results (516 bytes per query row, head and

@@ -345,3 +345,21 @@ def test_shared_prefix_attention_on_every_path(i):
     sa.sa_sync_check(ctx)
     check_attention(w, o2, lse2, D ** -0.5)
     assert torch.equal(o, o2) == (not any(once))         # not any: the segment attention's own launch
+
+
+@pytest.mark.parametrize("heads,q,anchored", [((4, 1), 150, False), ((32, 8), 64, True), ((8, 2), 150, True)])
+def test_a_masked_value_that_is_not_finite_stays_in_its_work_item(heads, q, anchored):
+    """The last token's value: the rows of the work items before its own are the same bits."""
+    G, page = heads[0] // heads[1], 16
+    groups = [(320, [(q + 7, q), (q, q)])] + ([anchor(heads)] if anchored else [])
+    w = branch_batch(np.random.default_rng(q), heads, page, groups)
+    ctx = sa.Context(0)
+    o, lse = (x.clone() for x in run_shared(ctx, w))
+    at = w["kv_len"][1] - 1
+    slot = int(w["indices"][int(w["indptr"][1]) + at // page])
+    w["vp"].view(torch.bfloat16)[0, slot, :, at % page, 64] = float("nan")
+    o2, lse2 = run_shared(ctx, w)
+    first = (q * G - 1) // 128 * 128                                     # packed row of the last work item
+    whole = q + first // G                                               # tokens of the call that are before it
+    assert first > 0 and o2[2 * q - 1, :, 64].isnan().all()
+    assert same_bits(o[:whole], o2[:whole]) and same_bits(o[2 * q:], o2[2 * q:]) and same_bits(lse, lse2)
