@@ -665,9 +665,8 @@ sa_status sa_shared_prefix_attn(sa_ctx *ctx, const sa_layout *layout, int32_t la
  * groups whose prefix is computed once for their members (0: the batch goes to
  * the segment attention's launch, and the other numbers are 0); out[1]:
  * workgroups; out[2]: rows of partial results, 516 bytes each; out[3]: the most
- * parts that a row is joined from; out[4]: 1 if the prefix parts are of two
- * lengths with the members' own workgroups between them.  h_once (nullable,
- * [num_groups]): 1 for each group whose prefix is computed once, else 0.
+ * parts that a row is joined from.  h_once (nullable, [num_groups]): 1 for each
+ * group whose prefix is computed once, else 0.
  * Errors: those of sa_shared_prefix_attn's shape checks; SA_ERR_NULL for a NULL
  * out; SA_ERR_SHAPE for num_cu < 1.
  */

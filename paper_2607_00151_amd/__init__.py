@@ -669,17 +669,15 @@ def sa_shared_prefix_attn(ctx, layout: Layout, layer: int, q, k_pool, v_pool, q_
 
 def sa_shared_plan_stats(layout: Layout, q_len, kv_len, group_indptr, shared_len, num_cu: int = 256) -> dict:
     """What sa_shared_prefix_attn would make of these lengths (host only, no GPU): which groups' prefixes are computed
-    once (none: the batch goes to the segment attention), workgroups, rows of partial results, most parts of a row, and
-    whether prefix parts of two lengths enclose the members' own workgroups."""
+    once (none: the batch goes to the segment attention), workgroups, rows of partial results, most parts of a row."""
     q_len, kv_len = _host_i32(q_len), _host_i32(kv_len)
     groups, shared = _host_i32(group_indptr), _host_i32(shared_len)
     if q_len.shape != kv_len.shape:
         raise ValueError("q_len and kv_len differ in length")
     if len(groups) != len(shared) + 1:
         raise ValueError("group_indptr must have one entry more than shared_len")
-    out, once = np.zeros(5, dtype=np.int64), np.zeros(len(shared), dtype=np.int32)
+    out, once = np.zeros(4, dtype=np.int64), np.zeros(len(shared), dtype=np.int32)
     _check(load_library().sa_shared_plan_stats(
         ctypes.byref(layout), len(q_len), _ptr(q_len), _ptr(kv_len), len(shared), _ptr(groups), _ptr(shared),
         int(num_cu), out.ctypes.data, once.ctypes.data))
-    return {"once": [bool(x) for x in once], "items": int(out[1]), "part_rows": int(out[2]), "most_parts": int(out[3]),
-            "ahead": bool(out[4])}
+    return {"once": [bool(x) for x in once], "items": int(out[1]), "part_rows": int(out[2]), "most_parts": int(out[3])}

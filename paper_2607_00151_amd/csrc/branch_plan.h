@@ -124,7 +124,6 @@ inline int merge_block_rows(int most_parts) { return most_parts <= 8 ? 8 : most_
 // part of an item: the row its partial starts at among all partials (-1: none)
 struct SharedPlan {
   bool shared = false;                 // some group's prefix is computed once for its members
-  bool ahead = false;                  // prefix parts of two lengths, the members' own blocks between them
   std::vector<uint8_t> once;           // per group: its prefix is computed once (where shared)
   std::vector<AttnItem> items;         // one per workgroup, in launch order
   std::vector<MergeUnit> units;
@@ -193,11 +192,6 @@ struct SharedShape {
   int64_t count, rows;       // how many, and their packed rows in all
 };
 
-struct SharedCost {
-  int64_t total;             // units of 10 ns
-  bool compute;              // bound by the blocks' work, not by the stream of keys
-};
-
 inline int64_t shared_parts(int64_t tiles, int64_t chunk) {
   return std::max<int64_t>(1, std::min<int64_t>((tiles + chunk - 1) / chunk, kMaxItemParts));
 }
@@ -208,7 +202,7 @@ inline int64_t shared_parts(int64_t tiles, int64_t chunk) {
 // its block 300; the keys stream at 54.6 per tile and 100 blocks (6 TB/s), with a
 // quarter of the shorter of work and stream not overlapping; the merge 530, and
 // 1032 bytes written and read per row and part at 9 TB/s.
-inline SharedCost shared_chunk_cost(const std::vector<SharedShape>& shapes, int Hkv, int num_cu, int64_t chunk) {
+inline int64_t shared_chunk_cost(const std::vector<SharedShape>& shapes, int Hkv, int num_cu, int64_t chunk) {
   struct Run {
     int64_t time, blocks;
   };
@@ -240,7 +234,7 @@ inline SharedCost shared_chunk_cost(const std::vector<SharedShape>& shapes, int 
   }
   busy = std::max(busy, sum / slots);
   const int64_t stream = streamed * 546 / 1000;
-  return {std::max(busy, stream) + std::min(busy, stream) / 4 + 530 + part_rows * 1032 / 90000, busy > stream};
+  return std::max(busy, stream) + std::min(busy, stream) / 4 + 530 + part_rows * 1032 / 90000;
 }
 
 // The same work by sa_segment_prefill_attn, every member over all of its keys:
@@ -363,27 +357,22 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
   std::vector<SharedShape> shapes;
   for (const auto& c : classes)
     shapes.push_back({std::get<0>(c.first), std::get<1>(c.first), std::get<2>(c.first), c.second.first, c.second.second});
-  SharedCost best{INT64_MAX, false};
+  int64_t best = INT64_MAX;
   int64_t chunk = longest;
   const int64_t most = std::min<int64_t>(64, (longest + 3) / 4);
   for (int64_t k = 1; k <= most; k += 1 + k / 8) {
     const int64_t c = std::min(std::max<int64_t>((longest + k - 1) / k, 4), longest);
-    const SharedCost t = shared_chunk_cost(shapes, Hkv, num_cu, c);
-    if (t.total < best.total) {
+    const int64_t t = shared_chunk_cost(shapes, Hkv, num_cu, c);
+    if (t < best) {
       best = t;
       chunk = c;
     }
   }
-  if (best.total >= segment_cost(seqs, G, Hkv, num_cu)) return;
+  if (best >= segment_cost(seqs, G, Hkv, num_cu)) return;
   out.shared = true;
 
-  int64_t rows_used = 0, prefix_blocks = 0, fill = 0;           // fill: time of the other blocks, 10 ns
-  for (Tile& t : tiles) {
-    t.parts = (int32_t)shared_parts(t.tiles(), chunk);
-    if (t.prefix) prefix_blocks += (int64_t)t.parts * Hkv;
-    else if ((int64_t)t.q_len * G <= kDecodeRows) fill += (t.tiles() * 220 + 100 * t.parts) * Hkv;
-    else fill += (t.tiles() * 200 + 400 * t.parts) * Hkv;
-  }
+  int64_t rows_used = 0;
+  for (Tile& t : tiles) t.parts = (int32_t)shared_parts(t.tiles(), chunk);
   auto place = [&](Tile& t) {
     t.place = rows_used;
     rows_used += (int64_t)t.parts * Hkv * t.rows;
@@ -398,27 +387,13 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
   out.part_rows = rows_used;
   if (rows_used > kMaxPartRows) return;                         // refused by the caller
 
-  // Bound by work, with more prefix parts than CUs but at most two for each: every
-  // CU starts with one part, the members' own blocks fill its other slot, and the
-  // CU's second part follows them.  The parts of the first kind are then longer
-  // than those of the second by the tiles they are ahead, so that both end
-  // together.  (Beside a prefix part a block of few rows takes 2.2 us a tile,
-  // another own block 2.)  64 branches of 64K, 64/8 heads, the call in us: all
-  // blocks by length 178, in this order with equal parts 181, this 163; 16 segments
-  // of 16 to 64 tokens on 16K 184, 193, 183.
-  const bool fit = best.compute && prefix_blocks > num_cu && prefix_blocks <= 2 * num_cu && fill > 0;
-  const double ahead = fit ? fill / 127.0 / num_cu : 0.0;
-  out.ahead = fit;
-  auto part_begin = [&](const Tile& t, int k) {                 // in tiles from t.k0
-    const int64_t n = t.tiles();
-    const int n_long = t.prefix && fit ? (int)((int64_t)t.parts * num_cu / prefix_blocks) : 0;
-    if (n_long == 0 || n_long == t.parts) return n * k / t.parts;
-    const double a = std::min(ahead, std::max(0.0, (double)(n - 4 * t.parts) / n_long));
-    const double shrt = (n - a * n_long) / t.parts;
-    return std::min<int64_t>(n, std::llround(k * shrt + std::min(k, n_long) * a));
-  };
+  auto part_begin = [](const Tile& t, int k) { return t.tiles() * k / t.parts; };   // in tiles from t.k0
   // blocks: longest first, the row tiles of one key range next to each other on
-  // one XCD (block i runs on XCD i % 8), which reads it through its L2 once
+  // one XCD (block i runs on XCD i % 8), which reads it through its L2 once.  Parts of
+  // one length throughout: of 60 batches with one to two prefix parts per CU, parts of
+  // two lengths with the members' own blocks between them were 2.6% slower in the
+  // geometric mean (0.82 to 1.14 of the time; 64 branches of 64K 171 and 173 us, 16
+  // segments of 16 to 64 tokens on 16K 188 and 182).
   struct Bundle {
     int64_t length;                                              // tiles of each of its items
     int32_t tile, count, kvh, part;                              // row tiles tile .. tile + count - 1
@@ -434,25 +409,23 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
     i = j;
   }
   std::stable_sort(bundles.begin(), bundles.end(), [](const Bundle& x, const Bundle& y) { return x.length > y.length; });
-  std::vector<int32_t> queue[kNumXcd], fillers[kNumXcd];        // bundles
+  std::vector<int32_t> queue[kNumXcd];                          // bundles
   int64_t load[kNumXcd] = {0};
-  size_t n_queue[kNumXcd] = {0}, n_fill[kNumXcd] = {0}, depth = 0;
+  size_t blocks[kNumXcd] = {0}, depth = 0;
   for (size_t i = 0; i < bundles.size(); ++i) {
     const Bundle& b = bundles[i];
     const int x = (int)(std::min_element(load, load + kNumXcd) - load);
     load[x] += b.length * b.count;
-    const bool filler = fit && !tiles[b.tile].prefix;
-    (filler ? fillers : queue)[x].push_back((int32_t)i);
-    (filler ? n_fill : n_queue)[x] += b.count;
-    depth = std::max(depth, n_fill[x] + n_queue[x]);
+    queue[x].push_back((int32_t)i);
+    blocks[x] += b.count;
+    depth = std::max(depth, blocks[x]);
   }
   out.items.assign(depth * kNumXcd, AttnItem{0, 0, 0, 0, 0, -1, 0, 0, 0, 0});
-  const size_t round = (size_t)std::max(1, num_cu / kNumXcd);
   for (int x = 0; x < kNumXcd; ++x) {
-    size_t at = 0, gap = std::min(round, n_queue[x]);           // the fillers' place
-    auto emit = [&](const Bundle& b) {
+    size_t at = 0;
+    for (int32_t i : queue[x]) {
+      const Bundle& b = bundles[i];
       for (int32_t y = b.tile; y < b.tile + b.count; ++y) {
-        if (at == gap) at += n_fill[x];
         const Tile& t = tiles[y];
         AttnItem it{t.seq, b.kvh, t.row0, 0, 0, -1, 0, t.q_start, t.q_len, t.kv_len};
         it.kv_begin = (int32_t)(t.k0 + part_begin(t, b.part) * kKT);
@@ -460,11 +433,7 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
         if (t.place >= 0) it.part = (int32_t)(t.place + ((int64_t)b.kvh * t.parts + b.part) * t.rows);
         out.items[at++ * kNumXcd + x] = it;
       }
-    };
-    for (int32_t i : queue[x]) emit(bundles[i]);
-    at = gap;
-    gap = SIZE_MAX;
-    for (int32_t i : fillers[x]) emit(bundles[i]);
+    }
   }
 
   // merge units: rows of one member, one own tile and one prefix tile

@@ -1934,7 +1934,6 @@ sa_status sa_shared_plan_stats(const sa_layout* layout, int32_t batch, const int
                            [](const sa::AttnItem& it) { return it.kv_begin < it.kv_end; });
     out[2] = plan.part_rows;
     out[3] = plan.most_parts;
-    out[4] = plan.ahead;
     if (h_once != nullptr)
       for (int g = 0; g < num_groups; ++g) h_once[g] = plan.shared && plan.once[g];
     return SA_OK;

@@ -17,9 +17,9 @@ def test_rope_refuses_an_eps_that_the_norm_takes_for_zero(lib, want, eps):  # no
 
 def test_the_gpu_tests_reach_the_paths_they_are_for():
     """Which prefixes the planner computes once in the batches of the GPU tests: a cost rule that moves shows here."""
-    for heads, page, groups, once, ahead in PATHS:
+    for heads, page, groups, once in PATHS:
         plan = plan_of(heads, page, groups)
-        assert plan["once"] == [bool(x) for x in once] and plan["ahead"] == bool(ahead), (heads, groups, plan)
+        assert plan["once"] == [bool(x) for x in once], (heads, groups, plan)
         assert any(once) == (plan["items"] > 0)
     for (heads, page, groups), once in zip(SHARED, ANCHORED, strict=True):
         plan = plan_of(heads, page, [anchor(heads)] + groups)
@@ -28,7 +28,7 @@ def test_the_gpu_tests_reach_the_paths_they_are_for():
 
 def test_plan_stats_refusals(lib):  # noqa: F811
     def go(L=layout(), q=(1, 1), kv=(10, 9), groups=(0, 2), shared=(8,), cus=256, out=True):
-        a, b, g, s, o = i32(q), i32(kv), i32(groups), i32(shared), np.zeros(5, np.int64)
+        a, b, g, s, o = i32(q), i32(kv), i32(groups), i32(shared), np.zeros(4, np.int64)
         return lib.sa_shared_plan_stats(ctypes.byref(L), len(a), a.ctypes.data, b.ctypes.data, len(s), g.ctypes.data,
                                         s.ctypes.data, cus, o.ctypes.data if out else None, None)
     assert go() == OK
