@@ -9,8 +9,8 @@ import pytest
 import torch
 
 import paper_2607_00151_amd as sa
-from test_gpu_branches import (D, anchor, bits, branch_batch, check_attention, compact_reference, dev, lay, pool_bits,
-                               run_shared)
+from test_gpu_branches import (D, FILL, anchor, bits, branch_batch, check_attention, close_bf16, compact_reference, dev,
+                               fork_reference, lay, pool_bits, rope_reference, run_shared, tables)
 
 pytestmark = pytest.mark.gpu
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -362,3 +362,90 @@ def test_a_masked_value_that_is_not_finite_stays_in_its_work_item(heads, q, anch
     whole = q + first // G                                               # tokens of the call that are before it
     assert first > 0 and o2[2 * q - 1, :, 64].isnan().all()
     assert same_bits(o[:whole], o2[:whole]) and same_bits(o[2 * q:], o2[2 * q:]) and same_bits(lse, lse2)
+
+
+# ------------------------------------------------------------------------- large batches, odd heads, two streams
+
+@pytest.mark.parametrize("heads,page,groups,once", [
+    ((8, 2), 16, [(2005, [(1 + i % 40, 1) for i in range(700)])], [1]),            # a plan of 200 KB
+    ((192, 1), 32, [(9000, [(5 + i, 1) for i in range(8)])], [1]),                 # a token in two row tiles
+    ((130, 2), 16, [(9000, [(i + 1, 1) for i in range(20)])], [1]),                # 65 query heads to a key head
+    ((1, 1), 16, [(30000, [(i + 3, 3) for i in range(40)])], [1]),
+])
+def test_shared_prefix_attention_of_many_members_and_odd_heads(heads, page, groups, once):
+    assert plan_of(heads, page, groups)["once"] == [bool(x) for x in once]
+    w = branch_batch(np.random.default_rng(len(groups[0][1])), heads, page, groups)
+    check_attention(w, *run_shared(sa.Context(0), w), D ** -0.5)
+
+
+def test_append_rope_of_thousands_of_sequences():
+    """5000 sequences of none to two tokens: the token search takes three rounds."""
+    r = np.random.default_rng(61)
+    new, start = r.integers(0, 3, 5000), r.integers(0, 40, 5000)
+    pages = -(-(start + new) // 16)
+    T = int(new.sum())
+    L = lay((2, 1), 16, int(pages.sum()) + 1)
+    indptr, indices, _ = tables(r, pages, L.num_slots)
+    both = (torch.randn((T, 4, D), device="cuda") * 0.5).to(torch.bfloat16)
+    q, k, v = both.split([2, 1, 1], dim=1)
+    kp, vp = pool_bits(r, L, FILL), pool_bits(r, L, FILL)
+    out, inv = torch.empty((T, 2, D), dtype=torch.bfloat16, device="cuda"), 10000.0 ** (-np.arange(64) / 64)
+    ctx = sa.Context(0)
+    sa.sa_kv_append_rope(ctx, L, 0, sa.Rope(inv), q, k, v, out, kp, vp, start, new, dev(indptr), dev(indices))
+    sa.sa_sync_check(ctx)
+    seq = np.repeat(np.arange(5000), new)
+    at = np.repeat(start, new) + np.arange(T) - np.repeat(np.cumsum(new) - new, new)
+    slot, row = indices[indptr[seq] + at // 16], at % 16
+    want = torch.full_like(vp, np.uint16(FILL).view(np.int16))
+    want[0, slot, 0, row] = v[:, 0].contiguous().view(torch.int16)
+    assert torch.equal(vp, want)
+    close_bf16(out, *rope_reference(q.cpu(), None, at, inv, 0, False, 0.0))
+    close_bf16(kp.view(torch.bfloat16)[0, slot, 0, row][:, None], *rope_reference(k.cpu(), None, at, inv, 0, False, 0.0))
+
+
+def test_fork_of_thousands_of_children():
+    r = np.random.default_rng(62)
+    src_len, page = [37, 16, 0, 5], 16
+    parent, reserve = r.integers(0, 4, 4500), r.integers(0, 20, 4500)
+    pages = [-(-n // page) for n in src_len]
+    need = sum(-(-(src_len[b] + x) // page) - src_len[b] // page for b, x in zip(parent, reserve))
+    L = lay((1, 1), page, sum(pages) + need)
+    indptr, indices, fresh = tables(r, pages, L.num_slots)
+    kp, vp = pool_bits(r, L), pool_bits(r, L)
+    wip, wix, used, wk = fork_reference(bits(kp), indptr, indices, src_len, parent, reserve, fresh, page)
+    ref, dip, dix = dev(np.zeros(L.num_slots)), dev(np.zeros(4501)), dev(np.zeros(len(wix)))
+    ctx = sa.Context(0)
+    sa.sa_kv_retain(ctx, L, dev(indptr), dev(indices), ref)
+    assert sa.sa_kv_fork(ctx, L, kp, vp, src_len, parent, reserve, dev(indptr), dev(indices), dev(fresh), dip, dix,
+                         ref=ref) == used == need
+    sa.sa_sync_check(ctx)
+    np.testing.assert_array_equal(dip.cpu(), wip)
+    np.testing.assert_array_equal(dix.cpu(), wix)
+    np.testing.assert_array_equal(bits(kp), wk)
+    np.testing.assert_array_equal(ref.cpu(), np.bincount(np.concatenate([indices, wix]), minlength=L.num_slots))
+
+
+def test_two_contexts_at_once_on_two_streams():
+    """Attention and counts of two contexts overlap in time; each gives what it gives alone."""
+    works = [branch_batch(np.random.default_rng(70 + i), (8, 2), 16, [(700 + i, [(9, 1)] * 6), anchor((8, 2))])
+             for i in range(2)]
+    ctxs, streams = [sa.Context(0) for _ in works], [torch.cuda.Stream() for _ in works]
+    alone = [run_shared(sa.Context(0), w) for w in works]
+    qs = [w["q"].cuda() for w in works]
+    outs = [[torch.empty_like(alone[i][0]) for _ in range(8)] for i in range(2)]
+    L, n = lay((1, 1), 16, 9000), 9000
+    refs = [dev(np.arange(n) % 3) for _ in works]
+    free, nfree = [dev(np.zeros(n)) for _ in works], [dev([0]) for _ in works]
+    ip, ix = dev([0, 3000]), dev(np.arange(3000) * 3 + 1)                # every count of one
+    torch.cuda.synchronize()
+    for k in range(8):
+        for i, w in enumerate(works):
+            sa.sa_shared_prefix_attn(ctxs[i], w["L"], 0, qs[i], w["kp"], w["vp"], w["q_len"], w["kv_len"], w["indptr"],
+                                     w["indices"], w["groups"], w["shared"], D ** -0.5, outs[i][k], stream=streams[i])
+            sa.sa_kv_release(ctxs[i], L, ip, ix, refs[i], free[i], nfree[i], stream=streams[i])
+            sa.sa_kv_retain(ctxs[i], L, ip, ix, refs[i], stream=streams[i])
+    for i in range(2):
+        sa.sa_sync_check(ctxs[i], streams[i])
+        assert all(torch.equal(o, alone[i][0]) for o in outs[i])
+        assert int(nfree[i]) == 6000 and torch.equal(refs[i], dev(np.arange(n) % 3))
+        np.testing.assert_array_equal(free[i].cpu()[:6000], np.flatnonzero(np.arange(n) % 3 < 2))
