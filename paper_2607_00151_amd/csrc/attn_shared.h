@@ -11,10 +11,13 @@
 // prefix tile is an item of attn_pipe_kernel's body whose "sequence" is the
 // whole group), a second joins them row by row.
 //
-// Bound by HBM for one token per member (32 of 16K keys, 32/8 heads: 110 MB in 24
-// us and the merge's 6.7, against 154 by the segment attention), by the matrix
+// Probabilities are rounded to bf16 for the PV product (its matrix instruction's
+// operand), as in attn_pipe.h; scores, sums, partials and their join are fp32.
+//
+// Bound by HBM for one token per member (32 of 16K keys, 32/8 heads: 110 MB in 25
+// us and the merge's 7, against 154 by the segment attention), by the matrix
 // cores and the softmax beside them from some 200 rows on (64 of 64K, 64/8 heads: 139
-// GFLOP in 150 us and 12, against 1155).
+// GFLOP in 175 us and 14, the shortest 150 and 12, against 1155).
 #pragma once
 
 #include "attn_pipe.h"
@@ -69,8 +72,8 @@ __device__ __forceinline__ float half_sum(float x) {
 // the partial rows are loaded eight ahead of their use.  With block_rows = 1, 2,
 // 4 or 8 by the most parts of a row (merge_block_rows) a half wave has at most
 // about eight parts, whose loads are all in flight at once: the launch is bound
-// by that latency.  32 branches of 16K, 33 parts a row:
-// 13.4 us with a row's loads one after another, 6.7.
+// by that latency.  32 branches of 16K, 30 parts a row:
+// 13.4 us with a row's loads one after another, 7.
 __global__ __launch_bounds__(256) void merge_rows_kernel(MergeRowsArgs a) {
   __shared__ f32x4 red[8][32];
   __shared__ float red_m[8], red_den[8];

@@ -390,8 +390,8 @@ inline void plan_shared_items(const sa_layout* layout, const std::vector<SeqDesc
   auto part_begin = [](const Tile& t, int k) { return t.tiles() * k / t.parts; };   // in tiles from t.k0
   // blocks: longest first, the row tiles of one key range next to each other on
   // one XCD (block i runs on XCD i % 8), which reads it through its L2 once.  Parts of
-  // one length throughout: of 60 batches with one to two prefix parts per CU, parts of
-  // two lengths with the members' own blocks between them were 2.6% slower in the
+  // one length throughout: of 58 batches with one to two prefix parts per CU, parts of
+  // two lengths with the members' own blocks between them were 2.7% slower in the
   // geometric mean (0.82 to 1.14 of the time; 64 branches of 64K 171 and 173 us, 16
   // segments of 16 to 64 tokens on 16K 188 and 182).
   struct Bundle {
