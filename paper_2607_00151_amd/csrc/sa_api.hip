@@ -1703,6 +1703,14 @@ void launch_shared(bool pool_rsrc, dim3 grid, hipStream_t st, const hipEvent_t* 
   else launch_timed(sa::attn_shared_kernel<P, false>, grid, dim3(256), st, ev, a);
 }
 
+// The bounds of the two launches' grids and of the places of partials.
+sa_status check_shared_plan(const sa_layout* layout, const sa::SharedPlan& plan) {
+  if (plan.part_rows > sa::kMaxPartRows || (int64_t)plan.items.size() > kMaxBlocks ||
+      (int64_t)plan.units.size() * layout->num_kv_heads > kMaxBlocks)
+    return fail(SA_ERR_SHAPE, "the batch is too large for one launch (%lld partial rows)", (long long)plan.part_rows);
+  return SA_OK;
+}
+
 // SA_DEBUG: what a group is said to share is the same in all of its members' caches, bit for bit.
 sa_status debug_shared(const sa_layout* layout, int32_t layer, const void* k_pool, const void* v_pool, int32_t batch,
                        const int32_t* h_q_len, sa_pages pages, int32_t num_groups, const int32_t* h_group_indptr,
@@ -1782,9 +1790,8 @@ sa_status shared_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   uint8_t* dev = ctx->plans[kPlanShared].dev;
   if (!same) {
     sa::plan_shared_items(layout, seqs, num_groups, h_group_indptr, h_shared_len, ctx->num_cu, plan);
-    if (plan.part_rows > sa::kMaxPartRows || (int64_t)plan.items.size() > kMaxBlocks ||
-        (int64_t)plan.units.size() * layout->num_kv_heads > kMaxBlocks)
-      return fail(SA_ERR_SHAPE, "the batch is too large for one launch (%lld partial rows)", (long long)plan.part_rows);
+    s = check_shared_plan(layout, plan);
+    if (s != SA_OK) return s;
     rec.shared = plan.shared;
     rec.n_items = plan.items.size();
     rec.n_units = plan.units.size();
@@ -1929,6 +1936,8 @@ sa_status sa_shared_plan_stats(const sa_layout* layout, int32_t batch, const int
     if (num_cu < 1) return fail(SA_ERR_SHAPE, "num_cu %d < 1", num_cu);
     sa::SharedPlan plan;
     sa::plan_shared_items(layout, seqs, num_groups, h_group_indptr, h_shared_len, num_cu, plan);
+    s = check_shared_plan(layout, plan);
+    if (s != SA_OK) return s;
     out[0] = plan.shared ? std::count(plan.once.begin(), plan.once.end(), 1) : 0;
     out[1] = std::count_if(plan.items.begin(), plan.items.end(),
                            [](const sa::AttnItem& it) { return it.kv_begin < it.kv_end; });
