@@ -1,11 +1,14 @@
 """Calls for branches of one context where they can go wrong, without a GPU."""
 import ctypes
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
 
 import paper_2607_00151_amd as sa
-from test_branches_cpu import CTX, NULL, OK, SHAPE, UNSUPPORTED, i32, layout, lib, rope  # noqa: F401
+from test_branches_cpu import CTX, NULL, OK, ROOT, SHAPE, UNSUPPORTED, i32, layout, lib, rope  # noqa: F401
 from test_gpu_branch_edges import ANCHORED, PATHS, plan_of
 from test_gpu_branches import SHARED, anchor
 
@@ -45,3 +48,18 @@ def test_rope_frequencies_may_be_set_from_any_array(value):
     s, want = rope._struct(128, None), np.float64(value).reshape(-1)
     assert s.rot_dim == 2 * len(want)
     np.testing.assert_array_equal((ctypes.c_double * len(want)).from_address(s.h_inv_freq), want)
+
+
+@pytest.mark.timeout(300)
+def test_debug_check_of_shared_prefixes_under_asan_ubsan(tmp_path):
+    if shutil.which("g++") is None:
+        pytest.skip("g++ not available")
+    exe = str(tmp_path / "shared_check")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined",
+                           "-fno-sanitize-recover=all", "-fno-omit-frame-pointer", "-Wall", "-Werror",
+                           "-I", os.path.join(ROOT, "include"),
+                           "-I", os.path.join(ROOT, "paper_2607_00151_amd", "csrc"),
+                           os.path.join(ROOT, "tests", "host", "shared_check.cpp"), "-o", exe])
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=240)
+    print(r.stdout[-2000:], r.stderr[-4000:])
+    assert r.returncode == 0 and "ALL OK" in r.stdout
