@@ -1312,11 +1312,16 @@ sa_status reserve_work(sa_ctx* ctx, size_t need, hipStream_t stream) {
   const sa_status s = refuse_capture(stream, "a call that has to allocate for a pool of this size");
   if (s != SA_OK) return s;
   // at least doubled, as reserve_parts: a pool that grows by steps does not leave a buffer behind at each
-  const size_t cap = std::max(need, 2 * ctx->work_cap);
+  size_t cap = std::max(need, 2 * ctx->work_cap);
   if (ctx->work) ctx->retired_dev.push_back(ctx->work);
   ctx->work = nullptr;
   ctx->work_cap = 0;
-  SA_HIP(hipMalloc(&ctx->work, cap));
+  if (cap > need && hipMalloc(&ctx->work, cap) != hipSuccess) {
+    (void)hipGetLastError();
+    ctx->work = nullptr;
+    cap = need;                                            // no room for twice as much: what the call takes
+  }
+  if (ctx->work == nullptr) SA_HIP(hipMalloc(&ctx->work, cap));
   ctx->work_cap = cap;
   return SA_OK;
 }
