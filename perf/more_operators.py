@@ -1,0 +1,620 @@
+"""Contexts of text and images in a cache of 4 bits, as timed cases, with their plain forms.
+
+A case is a dict of plain values; `kind` names the calls that one pass makes:
+
+  axes     sa_kv_append_rope_axes: norms of the query and key heads, their rotation by
+           positions on several axes (time, height, width), rows into bf16 pages
+  append   sa_kv4_append: the same (or no rotation at all) into pages of 4 bits; the pages
+           that got rows are then read back with sa_kv4_unpack, so that the pass gives the
+           values they stand for (keys in 8 bits, which hold them exactly)
+  convert  sa_kv4_pack and sa_kv4_unpack: pages of a bf16 pool go into a pool of 4 bits
+           and come back, every layer of them
+  attn     sa_kv4_attn: attention over pages of 4 bits, causal
+  cross    sa_kv4_attn without a mask: every query row sees all of its sequence's keys,
+           an encoder's states, of which there may be none
+
+The format: 32 neighbouring dims of a head row share a power of two 2^(s - 127), s one
+byte; each value is a 4-bit float (sign, 0 0.5 1 1.5 2 3 4 6) times it.  A page of one
+head holds its rows' codes (64 bytes a row, the even dim in a byte's low half) and then
+their scale bytes (4 a row).
+
+With `own` false a pass computes the same in elementary torch operations, in 32 bits
+(angles in 64), rounded once at the end.  Rows are N(0, 1) / 2 rounded to bf16 on a
+shuffled page pool, the distribution of the configurations c1..c5, with 1% of the key
+rows times 8 where `outliers` is set (c4's recipe).
+"""
+import math
+import random
+
+import numpy as np
+import torch
+
+own = False
+
+D = 128
+ROW4 = 68                                                    # bytes of a head row of 4 bits: codes and scales
+
+
+# ------------------------------------------------------------------------- cases
+
+def _attn(name, heads, page, n=1, kv=(1, 1), q=(1, 1), causal=True, lens=1, outliers=False):
+    c = {"kind": "attn" if causal else "cross", "Hq": heads[0], "Hkv": heads[1], "page": page, "n": n,
+         "kv_lo": kv[0], "kv_hi": kv[1], "q_lo": q[0], "q_hi": q[1], "lens": lens, "outliers": outliers}
+    return dict(c, name=name) if name else c
+
+
+def _rows_case(kind, name, heads, page, n=1, start=(0, 0), new=(1, 1), axes=3, mixed=False, rot=128, interleaved=False,
+               norm=True, fused=True, theta=1e6, far=0, lens=1):
+    c = {"kind": kind, "Hq": heads[0], "Hkv": heads[1], "page": page, "n": n, "start_lo": start[0],
+         "start_hi": start[1], "new_lo": new[0], "new_hi": new[1], "axes": axes, "mixed": mixed, "rot": rot,
+         "interleaved": interleaved, "norm": norm, "fused": fused, "theta": theta, "far": far, "lens": lens}
+    return dict(c, name=name) if name else c
+
+
+def _convert(name, heads, page, pages=16, layers=1, spare=0.25, outliers=False):
+    c = {"kind": "convert", "Hq": heads[0], "Hkv": heads[1], "page": page, "pages": pages, "layers": layers,
+         "spare": spare, "outliers": outliers}
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # the new rows of one decode step of c5's 64 requests, whose contexts hold images: three axes
+        _rows_case("axes", "axes_decode_c5", (32, 8), 16, n=64, start=(4095, 16383), new=(1, 1)),
+        # c3's 16 ragged segments, as frames of a video
+        _rows_case("axes", "axes_video_c3", (32, 8), 16, n=16, start=(4096, 32768), new=(512, 4096), lens=3),
+        # the same decode step into a cache of 4 bits
+        _rows_case("append", "kv4_append_decode", (32, 8), 16, n=64, start=(4095, 16383), new=(1, 1)),
+        # c3's segments into a cache of 4 bits, text only: one position, given with the sequence
+        _rows_case("append", "kv4_append_ragged", (32, 8), 16, n=16, start=(4096, 32768), new=(512, 4096), axes=0,
+                   lens=3),
+        # a context of 2K tokens goes to 4 bits and comes back, four layers of it
+        _convert("convert_few", (32, 8), 16, pages=128, layers=4),
+        # c2's 8K prefix, 32 layers of it
+        _convert("convert_layers", (32, 8), 16, pages=512, layers=32),
+        # a decode step of four requests with short contexts: the smallest call of a serving loop
+        _attn("kv4_decode_few", (32, 8), 16, n=4, kv=(1024, 4096)),
+        # a decode step of 64 requests with contexts as long as c5's decode rows
+        _attn("kv4_decode_batch", (32, 8), 16, n=64, kv=(4096, 32768)),
+        # short instruction chunks on 32 contexts of 8K
+        _attn("kv4_segments", (32, 8), 16, n=32, kv=(8192, 8600), q=(16, 64)),
+        # c2's segment behind its prefix, the cache in 4 bits
+        _attn("kv4_prefill_c2", (32, 8), 16, n=1, kv=(10240, 10240), q=(2048, 2048)),
+        # a decode step of 64 requests over their images' encoder states; some have none
+        _attn("kv4_cross_decode", (32, 8), 16, n=64, kv=(0, 6400), causal=False),
+        # the prompts of 8 requests over their images' encoder states
+        _attn("kv4_cross_prompt", (32, 8), 16, n=8, kv=(1500, 6400), q=(64, 700), causal=False),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _span(rng, lo, hi):
+    return tuple(sorted((_log(rng, lo, hi), _log(rng, lo, hi))))
+
+
+def draw(rng):
+    """One more case of the ranges the listed ones span."""
+    while True:
+        kind = rng.choice(["axes", "append", "convert", "attn", "attn", "attn", "cross"])
+        heads, page = rng.choice([((32, 8), 16), ((64, 8), 32), ((8, 2), 16), ((32, 4), 32), ((40, 8), 16)])
+        lens = rng.randrange(1 << 20)
+        if kind in ("axes", "append"):
+            c = _rows_case(kind, None, heads, page, n=_log(rng, 1, 64), start=_span(rng, 1, 32768),
+                           new=_span(rng, 1, 4096), axes=rng.choice([1, 2, 3, 3, 4] + [0, 0] * (kind == "append")),
+                           mixed=rng.random() < 0.4, rot=rng.choice([128, 128, 64, 96, 32]),
+                           interleaved=rng.random() < 0.3, norm=rng.random() < 0.7, fused=rng.random() < 0.6,
+                           theta=rng.choice([1e4, 5e5, 1e6]), far=rng.choice([0, 0, _log(rng, 1000, 1 << 21)]),
+                           lens=lens)
+        elif kind == "convert":
+            c = _convert(None, heads, page, pages=_log(rng, 1, 4096), layers=rng.choice([1, 2, 4, 8, 32]),
+                         spare=rng.uniform(0.0, 0.5), outliers=rng.random() < 0.3)
+        else:
+            many = rng.random() < 0.4                         # segments, else a token each
+            q = _span(rng, 1, 2048) if many else (1, 1)
+            kv = _span(rng, max(q), 131072) if kind == "attn" else _span(rng, 1, 16384)
+            if kind == "cross" and rng.random() < 0.5:
+                kv = (0, kv[1])
+            c = _attn(None, heads, page, n=_log(rng, 1, 64), kv=kv, q=q, causal=kind == "attn", lens=lens,
+                      outliers=rng.random() < 0.2)
+        w = work(c)
+        if w["flops"] <= 3e11 and w["bytes"] <= 2.6e9 and _tokens(c) <= 1 << 20:
+            return c
+
+
+# ------------------------------------------------------------------------- shapes
+
+def _pages(x, P):
+    return -(-np.asarray(x, dtype=np.int64) // P)
+
+
+def _attn_lengths(case):
+    """(query tokens, cached tokens) of each sequence."""
+    r = random.Random(case["lens"])
+    q = [r.randint(case["q_lo"], case["q_hi"]) for _ in range(case["n"])]
+    kv = [r.randint(case["kv_lo"], case["kv_hi"]) for _ in q]
+    if case["kind"] == "attn":
+        kv = [max(a, b) for a, b in zip(q, kv)]
+    return np.array(q, dtype=np.int64), np.array(kv, dtype=np.int64)
+
+
+def _row_lengths(case):
+    """(first position, new tokens) of each sequence."""
+    r = random.Random(case["lens"])
+    start = [r.randint(case["start_lo"], case["start_hi"]) for _ in range(case["n"])]
+    new = [r.randint(case["new_lo"], case["new_hi"]) for _ in range(case["n"])]
+    return np.array(start, dtype=np.int64), np.array(new, dtype=np.int64)
+
+
+def _touched_pages(case):
+    """Per sequence: pages before its new rows, pages that get rows."""
+    start, new = _row_lengths(case)
+    first = start // case["page"]
+    return first, _pages(start + new, case["page"]) - first
+
+
+def _tokens(case):
+    if case["kind"] == "convert":
+        return case["pages"] * case["page"] * case["layers"]
+    if case["kind"] in ("attn", "cross"):
+        return int(_attn_lengths(case)[1].sum())
+    return int(sum(_row_lengths(case)).sum())
+
+
+def work(case):
+    Hq, Hkv, P = case["Hq"], case["Hkv"], case["page"]
+    row, row4 = Hkv * D * 2 * 2, Hkv * ROW4 * 2              # K and V of one token, in bf16 and in 4 bits
+    if case["kind"] in ("attn", "cross"):
+        q, kv = _attn_lengths(case)
+        pairs = int((q * (kv - q) + q * (q + 1) // 2).sum() if case["kind"] == "attn" else (q * kv).sum())
+        return {"bytes": float(int(kv.sum()) * row4 + int(q.sum()) * Hq * (2 * D * 2 + 4)),
+                "flops": 4.0 * D * Hq * pairs}
+    if case["kind"] == "convert":
+        n = case["pages"] * P * case["layers"]
+        return {"bytes": 2.0 * n * (row + row4), "flops": 0.0}
+    _, new = _row_lengths(case)
+    n = int(new.sum())
+    at = 4 * case["axes"] * n                                # positions
+    flops = float(n * (Hq + Hkv) * (3 * case["rot"] + (4 * D if case["norm"] else 0)))
+    if case["kind"] == "axes":
+        return {"bytes": 2.0 * n * (Hq * D * 2 + row) + at, "flops": flops}
+    back = int(_touched_pages(case)[1].sum()) * P * (row4 + Hkv * D * 3)   # keys come back in 8 bits, values in 16
+    return {"bytes": float(n * (2 * Hq * D * 2 + row + row4) + at + back), "flops": flops}
+
+
+# ------------------------------------------------------------------------- the 4-bit format
+
+def _quantise(x):
+    """The codes and scale bytes of fp32 rows [..., D], as the bytes of the format: [..., 64] and [..., 4].
+
+    The block's scale exponent is that of its largest magnitude rounded half up to one bit behind the point, less 2,
+    so that the largest is at least 3.5 and less than 7 times the scale; values are rounded to the nearest, ties to
+    the even code, beyond 6 to 6.  The byte is held to 1..252; a block that holds an infinity or a NaN has 255 and
+    codes of 0."""
+    x = x.unflatten(-1, (4, 32))
+    top = x.abs().amax(-1).view(torch.int32)                 # a NaN is larger than any number
+    fine = top < 0x7F800000
+    s = torch.where(fine, torch.clamp(((top + 0x200000) >> 23) - 2, 1, 252), 255)
+    unscale = ((254 - torch.where(fine, s, 127)) << 23).view(torch.float32)[..., None]
+    y = torch.where(fine[..., None], x, 0.0) * unscale
+    a = y.abs()
+    code = torch.signbit(y).to(torch.uint8) << 3
+    code += (a > 0.25).to(torch.uint8) + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5)
+    code = code.flatten(-2)
+    return code[..., 0::2] | (code[..., 1::2] << 4), s.to(torch.uint8)
+
+
+def _values(page4, P):
+    """The fp32 values [..., P, D] of pages [..., P * 68]."""
+    table = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, -0.0, -0.5, -1, -1.5, -2, -3, -4, -6], device=page4.device)
+    both = page4[..., :64 * P].unflatten(-1, (P, 64))
+    codes = torch.stack([both & 15, both >> 4], dim=-1).flatten(-2)
+    s = page4[..., 64 * P:].unflatten(-1, (P, 4)).to(torch.int32)
+    scale = torch.where(s == 255, math.nan, torch.where(s == 0, 2.0 ** -127, (s << 23).view(torch.float32)))
+    return (table[codes.int()].unflatten(-1, (4, 32)) * scale[..., None]).flatten(-2)
+
+
+def _pack_pages(x):
+    """Pages [..., P * 68] of fp32 rows [..., P, D]."""
+    codes, s = _quantise(x)
+    return torch.cat([codes.flatten(-2), s.flatten(-2)], dim=-1)
+
+
+# ------------------------------------------------------------------------- inputs
+
+def _rows(g, shape):
+    t = torch.empty(shape, dtype=torch.bfloat16, device="cuda")
+    flat = t.view(-1)
+    step = 1 << 28
+    for i in range(0, flat.numel(), step):
+        n = min(step, flat.numel() - i)
+        flat[i:i + n] = torch.randn(n, generator=g, device="cuda").mul_(0.5)
+    return t
+
+
+def _outliers(g, k):
+    flat = k.view(-1, D)
+    hit = torch.randperm(flat.shape[0], generator=g, device="cuda")[:flat.shape[0] // 100]
+    flat[hit] = flat[hit] * 8
+
+
+def _pool4(g, slots, Hkv, P, outliers=False):
+    """A pool of 4 bits of one layer, its slots made a few thousand at a time."""
+    pool = torch.empty((1, slots, Hkv, P * ROW4), dtype=torch.uint8, device="cuda")
+    for i in range(0, slots, 4096):
+        rows = _rows(g, (min(4096, slots - i), Hkv, P, D))
+        if outliers:
+            _outliers(g, rows)
+        pool[0, i:i + 4096] = _pack_pages(rows.float())
+    return pool
+
+
+def _table(lists):
+    indptr = np.concatenate([[0], np.cumsum([len(x) for x in lists])]).astype(np.int32)
+    return torch.from_numpy(indptr).cuda(), torch.cat(lists).contiguous()
+
+
+def _shuffled(g, x, counts, spare):
+    """A pool of `spare` more slots than pages, the pages of each sequence anywhere in it."""
+    need = sum(counts)
+    x["num_slots"] = max(16, need + int(need * spare))
+    perm = torch.randperm(x["num_slots"], generator=g, device="cuda").to(torch.int32)
+    x["indptr"], x["indices"] = _table(list(perm[:need].split(counts)))
+
+
+def _attn_inputs(case, g, x):
+    q, kv = _attn_lengths(case)
+    P, Hq, T = case["page"], case["Hq"], int(q.sum())
+    _shuffled(g, x, _pages(kv, P).tolist(), 0.25)
+    x["k4"] = _pool4(g, x["num_slots"], case["Hkv"], P, case["outliers"])
+    x["v4"] = _pool4(g, x["num_slots"], case["Hkv"], P)
+    x["q_len"], x["kv_len"] = q.astype(np.int32), kv.astype(np.int32)
+    x["q"] = _rows(g, (T, Hq, D))
+    x["o"] = torch.empty((T, Hq, D), dtype=torch.bfloat16, device="cuda")
+    x["lse"] = torch.empty((T, Hq), dtype=torch.float32, device="cuda")
+
+
+def _row_inputs(case, g, x):
+    start, new = _row_lengths(case)
+    P, Hq, Hkv, T = case["page"], case["Hq"], case["Hkv"], int(new.sum())
+    _shuffled(g, x, _pages(start + new, P).tolist(), 0.25)
+    x["start"], x["new_len"] = start.astype(np.int32), new.astype(np.int32)
+    if case["fused"]:
+        both = _rows(g, (T, Hq + 2 * Hkv, D))
+        x["q"], x["k_new"], x["v_new"] = both.split([Hq, Hkv, Hkv], dim=1)
+    else:
+        x["q"], x["k_new"], x["v_new"] = _rows(g, (T, Hq, D)), _rows(g, (T, Hkv, D)), _rows(g, (T, Hkv, D))
+    x["q_out"] = torch.empty((T, Hq, D), dtype=torch.bfloat16, device="cuda")
+    half = case["rot"] // 2
+    x["inv_freq"] = case["theta"] ** (-2.0 * np.arange(half, dtype=np.float64) / case["rot"])
+    x["q_weight"] = x["k_weight"] = None
+    if case["norm"]:
+        w = 1.0 + 0.2 * torch.randn((2, D), generator=g, device="cuda")
+        x["q_weight"], x["k_weight"] = w.to(torch.bfloat16).unbind(0)
+    # text counts up on every axis alike; frames of 8 x 16 tokens count their rows and columns from their first token on
+    A = case["axes"]
+    x["axis"] = x["axis_pos"] = x["pos"] = None
+    step = np.arange(T) - np.repeat(np.cumsum(new) - new, new)
+    base = np.repeat(start + case["far"], new)
+    if A:
+        j = np.arange(half)
+        x["axis"] = (j % A if case["mixed"] else j * A // half).astype(np.int32)
+        at = np.stack([base + (step // 128 * 16 if A > 1 and a == 0 else step if A == 1 else
+                               step // 128 * 16 + (step // 16 % 8 if a == 1 else step % 16)) for a in range(A)])
+        x["axis_pos"] = torch.from_numpy(at.astype(np.int32)).cuda()
+    else:
+        x["pos"] = (start + case["far"]).astype(np.int32) if case["far"] else None
+    if case["kind"] == "axes":
+        x["k"], x["v"] = _rows(g, (1, x["num_slots"], Hkv, P, D)), _rows(g, (1, x["num_slots"], Hkv, P, D))
+        return
+    x["k4"], x["v4"] = _pool4(g, x["num_slots"], Hkv, P), _pool4(g, x["num_slots"], Hkv, P)
+    first, count = _touched_pages(case)
+    ip = np.concatenate([[0], np.cumsum(_pages(start + new, P))])
+    at = np.concatenate([np.arange(ip[b] + first[b], ip[b] + first[b] + count[b]) for b in range(case["n"])])
+    x["touched"] = x["indices"][torch.from_numpy(at).cuda()].contiguous()
+    n = len(at)
+    x["places"] = torch.arange(n, dtype=torch.int32, device="cuda")
+    x["k_back"] = torch.empty((1, n, Hkv, P, D), dtype=torch.bfloat16, device="cuda")
+    x["v_back"] = torch.empty_like(x["k_back"])
+
+
+def _convert_inputs(case, g, x):
+    n, Hkv, P = case["pages"], case["Hkv"], case["page"]
+    x["num_slots"] = n + int(n * case["spare"])
+    x["k"] = _rows(g, (case["layers"], x["num_slots"], Hkv, P, D))
+    x["v"] = _rows(g, (case["layers"], x["num_slots"], Hkv, P, D))
+    if case["outliers"]:
+        _outliers(g, x["k"])
+    x["src"] = torch.randperm(x["num_slots"], generator=g, device="cuda")[:n].to(torch.int32)
+    x["slots4"] = torch.randperm(n, generator=g, device="cuda").to(torch.int32)
+    x["back"] = torch.randperm(n, generator=g, device="cuda").to(torch.int32)
+    x["k4"] = torch.empty((case["layers"], n, Hkv, P * ROW4), dtype=torch.uint8, device="cuda")
+    x["v4"] = torch.empty_like(x["k4"])
+    x["k_back"] = torch.empty((case["layers"], n, Hkv, P, D), dtype=torch.bfloat16, device="cuda")
+    x["v_back"] = torch.empty_like(x["k_back"])
+
+
+def _inputs(case, seed):
+    """Everything in plain torch and numpy: pools, tables, rows and host lengths."""
+    g = torch.Generator(device="cuda").manual_seed(int(seed))
+    x = {}
+    {"attn": _attn_inputs, "cross": _attn_inputs, "axes": _row_inputs, "append": _row_inputs,
+     "convert": _convert_inputs}[case["kind"]](case, g, x)
+    return x
+
+
+def prepare(case, seed):
+    s = _inputs(case, seed)
+    s["case"] = case
+    if own:
+        import paper_2607_00151_amd as sa
+
+        def layout(slots):
+            return sa.Layout(num_q_heads=case["Hq"], num_kv_heads=case["Hkv"], head_dim=D, page_size=case["page"],
+                             num_layers=case.get("layers", 1), num_slots=slots)
+
+        s["ctx"], s["layout"] = sa.Context(0), layout(s["num_slots"])
+        if "k_back" in s:
+            s["layout_back"] = layout(s["k_back"].shape[1])
+        if case["kind"] in ("axes", "append"):
+            s["rope"] = sa.Rope(inv_freq=s["inv_freq"], q_weight=s["q_weight"], k_weight=s["k_weight"], eps=1e-6,
+                                interleaved=case["interleaved"])
+    return s
+
+
+# ------------------------------------------------------------------------- one pass
+
+def run(s):
+    kind = s["case"]["kind"]
+    if not own:
+        return {"attn": _plain_attn, "cross": _plain_attn, "axes": _plain_axes, "append": _plain_append,
+                "convert": _plain_convert}[kind](s)
+    import paper_2607_00151_amd as sa
+    ctx, L = s["ctx"], s["layout"]
+    if kind in ("attn", "cross"):
+        sa.sa_kv4_attn(ctx, L, 0, s["q"], s["k4"], s["v4"], s["q_len"], s["kv_len"], s["indptr"], s["indices"],
+                       D ** -0.5, s["o"], s["lse"], causal=kind == "attn")
+        return [s["o"], s["lse"]]
+    if kind == "axes":
+        sa.sa_kv_append_rope_axes(ctx, L, 0, s["rope"], s["axis"], s["q"], s["k_new"], s["v_new"], s["q_out"], s["k"],
+                                  s["v"], s["start"], s["new_len"], s["indptr"], s["indices"], s["axis_pos"])
+        return [s["q_out"], s["k"], s["v"]]
+    if kind == "append":
+        sa.sa_kv4_append(ctx, L, 0, s["k_new"], s["v_new"], s["k4"], s["v4"], s["start"], s["new_len"], s["indptr"],
+                         s["indices"], rope=s["rope"], q=s["q"], q_out=s["q_out"], pos=s["pos"], axis=s["axis"],
+                         axis_pos=s["axis_pos"])
+        sa.sa_kv4_unpack(ctx, s["layout_back"], s["k4"], s["v4"], s["touched"], s["k_back"], s["v_back"], s["places"])
+        return [s["q_out"], s["k_back"].to(torch.float8_e4m3fn), s["v_back"]]
+    sa.sa_kv4_pack(ctx, L, s["k"], s["v"], s["src"], s["k4"], s["v4"], s["slots4"])
+    sa.sa_kv4_unpack(ctx, s["layout_back"], s["k4"], s["v4"], s["slots4"], s["k_back"], s["v_back"], s["back"])
+    return [s["k_back"], s["v_back"]]
+
+
+def _int(a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int64)).cuda()
+
+
+def _plain_attn(s):
+    """Sequence by sequence: values of the pages, scores of all heads, one softmax."""
+    c, scale = s["case"], D ** -0.5
+    Hkv, G, P = c["Hkv"], c["Hq"] // c["Hkv"], c["page"]
+    q_len, kv_len = s["q_len"].tolist(), s["kv_len"].tolist()
+    first = np.concatenate([[0], np.cumsum(_pages(s["kv_len"], P))]).tolist()
+    indices = s["indices"].long()
+
+    def gather(pool, slots, n):
+        return _values(pool[0][slots], P).transpose(0, 1).reshape(Hkv, -1, D)[:, :n]
+
+    t0 = 0
+    for b, (n, kv) in enumerate(zip(q_len, kv_len)):
+        if kv == 0:
+            s["o"][t0:t0 + n] = 0
+            s["lse"][t0:t0 + n] = -math.inf
+        else:
+            slots = indices[first[b]:first[b + 1]]
+            q = s["q"][t0:t0 + n].float().view(n, Hkv, G, D).transpose(0, 1).reshape(Hkv, n * G, D) * scale
+            a = q @ gather(s["k4"], slots, kv).transpose(1, 2).contiguous()
+            if c["kind"] == "attn":
+                last = torch.arange(kv - n, kv, device=q.device).repeat_interleave(G)
+                a = torch.where(torch.arange(kv, device=q.device) > last[:, None], -math.inf, a)
+            m = a.amax(2, keepdim=True)
+            p = torch.exp(a - m)
+            total = p.sum(2, keepdim=True)
+            o = p @ gather(s["v4"], slots, kv) / total
+            s["o"][t0:t0 + n] = o.view(Hkv, n, G, D).transpose(0, 1).reshape(n, Hkv * G, D).to(torch.bfloat16)
+            s["lse"][t0:t0 + n] = (m + torch.log(total)).view(Hkv, n, G).transpose(0, 1).reshape(n, Hkv * G)
+        t0 += n
+    return [s["o"], s["lse"]]
+
+
+def _plain_turned(s):
+    """The query and key heads, normed and rotated, in fp32."""
+    c = s["case"]
+    new, start = s["new_len"].astype(np.int64), s["start"].astype(np.int64)
+    freq = torch.from_numpy(s["inv_freq"]).cuda()
+    if c["axes"]:
+        angle = s["axis_pos"][_int(s["axis"])].t().double() * freq
+    else:
+        step = np.arange(int(new.sum())) - np.repeat(np.cumsum(new) - new, new)
+        pos0 = start if s["pos"] is None else s["pos"].astype(np.int64)
+        angle = _int(np.repeat(pos0, new) + step).double()[:, None] * freq
+    cos, sin = angle.cos().float()[:, None, :], angle.sin().float()[:, None, :]
+    half = c["rot"] // 2
+
+    def turned(x, w):
+        x = x.float()
+        if w is not None:
+            x = x * torch.rsqrt((x * x).mean(-1, keepdim=True) + 1e-6) * w.float()
+        y = x.clone()
+        if c["interleaved"]:
+            a, b = x[..., 0:c["rot"]:2], x[..., 1:c["rot"]:2]
+            y[..., 0:c["rot"]:2], y[..., 1:c["rot"]:2] = a * cos - b * sin, b * cos + a * sin
+        else:
+            a, b = x[..., :half], x[..., half:c["rot"]]
+            y[..., :half], y[..., half:c["rot"]] = a * cos - b * sin, b * cos + a * sin
+        return y
+
+    return turned(s["q"], s["q_weight"]), turned(s["k_new"], s["k_weight"])
+
+
+def _plain_places(s):
+    """Slot and row of every new token."""
+    P = s["case"]["page"]
+    new, start = s["new_len"].astype(np.int64), s["start"].astype(np.int64)
+    at = np.repeat(start, new) + np.arange(int(new.sum())) - np.repeat(np.cumsum(new) - new, new)
+    first = np.cumsum(_pages(start + new, P)) - _pages(start + new, P)
+    return s["indices"].long()[_int(np.repeat(first, new) + at // P)], _int(at % P)
+
+
+def _plain_axes(s):
+    q, k = _plain_turned(s)
+    slot, row = _plain_places(s)
+    s["q_out"].copy_(q)
+    s["k"][0].transpose(1, 2)[slot, row] = k.to(torch.bfloat16)
+    s["v"][0].transpose(1, 2)[slot, row] = s["v_new"]
+    return [s["q_out"], s["k"], s["v"]]
+
+
+def _plain_append(s):
+    P = s["case"]["page"]
+    q, k = _plain_turned(s)
+    slot, row = _plain_places(s)
+    s["q_out"].copy_(q)
+    for pool, x in ((s["k4"], k), (s["v4"], s["v_new"].float())):
+        codes, scales = _quantise(x)
+        pool[0, ..., :64 * P].unflatten(-1, (P, 64)).transpose(1, 2)[slot, row] = codes
+        pool[0, ..., 64 * P:].unflatten(-1, (P, 4)).transpose(1, 2)[slot, row] = scales
+    touched = s["touched"].long()
+    s["k_back"].copy_(_values(s["k4"][:, touched], P))
+    s["v_back"].copy_(_values(s["v4"][:, touched], P))
+    return [s["q_out"], s["k_back"].to(torch.float8_e4m3fn), s["v_back"]]
+
+
+def _plain_convert(s):
+    P, src, slots4, back = s["case"]["page"], s["src"].long(), s["slots4"].long(), s["back"].long()
+    for x, x4, y in ((s["k"], s["k4"], s["k_back"]), (s["v"], s["v4"], s["v_back"])):
+        x4[:, slots4] = _pack_pages(x[:, src].float())
+        y[:, back] = _values(x4[:, slots4], P).to(torch.bfloat16)
+    return [s["k_back"], s["v_back"]]
+
+
+# ------------------------------------------------------------------------- 64-bit reference
+
+def exact(case, seed):
+    """The outputs from the definitions, in float64."""
+    x = _inputs(case, seed)
+    if case["kind"] in ("attn", "cross"):
+        return _exact_attn(case, x)
+    if case["kind"] == "convert":
+        return _exact_convert(case, x)
+    return _exact_rows(case, x)
+
+
+def _nearest(x):
+    """Rows in float64, as what the format holds of them."""
+    blocks = x.reshape(*x.shape[:-1], 4, 32)
+    mantissa, power = torch.frexp(blocks.abs().amax(-1, keepdim=True))          # mantissa in [0.5, 1)
+    power = power.double() - 3 + (mantissa >= 0.875)
+    scale = torch.exp2(power.clamp(-126, 125))
+    grid = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6], dtype=torch.float64, device=x.device)
+    y = (blocks / scale).abs().clamp(max=6)
+    up = torch.searchsorted(grid, y.contiguous()).clamp(max=7)                  # the first value that is not below
+    low = (up - 1).clamp(min=0)
+    over, under = grid[up] - y, y - grid[low]
+    chosen = torch.where((over < under) | ((over == under) & (up % 2 == 0)), up, low)
+    chosen = torch.where(y == grid[up], up, chosen)
+    return (grid[chosen] * scale * torch.sign(blocks)).reshape(x.shape)
+
+
+def _held(page4, P):
+    """Pages of 4 bits as float64 rows [..., P, D], from the format's bits."""
+    def element(nibble):
+        e, m = (nibble >> 1) & 3, (nibble & 1).double()
+        v = torch.where(e == 0, 0.5 * m, (1 + 0.5 * m) * torch.exp2(e.double() - 1))
+        return torch.where(nibble >= 8, -v, v)
+
+    b = page4[..., :64 * P].reshape(*page4.shape[:-1], P, 4, 16).to(torch.int32)
+    rows = torch.empty(*b.shape[:-1], 32, dtype=torch.float64, device=b.device)
+    rows[..., 0::2], rows[..., 1::2] = element(b % 16), element(b // 16)
+    s = page4[..., 64 * P:].reshape(*page4.shape[:-1], P, 4).double()
+    return (rows * torch.exp2(s - 127)[..., None]).reshape(*page4.shape[:-1], P, D)
+
+
+def _exact_attn(case, x):
+    """Every sequence by itself over its whole cache, head by head."""
+    G, P = case["Hq"] // case["Hkv"], case["page"]
+    ip = x["indptr"].tolist()
+    o = torch.zeros(x["o"].shape, dtype=torch.float64, device="cuda")
+    lse = torch.full(x["lse"].shape, -math.inf, dtype=torch.float64, device="cuda")
+    t0 = 0
+    for b, (n, kv) in enumerate(zip(x["q_len"].tolist(), x["kv_len"].tolist())):
+        slots = x["indices"][ip[b]:ip[b + 1]].long()
+        visible = torch.arange(kv - n + 1, kv + 1, device="cuda") if case["kind"] == "attn" else \
+            torch.full((n,), kv, device="cuda")
+        dead = torch.arange(kv, device="cuda")[None, :] >= visible[:, None]
+        for h in range(case["Hkv"] if kv else 0):
+            keys = _held(x["k4"][0, slots, h], P).reshape(-1, D)[:kv]
+            values = _held(x["v4"][0, slots, h], P).reshape(-1, D)[:kv]
+            for i in range(h * G, (h + 1) * G):
+                scores = (x["q"][t0:t0 + n, i].double() @ keys.t()) / math.sqrt(D)
+                scores[dead] = -math.inf
+                lse[t0:t0 + n, i] = torch.logsumexp(scores, 1)
+                o[t0:t0 + n, i] = torch.exp(scores - lse[t0:t0 + n, i, None]) @ values
+        t0 += n
+    return [o, lse]
+
+
+def _exact_rows(case, x):
+    """Pairs as complex numbers, turned by a unit number of their axis' angle, sequence by sequence."""
+    r, half, P = case["rot"], case["rot"] // 2, case["page"]
+    freq = torch.from_numpy(x["inv_freq"]).cuda()
+
+    def heads(t, w, angle):
+        y = t.double()
+        if w is not None:
+            y = y / torch.sqrt(y.square().sum(-1, keepdim=True) / D + 1e-6) * w.double()
+        unit = torch.polar(torch.ones_like(angle), angle)
+        z = y[..., :r].reshape(*y.shape[:-1], half, 2) if case["interleaved"] else \
+            torch.stack([y[..., :half], y[..., half:r]], dim=-1)
+        z = torch.view_as_real(torch.view_as_complex(z.contiguous()) * unit[:, None, :])
+        z = z.flatten(-2) if case["interleaved"] else torch.cat(z.unbind(-1), dim=-1)
+        return torch.cat([z, y[..., r:]], dim=-1)
+
+    q = torch.empty(x["q"].shape, dtype=torch.float64, device="cuda")
+    quantised = case["kind"] == "append"
+    if quantised:                                            # the whole pools: what was there, then the new rows
+        k, v = _held(x["k4"][0, x["touched"].long()], P)[None], _held(x["v4"][0, x["touched"].long()], P)[None]
+    else:
+        k, v = x["k"].double(), x["v"].double()
+    ip, t0, place = x["indptr"].tolist(), 0, 0
+    for b, (a, n) in enumerate(zip(x["start"].tolist(), x["new_len"].tolist())):
+        at = torch.arange(a, a + n, device="cuda")
+        if case["axes"]:
+            angle = torch.stack([x["axis_pos"][ax, t0:t0 + n].double() * freq[j] for j, ax in
+                                 enumerate(x["axis"].tolist())], dim=1)
+        else:
+            angle = (at + case["far"]).double()[:, None] * freq[None, :]
+        q[t0:t0 + n] = heads(x["q"][t0:t0 + n], x["q_weight"], angle)
+        kn, vn = heads(x["k_new"][t0:t0 + n], x["k_weight"], angle), x["v_new"][t0:t0 + n].double()
+        if quantised:
+            slots = place + at // P - a // P
+            kn, vn = _nearest(kn), _nearest(vn)
+            place += int(_pages(a + n, P)) - a // P
+        else:
+            slots = x["indices"][ip[b]:ip[b + 1]].long()[at // P]
+        k[0, slots, :, at % P] = kn
+        v[0, slots, :, at % P] = vn
+        t0 += n
+    return [q, k, v]
+
+
+def _exact_convert(case, x):
+    out = []
+    for pool in (x["k"], x["v"]):
+        y = torch.empty(x["k_back"].shape, dtype=torch.float64, device="cuda")
+        for layer in range(case["layers"]):
+            y[layer, x["back"].long()] = _nearest(pool[layer, x["src"].long()].double())
+        out.append(y)
+    return out
