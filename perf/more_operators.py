@@ -4,13 +4,13 @@ A case is a dict of plain values; `kind` names the calls that one pass makes:
 
   axes     sa_kv_append_rope_axes: norms of the query and key heads, their rotation by
            positions on several axes (time, height, width), rows into bf16 pages
-  append   sa_kv4_append: the same (or no rotation at all) into pages of 4 bits; the pages
-           that got rows are then read back with sa_kv4_unpack, so that the pass gives the
+  append   sa_kvq_append: the same (or no rotation at all) into pages of 4 bits; the pages
+           that got rows are then read back with sa_kvq_unpack, so that the pass gives the
            values they stand for (keys in 8 bits, which hold them exactly)
-  convert  sa_kv4_pack and sa_kv4_unpack: pages of a bf16 pool go into a pool of 4 bits
+  convert  sa_kvq_pack and sa_kvq_unpack: pages of a bf16 pool go into a pool of 4 bits
            and come back, every layer of them
-  attn     sa_kv4_attn: attention over pages of 4 bits, causal
-  cross    sa_kv4_attn without a mask: every query row sees all of its sequence's keys,
+  attn     sa_kvq_attn: attention over pages of 4 bits, causal
+  cross    sa_kvq_attn without a mask: every query row sees all of its sequence's keys,
            an encoder's states, of which there may be none
 
 The format: 32 neighbouring dims of a head row share a power of two 2^(s - 127), s one
@@ -374,7 +374,7 @@ def run(s):
     import paper_2607_00151_amd as sa
     ctx, L = s["ctx"], s["layout"]
     if kind in ("attn", "cross"):
-        sa.sa_kv4_attn(ctx, L, 0, s["q"], s["k4"], s["v4"], s["q_len"], s["kv_len"], s["indptr"], s["indices"],
+        sa.sa_kvq_attn(ctx, L, 0, s["q"], s["k4"], s["v4"], s["q_len"], s["kv_len"], s["indptr"], s["indices"],
                        D ** -0.5, s["o"], s["lse"], causal=kind == "attn")
         return [s["o"], s["lse"]]
     if kind == "axes":
@@ -382,13 +382,13 @@ def run(s):
                                   s["v"], s["start"], s["new_len"], s["indptr"], s["indices"], s["axis_pos"])
         return [s["q_out"], s["k"], s["v"]]
     if kind == "append":
-        sa.sa_kv4_append(ctx, L, 0, s["k_new"], s["v_new"], s["k4"], s["v4"], s["start"], s["new_len"], s["indptr"],
+        sa.sa_kvq_append(ctx, L, 0, s["k_new"], s["v_new"], s["k4"], s["v4"], s["start"], s["new_len"], s["indptr"],
                          s["indices"], rope=s["rope"], q=s["q"], q_out=s["q_out"], pos=s["pos"], axis=s["axis"],
                          axis_pos=s["axis_pos"])
-        sa.sa_kv4_unpack(ctx, s["layout_back"], s["k4"], s["v4"], s["touched"], s["k_back"], s["v_back"], s["places"])
+        sa.sa_kvq_unpack(ctx, s["layout_back"], s["k4"], s["v4"], s["touched"], s["k_back"], s["v_back"], s["places"])
         return [s["q_out"], s["k_back"].to(torch.float8_e4m3fn), s["v_back"]]
-    sa.sa_kv4_pack(ctx, L, s["k"], s["v"], s["src"], s["k4"], s["v4"], s["slots4"])
-    sa.sa_kv4_unpack(ctx, s["layout_back"], s["k4"], s["v4"], s["slots4"], s["k_back"], s["v_back"], s["back"])
+    sa.sa_kvq_pack(ctx, L, s["k"], s["v"], s["src"], s["k4"], s["v4"], s["slots4"])
+    sa.sa_kvq_unpack(ctx, s["layout_back"], s["k4"], s["v4"], s["slots4"], s["k_back"], s["v_back"], s["back"])
     return [s["k_back"], s["v_back"]]
 
 
