@@ -22,7 +22,10 @@
  * sa_segment_prefill_attn_append (append + attention, one launch) and the
  * copy-free splice sa_kv_splice_alias.  Several branches of one context are kept
  * by sa_kv_fork, sa_kv_retain, sa_kv_release and sa_kv_compact, written by
- * sa_kv_append_rope and attended by sa_shared_prefix_attn.
+ * sa_kv_append_rope and attended by sa_shared_prefix_attn.  Contexts of text and
+ * images are rotated by several axes' positions (sa_kv_append_rope_axes), and a
+ * cache may be held in 4 bits (sa_kvq_append, sa_kvq_pack, sa_kvq_unpack,
+ * sa_kvq_attn).
  *
  * Data layout (all device memory is owned by the caller):
  *   bf16 values are IEEE bfloat16 bit patterns (uint16).
@@ -674,6 +677,139 @@ sa_status sa_shared_plan_stats(const sa_layout *layout, int32_t batch, const int
                                const int32_t *h_kv_len, int32_t num_groups,
                                const int32_t *h_group_indptr, const int32_t *h_shared_len,
                                int32_t num_cu, int64_t *out, int32_t *h_once);
+
+/* --------------------------------------- several axes, and a cache of 4 bits
+ *
+ * Contexts of agents that look at screens hold images and video beside text:
+ * their tokens have a position on each of a few axes (time, height, width), and
+ * their caches are long.  The calls below rotate by such positions, keep a cache
+ * in 4.25 bits a value, and attend over it, with a causal mask or, over an
+ * encoder's states, without one.
+ *
+ * Format of a 4-bit cache.  A head row of 128 is four blocks of 32 neighbouring
+ * dims.  A block has a scale byte s, worth 2^(s - 127) (255: the block is NaN),
+ * and 32 elements of 4 bits: the sign in bit 3, and 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * for bits 2..0 = 0..7.  A row's codes take 64 bytes (dim 2 d in the low half of
+ * byte d, 2 d + 1 in the high half) and its scales 4.  Pools:
+ *   kq_pool, vq_pool  uint8 [num_layers][num_slots][num_kv_heads][page_size * 68]:
+ *                     a head's page holds its rows' codes, page_size * 64 bytes, and
+ *                     then their scales, page_size * 4
+ * Rows are quantised block by block: s = e - 2 with e the exponent byte of the
+ * block's largest magnitude in fp32, rounded half up to one bit behind the point,
+ * held to 1..252; each value divided by 2^(s - 127) goes to the nearest element,
+ * halves to the one with an even code, beyond 6 to 6.  A block that holds an
+ * infinity or a NaN becomes 255 with codes of 0.  Page tables, slots and their
+ * counts are those of a bf16 cache (sa_kv_splice_alias, sa_kv_retain and
+ * sa_kv_release work on them as they are; sa_kv_assemble, sa_kv_fork and
+ * sa_kv_compact move bf16 pages and do not take these pools).
+ *
+ * They use the calling thread's device only within the call.  The calls that plan
+ * on the host (sa_kv_append_rope_axes, sa_kvq_append, sa_kvq_attn) return
+ * SA_ERR_UNSUPPORTED on a stream that is being captured into a graph;
+ * sa_kvq_pack and sa_kvq_unpack keep nothing in the context and can be captured.
+ * Slots of more than 2^30 elements and pools of 2^31 - 4096 slots or more are
+ * refused (SA_ERR_UNSUPPORTED).
+ */
+
+/* Positions on several axes (sa_kv_append_rope_axes, sa_kvq_append). */
+typedef struct sa_axes {
+    int32_t num_axes;         /* 1 to 8                                                 */
+    const int32_t *h_axis;    /* host [rot_dim / 2]: the axis that turns each pair, from
+                                 0 to num_axes - 1 (sections or mixed, as the model has it) */
+    const int32_t *d_pos;     /* device [num_axes][pos_stride]: each new token's position
+                                 on each axis, any int32                                */
+    int64_t pos_stride;       /* at least the number of new tokens                      */
+} sa_axes;
+
+/*
+ * sa_kv_append_rope_axes — sa_kv_append_rope with a position per token and axis:
+ * pair j of new token t (counted over all sequences) turns by
+ *   a = axes.d_pos[axes.h_axis[j] * axes.pos_stride + t] * inv_freq[j]
+ * (negative positions turn back).  h_start gives the cache positions, as there.
+ *
+ * Errors: those of sa_kv_append_rope; SA_ERR_NULL for NULL axes, axis numbers
+ * (with a rot_dim) or positions, SA_ERR_SHAPE for a number of axes or an axis
+ * out of range or a pos_stride below the new tokens, SA_ERR_ALIGN for positions
+ * that are not 4-byte aligned.
+ */
+sa_status sa_kv_append_rope_axes(sa_ctx *ctx, const sa_layout *layout, int32_t layer, const sa_rope *rope,
+                                 const sa_axes *axes, const void *q, int64_t q_stride, const void *k_new,
+                                 int64_t k_stride, const void *v_new, int64_t v_stride, void *q_out,
+                                 void *k_pool, void *v_pool, int32_t batch, const int32_t *h_start,
+                                 const int32_t *h_new_len, sa_pages pages, void *stream);
+
+/*
+ * sa_kvq_append — new rows into a 4-bit cache, normed and rotated on the way.
+ *
+ * rope NULL: the key and value rows are quantised as they are; q and q_out must be
+ * NULL, h_pos and axes too, and q_stride is not read.  Otherwise the key heads, and
+ * the query heads where q and q_out are given (both or neither), are normed and
+ * rotated as by sa_kv_append_rope (axes NULL; positions from h_pos, or h_start) or
+ * sa_kv_append_rope_axes (h_pos NULL); keys are quantised from the fp32 results,
+ * query rows rounded to bf16.  Value rows are quantised as they are.  Rows go to the
+ * positions sa_kv_append would give them; nothing else in the pools changes.
+ *
+ * Errors: as sa_kv_append_rope and sa_kv_append_rope_axes, for the arguments given;
+ * SA_ERR_SHAPE for q without q_out, or queries, positions or axes without a rope,
+ * or both h_pos and axes.  A missing or out-of-range page is latched for
+ * sa_sync_check; its rows are not written, q_out is.
+ */
+sa_status sa_kvq_append(sa_ctx *ctx, const sa_layout *layout, int32_t layer, const sa_rope *rope,
+                        const sa_axes *axes, const void *q, int64_t q_stride, const void *k_new,
+                        int64_t k_stride, const void *v_new, int64_t v_stride, void *q_out, void *kq_pool,
+                        void *vq_pool, int32_t batch, const int32_t *h_start, const int32_t *h_new_len,
+                        const int32_t *h_pos, sa_pages pages, void *stream);
+
+/*
+ * sa_kvq_pack — quantise pages: for i in 0 .. num_pages - 1, slot d_slots[i] of the
+ * bf16 pools (layout, whole pages, every head and layer) into slot d_slots4[i] of
+ * the 4-bit pools, which hold num_slots4 slots a layer.  Both lists are on the
+ * device; a slot may be packed more than once, and d_slots4 must not repeat.
+ * sa_kvq_unpack — the way back: slot d_slots4[i] of the 4-bit pools into slot
+ * d_slots[i] of the bf16 pools, exactly (every value is a bf16 number; an element
+ * of 4 or 6 under a scale byte of 253, or of 2 and more under 254, which the
+ * quantisation never makes, becomes an infinity).  There d_slots must not repeat.
+ * A slot outside its pool is latched for sa_sync_check and its page skipped;
+ * SA_DEBUG=1 refuses it (SA_ERR_RANGE), and repeated destinations (SA_ERR_OVERLAP),
+ * before launching, except on a stream that is being captured.
+ *
+ * Errors: SA_ERR_SHAPE (num_pages < 0, num_slots4 < 1, more pages than a launch
+ * takes: layers * pages up to 2^23), SA_ERR_UNSUPPORTED, SA_ERR_NULL, SA_ERR_ALIGN,
+ * SA_ERR_HIP.
+ */
+sa_status sa_kvq_pack(sa_ctx *ctx, const sa_layout *layout, const void *k_pool, const void *v_pool,
+                      const int32_t *d_slots, int64_t num_slots4, void *kq_pool, void *vq_pool,
+                      const int32_t *d_slots4, int32_t num_pages, void *stream);
+sa_status sa_kvq_unpack(sa_ctx *ctx, const sa_layout *layout, int64_t num_slots4, const void *kq_pool,
+                        const void *vq_pool, const int32_t *d_slots4, void *k_pool, void *v_pool,
+                        const int32_t *d_slots, int32_t num_pages, void *stream);
+
+/*
+ * sa_kvq_attn — grouped-query attention over a 4-bit cache.
+ *
+ * causal != 0: sa_segment_prefill_attn's rows and keys (0 <= q_len <= kv_len; row i
+ * sees kv_len - q_len + i + 1 keys).  causal == 0: every query row of a sequence
+ * sees all of its kv_len keys (cross attention to states of another length; any
+ * q_len, kv_len >= 0); where kv_len is 0 the rows are zeros and their LSE is
+ * -infinity.  Lengths of keys are at most 2^31 - 64.
+ * O = softmax(softmax_scale * q . K^T) V with the values the cache stands for.
+ * Scores are the exact products of the cached keys with the bf16 query rows, held
+ * as three 6-bit floats per value (within 2^-14 of the largest of its 32 dims),
+ * summed in fp32; probabilities are rounded to bf16 before the PV product, the rest
+ * is fp32.  A row that sees a key with a NaN block has a NaN output and a NaN LSE; a
+ * NaN block of a value it sees makes those 32 dims of its output NaN.  What a row
+ * does not see does not reach it.  A page that is missing or outside the pool reads
+ * as zeros and is latched for sa_sync_check.  `lse` may be NULL; pages.indices may
+ * be NULL where no sequence with queries has keys.  Parts of a launch split by key
+ * range are joined by a second kernel (516 bytes of the split-KV partials per query
+ * row, head and part; plans take 40 bytes per work item and 36 per split row tile).
+ * sa_set_kernel_events times the first kernel (SA_TIMED_ATTN).
+ *
+ * Errors: those of sa_segment_prefill_attn, SA_ERR_UNSUPPORTED for a capturing stream.
+ */
+sa_status sa_kvq_attn(sa_ctx *ctx, const sa_layout *layout, int32_t layer, const void *q, const void *kq_pool,
+                      const void *vq_pool, int32_t batch, const int32_t *h_q_len, const int32_t *h_kv_len,
+                      sa_pages pages, int32_t causal, float softmax_scale, void *o, float *lse, void *stream);
 
 #ifdef __cplusplus
 }

@@ -18,7 +18,9 @@ __all__ = [
     "sa_segment_prefill_attn", "sa_segment_prefill_attn_append", "sa_set_exact_scale", "sa_set_fused_append",
     "sa_set_kernel_events", "sa_set_block_clock", "sa_set_xcd_weights", "sa_sync_check", "sa_reserve",
     "sa_segment_prefill_attn_noalloc", "sa_attn_plan_stats", "Rope", "sa_kv_append_rope", "sa_kv_fork",
-    "sa_kv_retain", "sa_kv_release", "sa_kv_compact", "sa_shared_prefix_attn", "sa_shared_plan_stats", "EXPORTED_SYMBOLS",
+    "sa_kv_retain", "sa_kv_release", "sa_kv_compact", "sa_shared_prefix_attn", "sa_shared_plan_stats",
+    "sa_kv_append_rope_axes", "kvq_pool_shape", "sa_kvq_append", "sa_kvq_pack", "sa_kvq_unpack", "sa_kvq_attn",
+    "EXPORTED_SYMBOLS",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -32,7 +34,8 @@ EXPORTED_SYMBOLS = ("sa_create", "sa_destroy", "sa_status_string", "sa_last_erro
                     "sa_set_block_clock", "sa_set_xcd_weights", "sa_reserve",
                     "sa_segment_prefill_attn_noalloc", "sa_attn_plan_stats", "sa_kv_append_rope",
                     "sa_kv_fork", "sa_kv_retain", "sa_kv_release", "sa_kv_compact", "sa_shared_prefix_attn",
-                    "sa_shared_plan_stats")
+                    "sa_shared_plan_stats", "sa_kv_append_rope_axes", "sa_kvq_append", "sa_kvq_pack",
+                    "sa_kvq_unpack", "sa_kvq_attn")
 
 STATUS = {0: "SA_OK", 1: "SA_ERR_NULL", 2: "SA_ERR_SHAPE", 3: "SA_ERR_UNSUPPORTED",
           4: "SA_ERR_ALIGN", 5: "SA_ERR_RANGE", 6: "SA_ERR_NO_PAGES", 7: "SA_ERR_HIP",
@@ -60,6 +63,11 @@ class _Rope(ctypes.Structure):
     _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("h_inv_freq", ctypes.c_void_p),
                 ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
                 ("weight_offset", ctypes.c_float)]
+
+
+class _Axes(ctypes.Structure):
+    _fields_ = [("num_axes", ctypes.c_int32), ("h_axis", ctypes.c_void_p), ("d_pos", ctypes.c_void_p),
+                ("pos_stride", ctypes.c_int64)]
 
 
 def library_path() -> str:
@@ -110,13 +118,20 @@ def load_library():
     lib.sa_kv_compact.argtypes = [P, LP, P, P, I32, P, P, P, P, I64, P, P, P]
     lib.sa_shared_prefix_attn.argtypes = [P, LP, I32, P, P, P, I32, P, P, _Pages, I32, P, P, ctypes.c_float, P, P, P]
     lib.sa_shared_plan_stats.argtypes = [LP, I32, P, P, I32, P, P, I32, P, P]
+    RP, AP = ctypes.POINTER(_Rope), ctypes.POINTER(_Axes)
+    lib.sa_kv_append_rope_axes.argtypes = [P, LP, I32, RP, AP, P, I64, P, I64, P, I64, P, P, P, I32, P, P, _Pages, P]
+    lib.sa_kvq_append.argtypes = [P, LP, I32, RP, AP, P, I64, P, I64, P, I64, P, P, P, I32, P, P, P, _Pages, P]
+    lib.sa_kvq_pack.argtypes = [P, LP, P, P, P, I64, P, P, P, I32, P]
+    lib.sa_kvq_unpack.argtypes = [P, LP, I64, P, P, P, P, P, P, I32, P]
+    lib.sa_kvq_attn.argtypes = [P, LP, I32, P, P, P, I32, P, P, _Pages, I32, ctypes.c_float, P, P, P]
     for name in ("sa_create", "sa_sync_check", "sa_kv_append", "sa_kv_assemble", "sa_kv_assemble_append",
                  "sa_kv_splice_alias", "sa_segment_prefill_attn", "sa_segment_prefill_attn_append",
                  "sa_set_exact_scale", "sa_set_fused_append", "sa_set_kernel_events", "sa_set_block_clock",
                  "sa_set_xcd_weights",
                  "sa_reserve", "sa_segment_prefill_attn_noalloc", "sa_attn_plan_stats", "sa_kv_append_rope",
                  "sa_kv_fork", "sa_kv_retain", "sa_kv_release", "sa_kv_compact", "sa_shared_prefix_attn",
-                 "sa_shared_plan_stats"):
+                 "sa_shared_plan_stats", "sa_kv_append_rope_axes", "sa_kvq_append", "sa_kvq_pack", "sa_kvq_unpack",
+                 "sa_kvq_attn"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -151,7 +166,7 @@ def _load_torch():
     global _torch, _KINDS, _raw_stream
     import torch
     two = {d for d in (getattr(torch, n, None) for n in ("bfloat16", "float16", "int16", "uint16")) if d is not None}
-    _KINDS = {"i32": {torch.int32}, "b16": two, "f32": {torch.float32}, "bf16": two - {torch.float16}}
+    _KINDS = {"i32": {torch.int32}, "b16": two, "f32": {torch.float32}, "u8": {torch.uint8}, "bf16": two - {torch.float16}}
     # the current stream's handle without a Stream object around it, where torch has it
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     _torch = torch
@@ -179,7 +194,7 @@ def _dev(t, what: str, kind: str, min_numel: int = 0, nullable: bool = False):
     # the types in everyday use by a table; any other 2-byte type that is not bool by its size
     if t.dtype not in _KINDS[kind] and not (kind == "b16" and t.element_size() == 2 and t.dtype != torch.bool):
         want = {"i32": "torch.int32", "b16": "a 2-byte dtype (bf16 bits)", "f32": "torch.float32",
-                "bf16": "torch.bfloat16 (or its bits in a 2-byte integer)"}[kind]
+                "bf16": "torch.bfloat16 (or its bits in a 2-byte integer)", "u8": "torch.uint8"}[kind]
         raise ValueError(f"{what}: dtype {t.dtype}, expected {want}")
     if t.numel() < min_numel:
         raise ValueError(f"{what}: {t.numel()} elements, at least {min_numel} needed")
@@ -681,3 +696,123 @@ def sa_shared_plan_stats(layout: Layout, q_len, kv_len, group_indptr, shared_len
         ctypes.byref(layout), len(q_len), _ptr(q_len), _ptr(kv_len), len(shared), _ptr(groups), _ptr(shared),
         int(num_cu), out.ctypes.data, once.ctypes.data))
     return {"once": [bool(x) for x in once], "items": int(out[1]), "part_rows": int(out[2]), "most_parts": int(out[3])}
+
+
+# ---------------------------------------------------------------- several axes, and a cache of 4 bits
+
+_KVQ_ROW = 68            # bytes of a head row: 128 codes of 4 bits, 4 scale bytes
+
+
+def kvq_pool_shape(layout: Layout):
+    """Shape of one pool of 4 bits (torch.uint8) of this layout."""
+    return (int(layout.num_layers), int(layout.num_slots), int(layout.num_kv_heads), int(layout.page_size) * _KVQ_ROW)
+
+
+def _kvq_bytes(layout, slots) -> int:
+    return int(layout.num_layers) * int(slots) * int(layout.num_kv_heads) * int(layout.page_size) * _KVQ_ROW
+
+
+def _axes_of(rope, axis, pos, tokens: int, device):
+    """(sa_axes, the host array it points to) of axis numbers [rot_dim / 2] and positions [num_axes][tokens]."""
+    axis = _host_i32(axis)
+    if axis.ndim != 1 or len(axis) != len(rope.inv_freq):
+        raise ValueError(f"axis: {axis.shape}, expected one axis for each of the {len(rope.inv_freq)} frequencies")
+    torch = _torch or _load_torch()
+    if not isinstance(pos, torch.Tensor) or pos.dim() != 2:
+        raise ValueError("pos: expected a device tensor [num_axes][tokens]")
+    if pos.shape[1] < tokens:
+        raise ValueError(f"pos: {pos.shape[1]} tokens, at least {tokens} needed")
+    return _Axes(pos.shape[0], _ptr(axis) if len(axis) else None, _on(pos, "pos", "i32", 0, device), pos.shape[1]), axis
+
+
+def sa_kv_append_rope_axes(ctx, layout: Layout, layer: int, rope: Rope, axis, q, k_new, v_new, q_out, k_pool, v_pool,
+                           start, new_len, pages_indptr, pages_indices, pos, stream=None):
+    """sa_kv_append_rope with a position per token and axis: pair j of token t turns by pos[axis[j], t] * inv_freq[j].
+    axis: host integers, one for each frequency; pos: device int32 [num_axes][tokens]."""
+    start, new_len = _host_i32(start), _host_i32(new_len)
+    if start.shape != new_len.shape:
+        raise ValueError("start and new_len differ in length")
+    B, T, D, at = len(new_len), max(0, _total(new_len)), layout.head_dim, _device_of(ctx)
+    Hq, Hkv = layout.num_q_heads, layout.num_kv_heads
+    qp, qs = _head_rows(q, "q", T, Hq, D, at)
+    kp, ks = _head_rows(k_new, "k_new", T, Hkv, D, at)
+    vp, vs = _head_rows(v_new, "v_new", T, Hkv, D, at)
+    axes, kept = _axes_of(rope, axis, pos, T, at)
+    n = _pool_numel(layout)
+    _check(load_library().sa_kv_append_rope_axes(
+        _ctx_handle(ctx), ctypes.byref(layout), int(layer), ctypes.byref(rope._struct(D, at)), ctypes.byref(axes), qp,
+        qs, kp, ks, vp, vs, _on(q_out, "q_out", "bf16", T * Hq * D, at, nullable=T == 0),
+        _on(k_pool, "k_pool", "bf16", n, at), _on(v_pool, "v_pool", "bf16", n, at), B, _ptr(start), _ptr(new_len),
+        _table_on(pages_indptr, pages_indices, B, at, "page table"), _stream_of(ctx, stream)))
+
+
+def sa_kvq_append(ctx, layout: Layout, layer: int, k_new, v_new, kq_pool, vq_pool, start, new_len, pages_indptr,
+                  pages_indices, rope: Rope = None, q=None, q_out=None, pos=None, axis=None, axis_pos=None, stream=None):
+    """New key and value rows into pages of 4 bits.  With a rope the key heads, and the query heads of q (to q_out),
+    are normed and rotated first: by pos (host, None: start), or by axis and axis_pos as in sa_kv_append_rope_axes."""
+    start, new_len = _host_i32(start), _host_i32(new_len)
+    pos = None if pos is None else _host_i32(pos)
+    if start.shape != new_len.shape or (pos is not None and pos.shape != start.shape):
+        raise ValueError("start, new_len and pos differ in length")
+    if (axis is None) != (axis_pos is None):
+        raise ValueError("axis and axis_pos go together")
+    if rope is None and axis is not None:
+        raise ValueError("axes without a rope")
+    B, T, D, at = len(new_len), max(0, _total(new_len)), layout.head_dim, _device_of(ctx)
+    Hq, Hkv = layout.num_q_heads, layout.num_kv_heads
+    qp, qs = (None, 0) if q is None else _head_rows(q, "q", T, Hq, D, at)
+    kp, ks = _head_rows(k_new, "k_new", T, Hkv, D, at)
+    vp, vs = _head_rows(v_new, "v_new", T, Hkv, D, at)
+    axes, kept = (None, None) if axis is None else _axes_of(rope, axis, axis_pos, T, at)
+    n = _kvq_bytes(layout, layout.num_slots)
+    _check(load_library().sa_kvq_append(
+        _ctx_handle(ctx), ctypes.byref(layout), int(layer), None if rope is None else ctypes.byref(rope._struct(D, at)),
+        None if axes is None else ctypes.byref(axes), qp, qs, kp, ks, vp, vs,
+        None if q_out is None else _on(q_out, "q_out", "bf16", T * Hq * D, at), _on(kq_pool, "kq_pool", "u8", n, at),
+        _on(vq_pool, "vq_pool", "u8", n, at), B, _ptr(start), _ptr(new_len), _ptr(pos),
+        _table_on(pages_indptr, pages_indices, B, at, "page table"), _stream_of(ctx, stream)))
+
+
+def _convert_args(ctx, layout, k_pool, v_pool, slots, kq_pool, vq_pool, slots4):
+    at, n, page = _device_of(ctx), _pool_numel(layout), _kvq_bytes(layout, 1)
+    pages = 0 if slots is None else slots.numel()
+    if (0 if slots4 is None else slots4.numel()) != pages:
+        raise ValueError("slots and slots4 differ in length")
+    k4, v4 = _on(kq_pool, "kq_pool", "u8", page, at), _on(vq_pool, "vq_pool", "u8", page, at)
+    if kq_pool.numel() != vq_pool.numel() or kq_pool.numel() % page:
+        raise ValueError(f"4-bit pools of {kq_pool.numel()} and {vq_pool.numel()} bytes, expected the same multiple of {page}")
+    return (_on(k_pool, "k_pool", "bf16", n, at), _on(v_pool, "v_pool", "bf16", n, at),
+            _on(slots, "slots", "i32", 0, at, nullable=pages == 0), kq_pool.numel() // page, k4, v4,
+            _on(slots4, "slots4", "i32", 0, at, nullable=pages == 0), pages)
+
+
+def sa_kvq_pack(ctx, layout: Layout, k_pool, v_pool, slots, kq_pool, vq_pool, slots4, stream=None):
+    """Quantises pages: slots[i] of the bf16 pools, every layer, into slots4[i] of the 4-bit pools (whose number of
+    slots follows from their size).  slots, slots4: device int32."""
+    k, v, s, n4, k4, v4, s4, pages = _convert_args(ctx, layout, k_pool, v_pool, slots, kq_pool, vq_pool, slots4)
+    _check(load_library().sa_kvq_pack(_ctx_handle(ctx), ctypes.byref(layout), k, v, s, n4, k4, v4, s4, pages,
+                                      _stream_of(ctx, stream)))
+
+
+def sa_kvq_unpack(ctx, layout: Layout, kq_pool, vq_pool, slots4, k_pool, v_pool, slots, stream=None):
+    """The way back: slots4[i] of the 4-bit pools, every layer, into slots[i] of the bf16 pools, exactly."""
+    k, v, s, n4, k4, v4, s4, pages = _convert_args(ctx, layout, k_pool, v_pool, slots, kq_pool, vq_pool, slots4)
+    _check(load_library().sa_kvq_unpack(_ctx_handle(ctx), ctypes.byref(layout), n4, k4, v4, s4, k, v, s, pages,
+                                        _stream_of(ctx, stream)))
+
+
+def sa_kvq_attn(ctx, layout: Layout, layer: int, q, kq_pool, vq_pool, q_len, kv_len, pages_indptr, pages_indices,
+                softmax_scale: float, o, lse=None, causal: bool = True, stream=None):
+    """Attention over a 4-bit cache: causal (as sa_segment_prefill_attn), or every query row over all keys of its
+    sequence (causal=False; kv_len may be 0: rows of zeros, lse -inf)."""
+    q_len, kv_len = _host_i32(q_len), _host_i32(kv_len)
+    if q_len.shape != kv_len.shape:
+        raise ValueError("q_len and kv_len differ in length")
+    B, T, at = len(q_len), max(0, _total(q_len)), _device_of(ctx)
+    n, rows = _kvq_bytes(layout, layout.num_slots), T * layout.num_q_heads
+    _check(load_library().sa_kvq_attn(
+        _ctx_handle(ctx), ctypes.byref(layout), int(layer), _on(q, "q", "bf16", rows * layout.head_dim, at, T == 0),
+        _on(kq_pool, "kq_pool", "u8", n, at), _on(vq_pool, "vq_pool", "u8", n, at), B, _ptr(q_len), _ptr(kv_len),
+        _table_on(pages_indptr, pages_indices, B, at, "page table", max(kv_len.tolist(), default=0) <= 0),
+        int(bool(causal)), float(softmax_scale), _on(o, "o", "bf16", rows * layout.head_dim, at, T == 0),
+        None if lse is None else _on(lse, "lse", "f32", rows, at), _stream_of(ctx, stream)))

@@ -29,6 +29,7 @@
 #include <stdint.h>
 
 #include "common.h"
+#include "kvq_kernels.h"
 #include "kv_kernels.h"
 #include "plan.h"
 
@@ -42,6 +43,8 @@ struct RopeArgs {
   uint16_t* q_out;           // [T][Hq][128]
   uint16_t* k_pool;          // offset to the layer
   uint16_t* v_pool;
+  uint8_t* kq_pool;          // the same of 4 bits
+  uint8_t* vq_pool;
   const uint16_t* q_weight;  // [128] or null
   const uint16_t* k_weight;
   const int32_t* tok_begin;  // [B + 1]
@@ -56,6 +59,10 @@ struct RopeArgs {
   int32_t rounds;            // rounds of kRopeRows head rows per wave
   float eps, offset;
   const uint64_t* freq;      // [rot / 2] turns per position, as fractions of 2^64
+  const int32_t* axis;       // [rot / 2] axis of each pair, and
+  const int32_t* axis_pos;   // the tokens' positions on axis i from i * axis_stride on
+  int64_t axis_stride;
+  int32_t num_axes;
 };
 
 constexpr int kRopeRows = 16;        // head rows of a round: 4 loads of 16 bytes per lane
@@ -107,7 +114,14 @@ enum RopePair { kPairInLane, kPairFull, kPairAny };
 // 33.5; 4096 with the segment's attention behind them 197.5, 193.8.
 constexpr int64_t kRopeStreamBytes = int64_t(256) << 20;
 
-template <RopePair kPair, bool kStream>
+// kAxes: each pair turns by the position on its own axis, of a few per token.  The
+// token's positions are loaded by as many lanes beside the axis numbers, not behind
+// them, and handed round.
+//
+// kKvq: key and value rows go into pages of 4 bits (kvq_kernels.h), keys from the fp32
+// results: a lane's 8 dims are a quarter of a block, so the scale is a maximum over
+// 4 lanes.  With Hq = 0 and nothing to norm or rotate the keys are the input's bits.
+template <RopePair kPair, bool kStream, bool kAxes = false, bool kKvq = false>
 __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
   const int lane = threadIdx.x & 63;
   const int c = lane & 15, sub = lane >> 4;                 // 16-byte chunk of the row, row within a load
@@ -138,6 +152,8 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
   };
   u32x4 x[4];
   load(row_begin, x);
+  int32_t token_pos = 0;
+  if constexpr (kAxes) token_pos = lane < a.num_axes ? a.axis_pos[lane * a.axis_stride + t] : 0;
 
   const int b = __builtin_amdgcn_readfirstlane(wave_find_seq(a.tok_begin, a.B, t));
   const int step = t - a.tok_begin[b];
@@ -159,7 +175,8 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
   const bool rotates = kPair == kPairFull ? true : kPair == kPairAny ? c < 2 * hl : 8 * c < a.rot;
   const bool upper = kPair == kPairFull ? c >= 8 : kPair == kPairAny && c >= hl;
   const int partner = kPair == kPairInLane || !rotates ? c : kPair == kPairFull ? c ^ 8 : upper ? c - hl : c + hl;
-  const uint32_t pos = (uint32_t)(a.pos[b] + step);
+  uint32_t pos = 0;
+  if constexpr (!kAxes) pos = (uint32_t)(a.pos[b] + step);
   float cs[8], sn[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
@@ -171,9 +188,11 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
     const int j = kPair == kPairInLane ? 4 * c + e / 2 : 8 * (upper ? partner : c) + e;
     cs[e] = 1.f;
     sn[e] = 0.f;
+    if constexpr (kAxes) pos = (uint32_t)__shfl(token_pos, rotates ? a.axis[j] : 0);
     if (rotates) {
       const uint64_t f = a.freq[j];
-      const uint32_t phase = __umulhi((uint32_t)f, pos) + (uint32_t)(f >> 32) * pos;
+      uint32_t phase = __umulhi((uint32_t)f, pos) + (uint32_t)(f >> 32) * pos;
+      if constexpr (kAxes) phase -= (int32_t)pos < 0 ? (uint32_t)f : 0u;   // pos stands for pos - 2^32
       const float turns = (float)(int32_t)phase * 2.3283064365386963e-10f;   // 2^-32
       cs[e] = __builtin_amdgcn_cosf(turns);
       const float s = __builtin_amdgcn_sinf(turns);
@@ -202,7 +221,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
     }
     return k;
   };
-  auto turn = [&](u32x4 raw, const Coef& k) __attribute__((always_inline)) {
+  auto turn = [&](u32x4 raw, const Coef& k, float (&z)[8]) __attribute__((always_inline)) {
     float y[8], p[8];
     unpack8(raw, y);
     if constexpr (kPair == kPairInLane) {
@@ -226,14 +245,25 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
       for (int e = 0; e < 8; ++e) ss[e & 1] = __builtin_fmaf(y[e], y[e], ss[e & 1]);
       r = __builtin_amdgcn_rsqf(row16_sum(ss[0] + ss[1]) * (1.f / kHD) + a.eps);
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      z[e] = __builtin_fmaf(y[e], k.own[e], p[e] * k.other[e]);
+      if (k.normed) z[e] = r * z[e];
+    }
+  };
+  auto rounded = [](const float (&z)[8]) __attribute__((always_inline)) {
     typedef __bf16 b8 __attribute__((ext_vector_type(8)));
     b8 out;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float z = __builtin_fmaf(y[e], k.own[e], p[e] * k.other[e]);
-      out[e] = (__bf16)(k.normed ? r * z : z);
-    }
+    for (int e = 0; e < 8; ++e) out[e] = (__bf16)z[e];
     return __builtin_bit_cast(u32x4, out);
+  };
+  // a row into its page of 4 bits; rows of other lanes may be none of this pool's (`mine`)
+  auto store4 = [&](uint8_t* pool, int head, uint32_t codes, uint32_t scale, bool mine) __attribute__((always_inline)) {
+    if (!mine) return;
+    uint8_t* const p = pool + ((int64_t)slot * a.Hkv + head) * a.P * kKvqRow;
+    *(uint32_t*)(p + prow * kKvqCodes + c * 4) = codes;
+    if ((c & 3) == 0) p[a.P * kKvqCodes + prow * 4 + (c >> 2)] = (uint8_t)scale;
   };
 
   uint16_t* const q_out = a.q_out + (int64_t)t * a.Hq * kHD + c * 8;
@@ -247,17 +277,35 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int first = row0 + 4 * i, row = first + sub;    // first: the same for the whole wave
+      float z[8];
       if (first < a.Hq) {
-        const u32x4 out = turn(x[i], cq);
-        if (row < a.Hq) store(q_out + row * kHD, out);
+        turn(x[i], cq, z);
+        if (row < a.Hq) store(q_out + row * kHD, rounded(z));
       }
-      if (first + 3 >= a.Hq && first < n_qk) {
-        const u32x4 out = turn(x[i], ck);
-        if (row >= a.Hq && row < n_qk && slot >= 0)
-          store(a.k_pool + page_at + (int64_t)(row - a.Hq) * a.P * kHD, out);
+      if constexpr (kKvq) {
+        uint32_t codes, scale;
+        if (first + 3 >= a.Hq && first < n_qk) {
+          if (a.rot == 0 && !ck.normed) {
+            codes = kvq_codes_bf16(x[i], scale);
+          } else {
+            turn(x[i], ck, z);
+            codes = kvq_codes(z, scale);
+          }
+          store4(a.kq_pool, row - a.Hq, codes, scale, row >= a.Hq && row < n_qk && slot >= 0);
+        }
+        if (first + 3 >= n_qk) {
+          codes = kvq_codes_bf16(x[i], scale);
+          store4(a.vq_pool, row - n_qk, codes, scale, row >= n_qk && row < row_end && slot >= 0);
+        }
+      } else {
+        if (first + 3 >= a.Hq && first < n_qk) {
+          turn(x[i], ck, z);
+          if (row >= a.Hq && row < n_qk && slot >= 0)
+            store(a.k_pool + page_at + (int64_t)(row - a.Hq) * a.P * kHD, rounded(z));
+        }
+        if (first + 3 >= n_qk && row >= n_qk && row < row_end && slot >= 0)
+          store(a.v_pool + page_at + (int64_t)(row - n_qk) * a.P * kHD, x[i]);
       }
-      if (first + 3 >= n_qk && row >= n_qk && row < row_end && slot >= 0)
-        store(a.v_pool + page_at + (int64_t)(row - n_qk) * a.P * kHD, x[i]);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = next[i];

@@ -25,6 +25,9 @@
 #include "branch_kernels.h"
 #include "branch_plan.h"
 #include "rope_kernels.h"
+#include "kvq_kernels.h"
+#include "kvq_plan.h"
+#include "attn_kvq.h"
 
 namespace {
 
@@ -108,7 +111,7 @@ class PlanKey {
 
 enum PlanKind {
   kPlanAppend = 0, kPlanAssemble = 1, kPlanAttn = 2, kPlanAlias = 3, kPlanRope = 4, kPlanFork = 5, kPlanShared = 6,
-  kPlanKinds = 7
+  kPlanKvqAppend = 7, kPlanKvqAttn = 8, kPlanKinds = 9
 };
 
 // Fixed device scratch of sa_segment_prefill_attn_noalloc: the launch's plan
@@ -191,9 +194,9 @@ struct sa_ctx {
     int64_t total_q = 0;
   } attn_rec, na_rec;
   struct RopeRec {
-    size_t o_tok = 0, o_start = 0, o_pos = 0, o_freq = 0;
+    size_t o_tok = 0, o_start = 0, o_pos = 0, o_freq = 0, o_axis = 0;
     int64_t total = 0;
-  } rope_rec;
+  } rope_rec, kvq_append_rec;
   struct ForkRec {
     size_t o_ch = 0, o_ip = 0, o_cp = 0;
     int64_t n_dst = 0, fresh_used = 0, n_copies = 0;
@@ -204,6 +207,11 @@ struct sa_ctx {
     int most_rows = 0, block_rows = 8;
     bool shared = false;           // else the batch goes to the segment attention
   } shared_rec;
+  struct KvqRec {
+    size_t o_it[sa::kKvqClasses] = {}, n_items[sa::kKvqClasses] = {}, o_un = 0, n_units = 0;
+    int64_t total_q = 0, total_kv = 0, part_rows = 0;
+    int most_rows = 0, block_rows = 8;
+  } kvq_rec;
   uint8_t* work = nullptr;         // slot scans of sa_kv_release and sa_kv_compact
   size_t work_cap = 0;
   PlanKey na_key;                  // sa_segment_prefill_attn_noalloc: the plan na_host holds
@@ -1270,6 +1278,10 @@ sa_status check_sizes(const sa_layout* layout) {
   return SA_OK;
 }
 
+int64_t kvq_layer_bytes(const sa_layout* layout, int64_t num_slots) {
+  return num_slots * layout->num_kv_heads * layout->page_size * sa::kKvqRow;
+}
+
 // The calling thread's device, put back when the call returns.
 struct DeviceGuard {
   int before = -1;
@@ -1326,33 +1338,79 @@ sa_status reserve_work(sa_ctx* ctx, size_t need, hipStream_t stream) {
   return SA_OK;
 }
 
-sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const sa_rope* rope, const void* q,
-                      int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
-                      void* q_out, void* k_pool, void* v_pool, int32_t batch, const int32_t* h_start,
-                      const int32_t* h_new_len, const int32_t* h_pos, sa_pages pages, void* stream) {
+// sa_kv_append_rope, sa_kv_append_rope_axes and sa_kvq_append: norms, rotation and cache write of new rows.
+struct RowsCall {
+  const char* name;
+  bool kvq;                    // the pools are of 4 bits
+  const sa_rope* rope;         // null (kvq only): rows as they are
+  const sa_axes* axes;         // null: one position per sequence
+  const void* q;               // null (kvq only): keys and values alone
+  int64_t q_stride;
+  const void* k;
+  int64_t k_stride;
+  const void* v;
+  int64_t v_stride;
+  void* q_out;
+  void *k_pool, *v_pool;
+  const int32_t *h_start, *h_new_len, *h_pos;
+};
+
+template <sa::RopePair kPair>
+auto rows_kernel(bool streams, bool axes, bool kvq) -> void (*)(sa::RopeArgs) {
+  if (kvq)
+    return streams ? (axes ? sa::rope_append_kernel<kPair, true, true, true> : sa::rope_append_kernel<kPair, true, false, true>)
+                   : (axes ? sa::rope_append_kernel<kPair, false, true, true> : sa::rope_append_kernel<kPair, false, false, true>);
+  return streams ? (axes ? sa::rope_append_kernel<kPair, true, true> : sa::rope_append_kernel<kPair, true>)
+                 : (axes ? sa::rope_append_kernel<kPair, false, true> : sa::rope_append_kernel<kPair, false>);
+}
+
+sa_status check_axes(const sa_axes* axes, int n_freq) {
+  if (axes->num_axes < 1 || axes->num_axes > 8) return fail(SA_ERR_SHAPE, "%d axes (1 to 8)", axes->num_axes);
+  if (n_freq > 0 && !axes->h_axis) return fail(SA_ERR_NULL, "h_axis is NULL");
+  for (int j = 0; j < n_freq; ++j)
+    if (axes->h_axis[j] < 0 || axes->h_axis[j] >= axes->num_axes)
+      return fail(SA_ERR_SHAPE, "axis[%d] = %d outside [0, %d)", j, axes->h_axis[j], axes->num_axes);
+  return SA_OK;
+}
+
+sa_status append_rows(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const RowsCall& c, int32_t batch,
+                      sa_pages pages, void* stream) {
   sa_status s = check_sizes(layout);
   if (s != SA_OK) return s;
   if (layer < 0 || layer >= layout->num_layers)
     return fail(SA_ERR_SHAPE, "layer %d outside [0, %d)", layer, layout->num_layers);
   if (batch < 1) return fail(SA_ERR_SHAPE, "batch %d < 1", batch);
-  const int Hq = layout->num_q_heads, Hkv = layout->num_kv_heads;
+  const sa_rope* const rope = c.rope;
+  const bool queries = !c.kvq || c.q != nullptr || c.q_out != nullptr;
+  const int Hq = queries ? layout->num_q_heads : 0, Hkv = layout->num_kv_heads;
   if ((int64_t)Hq + 2 * (int64_t)Hkv > (1 << 16))
     return fail(SA_ERR_UNSUPPORTED, "%d + 2 * %d heads (at most 65536)", Hq, Hkv);
-  if (!rope) return fail(SA_ERR_NULL, "rope is NULL");
-  if (rope->rot_dim < 0 || rope->rot_dim > sa::kHD || rope->rot_dim % 16 != 0)
-    return fail(SA_ERR_UNSUPPORTED, "rot_dim %d (a multiple of 16 up to 128)", rope->rot_dim);
-  if (rope->rot_dim > 0 && !rope->h_inv_freq) return fail(SA_ERR_NULL, "h_inv_freq is NULL");
-  if ((rope->q_weight || rope->k_weight) &&
-      (!std::isfinite(rope->eps) || rope->eps < FLT_MIN || !std::isfinite(rope->weight_offset)))
-    // v_rsq takes a denormal for zero: a row of zeros would come out as 0 * inf
-    return fail(SA_ERR_SHAPE, "eps %g must be finite and at least 2^-126, weight_offset %g finite", rope->eps,
-                rope->weight_offset);
-  const int n_freq = rope->rot_dim / 2;
-  for (int j = 0; j < n_freq; ++j)
-    if (!std::isfinite(rope->h_inv_freq[j]) || rope->h_inv_freq[j] < 0. || rope->h_inv_freq[j] > 1024.)
-      return fail(SA_ERR_SHAPE, "inv_freq[%d] = %g outside [0, 1024]", j, rope->h_inv_freq[j]);
+  int n_freq = 0;
+  if (rope) {
+    if (rope->rot_dim < 0 || rope->rot_dim > sa::kHD || rope->rot_dim % 16 != 0)
+      return fail(SA_ERR_UNSUPPORTED, "rot_dim %d (a multiple of 16 up to 128)", rope->rot_dim);
+    if (rope->rot_dim > 0 && !rope->h_inv_freq) return fail(SA_ERR_NULL, "h_inv_freq is NULL");
+    if ((rope->q_weight || rope->k_weight) &&
+        (!std::isfinite(rope->eps) || rope->eps < FLT_MIN || !std::isfinite(rope->weight_offset)))
+      // v_rsq takes a denormal for zero: a row of zeros would come out as 0 * inf
+      return fail(SA_ERR_SHAPE, "eps %g must be finite and at least 2^-126, weight_offset %g finite", rope->eps,
+                  rope->weight_offset);
+    n_freq = rope->rot_dim / 2;
+    for (int j = 0; j < n_freq; ++j)
+      if (!std::isfinite(rope->h_inv_freq[j]) || rope->h_inv_freq[j] < 0. || rope->h_inv_freq[j] > 1024.)
+        return fail(SA_ERR_SHAPE, "inv_freq[%d] = %g outside [0, 1024]", j, rope->h_inv_freq[j]);
+  } else if (!c.kvq) {
+    return fail(SA_ERR_NULL, "rope is NULL");
+  } else if (queries || c.axes || c.h_pos) {
+    return fail(SA_ERR_SHAPE, "queries, positions or axes without a rope");
+  }
+  if (c.kvq && c.axes && c.h_pos) return fail(SA_ERR_SHAPE, "both h_pos and axes");
+  if (c.axes) {
+    s = check_axes(c.axes, n_freq);
+    if (s != SA_OK) return s;
+  }
   const int64_t widths[3] = {(int64_t)Hq * sa::kHD, (int64_t)Hkv * sa::kHD, (int64_t)Hkv * sa::kHD};
-  const int64_t strides[3] = {q_stride, k_stride, v_stride};
+  const int64_t strides[3] = {queries ? c.q_stride : 0, c.k_stride, c.v_stride};
   for (int i = 0; i < 3; ++i) {
     if (strides[i] < widths[i] || strides[i] > INT32_MAX)
       return fail(SA_ERR_SHAPE, "%c token stride %lld, at least %lld needed", "qkv"[i], (long long)strides[i],
@@ -1360,24 +1418,27 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
     if (strides[i] % 8 != 0) return fail(SA_ERR_ALIGN, "%c token stride %lld is not a multiple of 8", "qkv"[i],
                                          (long long)strides[i]);
   }
+  const int32_t *const h_start = c.h_start, *const h_new_len = c.h_new_len;
   if (!h_start || !h_new_len) return fail(SA_ERR_NULL, "h_start / h_new_len is NULL");
-  const int32_t* const h_rot = h_pos ? h_pos : h_start;
+  const int32_t* const h_rot = c.h_pos ? c.h_pos : h_start;
+  const PlanKind kind = c.kvq ? kPlanKvqAppend : kPlanRope;
   bool same = false;
   sa_ctx::RopeRec rec;
   if (ctx) {
-    sa_ctx::DevPlan& dp = ctx->plans[kPlanRope];
-    const int32_t head[2] = {batch, n_freq};
+    sa_ctx::DevPlan& dp = ctx->plans[kind];
+    const int32_t head[3] = {batch, n_freq, c.axes ? c.axes->num_axes : 0};
     dp.key.begin();
-    dp.key.add(head, 2);
+    dp.key.add(head, 3);
     dp.key.add(h_start, (size_t)batch);
     dp.key.add(h_new_len, (size_t)batch);
-    dp.key.add(h_rot, (size_t)batch);
+    if (!c.axes) dp.key.add(h_rot, (size_t)batch);
+    else if (n_freq > 0) dp.key.add(c.axes->h_axis, (size_t)n_freq);
     int32_t words[sa::kHD];
     if (n_freq > 0) memcpy(words, rope->h_inv_freq, n_freq * sizeof(double));
     dp.key.add(words, 2 * (size_t)n_freq);
     same = dp.reusable(dp.key.end(), (hipStream_t)stream) && !debug_checks();
     if (!same) dp.key_valid = false;
-    rec = ctx->rope_rec;
+    rec = c.kvq ? ctx->kvq_append_rec : ctx->rope_rec;
   }
   std::vector<int32_t> tok_begin;
   if (!same) {
@@ -1394,17 +1455,25 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
     }
     tok_begin[batch] = (int32_t)rec.total;
   }
-  if (!k_pool || !v_pool || !pages.indptr || !pages.indices)
+  if (c.axes && c.axes->pos_stride < rec.total)
+    return fail(SA_ERR_SHAPE, "pos_stride %lld for %lld new tokens", (long long)c.axes->pos_stride,
+                (long long)rec.total);
+  if (c.kvq && rec.total > 0 && queries && (!c.q || !c.q_out))
+    return fail(SA_ERR_SHAPE, "q and q_out go together");
+  if (!c.k_pool || !c.v_pool || !pages.indptr || !pages.indices)
     return fail(SA_ERR_NULL, "pool or page table pointer is NULL");
-  if (rec.total > 0 && (!q || !k_new || !v_new || !q_out)) return fail(SA_ERR_NULL, "a row pointer is NULL");
-  for (const void* p : {q, k_new, v_new, (const void*)q_out, (const void*)k_pool, (const void*)v_pool, rope->q_weight,
-                        rope->k_weight})
+  if (rec.total > 0 && (!c.k || !c.v || (queries && (!c.q || !c.q_out)) || (c.axes && !c.axes->d_pos)))
+    return fail(SA_ERR_NULL, "a row pointer or the axes' positions are NULL");
+  for (const void* p : {c.q, c.k, c.v, (const void*)c.q_out, (const void*)c.k_pool, (const void*)c.v_pool,
+                        rope ? rope->q_weight : nullptr, rope ? rope->k_weight : nullptr})
     if (!aligned16(p)) return fail(SA_ERR_ALIGN, "a row, weight or pool pointer is not 16-byte aligned");
+  if (c.axes && (reinterpret_cast<uintptr_t>(c.axes->d_pos) & 3u))
+    return fail(SA_ERR_ALIGN, "the axes' positions are not 4-byte aligned");
   DeviceGuard guard;
   s = check_ctx(ctx);
   if (s != SA_OK) return s;
   if (rec.total == 0) return SA_OK;
-  s = refuse_capture((hipStream_t)stream, "sa_kv_append_rope keeps its plan in the context and");
+  s = refuse_capture((hipStream_t)stream, c.name);
   if (s != SA_OK) return s;
   if (debug_checks()) {
     std::vector<int32_t> ip, ix;
@@ -1422,12 +1491,13 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   const int rows_wave = rounds * sa::kRopeRows;
   const int64_t blocks = (rec.total * ((n_rows + rows_wave - 1) / rows_wave) + 3) / 4;
   if (blocks > kMaxBlocks) return fail(SA_ERR_SHAPE, "too many new tokens for one launch");
-  uint8_t* dev = ctx->plans[kPlanRope].dev;
+  uint8_t* dev = ctx->plans[kind].dev;
   if (!same) {
     PlanImage img;
     rec.o_tok = img.add(tok_begin.data(), tok_begin.size());
     rec.o_start = img.add(h_start, (size_t)batch);
-    rec.o_pos = img.add(h_rot, (size_t)batch);
+    if (!c.axes) rec.o_pos = img.add(h_rot, (size_t)batch);
+    else rec.o_axis = img.add(c.axes->h_axis, (size_t)n_freq);
     uint64_t turns[sa::kHD / 2];                   // per position, modulo 1, in units of 2^-64
     for (int j = 0; j < n_freq; ++j) {
       const long double x = (long double)rope->h_inv_freq[j] / 6.283185307179586476925286766559L;
@@ -1435,27 +1505,30 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
       turns[j] = frac >= 18446744073709551616.0L ? 0 : (uint64_t)frac;
     }
     rec.o_freq = img.add(turns, (size_t)n_freq);
-    s = upload_plan(ctx, kPlanRope, img, (hipStream_t)stream, &dev);
+    s = upload_plan(ctx, kind, img, (hipStream_t)stream, &dev);
     if (s != SA_OK) return s;
-    ctx->rope_rec = rec;
-    ctx->plans[kPlanRope].key_valid = true;
+    (c.kvq ? ctx->kvq_append_rec : ctx->rope_rec) = rec;
+    ctx->plans[kind].key_valid = true;
   }
   sa::RopeArgs a{};
-  const int64_t lo = (int64_t)layer * layer_elems(layout);
-  a.q = (const uint16_t*)q;
-  a.k = (const uint16_t*)k_new;
-  a.v = (const uint16_t*)v_new;
-  a.q_stride = q_stride;
-  a.k_stride = k_stride;
-  a.v_stride = v_stride;
-  a.q_out = (uint16_t*)q_out;
-  a.k_pool = (uint16_t*)k_pool + lo;
-  a.v_pool = (uint16_t*)v_pool + lo;
-  a.q_weight = (const uint16_t*)rope->q_weight;
-  a.k_weight = (const uint16_t*)rope->k_weight;
+  a.q = (const uint16_t*)c.q;
+  a.k = (const uint16_t*)c.k;
+  a.v = (const uint16_t*)c.v;
+  a.q_stride = c.q_stride;
+  a.k_stride = c.k_stride;
+  a.v_stride = c.v_stride;
+  a.q_out = (uint16_t*)c.q_out;
+  if (c.kvq) {
+    const int64_t lo = (int64_t)layer * kvq_layer_bytes(layout, layout->num_slots);
+    a.kq_pool = (uint8_t*)c.k_pool + lo;
+    a.vq_pool = (uint8_t*)c.v_pool + lo;
+  } else {
+    const int64_t lo = (int64_t)layer * layer_elems(layout);
+    a.k_pool = (uint16_t*)c.k_pool + lo;
+    a.v_pool = (uint16_t*)c.v_pool + lo;
+  }
   a.tok_begin = (const int32_t*)(dev + rec.o_tok);
   a.start = (const int32_t*)(dev + rec.o_start);
-  a.pos = (const int32_t*)(dev + rec.o_pos);
   a.freq = (const uint64_t*)(dev + rec.o_freq);
   a.indptr = pages.indptr;
   a.indices = pages.indices;
@@ -1466,18 +1539,26 @@ sa_status append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   a.Hq = Hq;
   a.Hkv = Hkv;
   a.P = layout->page_size;
-  a.rot = rope->rot_dim;
-  a.eps = rope->eps;
-  a.offset = rope->weight_offset;
+  if (rope) {
+    a.q_weight = (const uint16_t*)rope->q_weight;
+    a.k_weight = (const uint16_t*)rope->k_weight;
+    a.rot = rope->rot_dim;
+    a.eps = rope->eps;
+    a.offset = rope->weight_offset;
+  }
+  if (c.axes) {
+    a.axis = (const int32_t*)(dev + rec.o_axis);
+    a.axis_pos = c.axes->d_pos;
+    a.axis_stride = c.axes->pos_stride;
+    a.num_axes = c.axes->num_axes;
+  } else {
+    a.pos = (const int32_t*)(dev + rec.o_pos);
+  }
   a.rounds = rounds;
   const bool streams = rec.total * n_rows * sa::kHD * 4 > sa::kRopeStreamBytes;
-  const sa::RopePair pair = rope->interleaved ? sa::kPairInLane : rope->rot_dim == sa::kHD ? sa::kPairFull : sa::kPairAny;
-  auto kernel = pair == sa::kPairInLane ? (streams ? sa::rope_append_kernel<sa::kPairInLane, true>
-                                                   : sa::rope_append_kernel<sa::kPairInLane, false>)
-              : pair == sa::kPairFull   ? (streams ? sa::rope_append_kernel<sa::kPairFull, true>
-                                                   : sa::rope_append_kernel<sa::kPairFull, false>)
-                                        : (streams ? sa::rope_append_kernel<sa::kPairAny, true>
-                                                   : sa::rope_append_kernel<sa::kPairAny, false>);
+  auto kernel = rope && rope->interleaved             ? rows_kernel<sa::kPairInLane>(streams, c.axes, c.kvq)
+                : rope && rope->rot_dim == sa::kHD    ? rows_kernel<sa::kPairFull>(streams, c.axes, c.kvq)
+                                                      : rows_kernel<sa::kPairAny>(streams, c.axes, c.kvq);
   launch_timed(kernel, dim3((unsigned)blocks), dim3(256), (hipStream_t)stream, ctx->kernel_ev[SA_TIMED_PAGES], a);
   SA_HIP(hipGetLastError());
   return SA_OK;
@@ -1859,6 +1940,170 @@ sa_status shared_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const
   return SA_OK;
 }
 
+// ------------------------------------------------------------ a cache of 4 bits
+
+// SA_DEBUG check of a conversion's slot lists: within their pools, destinations not repeated.
+sa_status debug_convert(const int32_t* d_slots, int64_t num_slots, const int32_t* d_slots4, int64_t num_slots4,
+                        int32_t n, bool pack, hipStream_t stream) {
+  std::vector<int32_t> x((size_t)n), x4((size_t)n);
+  SA_HIP(hipStreamSynchronize(stream));
+  SA_HIP(hipMemcpy(x.data(), d_slots, sizeof(int32_t) * n, hipMemcpyDeviceToHost));
+  SA_HIP(hipMemcpy(x4.data(), d_slots4, sizeof(int32_t) * n, hipMemcpyDeviceToHost));
+  for (int i = 0; i < n; ++i)
+    if (x[i] < 0 || x[i] >= num_slots || x4[i] < 0 || x4[i] >= num_slots4)
+      return fail(SA_ERR_RANGE, "page %d: slot %d of %lld, 4-bit slot %d of %lld", i, x[i], (long long)num_slots, x4[i],
+                  (long long)num_slots4);
+  std::vector<int32_t>& to = pack ? x4 : x;
+  std::sort(to.begin(), to.end());
+  const auto twice = std::adjacent_find(to.begin(), to.end());
+  if (twice != to.end()) return fail(SA_ERR_OVERLAP, "slot %d is written twice", *twice);
+  return SA_OK;
+}
+
+sa_status kvq_convert(sa_ctx* ctx, const sa_layout* layout, bool pack, const void* k_pool, const void* v_pool,
+                      const int32_t* d_slots, int64_t num_slots4, const void* kq_pool, const void* vq_pool,
+                      const int32_t* d_slots4, int32_t num_pages, void* stream) {
+  sa_status s = check_sizes(layout);
+  if (s != SA_OK) return s;
+  if (num_slots4 < 1 || num_slots4 > INT32_MAX - sa::kScanChunk)
+    return fail(SA_ERR_SHAPE, "num_slots4 %lld", (long long)num_slots4);
+  if (num_pages < 0) return fail(SA_ERR_SHAPE, "num_pages %d", num_pages);
+  if ((int64_t)num_pages * layout->num_layers * 2 > kMaxBlocks || layout->num_layers > 32767)
+    return fail(SA_ERR_SHAPE, "%d pages of %d layers are too many for one launch", num_pages, layout->num_layers);
+  if (!k_pool || !v_pool || !kq_pool || !vq_pool || (num_pages > 0 && (!d_slots || !d_slots4)))
+    return fail(SA_ERR_NULL, "a pool or slot list is NULL");
+  if (!aligned16(k_pool) || !aligned16(v_pool) || !aligned16(kq_pool) || !aligned16(vq_pool))
+    return fail(SA_ERR_ALIGN, "pool pointer not 16-byte aligned");
+  DeviceGuard guard;
+  s = check_ctx(ctx);
+  if (s != SA_OK) return s;
+  if (num_pages == 0) return SA_OK;
+  if (debug_checks() && refuse_capture((hipStream_t)stream, "") == SA_OK) {
+    s = debug_convert(d_slots, layout->num_slots, d_slots4, num_slots4, num_pages, pack, (hipStream_t)stream);
+    if (s != SA_OK) return s;
+  }
+  sa::KvqConvArgs a{};
+  a.k = (uint16_t*)const_cast<void*>(k_pool);
+  a.v = (uint16_t*)const_cast<void*>(v_pool);
+  a.k4 = (uint8_t*)const_cast<void*>(kq_pool);
+  a.v4 = (uint8_t*)const_cast<void*>(vq_pool);
+  a.slots = d_slots;
+  a.slots4 = d_slots4;
+  a.err = ctx->d_err;
+  a.num_slots = layout->num_slots;
+  a.num_slots4 = num_slots4;
+  a.Hkv = layout->num_kv_heads;
+  a.P = layout->page_size;
+  launch_timed(pack ? sa::kvq_convert_kernel<true> : sa::kvq_convert_kernel<false>,
+               dim3((unsigned)num_pages, (unsigned)(2 * layout->num_layers)), dim3(256), (hipStream_t)stream,
+               ctx->kernel_ev[SA_TIMED_PAGES], a);
+  SA_HIP(hipGetLastError());
+  return SA_OK;
+}
+
+template <int P>
+void launch_kvq_attn(int cls, unsigned blocks, hipStream_t st, const hipEvent_t* ev, const sa::KvqAttnArgs& a) {
+  launch_timed(cls == 0   ? sa::attn_kvq_kernel<P, 1>
+               : cls == 1 ? sa::attn_kvq_kernel<P, 2>
+                          : sa::attn_kvq_kernel<P, 4>,
+               dim3(blocks), dim3(256), st, ev, a);
+}
+
+sa_status kvq_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const void* q, const void* kq_pool,
+                   const void* vq_pool, int32_t batch, const int32_t* h_q_len, const int32_t* h_kv_len, sa_pages pages,
+                   bool causal, float softmax_scale, void* o, float* lse, void* stream) {
+  sa_status s = check_sizes(layout);
+  if (s != SA_OK) return s;
+  // a call with the heads and lengths of the last one has its plan on the device, and its lengths passed the checks
+  bool same = false;
+  sa_ctx::KvqRec rec;
+  if (ctx && sa::check_attn_call(layout, layer, batch, h_q_len, h_kv_len, softmax_scale, g_err) == SA_OK) {
+    sa_ctx::DevPlan& dp = ctx->plans[kPlanKvqAttn];
+    const int32_t head[4] = {layout->num_q_heads, layout->num_kv_heads, batch, causal};
+    dp.key.begin();
+    dp.key.add(head, 4);
+    dp.key.add(h_q_len, (size_t)batch);
+    dp.key.add(h_kv_len, (size_t)batch);
+    same = dp.reusable(dp.key.end(), (hipStream_t)stream);
+    if (!same) dp.key_valid = false;
+    rec = ctx->kvq_rec;
+  }
+  if (!same) {
+    rec = sa_ctx::KvqRec{};
+    s = sa::kvq_attn_check(layout, layer, batch, h_q_len, h_kv_len, causal, softmax_scale, rec.total_q, rec.total_kv,
+                           g_err);
+    if (s != SA_OK) return s;
+  }
+  if (rec.total_q > 0 && (!q || !o)) return fail(SA_ERR_NULL, "q / o is NULL");
+  if (!kq_pool || !vq_pool || !pages.indptr || (rec.total_kv > 0 && !pages.indices))
+    return fail(SA_ERR_NULL, "pool or page table pointer is NULL");
+  if (!aligned16(q) || !aligned16(o) || !aligned16(kq_pool) || !aligned16(vq_pool) ||
+      (reinterpret_cast<uintptr_t>(lse) & 3u))
+    return fail(SA_ERR_ALIGN, "q, o, pools must be 16-byte aligned (lse 4-byte)");
+  DeviceGuard guard;
+  s = check_ctx(ctx);
+  if (s != SA_OK) return s;
+  if (rec.total_q == 0) return SA_OK;
+  s = refuse_capture((hipStream_t)stream, "sa_kvq_attn keeps its plan in the context and");
+  if (s != SA_OK) return s;
+  uint8_t* dev = ctx->plans[kPlanKvqAttn].dev;
+  if (!same) {
+    sa::KvqPlan plan;
+    s = sa::plan_kvq_items(layout, batch, h_q_len, h_kv_len, causal, ctx->num_cu, plan, g_err);
+    if (s != SA_OK) return s;
+    PlanImage img;
+    for (int i = 0; i < sa::kKvqClasses; ++i) {
+      rec.n_items[i] = plan.items[i].size();
+      rec.o_it[i] = img.add(plan.items[i].data(), plan.items[i].size());
+    }
+    rec.n_units = plan.units.size();
+    rec.o_un = img.add(plan.units.data(), plan.units.size());
+    rec.part_rows = plan.part_rows;
+    rec.most_rows = plan.most_rows;
+    rec.block_rows = sa::merge_block_rows(plan.most_parts);
+    s = upload_plan(ctx, kPlanKvqAttn, img, (hipStream_t)stream, &dev);
+    if (s != SA_OK) return s;
+    ctx->kvq_rec = rec;
+    ctx->plans[kPlanKvqAttn].key_valid = true;
+  }
+  s = reserve_parts(ctx, (size_t)rec.part_rows * (sa::kHD + 1) * sizeof(float));
+  if (s != SA_OK) return s;
+  sa::KvqAttnArgs a{};
+  const int64_t lo = (int64_t)layer * kvq_layer_bytes(layout, layout->num_slots);
+  a.q = (const uint16_t*)q;
+  a.k = (const uint8_t*)kq_pool + lo;
+  a.v = (const uint8_t*)vq_pool + lo;
+  a.o = (uint16_t*)o;
+  a.lse = lse;
+  a.part_o = ctx->part;
+  a.part_lse = ctx->part + (size_t)rec.part_rows * sa::kHD;
+  a.indptr = pages.indptr;
+  a.indices = pages.indices;
+  a.err = ctx->d_err;
+  a.num_slots = (int32_t)layout->num_slots;
+  a.Hq = layout->num_q_heads;
+  a.Hkv = layout->num_kv_heads;
+  a.G = a.Hq / a.Hkv;
+  a.causal = causal;
+  a.c = softmax_scale * 1.4426950408889634f;
+  for (int i = 0; i < sa::kKvqClasses; ++i) {
+    if (rec.n_items[i] == 0) continue;
+    a.items = (const sa::AttnItem*)(dev + rec.o_it[i]);
+    if (layout->page_size == 16)
+      launch_kvq_attn<16>(i, (unsigned)rec.n_items[i], (hipStream_t)stream, ctx->kernel_ev[SA_TIMED_ATTN], a);
+    else
+      launch_kvq_attn<32>(i, (unsigned)rec.n_items[i], (hipStream_t)stream, ctx->kernel_ev[SA_TIMED_ATTN], a);
+    SA_HIP(hipGetLastError());
+  }
+  if (rec.n_units > 0) {
+    sa::MergeRowsArgs m{a.part_o, a.part_lse, (const sa::MergeUnit*)(dev + rec.o_un), a.o, lse, a.Hq, a.Hkv, a.G, rec.block_rows};
+    const dim3 blocks((unsigned)(rec.n_units * a.Hkv), (unsigned)((rec.most_rows + rec.block_rows - 1) / rec.block_rows));
+    hipLaunchKernelGGL(sa::merge_rows_kernel, blocks, dim3(256), 0, (hipStream_t)stream, m);
+    SA_HIP(hipGetLastError());
+  }
+  return SA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1869,8 +2114,9 @@ sa_status sa_kv_append_rope(sa_ctx* ctx, const sa_layout* layout, int32_t layer,
                             const int32_t* h_start, const int32_t* h_new_len, const int32_t* h_pos, sa_pages pages,
                             void* stream) {
   return no_throw([&] {
-    return append_rope(ctx, layout, layer, rope, q, q_stride, k_new, k_stride, v_new, v_stride, q_out, k_pool, v_pool,
-                       batch, h_start, h_new_len, h_pos, pages, stream);
+    const RowsCall c{"sa_kv_append_rope keeps its plan in the context and", false, rope, nullptr, q, q_stride, k_new,
+                     k_stride, v_new, v_stride, q_out, k_pool, v_pool, h_start, h_new_len, h_pos};
+    return append_rows(ctx, layout, layer, c, batch, pages, stream);
   });
 }
 
@@ -1951,6 +2197,59 @@ sa_status sa_shared_plan_stats(const sa_layout* layout, int32_t batch, const int
     if (h_once != nullptr)
       for (int g = 0; g < num_groups; ++g) h_once[g] = plan.shared && plan.once[g];
     return SA_OK;
+  });
+}
+
+
+sa_status sa_kv_append_rope_axes(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const sa_rope* rope,
+                                 const sa_axes* axes, const void* q, int64_t q_stride, const void* k_new,
+                                 int64_t k_stride, const void* v_new, int64_t v_stride, void* q_out, void* k_pool,
+                                 void* v_pool, int32_t batch, const int32_t* h_start, const int32_t* h_new_len,
+                                 sa_pages pages, void* stream) {
+  return no_throw([&] {
+    if (!axes) return fail(SA_ERR_NULL, "axes is NULL");
+    const RowsCall c{"sa_kv_append_rope_axes keeps its plan in the context and", false, rope, axes, q, q_stride, k_new,
+                     k_stride, v_new, v_stride, q_out, k_pool, v_pool, h_start, h_new_len, nullptr};
+    return append_rows(ctx, layout, layer, c, batch, pages, stream);
+  });
+}
+
+sa_status sa_kvq_append(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const sa_rope* rope, const sa_axes* axes,
+                        const void* q, int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new,
+                        int64_t v_stride, void* q_out, void* kq_pool, void* vq_pool, int32_t batch,
+                        const int32_t* h_start, const int32_t* h_new_len, const int32_t* h_pos, sa_pages pages,
+                        void* stream) {
+  return no_throw([&] {
+    const RowsCall c{"sa_kvq_append keeps its plan in the context and", true, rope, axes, q, q_stride, k_new, k_stride,
+                     v_new, v_stride, q_out, kq_pool, vq_pool, h_start, h_new_len, h_pos};
+    return append_rows(ctx, layout, layer, c, batch, pages, stream);
+  });
+}
+
+sa_status sa_kvq_pack(sa_ctx* ctx, const sa_layout* layout, const void* k_pool, const void* v_pool,
+                      const int32_t* d_slots, int64_t num_slots4, void* kq_pool, void* vq_pool, const int32_t* d_slots4,
+                      int32_t num_pages, void* stream) {
+  return no_throw([&] {
+    return kvq_convert(ctx, layout, true, k_pool, v_pool, d_slots, num_slots4, kq_pool, vq_pool, d_slots4, num_pages,
+                       stream);
+  });
+}
+
+sa_status sa_kvq_unpack(sa_ctx* ctx, const sa_layout* layout, int64_t num_slots4, const void* kq_pool,
+                        const void* vq_pool, const int32_t* d_slots4, void* k_pool, void* v_pool,
+                        const int32_t* d_slots, int32_t num_pages, void* stream) {
+  return no_throw([&] {
+    return kvq_convert(ctx, layout, false, k_pool, v_pool, d_slots, num_slots4, kq_pool, vq_pool, d_slots4, num_pages,
+                       stream);
+  });
+}
+
+sa_status sa_kvq_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const void* q, const void* kq_pool,
+                      const void* vq_pool, int32_t batch, const int32_t* h_q_len, const int32_t* h_kv_len,
+                      sa_pages pages, int32_t causal, float softmax_scale, void* o, float* lse, void* stream) {
+  return no_throw([&] {
+    return kvq_attn(ctx, layout, layer, q, kq_pool, vq_pool, batch, h_q_len, h_kv_len, pages, causal != 0,
+                    softmax_scale, o, lse, stream);
   });
 }
 
