@@ -14,8 +14,11 @@
 namespace sa {
 
 constexpr int kKvqKeys = 64;                 // keys of a tile
-constexpr int kKvqClasses = 3;               // row tiles of 16, 32 and 64 packed rows
-constexpr int kKvqRows[kKvqClasses] = {16, 32, 64};
+// Classes of items by their packed rows: up to 16 and 32, whose waves split the keys, and
+// up to 64 and 128, whose waves split the rows.
+constexpr int kKvqClasses = 4;
+constexpr int kKvqRows[kKvqClasses] = {16, 32, 64, 128};
+constexpr int kKvqCost[kKvqClasses] = {4, 5, 12, 16};   // of a tile of keys, relative
 constexpr int32_t kKvqMaxLen = INT32_MAX / kKvqKeys * kKvqKeys;   // the end of its last tile fits an int32
 constexpr int64_t kKvqMaxItems = int64_t(1) << 22;   // work items before they are cut
 
@@ -46,11 +49,12 @@ inline sa_status kvq_attn_check(const sa_layout* layout, int32_t layer, int32_t 
   return SA_OK;
 }
 
-// Items of up to kKvqRows packed rows, the smallest tile that holds a sequence's rows or
-// the largest, each cut by key range into parts of at most `chunk` tiles.
+// Row tiles of kKvqRows rows, the last one of a sequence in the smallest class that
+// holds it, each cut by key range into parts of about equal cost.
 inline sa_status plan_kvq_items(const sa_layout* layout, int32_t batch, const int32_t* h_q_len, const int32_t* h_kv_len,
                                 bool causal, int num_cu, KvqPlan& out, std::string& err) {
   const int Hkv = layout->num_kv_heads, G = layout->num_q_heads / Hkv;
+  constexpr int kMost = kKvqRows[kKvqClasses - 1];
   out = KvqPlan{};
   struct Tile {
     int seq, row0, rows, cls, keys, q_start;
@@ -60,25 +64,25 @@ inline sa_status plan_kvq_items(const sa_layout* layout, int32_t batch, const in
   int32_t q_start = 0;
   for (int b = 0; b < batch; ++b) {
     const int rows = h_q_len[b] * G;
-    int cls = 0;
-    while (cls + 1 < kKvqClasses && rows > kKvqRows[cls]) ++cls;
-    n_items += (int64_t)Hkv * ((rows + kKvqRows[cls] - 1) / kKvqRows[cls]);
+    n_items += (int64_t)Hkv * ((rows + kMost - 1) / kMost);
     if (n_items > kKvqMaxItems)
       return plan_fail(err, SA_ERR_SHAPE, "too many query rows for one launch (%lld work items)", (long long)n_items);
-    for (int r0 = 0; r0 < rows; r0 += kKvqRows[cls]) {
-      const int n = std::min(kKvqRows[cls], rows - r0);
+    for (int r0 = 0; r0 < rows; r0 += kMost) {
+      const int n = std::min(kMost, rows - r0);
+      int cls = 0;
+      while (n > kKvqRows[cls]) ++cls;
       const int keys = causal ? h_kv_len[b] - h_q_len[b] + (r0 + n - 1) / G + 1 : h_kv_len[b];
       tiles.push_back({b, r0, n, cls, keys, q_start});
-      work += (int64_t)Hkv * ((keys + kKvqKeys - 1) / kKvqKeys);
+      work += (int64_t)Hkv * kKvqCost[cls] * ((keys + kKvqKeys - 1) / kKvqKeys);
     }
     q_start += h_q_len[b];
   }
-  const int64_t chunk = std::max<int64_t>(8, (work + 2 * num_cu - 1) / (2 * num_cu));
+  const int64_t share = std::max<int64_t>(32, (work + 2 * num_cu - 1) / (2 * num_cu));
   for (const Tile& t : tiles) {
     const int n_tiles = (t.keys + kKvqKeys - 1) / kKvqKeys;
-    const int parts = std::max<int>(1, (int)((n_tiles + chunk - 1) / chunk));
-    const int per = (n_tiles + parts - 1) / parts;
-    const int used = n_tiles == 0 ? 1 : (n_tiles + per - 1) / per;
+    const int parts = (int)std::max<int64_t>(1, ((int64_t)n_tiles * kKvqCost[t.cls] + share - 1) / share);
+    const int per = std::max(1, (n_tiles + parts - 1) / parts);
+    const int used = std::max(1, (n_tiles + per - 1) / per);
     const int64_t row = out.part_rows;
     if (used > 1) {
       out.units.push_back({t.q_start, t.row0, t.rows, (int32_t)row, used, t.rows, 0, 0, 0});

@@ -2005,7 +2005,8 @@ template <int P>
 void launch_kvq_attn(int cls, unsigned blocks, hipStream_t st, const hipEvent_t* ev, const sa::KvqAttnArgs& a) {
   launch_timed(cls == 0   ? sa::attn_kvq_kernel<P, 1>
                : cls == 1 ? sa::attn_kvq_kernel<P, 2>
-                          : sa::attn_kvq_kernel<P, 4>,
+               : cls == 2 ? sa::attn_kvq_rows_kernel<P, 1>
+                          : sa::attn_kvq_rows_kernel<P, 2>,
                dim3(blocks), dim3(256), st, ev, a);
 }
 

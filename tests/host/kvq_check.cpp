@@ -35,7 +35,7 @@ static void check(const sa_layout& L, const std::vector<int32_t>& q, const std::
     for (const sa::AttnItem& it : plan.items[c]) {
       CHECK(it.seq >= 0 && it.seq < B && it.kvh >= 0 && it.kvh < L.num_kv_heads);
       CHECK(it.q_start == q_start[it.seq] && it.q_len == q[it.seq] && it.kv_len == kv[it.seq]);
-      CHECK(it.row0 % sa::kKvqRows[c] == 0 && it.row0 < it.q_len * G);
+      CHECK(it.row0 % 128 == 0 && it.row0 < it.q_len * G);
       CHECK(it.kv_begin % sa::kKvqKeys == 0 && it.kv_begin <= it.kv_end && it.kv_end <= it.kv_len);
       tiles[{it.seq, it.kvh, it.row0}].push_back({it.kv_begin, it.kv_end, it.part, c});
     }
@@ -58,7 +58,8 @@ static void check(const sa_layout& L, const std::vector<int32_t>& q, const std::
         CHECK(found != tiles.end());
         auto parts = found->second;
         ++n_tiles;
-        step = sa::kKvqRows[parts[0].cls];
+        step = 128;
+        for (const Part& x : parts) CHECK(std::min(128, rows - r0) <= sa::kKvqRows[x.cls] && x.cls == parts[0].cls);
         const int n = std::min(step, rows - r0);
         const int keys = causal ? kv[b] - q[b] + (r0 + n - 1) / G + 1 : kv[b];
         std::sort(parts.begin(), parts.end(), [](const Part& x, const Part& y) { return x.begin < y.begin; });
