@@ -28,6 +28,8 @@
 #include "kvq_kernels.h"
 #include "kvq_plan.h"
 
+#include <type_traits>
+
 namespace sa {
 
 struct KvqAttnArgs {
@@ -44,7 +46,7 @@ struct KvqAttnArgs {
   int32_t* err;
   int32_t num_slots, Hq, Hkv, G;
   int32_t causal;
-  float c;                   // softmax scale times log2 e
+  float c;                   // softmax scale times log2 e, which goes into the query rows
 };
 
 // What absent pages read as: codes and scale bytes of 0.
@@ -52,11 +54,12 @@ static __device__ uint8_t kvq_zero_page[32 * kKvqRow];
 
 typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x32 __attribute__((ext_vector_type(32)));
+typedef float f32x32 __attribute__((ext_vector_type(32)));
 
-// 32 dims of a query row as three 6-bit pieces; scales: their bytes (255: the block holds
-// an infinity or a NaN).
-__device__ __forceinline__ void kvq_split_q(const uint16_t* p, u32x6 (&piece)[3], int& scales) {
+// c times 32 dims of a query row as three 6-bit pieces; scales: their bytes (255: the
+// block holds an infinity or a NaN).  Every rest is exact: hardly more than the bits
+// that the piece before it left.
+__device__ __forceinline__ void kvq_split_q(const uint16_t* p, float c, u32x6 (&piece)[3], int& scales) {
   u32x4 w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = ld_u32x4(p + 8 * i);
@@ -65,35 +68,37 @@ __device__ __forceinline__ void kvq_split_q(const uint16_t* p, u32x6 (&piece)[3]
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) top = max(top, max(w[i][e] & 0x7FFF0000u, (w[i][e] << 16) & 0x7FFF0000u));
+  top = top < 0x7F800000u ? __float_as_uint(__uint_as_float(top) * c) : top;
   const bool fine = top < 0x7F800000u;
   const int s = max((int)(top >> 23) - 2, 10);               // the block's largest is 4 to 8 times the scale
-  bf16x32 x;
+  f32x16 even, odd;                                          // dims 2 i and 2 i + 1, as the conversion takes them
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bf16x2 two = __builtin_bit_cast(bf16x2, fine ? w[i][e] : 0u);
-      x[8 * i + 2 * e] = two[0];
-      x[8 * i + 2 * e + 1] = two[1];
-    }
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t two = fine ? w[i >> 2][i & 3] : 0u;
+    even[i] = __uint_as_float(two << 16) * c;
+    odd[i] = __uint_as_float(two & 0xFFFF0000u) * c;
+  }
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
     const float unit = __uint_as_float((uint32_t)(s - 4 * k) << 23);
-    piece[k] = __builtin_bit_cast(u32x6, __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x, unit));
+    const auto six = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, unit);
+    piece[k] = __builtin_bit_cast(u32x6, six);
     if (k == 2) break;
-    const bf16x32 back = __builtin_amdgcn_cvt_scalef32_pk32_bf16_fp6(__builtin_bit_cast(decltype(__builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x, unit)), piece[k]), unit);
+    const f32x32 back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(six, unit);
 #pragma unroll
-    for (int d = 0; d < 32; ++d) x[d] = (__bf16)((float)x[d] - (float)back[d]);   // exact: at most x's own bits are left
+    for (int i = 0; i < 16; ++i) {
+      even[i] -= back[2 * i];
+      odd[i] -= back[2 * i + 1];
+    }
   }
   scales = fine ? s | (s - 4) << 8 | (s - 8) << 16 : 0xFFFFFF;
 }
 
-// S += 16 keys (codes and scale byte kScale of `scales`) times 16 query rows in pieces,
+// s plus 16 keys (codes and scale byte kScale of `scales`) times 16 query rows in pieces,
 // the smallest first.
 template <int kScale>
-__device__ __forceinline__ f32x4 kvq_scores(u32x4 key, uint32_t scales, const u32x6 (&q)[3], int q_scales) {
+__device__ __forceinline__ f32x4 kvq_scores(u32x4 key, uint32_t scales, const u32x6 (&q)[3], int q_scales, f32x4 s) {
   const i32x8 a = {(int)key[0], (int)key[1], (int)key[2], (int)key[3], 0, 0, 0, 0};
-  f32x4 s{};
   auto piece = [&](const u32x6& w) __attribute__((always_inline)) {
     return i32x8{(int)w[0], (int)w[1], (int)w[2], (int)w[3], (int)w[4], (int)w[5], 0, 0};
   };
@@ -116,7 +121,13 @@ __device__ __forceinline__ float row4_sum(float x) {
 }
 
 constexpr int kKvqWaves = 4;
-constexpr int kKvqHalf = 32 * kHD * 2;       // 32 keys of bf16 values: one wave's LDS
+// Bytes of a key's bf16 values in LDS: 32 more than they take, so that the 8 keys x 32
+// bytes of half a wave's transposed reads, and the 8 rows' chunks of a quarter's
+// writes, lie in different banks.
+constexpr int kKvqVRow = kHD * 2 + 32;
+constexpr int kKvqHalf = 32 * kKvqVRow;      // 32 keys: one wave's LDS where the waves split the keys
+
+typedef __attribute__((address_space(3))) float KvqStats[2][kKvqWaves][16];   // of 16 rows: m and l of each wave
 
 // One tile of 64 keys as loaded: 16-key block kb, lane l key l % 16, block l / 16 of its dims.
 struct KvqTile {
@@ -125,11 +136,9 @@ struct KvqTile {
 };
 
 template <int P, int kNB>
-__global__ __launch_bounds__(256, kNB == 1 ? 3 : kNB == 2 ? 2 : 1) void attn_kvq_kernel(KvqAttnArgs a) {
+__device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const AttnItem& it, lds_u8* lds, KvqStats* stats_p) {
   static_assert(P == 16 || P == 32, "page size");
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[kKvqWaves * kKvqHalf];
-  __shared__ float stats[2][kKvqWaves][16];
-  const AttnItem it = ld_uniform(a.items + blockIdx.x);
+  auto& stats = *stats_p;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, r16 = lane & 15;
@@ -137,7 +146,7 @@ __global__ __launch_bounds__(256, kNB == 1 ? 3 : kNB == 2 ? 2 : 1) void attn_kvq
   const int pre = it.kv_len - it.q_len;
   const int32_t pt_base = ld_uniform(a.indptr + it.seq);
   const int32_t pt_count = ld_uniform(a.indptr + it.seq + 1) - pt_base;
-  lds_u8* const vbuf = (lds_u8*)lds + wave * kKvqHalf;
+  lds_u8* const vbuf = lds + wave * kKvqHalf;
 
   // this wave's tiles
   constexpr int kKeys = 64;
@@ -178,6 +187,7 @@ __global__ __launch_bounds__(256, kNB == 1 ? 3 : kNB == 2 ? 2 : 1) void attn_kvq
       x.vs[kb] = vp[scale_off + kIn[kb] * 4];
     }
   };
+  const int tr_at = (4 * g + (r16 >> 2)) * kKvqVRow + 8 * (r16 & 3);   // this lane's source of a transposed read
   KvqTile now, next;
   if (t0 < t1) load_tile(t0, now);
 
@@ -190,7 +200,7 @@ __global__ __launch_bounds__(256, kNB == 1 ? 3 : kNB == 2 ? 2 : 1) void attn_kvq
     const int tok = rr / G;
     const int head = it.kvh * G + (rr - tok * G);
     limit[nb] = min(it.kv_end, a.causal ? pre + tok + 1 : it.kv_len);
-    kvq_split_q(a.q + ((int64_t)(it.q_start + tok) * a.Hq + head) * kHD + g * 32, q[nb], qs[nb]);
+    kvq_split_q(a.q + ((int64_t)(it.q_start + tok) * a.Hq + head) * kHD + g * 32, a.c, q[nb], qs[nb]);
   }
   // keys below are seen by all rows
   const int all_see = min(it.kv_end, a.causal ? pre + it.row0 / G + 1 : it.kv_len);
@@ -239,7 +249,7 @@ __global__ __launch_bounds__(256, kNB == 1 ? 3 : kNB == 2 ? 2 : 1) void attn_kvq
       f32x4 s[4];
 #pragma unroll
       for (int kb = 0; kb < 4; ++kb) {
-        s[kb] = kvq_scores<0>(now.k[kb], now.ks[kb], q[nb], qs[nb]);
+        s[kb] = kvq_scores<0>(now.k[kb], now.ks[kb], q[nb], qs[nb], f32x4{});
       }
       if (masked) {
 #pragma unroll
@@ -251,7 +261,7 @@ __global__ __launch_bounds__(256, kNB == 1 ? 3 : kNB == 2 ? 2 : 1) void attn_kvq
       float top = s[0][0];
 #pragma unroll
       for (int j = 1; j < 16; ++j) top = vmax(top, s[j >> 2][j & 3]);
-      const float grown = vmax(m[nb], row4_max(top) * a.c);
+      const float grown = vmax(m[nb], row4_max(top));
       if (__ballot(!(grown == m[nb]))) {
         const float f = exp2f_fast(m[nb] - (grown == -INFINITY ? 0.f : grown));
         l[nb] *= f;
@@ -264,33 +274,29 @@ __global__ __launch_bounds__(256, kNB == 1 ? 3 : kNB == 2 ? 2 : 1) void attn_kvq
       for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float e = exp2f_fast(__builtin_fmaf(s[kb][i], a.c, -off));
+          const float e = exp2f_fast(s[kb][i] - off);
           l[nb] += e;
           p[nb][kb >> 1][4 * (kb & 1) + i] = (__bf16)e;
         }
     }
     // O^T += V^T P^T, 32 keys at a time.  Element j of a lane's operands is key
-    // 16 (j / 4) + 4 g + j % 4 of them.  16-byte chunks of an LDS row are XORed by its
-    // key, so that a column of 16 rows' chunks, and the transposed reads of 16 rows x 32
-    // bytes, touch every bank alike.
+    // 16 (j / 4) + 4 g + j % 4 of them.
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
         const u32x4 w = now.v[2 * half + kb];
-        lds_u8* const row = vbuf + (16 * kb + r16) * (kHD * 2);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          *(__attribute__((address_space(3))) u32x4*)(row + (((4 * g + j) ^ r16) << 4)) = kvq_values(w[j], now.vs[2 * half + kb]);
+          *(__attribute__((address_space(3))) u32x4*)(vbuf + (16 * kb + r16) * kKvqVRow + 64 * g + 16 * j) =
+              kvq_values(w[j], now.vs[2 * half + kb]);
       }
-      const int tr_key = 4 * g + (r16 >> 2);
 #pragma unroll
       for (int db = 0; db < 8; ++db) {
         bf16x8 v;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-          const auto four = lds_read_tr(vbuf + (16 * kb + tr_key) * (kHD * 2) + (((2 * db + ((r16 >> 1) & 1)) ^ tr_key) << 4) +
-                                    (r16 & 1) * 8);
+          const auto four = lds_read_tr(vbuf + tr_at + 16 * kb * kKvqVRow + 32 * db);
 #pragma unroll
           for (int i = 0; i < 4; ++i) v[4 * kb + i] = four[i];
         }
@@ -332,7 +338,7 @@ __global__ __launch_bounds__(256, kNB == 1 ? 3 : kNB == 2 ? 2 : 1) void attn_kvq
       den += f * stats[1][w][r];
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-        num[i] += f * *(__attribute__((address_space(3))) f32x4*)((lds_u8*)lds + w * kKvqHalf + r * (kHD * 4) + (((2 * ch + i) ^ r) << 4));
+        num[i] += f * *(__attribute__((address_space(3))) f32x4*)(lds + w * kKvqHalf + r * (kHD * 4) + (((2 * ch + i) ^ r) << 4));
     }
     const float inv = den == 0.f ? 0.f : 1.f / den;
     const float log2sum = den == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(den);
@@ -362,15 +368,19 @@ __global__ __launch_bounds__(256, kNB == 1 ? 3 : kNB == 2 ? 2 : 1) void attn_kvq
 // step t - 1 LDS holds the values of tile t (bf16) and the codes of the keys of t + 1;
 // step t writes the values of t + 1 and the keys of t + 2 from registers, whose
 // loads were issued a step before.
+constexpr int kKvqTile = 64 * kKvqVRow, kKvqKeyBytes = 64 * kKvqCodes;
+struct KvqRowsLds {
+  uint8_t v[2][kKvqTile];
+  uint8_t k[2][kKvqKeyBytes];
+  uint64_t nan[2][4];        // masked tiles: bit 16 g + r16 of a 16-key block, a value block that is NaN
+  uint32_t ks[2][64];        // lane (key r16, block g): the scale bytes of the four 16-key blocks
+};
+
 template <int P, int kNB>
-__global__ __launch_bounds__(256, 2) void attn_kvq_rows_kernel(KvqAttnArgs a) {
+__device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const AttnItem& it,
+                                               __attribute__((address_space(3))) KvqRowsLds* lds) {
   static_assert(P == 16 || P == 32, "page size");
-  constexpr int kTile = 64 * kHD * 2, kKeyBytes = 64 * kKvqCodes;
-  __shared__ __attribute__((aligned(1024))) uint8_t v_lds[2][kTile];
-  __shared__ __attribute__((aligned(1024))) uint8_t k_lds[2][kKeyBytes];
-  __shared__ uint32_t ks_lds[2][64];           // lane (key r16, block g): the scale bytes of the four 16-key blocks
-  __shared__ uint64_t nan_lds[2][4];           // masked tiles: bit 16 g + r16 of a 16-key block, a value block that is NaN
-  const AttnItem it = ld_uniform(a.items + blockIdx.x);
+  constexpr int kTile = kKvqTile, kKeyBytes = kKvqKeyBytes;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, r16 = lane & 15;
@@ -383,10 +393,10 @@ __global__ __launch_bounds__(256, 2) void attn_kvq_rows_kernel(KvqAttnArgs a) {
   // keys below are seen by all rows of the item
   const int all_see = min(it.kv_end, a.causal ? pre + it.row0 / G + 1 : it.kv_len);
 
-  // this wave stages 16-key block `wave` of every tile; lane i has the slot of tile ts + i
+  // This wave stages 16-key block `wave` of every tile; lane i has the slot of tile ts + i.
+  // Keys run a tile or two ahead of values, so the values' slots follow the keys'.
   bool bad = false;
-  int ts = t0;
-  auto load_slots = [&]() __attribute__((always_inline)) {
+  auto load_slots = [&](int ts) __attribute__((always_inline)) {
     const int64_t key = (int64_t)(ts + lane) * kKeys + 16 * wave;
     const bool need = key < it.kv_end;
     const int pg = (int)(key / P);
@@ -395,9 +405,19 @@ __global__ __launch_bounds__(256, 2) void attn_kvq_rows_kernel(KvqAttnArgs a) {
     bad |= need && s < 0;
     return s;
   };
-  int32_t slots = load_slots();
-  int ts_next = ts;                            // tiles ask for their slots in order, keys two before values
-  int32_t slots_next = slots;
+  int ts_k = t0, ts_v = t0;
+  int32_t slots_k = load_slots(t0), slots_v = slots_k;
+  // the slots of the keys of tile t and the values of tile t - 1 are at hand
+  auto need_slots = [&](int t) __attribute__((always_inline)) {
+    if (t - 1 - ts_v >= 64) {
+      ts_v = ts_k;
+      slots_v = slots_k;
+    }
+    if (t - ts_k >= 64) {
+      ts_k = t;
+      slots_k = load_slots(t);
+    }
+  };
   const int in = (16 * wave) % P;
   const uint32_t code_off = (uint32_t)((in + r16) * kKvqCodes + g * 16);
   const uint32_t scale_off = (uint32_t)(P * kKvqCodes + (in + r16) * 4 + g);
@@ -406,45 +426,40 @@ __global__ __launch_bounds__(256, 2) void attn_kvq_rows_kernel(KvqAttnArgs a) {
     u32x4 codes;
     uint32_t scale;
   };
+  // through a resource of the page, which holds nothing where the slot is -1: zeros then
+  const int64_t slot_bytes = a.Hkv * page_bytes;
   auto load = [&](const uint8_t* pool, int32_t s, Staged& x) __attribute__((always_inline)) {
-    const uint8_t* const p = s >= 0 ? pool + ((int64_t)s * a.Hkv + it.kvh) * page_bytes : kvq_zero_page;
-    x.codes = *(const u32x4*)(p + code_off);
-    x.scale = p[scale_off];
+    const __amdgpu_buffer_rsrc_t page = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t*>(pool + (int64_t)max(s, 0) * slot_bytes + it.kvh * page_bytes), (short)0,
+        s >= 0 ? (int)page_bytes : 0, 0x00020000);
+    x.codes = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(page, code_off, 0, 0));
+    x.scale = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(page, scale_off, 0, 0);
   };
-  // keys run ahead of values: their slots are refilled first, the values' follow when they get there
   auto load_k = [&](int t, Staged& x) __attribute__((always_inline)) {
-    if (t - ts_next >= 64) {
-      ts = ts_next = t;
-      slots_next = load_slots();
-    }
-    load(a.k, __builtin_amdgcn_readlane(slots_next, (t - ts_next) & 63), x);
+    load(a.k, __builtin_amdgcn_readlane(slots_k, (t - ts_k) & 63), x);
   };
-  int ts_v = t0;
   auto load_v = [&](int t, Staged& x) __attribute__((always_inline)) {
-    if (t - ts_v >= 64) {
-      ts_v = ts_next;
-      slots = slots_next;
-    }
-    load(a.v, __builtin_amdgcn_readlane(slots, (t - ts_v) & 63), x);
+    load(a.v, __builtin_amdgcn_readlane(slots_v, (t - ts_v) & 63), x);
   };
-  lds_u8* const v0 = (lds_u8*)v_lds;
-  lds_u8* const k0 = (lds_u8*)k_lds;
+  lds_u8* const v0 = (lds_u8*)lds->v;
+  lds_u8* const k0 = (lds_u8*)lds->k;
   auto put_k = [&](int b, const Staged& x) __attribute__((always_inline)) {
     *(__attribute__((address_space(3))) u32x4*)(k0 + b * kKeyBytes + wave * 1024 + lane * 16) = x.codes;
-    ((lds_u8*)ks_lds)[b * 256 + lane * 4 + wave] = (uint8_t)x.scale;
+    ((lds_u8*)lds->ks)[b * 256 + lane * 4 + wave] = (uint8_t)x.scale;
   };
-  auto put_v = [&](int t, int b, Staged x) __attribute__((always_inline)) {
-    if ((t + 1) * kKeys > all_see) {
-      // values that no row sees are zeros; NaN blocks that some rows see go round the product
-      if (t * kKeys + 16 * wave + r16 >= it.kv_end) x = Staged{u32x4{}, 127};
-      const uint64_t hit = __ballot(x.scale == 255);
-      if (lane == 0) nan_lds[b][wave] = hit;
-      if (x.scale == 255) x = Staged{u32x4{}, 127};
-    }
-    lds_u8* const row = v0 + b * kTile + (16 * wave + r16) * (kHD * 2);
+  auto put_v = [&](int b, const Staged& x) __attribute__((always_inline)) {
+    lds_u8* const row = v0 + b * kTile + (16 * wave + r16) * kKvqVRow + 64 * g;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      *(__attribute__((address_space(3))) u32x4*)(row + (((4 * g + j) ^ r16) << 4)) = kvq_values(x.codes[j], x.scale);
+      *(__attribute__((address_space(3))) u32x4*)(row + 16 * j) = kvq_values(x.codes[j], x.scale);
+  };
+  // of a tile that is masked for some row: values that no row sees are zeros, and NaN
+  // blocks, which would reach rows that do not see them, go round the product
+  auto filter_v = [&](int t, int b, Staged& x) __attribute__((always_inline)) {
+    if (t * kKeys + 16 * wave + r16 >= it.kv_end) x = Staged{u32x4{}, 127};
+    const uint64_t hit = __ballot(x.scale == 255);
+    if (lane == 0) lds->nan[b][wave] = hit;
+    if (x.scale == 255) x = Staged{u32x4{}, 127};
   };
 
   Staged kx, vx;
@@ -463,7 +478,7 @@ __global__ __launch_bounds__(256, 2) void attn_kvq_rows_kernel(KvqAttnArgs a) {
     const int tok = rr / G;
     const int head = it.kvh * G + (rr - tok * G);
     limit[nb] = min(it.kv_end, a.causal ? pre + tok + 1 : it.kv_len);
-    kvq_split_q(a.q + ((int64_t)(it.q_start + tok) * a.Hq + head) * kHD + g * 32, q[nb], qs[nb]);
+    kvq_split_q(a.q + ((int64_t)(it.q_start + tok) * a.Hq + head) * kHD + g * 32, a.c, q[nb], qs[nb]);
   }
   const int wave_sees = min(it.kv_end, a.causal ? pre + (it.row0 + min(wrow, rows - 1)) / G + 1 : it.kv_len);
 
@@ -479,40 +494,54 @@ __global__ __launch_bounds__(256, 2) void attn_kvq_rows_kernel(KvqAttnArgs a) {
     for (int db = 0; db < 8; ++db) o[nb][db] = f32x4{};
   }
 
-  f32x4 s[kNB][4];
+  f32x4 start[kNB];                            // of the scores: -m, or 0 where the row has met no key
+#pragma unroll
+  for (int nb = 0; nb < kNB; ++nb) start[nb] = f32x4{};
   auto scores = [&](int b, f32x4 (&x)[kNB][4]) __attribute__((always_inline)) {
-    const uint32_t scales = ((__attribute__((address_space(3))) uint32_t*)ks_lds)[b * 64 + lane];
+    const uint32_t scales = lds->ks[b][lane];
     const lds_u8* const k = k0 + b * kKeyBytes + lane * 16;
     u32x4 key[4];
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb) key[kb] = *(const __attribute__((address_space(3))) u32x4*)(k + kb * 1024);
 #pragma unroll
     for (int nb = 0; nb < kNB; ++nb) {
-      x[nb][0] = kvq_scores<0>(key[0], scales, q[nb], qs[nb]);
-      x[nb][1] = kvq_scores<1>(key[1], scales, q[nb], qs[nb]);
-      x[nb][2] = kvq_scores<2>(key[2], scales, q[nb], qs[nb]);
-      x[nb][3] = kvq_scores<3>(key[3], scales, q[nb], qs[nb]);
+      x[nb][0] = kvq_scores<0>(key[0], scales, q[nb], qs[nb], start[nb]);
+      x[nb][1] = kvq_scores<1>(key[1], scales, q[nb], qs[nb], start[nb]);
+      x[nb][2] = kvq_scores<2>(key[2], scales, q[nb], qs[nb], start[nb]);
+      x[nb][3] = kvq_scores<3>(key[3], scales, q[nb], qs[nb], start[nb]);
     }
   };
-  // m, l and O moved to the maxima of new scores
-  auto settle = [&](const float (&top)[kNB]) __attribute__((always_inline)) {
-    float grown[kNB];
-    bool moves = false;
+  // P of a tile's scores
+  auto weigh = [&](const f32x4 (&x)[kNB][4], bf16x8 (&p)[kNB][2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int nb = 0; nb < kNB; ++nb) {
-      grown[nb] = vmax(m[nb], row4_max(top[nb]) * a.c);
-      moves |= !(grown[nb] == m[nb]);
-    }
-    if (__ballot(moves)) {
+      float sum[2] = {0.f, 0.f};
 #pragma unroll
-      for (int nb = 0; nb < kNB; ++nb) {
-        const float f = exp2f_fast(m[nb] - (grown[nb] == -INFINITY ? 0.f : grown[nb]));
-        l[nb] *= f;
-#pragma unroll
-        for (int db = 0; db < 8; ++db) o[nb][db] *= f;
-        m[nb] = grown[nb];
+      for (int j = 0; j < 16; ++j) {
+        const float e = exp2f_fast(x[nb][j >> 2][j & 3]);
+        sum[j & 1] += e;
+        p[nb][j >> 3][j & 7] = (__bf16)e;
       }
+      l[nb] += sum[0] + sum[1];
     }
+  };
+  auto product = [&](int b, const bf16x8 (&p)[kNB][2]) __attribute__((always_inline)) {
+    const lds_u8* const vt = v0 + b * kTile + (4 * g + (r16 >> 2)) * kKvqVRow + 8 * (r16 & 3);
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int db = 0; db < 8; ++db) {
+        bf16x8 v;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          const auto four = lds_read_tr(vt + (32 * half + 16 * kb) * kKvqVRow + 32 * db);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[4 * kb + i] = four[i];
+        }
+#pragma unroll
+        for (int nb = 0; nb < kNB; ++nb)
+          o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[nb][half], o[nb][db], 0, 0, 0);
+      }
   };
   auto maxima = [&](const f32x4 (&x)[kNB][4], float (&top)[kNB]) __attribute__((always_inline)) {
 #pragma unroll
@@ -520,6 +549,27 @@ __global__ __launch_bounds__(256, 2) void attn_kvq_rows_kernel(KvqAttnArgs a) {
       top[nb] = x[nb][0][0];
 #pragma unroll
       for (int j = 1; j < 16; ++j) top[nb] = vmax(top[nb], x[nb][j >> 2][j & 3]);
+      top[nb] = vmax(m[nb], row4_max(top[nb]) - start[nb][0]);
+    }
+  };
+  // m, l, O and the scores themselves moved to their maxima
+  auto settle = [&](f32x4 (&x)[kNB][4], const float (&top)[kNB]) __attribute__((always_inline)) {
+    bool moves = false;
+#pragma unroll
+    for (int nb = 0; nb < kNB; ++nb) moves |= !(top[nb] == m[nb]);
+    if (__ballot(moves)) {
+#pragma unroll
+      for (int nb = 0; nb < kNB; ++nb) {
+        const float to = top[nb] == -INFINITY ? 0.f : top[nb];
+        const float f = exp2f_fast(m[nb] - to);
+        l[nb] *= f;
+#pragma unroll
+        for (int db = 0; db < 8; ++db) o[nb][db] *= f;
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) x[nb][kb] += -to - start[nb][0];
+        m[nb] = top[nb];
+        start[nb] = f32x4{-to, -to, -to, -to};
+      }
     }
   };
   auto mask = [&](int t, f32x4 (&x)[kNB][4]) __attribute__((always_inline)) {
@@ -530,16 +580,18 @@ __global__ __launch_bounds__(256, 2) void attn_kvq_rows_kernel(KvqAttnArgs a) {
         if (t * kKeys + 16 * (j >> 2) + 4 * g + (j & 3) >= limit[nb]) x[nb][j >> 2][j & 3] = -INFINITY;
   };
 
+  f32x4 s[2][kNB][4];
   if (t0 < t1) {
+    if ((t0 + 1) * kKeys > all_see) filter_v(t0, 0, vx);
     put_k(0, kx);
-    put_v(t0, 0, vx);
+    put_v(0, vx);
     if (t0 + 1 < t1) load_k(t0 + 1, kx);
     lds_barrier();
-    scores(0, s);
-    if ((t0 + 1) * kKeys > wave_sees) mask(t0, s);
+    scores(0, s[0]);
+    if ((t0 + 1) * kKeys > wave_sees) mask(t0, s[0]);
     float top[kNB];
-    maxima(s, top);
-    settle(top);
+    maxima(s[0], top);
+    settle(s[0], top);
     if (t0 + 1 < t1) {
       put_k(1, kx);
       load_v(t0 + 1, vx);
@@ -547,44 +599,39 @@ __global__ __launch_bounds__(256, 2) void attn_kvq_rows_kernel(KvqAttnArgs a) {
     }
     lds_barrier();
   }
-  for (int t = t0; t < t1; ++t) {
-    const int b = (t - t0) & 1;
-    // scores of the next tile (of whatever LDS holds behind the last one: not used)
-    f32x4 s_next[kNB][4];
-    scores(b ^ 1, s_next);
+  // steps whose tile and the next one all rows see, and behind which two more follow: no branch but the
+  // slots' and the rescale's, so that the compiler mixes their instructions
+  auto plain = [&](int t, auto buf) __attribute__((always_inline)) {
+    constexpr int b = decltype(buf)::value;
+    need_slots(t + 3);
     bf16x8 p[kNB][2];
-#pragma unroll
-    for (int nb = 0; nb < kNB; ++nb) {
-      const float off = m[nb] == -INFINITY ? 0.f : m[nb];
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const float e = exp2f_fast(__builtin_fmaf(s[nb][j >> 2][j & 3], a.c, -off));
-        l[nb] += e;
-        p[nb][j >> 3][j & 7] = (__bf16)e;
-      }
-    }
-    const lds_u8* const vt = v0 + b * kTile;
-    const int tr_key = 4 * g + (r16 >> 2);
-#pragma unroll
-    for (int half = 0; half < 2; ++half)
-#pragma unroll
-      for (int db = 0; db < 8; ++db) {
-        bf16x8 v;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          const auto four = lds_read_tr(vt + (32 * half + 16 * kb + tr_key) * (kHD * 2) +
-                                        (((2 * db + ((r16 >> 1) & 1)) ^ tr_key) << 4) + (r16 & 1) * 8);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[4 * kb + i] = four[i];
-        }
-#pragma unroll
-        for (int nb = 0; nb < kNB; ++nb)
-          o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[nb][half], o[nb][db], 0, 0, 0);
-      }
+    float top[kNB];
+    scores(b ^ 1, s[b ^ 1]);
+    weigh(s[b], p);
+    put_v(b ^ 1, vx);
+    put_k(b, kx);
+    load_v(t + 2, vx);
+    load_k(t + 3, kx);
+    product(b, p);
+    maxima(s[b ^ 1], top);
+    settle(s[b ^ 1], top);
+    lds_barrier();
+  };
+  int t = t0;
+  for (const int end = min(t1 - 3, all_see / kKeys - 1); t + 1 < end; t += 2) {
+    plain(t, std::integral_constant<int, 0>{});
+    plain(t + 1, std::integral_constant<int, 1>{});
+  }
+  for (; t < t1; ++t) {
+    const int b = (t - t0) & 1;
+    bf16x8 p[kNB][2];
+    if (t + 1 < t1) scores(b ^ 1, s[1]);
+    weigh(s[0], p);
+    product(b, p);
     if ((t + 1) * kKeys > all_see) {
 #pragma unroll
       for (int kb = 0; kb < 4; ++kb)
-        for (uint64_t hit = nan_lds[b][kb]; hit != 0; hit &= hit - 1) {
+        for (uint64_t hit = lds->nan[b][kb]; hit != 0; hit &= hit - 1) {
           const int from = __builtin_ctzll(hit);
 #pragma unroll
           for (int nb = 0; nb < kNB; ++nb)
@@ -592,21 +639,23 @@ __global__ __launch_bounds__(256, 2) void attn_kvq_rows_kernel(KvqAttnArgs a) {
         }
     }
     if (t + 1 < t1) {
-      put_v(t + 1, b ^ 1, vx);
+      if ((t + 2) * kKeys > all_see) filter_v(t + 1, b ^ 1, vx);
+      put_v(b ^ 1, vx);
       if (t + 2 < t1) {
         put_k(b, kx);
+        need_slots(t + 3);
         load_v(t + 2, vx);
         if (t + 3 < t1) load_k(t + 3, kx);
       }
-      if ((t + 2) * kKeys > wave_sees) mask(t + 1, s_next);
+      if ((t + 2) * kKeys > wave_sees) mask(t + 1, s[1]);
       float top[kNB];
-      maxima(s_next, top);
-      settle(top);
+      maxima(s[1], top);
+      settle(s[1], top);
     }
 #pragma unroll
     for (int nb = 0; nb < kNB; ++nb)
 #pragma unroll
-      for (int kb = 0; kb < 4; ++kb) s[nb][kb] = s_next[nb][kb];
+      for (int kb = 0; kb < 4; ++kb) s[0][nb][kb] = s[1][nb][kb];
     lds_barrier();
   }
   if (__ballot(bad) != 0 && lane == 0) atomicOr(a.err, 1);
@@ -632,6 +681,28 @@ __global__ __launch_bounds__(256, 2) void attn_kvq_rows_kernel(KvqAttnArgs a) {
       else if (a.lse != nullptr) a.lse[at] = log2sum * 0.69314718055994531f;
     }
   }
+}
+
+// A launch of items of up to 16 rows alone: three blocks on a CU.
+template <int P>
+__global__ __launch_bounds__(256, 3) void attn_kvq_few_kernel(KvqAttnArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kKvqWaves * kKvqHalf];
+  __shared__ float stats[2][kKvqWaves][16];
+  const AttnItem it = ld_uniform(a.items + blockIdx.x);
+  kvq_split_keys<P, 1>(a, it, (lds_u8*)lds, (KvqStats*)stats);
+}
+
+// Items of every class (KvqPlan: AttnItem::boost).
+template <int P>
+__global__ __launch_bounds__(256, 2) void attn_kvq_kernel(KvqAttnArgs a) {
+  constexpr int kBytes = sizeof(KvqRowsLds) > kKvqWaves * kKvqHalf ? sizeof(KvqRowsLds) : kKvqWaves * kKvqHalf;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kBytes];
+  __shared__ float stats[2][kKvqWaves][16];
+  const AttnItem it = ld_uniform(a.items + blockIdx.x);
+  if (it.boost == 0) kvq_split_keys<P, 1>(a, it, (lds_u8*)lds, (KvqStats*)stats);
+  else if (it.boost == 1) kvq_split_keys<P, 2>(a, it, (lds_u8*)lds, (KvqStats*)stats);
+  else if (it.boost == 2) kvq_split_rows<P, 1>(a, it, (__attribute__((address_space(3))) KvqRowsLds*)lds);
+  else kvq_split_rows<P, 2>(a, it, (__attribute__((address_space(3))) KvqRowsLds*)lds);
 }
 
 }  // namespace sa

@@ -18,12 +18,17 @@ constexpr int kKvqKeys = 64;                 // keys of a tile
 // up to 64 and 128, whose waves split the rows.
 constexpr int kKvqClasses = 4;
 constexpr int kKvqRows[kKvqClasses] = {16, 32, 64, 128};
-constexpr int kKvqCost[kKvqClasses] = {4, 5, 12, 16};   // of a tile of keys, relative
+// Microseconds of a tile of keys with the CUs' places taken, of an item's start and end,
+// and of the launch that joins parts.
+constexpr double kKvqTileUs[kKvqClasses] = {0.86, 1.1, 1.4, 2.1};
+constexpr double kKvqItemUs = 4.0, kKvqJoinUs = 6.0;
+constexpr int kKvqLeast[kKvqClasses] = {4, 4, 4, 2};    // tiles of a part
 constexpr int32_t kKvqMaxLen = INT32_MAX / kKvqKeys * kKvqKeys;   // the end of its last tile fits an int32
 constexpr int64_t kKvqMaxItems = int64_t(1) << 22;   // work items before they are cut
 
 struct KvqPlan {
-  std::vector<AttnItem> items[kKvqClasses];  // one per workgroup, in launch order; part: first row of its partial (-1: none)
+  std::vector<AttnItem> items;               // one per workgroup, in launch order; boost: its class; part: first row of its partial (-1: none)
+  bool few = false;                          // all of class 0
   std::vector<MergeUnit> units;
   int64_t part_rows = 0;
   int32_t most_rows = 0, most_parts = 0;     // of a unit
@@ -49,19 +54,22 @@ inline sa_status kvq_attn_check(const sa_layout* layout, int32_t layer, int32_t 
   return SA_OK;
 }
 
-// Row tiles of kKvqRows rows, the last one of a sequence in the smallest class that
-// holds it, each cut by key range into parts of about equal cost.
+// Row tiles of 128 rows, the last one of a sequence in the smallest class that holds it,
+// cut by key range into parts of at most `most` us: the one of a few such limits whose
+// launch, by the longest part and an even share of the work, ends first.
 inline sa_status plan_kvq_items(const sa_layout* layout, int32_t batch, const int32_t* h_q_len, const int32_t* h_kv_len,
                                 bool causal, int num_cu, KvqPlan& out, std::string& err) {
   const int Hkv = layout->num_kv_heads, G = layout->num_q_heads / Hkv;
   constexpr int kMost = kKvqRows[kKvqClasses - 1];
   out = KvqPlan{};
   struct Tile {
-    int seq, row0, rows, cls, keys, q_start;
+    int seq, row0, rows, cls, keys, q_start, n_tiles;
   };
   std::vector<Tile> tiles;
-  int64_t work = 0, n_items = 0;
+  double work = 0, longest = 0;
+  int64_t n_items = 0;
   int32_t q_start = 0;
+  out.few = true;
   for (int b = 0; b < batch; ++b) {
     const int rows = h_q_len[b] * G;
     n_items += (int64_t)Hkv * ((rows + kMost - 1) / kMost);
@@ -72,17 +80,43 @@ inline sa_status plan_kvq_items(const sa_layout* layout, int32_t batch, const in
       int cls = 0;
       while (n > kKvqRows[cls]) ++cls;
       const int keys = causal ? h_kv_len[b] - h_q_len[b] + (r0 + n - 1) / G + 1 : h_kv_len[b];
-      tiles.push_back({b, r0, n, cls, keys, q_start});
-      work += (int64_t)Hkv * kKvqCost[cls] * ((keys + kKvqKeys - 1) / kKvqKeys);
+      const int n_tiles = (keys + kKvqKeys - 1) / kKvqKeys;
+      tiles.push_back({b, r0, n, cls, keys, q_start, n_tiles});
+      const double us = n_tiles * kKvqTileUs[cls];
+      work += Hkv * us;
+      longest = std::max(longest, us);
+      out.few = out.few && cls == 0;
     }
     q_start += h_q_len[b];
   }
-  const int64_t share = std::max<int64_t>(32, (work + 2 * num_cu - 1) / (2 * num_cu));
+  const int slots = (out.few ? 3 : 2) * num_cu;
+  auto parts_of = [&](const Tile& t, double most) {
+    const int per = std::max(kKvqLeast[t.cls], (int)std::min<double>(t.n_tiles, most / kKvqTileUs[t.cls]));
+    const int parts = std::max(1, (t.n_tiles + per - 1) / per);
+    const int even = std::max(1, (t.n_tiles + parts - 1) / parts);
+    return std::pair<int, int>(std::max(1, (t.n_tiles + even - 1) / even), even);
+  };
+  double best = 0, best_us = -1;
+  for (const double f : {0., 2., 1.5, 1., 0.75, 0.5, 0.35, 0.25}) {
+    const double most = f == 0. ? longest : f * work / slots;
+    if (f != 0. && most >= longest) continue;
+    double blocks = 0, top = 0;
+    bool split = false;
+    for (const Tile& t : tiles) {
+      const auto [parts, even] = parts_of(t, most);
+      blocks += (double)Hkv * parts;
+      top = std::max(top, std::min(even, t.n_tiles) * kKvqTileUs[t.cls]);
+      split = split || parts > 1;
+    }
+    const double share = (work + blocks * kKvqItemUs) / slots;
+    const double us = (blocks <= slots ? top + kKvqItemUs : std::max(top + kKvqItemUs, share + 0.5 * top)) + (split ? kKvqJoinUs : 0.);
+    if (best_us < 0 || us < best_us) {
+      best = most;
+      best_us = us;
+    }
+  }
   for (const Tile& t : tiles) {
-    const int n_tiles = (t.keys + kKvqKeys - 1) / kKvqKeys;
-    const int parts = (int)std::max<int64_t>(1, ((int64_t)n_tiles * kKvqCost[t.cls] + share - 1) / share);
-    const int per = std::max(1, (n_tiles + parts - 1) / parts);
-    const int used = std::max(1, (n_tiles + per - 1) / per);
+    const auto [used, per] = parts_of(t, best);
     const int64_t row = out.part_rows;
     if (used > 1) {
       out.units.push_back({t.q_start, t.row0, t.rows, (int32_t)row, used, t.rows, 0, 0, 0});
@@ -94,14 +128,14 @@ inline sa_status plan_kvq_items(const sa_layout* layout, int32_t batch, const in
     }
     for (int h = 0; h < Hkv; ++h)
       for (int s = 0; s < used; ++s)
-        out.items[t.cls].push_back({t.seq, h, t.row0, s * per * kKvqKeys, (int32_t)std::min<int64_t>(t.keys, (int64_t)(s + 1) * per * kKvqKeys),
-                                    used > 1 ? (int32_t)(row + ((int64_t)h * used + s) * t.rows) : -1, 0, t.q_start,
-                                    h_q_len[t.seq], h_kv_len[t.seq]});
+        out.items.push_back({t.seq, h, t.row0, s * per * kKvqKeys, (int32_t)std::min<int64_t>(t.keys, (int64_t)(s + 1) * per * kKvqKeys),
+                             used > 1 ? (int32_t)(row + ((int64_t)h * used + s) * t.rows) : -1, t.cls, t.q_start,
+                             h_q_len[t.seq], h_kv_len[t.seq]});
   }
-  for (auto& items : out.items)
-    std::stable_sort(items.begin(), items.end(), [](const AttnItem& x, const AttnItem& y) {
-      return x.kv_end - x.kv_begin > y.kv_end - y.kv_begin;
-    });
+  std::stable_sort(out.items.begin(), out.items.end(), [](const AttnItem& x, const AttnItem& y) {
+    auto us = [](const AttnItem& it) { return (it.kv_end - it.kv_begin) * kKvqTileUs[it.boost]; };
+    return us(x) > us(y);
+  });
   return SA_OK;
 }
 

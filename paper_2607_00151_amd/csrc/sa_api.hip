@@ -208,7 +208,8 @@ struct sa_ctx {
     bool shared = false;           // else the batch goes to the segment attention
   } shared_rec;
   struct KvqRec {
-    size_t o_it[sa::kKvqClasses] = {}, n_items[sa::kKvqClasses] = {}, o_un = 0, n_units = 0;
+    size_t o_it = 0, n_items = 0, o_un = 0, n_units = 0;
+    bool few = false;
     int64_t total_q = 0, total_kv = 0, part_rows = 0;
     int most_rows = 0, block_rows = 8;
   } kvq_rec;
@@ -2001,15 +2002,6 @@ sa_status kvq_convert(sa_ctx* ctx, const sa_layout* layout, bool pack, const voi
   return SA_OK;
 }
 
-template <int P>
-void launch_kvq_attn(int cls, unsigned blocks, hipStream_t st, const hipEvent_t* ev, const sa::KvqAttnArgs& a) {
-  launch_timed(cls == 0   ? sa::attn_kvq_kernel<P, 1>
-               : cls == 1 ? sa::attn_kvq_kernel<P, 2>
-               : cls == 2 ? sa::attn_kvq_rows_kernel<P, 1>
-                          : sa::attn_kvq_rows_kernel<P, 2>,
-               dim3(blocks), dim3(256), st, ev, a);
-}
-
 sa_status kvq_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const void* q, const void* kq_pool,
                    const void* vq_pool, int32_t batch, const int32_t* h_q_len, const int32_t* h_kv_len, sa_pages pages,
                    bool causal, float softmax_scale, void* o, float* lse, void* stream) {
@@ -2053,10 +2045,9 @@ sa_status kvq_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const vo
     s = sa::plan_kvq_items(layout, batch, h_q_len, h_kv_len, causal, ctx->num_cu, plan, g_err);
     if (s != SA_OK) return s;
     PlanImage img;
-    for (int i = 0; i < sa::kKvqClasses; ++i) {
-      rec.n_items[i] = plan.items[i].size();
-      rec.o_it[i] = img.add(plan.items[i].data(), plan.items[i].size());
-    }
+    rec.few = plan.few;
+    rec.n_items = plan.items.size();
+    rec.o_it = img.add(plan.items.data(), plan.items.size());
     rec.n_units = plan.units.size();
     rec.o_un = img.add(plan.units.data(), plan.units.size());
     rec.part_rows = plan.part_rows;
@@ -2087,15 +2078,11 @@ sa_status kvq_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const vo
   a.G = a.Hq / a.Hkv;
   a.causal = causal;
   a.c = softmax_scale * 1.4426950408889634f;
-  for (int i = 0; i < sa::kKvqClasses; ++i) {
-    if (rec.n_items[i] == 0) continue;
-    a.items = (const sa::AttnItem*)(dev + rec.o_it[i]);
-    if (layout->page_size == 16)
-      launch_kvq_attn<16>(i, (unsigned)rec.n_items[i], (hipStream_t)stream, ctx->kernel_ev[SA_TIMED_ATTN], a);
-    else
-      launch_kvq_attn<32>(i, (unsigned)rec.n_items[i], (hipStream_t)stream, ctx->kernel_ev[SA_TIMED_ATTN], a);
-    SA_HIP(hipGetLastError());
-  }
+  a.items = (const sa::AttnItem*)(dev + rec.o_it);
+  auto kernel = layout->page_size == 16 ? (rec.few ? sa::attn_kvq_few_kernel<16> : sa::attn_kvq_kernel<16>)
+                                        : (rec.few ? sa::attn_kvq_few_kernel<32> : sa::attn_kvq_kernel<32>);
+  launch_timed(kernel, dim3((unsigned)rec.n_items), dim3(256), (hipStream_t)stream, ctx->kernel_ev[SA_TIMED_ATTN], a);
+  SA_HIP(hipGetLastError());
   if (rec.n_units > 0) {
     sa::MergeRowsArgs m{a.part_o, a.part_lse, (const sa::MergeUnit*)(dev + rec.o_un), a.o, lse, a.Hq, a.Hkv, a.G, rec.block_rows};
     const dim3 blocks((unsigned)(rec.n_units * a.Hkv), (unsigned)((rec.most_rows + rec.block_rows - 1) / rec.block_rows));

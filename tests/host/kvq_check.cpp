@@ -31,14 +31,17 @@ static void check(const sa_layout& L, const std::vector<int32_t>& q, const std::
   std::map<std::vector<int>, std::vector<Part>> tiles;
   std::vector<int32_t> q_start(B + 1, 0);
   for (int b = 0; b < B; ++b) q_start[b + 1] = q_start[b] + q[b];
-  for (int c = 0; c < sa::kKvqClasses; ++c)
-    for (const sa::AttnItem& it : plan.items[c]) {
+  {
+    for (const sa::AttnItem& it : plan.items) {
+      const int c = it.boost;
+      CHECK(c >= 0 && c < sa::kKvqClasses && (c == 0 || !plan.few));
       CHECK(it.seq >= 0 && it.seq < B && it.kvh >= 0 && it.kvh < L.num_kv_heads);
       CHECK(it.q_start == q_start[it.seq] && it.q_len == q[it.seq] && it.kv_len == kv[it.seq]);
       CHECK(it.row0 % 128 == 0 && it.row0 < it.q_len * G);
       CHECK(it.kv_begin % sa::kKvqKeys == 0 && it.kv_begin <= it.kv_end && it.kv_end <= it.kv_len);
       tiles[{it.seq, it.kvh, it.row0}].push_back({it.kv_begin, it.kv_end, it.part, c});
     }
+  }
   std::map<int, int> joined;                                 // first partial row -> rows
   int64_t joined_rows = 0;
   for (const sa::MergeUnit& u : plan.units) {
