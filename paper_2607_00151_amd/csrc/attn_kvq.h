@@ -3,7 +3,7 @@
 // Row i of a sequence sees keys j < limit_i (its position, or every key where there
 // is no mask):
 //   s_j = scale q . k_j,  m = max s_j,  O = sum 2^(s_j - m) v_j / l,  l = sum 2^(s_j - m)
-// in the exp2 domain, in one pass with m, l and O carried and rescaled when m grows.
+// in the exp2 domain, in one pass with m, l and O carried and rescaled when scores outgrow m.
 //
 // Scores come out of the block-scaled matrix instruction (16x16x128), which takes
 // the keys as they lie in the cache: lane l's operand is the 16 code bytes of key
@@ -121,6 +121,10 @@ __device__ __forceinline__ float row4_sum(float x) {
 }
 
 constexpr int kKvqWaves = 4;
+// How far (log2) scores may outgrow a row's offset before l and O are rescaled: weights
+// then reach 2^8, which their rounding to bf16, relative as it is, does not notice.  Moved
+// at every growth, some row of a wave moves in 45% of the tiles of 8K keys.
+constexpr float kKvqLag = 8.f;
 // Bytes of a key's bf16 values in LDS: 32 more than they take, so that the 8 keys x 32
 // bytes of half a wave's transposed reads, and the 8 rows' chunks of a quarter's
 // writes, lie in different banks.
@@ -262,7 +266,7 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const AttnI
 #pragma unroll
       for (int j = 1; j < 16; ++j) top = vmax(top, s[j >> 2][j & 3]);
       const float grown = vmax(m[nb], row4_max(top));
-      if (__ballot(!(grown == m[nb]))) {
+      if (__ballot(!(grown <= m[nb] + kKvqLag))) {
         const float f = exp2f_fast(m[nb] - (grown == -INFINITY ? 0.f : grown));
         l[nb] *= f;
 #pragma unroll
@@ -556,7 +560,7 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const AttnI
   auto settle = [&](f32x4 (&x)[kNB][4], const float (&top)[kNB]) __attribute__((always_inline)) {
     bool moves = false;
 #pragma unroll
-    for (int nb = 0; nb < kNB; ++nb) moves |= !(top[nb] == m[nb]);
+    for (int nb = 0; nb < kNB; ++nb) moves |= !(top[nb] <= m[nb] + kKvqLag);
     if (__ballot(moves)) {
 #pragma unroll
       for (int nb = 0; nb < kNB; ++nb) {
