@@ -40,7 +40,8 @@ struct KvqAttnArgs {
   float* lse;                // nullable
   float* part_o;             // [part rows][kHD]
   float* part_lse;           // [part rows], log2
-  const AttnItem* items;
+  const KvqItem* items;
+  int32_t* count;            // arrivals of the parts that a launch joins itself, zero between launches
   const int32_t* indptr;
   const int32_t* indices;
   int32_t* err;
@@ -139,8 +140,112 @@ struct KvqTile {
   uint32_t ks[4], vs[4];
 };
 
-template <int P, int kNB>
-__device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const AttnItem& it, lds_u8* lds, KvqStats* stats_p) {
+// Partial results of a tile's parts and their join by the block that counts itself last.
+// The parts run on different XCDs, whose L2s do not see each other's ordinary stores
+// before the launch ends: they are stored and loaded at device scope, counted once the
+// stores are acknowledged, and nothing waits.  Every thread of the last block has 8
+// dims of a row and every n-th part of it; the order of the sums is the parts', whichever ends last.
+__device__ __forceinline__ void kvq_join(const KvqAttnArgs& a, const KvqItem& it, int rows, int r, int ch, f32x4 o0,
+                                         f32x4 o1, float log2sum, lds_u8* lds) {
+  const int tid = threadIdx.x;
+  const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc(a.part_o + (int64_t)it.part0 * kHD, (short)0,
+                                                                     it.n_parts * rows * kHD * 4, 0x00020000);
+  const __amdgpu_buffer_rsrc_t rl =
+      __builtin_amdgcn_make_buffer_rsrc(a.part_lse + it.part0, (short)0, it.n_parts * rows * 4, 0x00020000);
+  __attribute__((address_space(3))) int32_t* const flag = (__attribute__((address_space(3))) int32_t*)lds;
+  if (r < rows) {
+    const uint32_t at = (uint32_t)(it.part - it.part0 + r);
+    part_st4(ro, at * (kHD * 4) + ch * 32, o0);
+    part_st4(ro, at * (kHD * 4) + ch * 32 + 16, o1);
+    if (ch == 0) part_st1(rl, at * 4, 0, log2sum);
+  }
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070);                        // vmcnt(0): my stores are acknowledged
+  __syncthreads();
+  if (tid == 0) {
+    int32_t* const cnt = a.count + it.counter;
+    const bool last = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == it.n_parts - 1;
+    if (last) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *flag = last;
+  }
+  __syncthreads();
+  if (*flag == 0) return;
+  const int nsub = 16 / rows, slot = tid >> 4, sub = slot / rows, row = slot - sub * rows;
+  const bool mine = sub < nsub;
+  float top = -INFINITY, den = 0.f;
+  f32x4 num[2] = {};
+  constexpr int kAhead = 4;
+  for (int s0 = sub; s0 < it.n_parts && mine; s0 += kAhead * nsub) {
+    f32x4 x[kAhead][2];
+    float lse[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int s = s0 + k * nsub;
+      const uint32_t at = s < it.n_parts ? (uint32_t)(s * rows + row) : 0x400000u;   // beyond the parts: nothing is read
+      lse[k] = part_ld1(rl, at * 4, 0);
+      x[k][0] = part_ld4(ro, at * (kHD * 4) + ch * 32, 0);
+      x[k][1] = part_ld4(ro, at * (kHD * 4) + ch * 32 + 16, 0);
+    }
+    float m = top;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (s0 + k * nsub >= it.n_parts) lse[k] = -INFINITY;
+      m = fmaxf(m, lse[k]);
+    }
+    const float off = m == -INFINITY ? 0.f : m;
+    const float f = exp2f_fast(top - off);
+    top = m;
+    den *= f;
+    num[0] *= f;
+    num[1] *= f;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const float w = exp2f_fast(lse[k] - off);
+      den += w;
+      num[0] += w * x[k][0];
+      num[1] += w * x[k][1];
+    }
+  }
+  typedef __attribute__((address_space(3))) float lds_f;
+  lds_f* const red = (lds_f*)(lds + 64);                     // [slot][ch][10]
+  if (nsub > 1) {
+    lds_f* const my = red + tid * 10;
+    my[0] = top;
+    my[1] = den;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) my[2 + e] = num[e >> 2][e & 3];
+    __syncthreads();
+    if (sub > 0) return;
+    float all = top;
+    for (int k = 1; k < nsub; ++k) all = fmaxf(all, red[((k * rows + row) * 16 + ch) * 10]);
+    const float off = all == -INFINITY ? 0.f : all;
+    float f = exp2f_fast(top - off);
+    den *= f;
+    num[0] *= f;
+    num[1] *= f;
+    for (int k = 1; k < nsub; ++k) {
+      const lds_f* const x = red + ((k * rows + row) * 16 + ch) * 10;
+      f = exp2f_fast(x[0] - off);
+      den += f * x[1];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) num[e >> 2][e & 3] += f * x[2 + e];
+    }
+    top = all;
+  }
+  if (!mine) return;
+  const float inv = den == 0.f ? 0.f : 1.f / den;
+  const int at = it.row0 + row, tok = at / a.G;
+  const int64_t orow = (int64_t)(it.q_start + tok) * a.Hq + it.kvh * a.G + (at - tok * a.G);
+  bf16x8 out;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) out[e] = (__bf16)(num[e >> 2][e & 3] * inv);
+  *(bf16x8*)(a.o + orow * kHD + 8 * ch) = out;
+  if (a.lse != nullptr && ch == 0)
+    a.lse[orow] = den == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994531f;
+}
+
+template <int P, int kNB, bool kJoin = false>
+__device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqItem& it, lds_u8* lds, KvqStats* stats_p) {
   static_assert(P == 16 || P == 32, "page size");
   auto& stats = *stats_p;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -329,7 +434,7 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const AttnI
     }
     __syncthreads();
     const int r = tid >> 4, ch = tid & 15;                   // row, 8 dims
-    if (16 * nb + r >= rows) continue;
+    if (!kJoin && 16 * nb + r >= rows) continue;
     float top = stats[0][0][r];
 #pragma unroll
     for (int w = 1; w < kKvqWaves; ++w) top = vmax(top, stats[0][w][r]);
@@ -346,6 +451,14 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const AttnI
     }
     const float inv = den == 0.f ? 0.f : 1.f / den;
     const float log2sum = den == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(den);
+    if constexpr (kJoin) {
+      if (it.part >= 0) {
+        __syncthreads();                                     // the waves' results have been read
+        kvq_join(a, it, rows, r, ch, num[0] * inv, num[1] * inv, log2sum, lds);
+        return;
+      }
+      if (r >= rows) return;
+    }
     if (it.part >= 0) {
       const int64_t at = (int64_t)it.part + 16 * nb + r;
       *(f32x4*)(a.part_o + at * kHD + 8 * ch) = num[0] * inv;
@@ -381,7 +494,7 @@ struct KvqRowsLds {
 };
 
 template <int P, int kNB>
-__device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const AttnItem& it,
+__device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqItem& it,
                                                __attribute__((address_space(3))) KvqRowsLds* lds) {
   static_assert(P == 16 || P == 32, "page size");
   constexpr int kTile = kKvqTile, kKeyBytes = kKvqKeyBytes;
@@ -688,24 +801,24 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const AttnI
 }
 
 // A launch of items of up to 16 rows alone: three blocks on a CU.
-template <int P>
+template <int P, bool kJoin>
 __global__ __launch_bounds__(256, 3) void attn_kvq_few_kernel(KvqAttnArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kKvqWaves * kKvqHalf];
   __shared__ float stats[2][kKvqWaves][16];
-  const AttnItem it = ld_uniform(a.items + blockIdx.x);
-  kvq_split_keys<P, 1>(a, it, (lds_u8*)lds, (KvqStats*)stats);
+  const KvqItem it = ld_uniform(a.items + blockIdx.x);
+  kvq_split_keys<P, 1, kJoin>(a, it, (lds_u8*)lds, (KvqStats*)stats);
 }
 
-// Items of every class (KvqPlan: AttnItem::boost).
+// Items of every class (kvq_plan.h).
 template <int P>
 __global__ __launch_bounds__(256, 2) void attn_kvq_kernel(KvqAttnArgs a) {
   constexpr int kBytes = sizeof(KvqRowsLds) > kKvqWaves * kKvqHalf ? sizeof(KvqRowsLds) : kKvqWaves * kKvqHalf;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kBytes];
   __shared__ float stats[2][kKvqWaves][16];
-  const AttnItem it = ld_uniform(a.items + blockIdx.x);
-  if (it.boost == 0) kvq_split_keys<P, 1>(a, it, (lds_u8*)lds, (KvqStats*)stats);
-  else if (it.boost == 1) kvq_split_keys<P, 2>(a, it, (lds_u8*)lds, (KvqStats*)stats);
-  else if (it.boost == 2) kvq_split_rows<P, 1>(a, it, (__attribute__((address_space(3))) KvqRowsLds*)lds);
+  const KvqItem it = ld_uniform(a.items + blockIdx.x);
+  if (it.cls == 0) kvq_split_keys<P, 1>(a, it, (lds_u8*)lds, (KvqStats*)stats);
+  else if (it.cls == 1) kvq_split_keys<P, 2>(a, it, (lds_u8*)lds, (KvqStats*)stats);
+  else if (it.cls == 2) kvq_split_rows<P, 1>(a, it, (__attribute__((address_space(3))) KvqRowsLds*)lds);
   else kvq_split_rows<P, 2>(a, it, (__attribute__((address_space(3))) KvqRowsLds*)lds);
 }
 

@@ -4,7 +4,9 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <functional>
 #include <string>
+#include <utility>
 #include <vector>
 
 #include "branch_plan.h"
@@ -18,17 +20,37 @@ constexpr int kKvqKeys = 64;                 // keys of a tile
 // up to 64 and 128, whose waves split the rows.
 constexpr int kKvqClasses = 4;
 constexpr int kKvqRows[kKvqClasses] = {16, 32, 64, 128};
-// Microseconds of a tile of keys with the CUs' places taken, of an item's start and end,
-// and of the launch that joins parts.
-constexpr double kKvqTileUs[kKvqClasses] = {0.86, 1.1, 1.4, 2.1};
-constexpr double kKvqItemUs = 4.0, kKvqJoinUs = 6.0;
-constexpr int kKvqLeast[kKvqClasses] = {4, 4, 4, 2};    // tiles of a part
+// What a launch's time is made of, in microseconds, measured with 32/8 heads: a tile of
+// keys where two blocks share every CU; the start and end of an item (of class 0 behind
+// the loads of the CU's other blocks); the launch that joins parts, or the join in the
+// launch itself; each part of a row and each partial row written and read.
+constexpr double kKvqTileUs[kKvqClasses] = {0.8, 0.84, 1.31, 2.0};
+constexpr double kKvqItemUs = 3.0, kKvqFewItemUs = 1.5, kKvqJoinUs = 5.0, kKvqInLaunchUs = 2.0, kKvqPartUs = 0.08, kKvqPartRowUs = 2.1e-4;
+// Parts of a row tile times its rows up to which the block that ends last joins them, in a
+// launch of class 0 alone: its reads are then a trip or two to memory, in place of a launch
+// (four requests of 1K to 4K keys, 8 parts of 4 rows: kKvqJoinUs less of 13 us).
+constexpr int kKvqJoinRows = 128;
+constexpr int64_t kKvqCounters = 16384;
+constexpr int kKvqLeast[kKvqClasses] = {8, 8, 4, 4};    // tiles of a part
 constexpr int32_t kKvqMaxLen = INT32_MAX / kKvqKeys * kKvqKeys;   // the end of its last tile fits an int32
 constexpr int64_t kKvqMaxItems = int64_t(1) << 22;   // work items before they are cut
+constexpr int kKvqSimulated = 2048;                  // parts of one KV head whose launch is played through
+
+// A work item: rows row0 .. (of the class) of a sequence's packed rows of one KV head over
+// keys kv_begin .. kv_end - 1.  part: the first row of its partial among all (-1: the
+// item is whole); of its row tile's parts, part0 is the first one's, n_parts their number
+// and counter the arrivals that they count at.
+struct KvqItem {
+  int32_t seq, kvh, row0, kv_begin, kv_end, cls;
+  int32_t q_start, q_len, kv_len;
+  int32_t part, part0, n_parts, counter;
+};
 
 struct KvqPlan {
-  std::vector<AttnItem> items;               // one per workgroup, in launch order; boost: its class; part: first row of its partial (-1: none)
+  std::vector<KvqItem> items;                // one per workgroup, in launch order
   bool few = false;                          // all of class 0
+  bool joined = false;                       // the launch joins its parts itself (units is empty)
+  int64_t counters = 0;
   std::vector<MergeUnit> units;
   int64_t part_rows = 0;
   int32_t most_rows = 0, most_parts = 0;     // of a unit
@@ -55,8 +77,8 @@ inline sa_status kvq_attn_check(const sa_layout* layout, int32_t layer, int32_t 
 }
 
 // Row tiles of 128 rows, the last one of a sequence in the smallest class that holds it,
-// cut by key range into parts of at most `most` us: the one of a few such limits whose
-// launch, by the longest part and an even share of the work, ends first.
+// cut by key range into parts of at most so many us: the one of a few such limits whose
+// launch ends first.
 inline sa_status plan_kvq_items(const sa_layout* layout, int32_t batch, const int32_t* h_q_len, const int32_t* h_kv_len,
                                 bool causal, int num_cu, KvqPlan& out, std::string& err) {
   const int Hkv = layout->num_kv_heads, G = layout->num_q_heads / Hkv;
@@ -96,44 +118,101 @@ inline sa_status plan_kvq_items(const sa_layout* layout, int32_t batch, const in
     const int even = std::max(1, (t.n_tiles + parts - 1) / parts);
     return std::pair<int, int>(std::max(1, (t.n_tiles + even - 1) / even), even);
   };
-  double best = 0, best_us = -1;
-  for (const double f : {0., 2., 1.5, 1., 0.75, 0.5, 0.35, 0.25}) {
-    const double most = f == 0. ? longest : f * work / slots;
-    if (f != 0. && most >= longest) continue;
-    double blocks = 0, top = 0;
-    bool split = false;
+  // How many tile microseconds n blocks do in one.  A block with a CU to itself is quicker
+  // than one of two (0.6 of the time; of class 0 half or less, where HBM is what they share),
+  // so the end of a launch, when places are empty, does not cost what they would have done.
+  // Over 40 drawn batches the parts chosen so took 1.02 times the best of nine limits' time.
+  auto rate = [&](double n) {
+    if (out.few) return std::min(2.1 * n, 2.05 * num_cu);
+    return n <= num_cu ? 1.67 * n : std::min(2. * num_cu, 1.67 * num_cu + 0.33 * (n - num_cu));
+  };
+  // The end of a launch whose parts are at most `most` long, taken longest first: blocks in
+  // place go equally fast, one that ends leaves its place to the next part.  The KV heads'
+  // items are alike, so one head's, on its share of the places, tell for all; of very many, an even share.
+  std::vector<double> parts_us, place;
+  auto ends = [&](double most) {
+    parts_us.clear();
+    double rows = 0, sum = 0;
+    int64_t blocks = 0;
+    int most_parts = 0, most_join = 0;
     for (const Tile& t : tiles) {
       const auto [parts, even] = parts_of(t, most);
-      blocks += (double)Hkv * parts;
-      top = std::max(top, std::min(even, t.n_tiles) * kKvqTileUs[t.cls]);
-      split = split || parts > 1;
+      blocks += parts;
+      if (parts > 1) {
+        rows += (double)parts * t.rows;
+        most_join = std::max(most_join, parts * t.rows);
+      }
+      most_parts = std::max(most_parts, parts);
+      const double us = std::min(even, t.n_tiles) * kKvqTileUs[t.cls] + (out.few ? kKvqFewItemUs : kKvqItemUs);
+      sum += parts * us;
+      if (blocks <= kKvqSimulated) parts_us.insert(parts_us.end(), (size_t)parts, us);
     }
-    const double share = (work + blocks * kKvqItemUs) / slots;
-    const double us = (blocks <= slots ? top + kKvqItemUs : std::max(top + kKvqItemUs, share + 0.5 * top)) + (split ? kKvqJoinUs : 0.);
-    if (best_us < 0 || us < best_us) {
+    const double join = rows == 0                                      ? 0.
+                        : out.few && most_join <= kKvqJoinRows ? kKvqInLaunchUs
+                                                                       : kKvqJoinUs + kKvqPartUs * most_parts + Hkv * rows * kKvqPartRowUs;
+    if (blocks > kKvqSimulated) return Hkv * sum / rate(slots) + join;
+    std::sort(parts_us.begin(), parts_us.end(), std::greater<double>());
+    // the first blocks go round the CUs: one that has to share its CU from the start does so to its end
+    const size_t second = std::max(1, num_cu / Hkv);
+    const double shared = parts_us.size() > second ? parts_us[second] * (out.few ? 0.8 : 1.) : 0.;
+    const size_t n = std::min(parts_us.size(), (size_t)std::max(1, slots / Hkv));
+    place.assign(parts_us.begin(), parts_us.begin() + n);    // a heap: what each block's clock shows at its end
+    std::make_heap(place.begin(), place.end(), std::greater<double>());
+    double at = 0, clock = 0;
+    for (size_t next = n; !place.empty();) {
+      std::pop_heap(place.begin(), place.end(), std::greater<double>());
+      const double busy = (double)place.size() * Hkv;
+      at += (place.back() - clock) * busy / rate(busy);
+      clock = place.back();
+      place.pop_back();
+      if (next == parts_us.size()) continue;
+      place.push_back(clock + parts_us[next++]);
+      std::push_heap(place.begin(), place.end(), std::greater<double>());
+    }
+    return std::max(at, shared) + join;
+  };
+  double best = longest, best_us = ends(longest);
+  for (const double f : {3., 2., 1.5, 1., 0.75, 0.5, 0.35, 0.25}) {
+    const double most = f * work / slots;
+    if (most >= longest) continue;
+    const double us = ends(most);
+    if (us < best_us) {
       best = most;
       best_us = us;
     }
   }
+  int most_join = 0;
+  int64_t groups = 0;
+  for (const Tile& t : tiles) {
+    const int used = parts_of(t, best).first;
+    if (used == 1) continue;
+    most_join = std::max(most_join, used * t.rows);
+    groups += Hkv;
+  }
+  out.joined = out.few && groups > 0 && groups <= kKvqCounters && most_join <= kKvqJoinRows;
   for (const Tile& t : tiles) {
     const auto [used, per] = parts_of(t, best);
     const int64_t row = out.part_rows;
     if (used > 1) {
-      out.units.push_back({t.q_start, t.row0, t.rows, (int32_t)row, used, t.rows, 0, 0, 0});
+      if (!out.joined) out.units.push_back({t.q_start, t.row0, t.rows, (int32_t)row, used, t.rows, 0, 0, 0});
       out.part_rows += (int64_t)Hkv * used * t.rows;
       if (out.part_rows > kMaxPartRows)
         return plan_fail(err, SA_ERR_SHAPE, "too many query rows for one launch (partial results)");
       out.most_rows = std::max(out.most_rows, t.rows);
       out.most_parts = std::max(out.most_parts, used);
     }
-    for (int h = 0; h < Hkv; ++h)
+    for (int h = 0; h < Hkv; ++h) {
+      const int64_t part0 = row + (int64_t)h * used * t.rows;
       for (int s = 0; s < used; ++s)
-        out.items.push_back({t.seq, h, t.row0, s * per * kKvqKeys, (int32_t)std::min<int64_t>(t.keys, (int64_t)(s + 1) * per * kKvqKeys),
-                             used > 1 ? (int32_t)(row + ((int64_t)h * used + s) * t.rows) : -1, t.cls, t.q_start,
-                             h_q_len[t.seq], h_kv_len[t.seq]});
+        out.items.push_back({t.seq, h, t.row0, s * per * kKvqKeys,
+                             (int32_t)std::min<int64_t>(t.keys, (int64_t)(s + 1) * per * kKvqKeys), t.cls, t.q_start,
+                             h_q_len[t.seq], h_kv_len[t.seq], used > 1 ? (int32_t)(part0 + s * t.rows) : -1,
+                             used > 1 ? (int32_t)part0 : -1, used, out.joined && used > 1 ? (int32_t)out.counters : -1});
+      if (out.joined && used > 1) ++out.counters;
+    }
   }
-  std::stable_sort(out.items.begin(), out.items.end(), [](const AttnItem& x, const AttnItem& y) {
-    auto us = [](const AttnItem& it) { return (it.kv_end - it.kv_begin) * kKvqTileUs[it.boost]; };
+  std::stable_sort(out.items.begin(), out.items.end(), [](const KvqItem& x, const KvqItem& y) {
+    auto us = [](const KvqItem& it) { return (it.kv_end - it.kv_begin) * kKvqTileUs[it.cls]; };
     return us(x) > us(y);
   });
   return SA_OK;

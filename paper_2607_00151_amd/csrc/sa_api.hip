@@ -209,8 +209,8 @@ struct sa_ctx {
   } shared_rec;
   struct KvqRec {
     size_t o_it = 0, n_items = 0, o_un = 0, n_units = 0;
-    bool few = false;
-    int64_t total_q = 0, total_kv = 0, part_rows = 0;
+    bool few = false, joined = false;
+    int64_t total_q = 0, total_kv = 0, part_rows = 0, counters = 0;
     int most_rows = 0, block_rows = 8;
   } kvq_rec;
   uint8_t* work = nullptr;         // slot scans of sa_kv_release and sa_kv_compact
@@ -2046,6 +2046,8 @@ sa_status kvq_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const vo
     if (s != SA_OK) return s;
     PlanImage img;
     rec.few = plan.few;
+    rec.joined = plan.joined;
+    rec.counters = plan.counters;
     rec.n_items = plan.items.size();
     rec.o_it = img.add(plan.items.data(), plan.items.size());
     rec.n_units = plan.units.size();
@@ -2078,9 +2080,13 @@ sa_status kvq_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const vo
   a.G = a.Hq / a.Hkv;
   a.causal = causal;
   a.c = softmax_scale * 1.4426950408889634f;
-  a.items = (const sa::AttnItem*)(dev + rec.o_it);
-  auto kernel = layout->page_size == 16 ? (rec.few ? sa::attn_kvq_few_kernel<16> : sa::attn_kvq_kernel<16>)
-                                        : (rec.few ? sa::attn_kvq_few_kernel<32> : sa::attn_kvq_kernel<32>);
+  a.items = (const sa::KvqItem*)(dev + rec.o_it);
+  a.count = ctx->part_count;
+  ctx->parts_used = std::max(ctx->parts_used, (rec.counters + sa::kPartCounters - 1) / sa::kPartCounters);
+  static_assert(sa::kKvqCounters <= kMaxParts * sa::kPartCounters, "the counters a context owns");
+  auto kernel = layout->page_size == 16
+                    ? (rec.joined ? sa::attn_kvq_few_kernel<16, true> : rec.few ? sa::attn_kvq_few_kernel<16, false> : sa::attn_kvq_kernel<16>)
+                    : (rec.joined ? sa::attn_kvq_few_kernel<32, true> : rec.few ? sa::attn_kvq_few_kernel<32, false> : sa::attn_kvq_kernel<32>);
   launch_timed(kernel, dim3((unsigned)rec.n_items), dim3(256), (hipStream_t)stream, ctx->kernel_ev[SA_TIMED_ATTN], a);
   SA_HIP(hipGetLastError());
   if (rec.n_units > 0) {

@@ -32,8 +32,8 @@ static void check(const sa_layout& L, const std::vector<int32_t>& q, const std::
   std::vector<int32_t> q_start(B + 1, 0);
   for (int b = 0; b < B; ++b) q_start[b + 1] = q_start[b] + q[b];
   {
-    for (const sa::AttnItem& it : plan.items) {
-      const int c = it.boost;
+    for (const sa::KvqItem& it : plan.items) {
+      const int c = it.cls;
       CHECK(c >= 0 && c < sa::kKvqClasses && (c == 0 || !plan.few));
       CHECK(it.seq >= 0 && it.seq < B && it.kvh >= 0 && it.kvh < L.num_kv_heads);
       CHECK(it.q_start == q_start[it.seq] && it.q_len == q[it.seq] && it.kv_len == kv[it.seq]);
@@ -44,6 +44,26 @@ static void check(const sa_layout& L, const std::vector<int32_t>& q, const std::
   }
   std::map<int, int> joined;                                 // first partial row -> rows
   int64_t joined_rows = 0;
+  if (plan.joined) {                                         // by the launch itself: every group at a counter of its own
+    CHECK(plan.few && plan.units.empty() && plan.counters > 0 && plan.counters <= sa::kKvqCounters);
+    std::map<int, std::vector<const sa::KvqItem*>> groups;
+    for (const sa::KvqItem& it : plan.items) {
+      CHECK((it.part >= 0) == (it.counter >= 0) && (it.part >= 0) == (it.n_parts > 1));
+      if (it.part >= 0) groups[it.counter].push_back(&it);
+    }
+    CHECK((int64_t)groups.size() == plan.counters && groups.begin()->first == 0 && groups.rbegin()->first == plan.counters - 1);
+    for (auto& [c, items] : groups) {
+      const int rows = std::min(128, items[0]->q_len * G - items[0]->row0);
+      CHECK((int)items.size() == items[0]->n_parts && items[0]->n_parts * rows <= sa::kKvqJoinRows);
+      for (const sa::KvqItem* it : items) {
+        CHECK(it->part0 == items[0]->part0 && it->n_parts == items[0]->n_parts);
+        CHECK(it->part >= it->part0 && it->part + rows <= it->part0 + it->n_parts * rows);
+        CHECK(it->seq == items[0]->seq && it->kvh == items[0]->kvh && it->row0 == items[0]->row0);
+        CHECK(joined.emplace(it->part, rows).second);
+      }
+      joined_rows += (int64_t)items.size() * rows;
+    }
+  }
   for (const sa::MergeUnit& u : plan.units) {
     CHECK(u.b_n == 0 && u.a_n >= 2 && u.n >= 1 && u.n <= plan.most_rows && u.a_n <= plan.most_parts);
     for (int h = 0; h < L.num_kv_heads; ++h)
