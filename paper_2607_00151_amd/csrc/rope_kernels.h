@@ -82,9 +82,37 @@ __device__ __forceinline__ int wave_find_seq(const int32_t* tok_begin, int B, in
   return lo;
 }
 
+// Sine and cosine of a phase in fractions of 2^32 of a turn, to about an fp32 rounding:
+// the nearest quarter turn goes by symmetry, the rest, up to an eighth, by the Taylor
+// series up to the 9th and 10th power (what is left out is below 2^-28).  v_sin and v_cos
+// are off by some 2^-21, which a rounding to bf16 hides but which decides more of the ties
+// between two elements of 4 bits, a whole step apart.
+__device__ __forceinline__ void turn_sincos(uint32_t phase, float& sine, float& cosine) {
+  const uint32_t quarter = (phase + 0x20000000u) >> 30;
+  const float a = (float)(int32_t)(phase - (quarter << 30)) * 1.4629180792671596e-9f;   // 2 pi / 2^32
+  const float x = a * a;
+  float s = __builtin_fmaf(x, 2.7557319e-6f, -1.9841270e-4f);
+  s = __builtin_fmaf(x, s, 8.3333333e-3f);
+  s = __builtin_fmaf(x, s, -1.6666667e-1f);
+  s = __builtin_fmaf(a * x, s, a);
+  float c = __builtin_fmaf(x, -2.7557319e-7f, 2.4801587e-5f);
+  c = __builtin_fmaf(x, c, -1.3888889e-3f);
+  c = __builtin_fmaf(x, c, 4.1666667e-2f);
+  c = __builtin_fmaf(x, c, -0.5f);
+  c = __builtin_fmaf(x, c, 1.f);
+  sine = quarter & 1 ? c : s;
+  cosine = quarter & 1 ? s : c;
+  if (quarter & 2) sine = -sine;
+  if ((quarter + 1) & 2) cosine = -cosine;
+}
+
 template <int kCtrl>
 __device__ __forceinline__ float row16(float x) {
   return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), kCtrl, 0xF, 0xF, true));
+}
+template <int kCtrl>
+__device__ __forceinline__ uint32_t row16u(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kCtrl, 0xF, 0xF, true);
 }
 // over the 16 lanes that share lane / 16
 __device__ __forceinline__ float row16_sum(float x) {
@@ -193,9 +221,14 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
       const uint64_t f = a.freq[j];
       uint32_t phase = __umulhi((uint32_t)f, pos) + (uint32_t)(f >> 32) * pos;
       if constexpr (kAxes) phase -= (int32_t)pos < 0 ? (uint32_t)f : 0u;   // pos stands for pos - 2^32
-      const float turns = (float)(int32_t)phase * 2.3283064365386963e-10f;   // 2^-32
-      cs[e] = __builtin_amdgcn_cosf(turns);
-      const float s = __builtin_amdgcn_sinf(turns);
+      float s;
+      if constexpr (kKvq) {
+        turn_sincos(phase, s, cs[e]);
+      } else {
+        const float turns = (float)(int32_t)phase * 2.3283064365386963e-10f;   // 2^-32
+        cs[e] = __builtin_amdgcn_cosf(turns);
+        s = __builtin_amdgcn_sinf(turns);
+      }
       sn[e] = upper ? s : -s;
     }
   }
@@ -263,7 +296,10 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
     if (!mine) return;
     uint8_t* const p = pool + ((int64_t)slot * a.Hkv + head) * a.P * kKvqRow;
     *(uint32_t*)(p + prow * kKvqCodes + c * 4) = codes;
-    if ((c & 3) == 0) p[a.P * kKvqCodes + prow * 4 + (c >> 2)] = (uint8_t)scale;
+    uint32_t scales = scale << (8 * (c >> 2));               // the row's four bytes from its four blocks
+    scales |= row16u<0x124>(scales);
+    scales |= row16u<0x128>(scales);
+    if (c == 0) *(uint32_t*)(p + a.P * kKvqCodes + prow * 4) = scales;
   };
 
   uint16_t* const q_out = a.q_out + (int64_t)t * a.Hq * kHD + c * 8;
