@@ -793,17 +793,19 @@ sa_status sa_kvq_unpack(sa_ctx *ctx, const sa_layout *layout, int64_t num_slots4
  * q_len, kv_len >= 0); where kv_len is 0 the rows are zeros and their LSE is
  * -infinity.  Lengths of keys are at most 2^31 - 64.
  * O = softmax(softmax_scale * q . K^T) V with the values the cache stands for.
- * Scores are the exact products of the cached keys with the bf16 query rows, held
- * as three 6-bit floats per value (within 2^-14 of the largest of its 32 dims),
- * summed in fp32; probabilities are rounded to bf16 before the PV product, the rest
+ * Scores are the products of the cached keys with the bf16 query rows, held
+ * times the scale as three 6-bit floats per value (within 2^-13 of the largest of
+ * its 32 dims), summed in fp32; probabilities are rounded to bf16 before the PV product, the rest
  * is fp32.  A row that sees a key with a NaN block has a NaN output and a NaN LSE; a
  * NaN block of a value it sees makes those 32 dims of its output NaN.  What a row
  * does not see does not reach it.  A page that is missing or outside the pool reads
  * as zeros and is latched for sa_sync_check.  `lse` may be NULL; pages.indices may
  * be NULL where no sequence with queries has keys.  Parts of a launch split by key
- * range are joined by a second kernel (516 bytes of the split-KV partials per query
- * row, head and part; plans take 40 bytes per work item and 36 per split row tile).
- * sa_set_kernel_events times the first kernel (SA_TIMED_ATTN).
+ * range (516 bytes of the split-KV partials per query row, head and part) are joined
+ * by the launch itself where all sequences have at most 16 query rows on a KV head
+ * and a row tile's parts are few, else by a second kernel.  Plans take 52 bytes per
+ * work item and 36 per split row tile.  sa_set_kernel_events times the first kernel
+ * (SA_TIMED_ATTN).
  *
  * Errors: those of sa_segment_prefill_attn, SA_ERR_UNSUPPORTED for a capturing stream.
  */

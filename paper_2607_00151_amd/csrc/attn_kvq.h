@@ -10,7 +10,7 @@
 // l % 16, block l / 16, with that block's scale byte, so a wave's load of 16 keys is
 // one contiguous KB.  The query goes in as three 6-bit floats per value (e2m3, scales
 // 2^e, 2^(e-4), 2^(e-8) per 32 dims, each the rounded rest of the one before), which
-// together are the bf16 value to 2^-14 of its block's largest: against a bf16 product
+// together are scale times the bf16 value to 2^-13 of the block's largest: against a bf16 product
 // of converted keys the matrix work is 3/4 and the conversion goes, and two 8-bit
 // pieces would cost 4/4 and lose 2^-14 in the instruction's sum (measured).
 // Values have a scale per key and 32 dims, which a sum over keys cannot take in that
@@ -50,16 +50,28 @@ struct KvqAttnArgs {
   float c;                   // softmax scale times log2 e, which goes into the query rows
 };
 
-// What absent pages read as: codes and scale bytes of 0.
-static __device__ uint8_t kvq_zero_page[32 * kKvqRow];
+// A head's page through a resource, which holds nothing where the slot is -1: zeros then.
+typedef __amdgpu_buffer_rsrc_t KvqPage;
+__device__ __forceinline__ KvqPage kvq_page(const uint8_t* pool, int32_t slot, int64_t slot_bytes, int64_t head_at,
+                                            int64_t page_bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(pool + (int64_t)max(slot, 0) * slot_bytes + head_at),
+                                           (short)0, slot >= 0 ? (int)page_bytes : 0, 0x00020000);
+}
+__device__ __forceinline__ u32x4 kvq_load_codes(KvqPage page, uint32_t at) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(page, at, 0, 0));
+}
+__device__ __forceinline__ uint32_t kvq_load_scale(KvqPage page, uint32_t at) {
+  return (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(page, at, 0, 0);
+}
 
 typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x32 __attribute__((ext_vector_type(32)));
 
 // c times 32 dims of a query row as three 6-bit pieces; scales: their bytes (255: the
-// block holds an infinity or a NaN).  Every rest is exact: hardly more than the bits
-// that the piece before it left.
+// block holds an infinity or a NaN).  The rests are exact.  With S the first piece's
+// scale, they are at most S / 4, S / 128 and in the end S / 4096: half a step each time,
+// of steps S / 2 (values from 4 S), S / 64 (rests from 2 S / 16) and S / 2048.
 __device__ __forceinline__ void kvq_split_q(const uint16_t* p, float c, u32x6 (&piece)[3], int& scales) {
   u32x4 w[4];
 #pragma unroll
@@ -71,7 +83,7 @@ __device__ __forceinline__ void kvq_split_q(const uint16_t* p, float c, u32x6 (&
     for (int e = 0; e < 4; ++e) top = max(top, max(w[i][e] & 0x7FFF0000u, (w[i][e] << 16) & 0x7FFF0000u));
   top = top < 0x7F800000u ? __float_as_uint(__uint_as_float(top) * c) : top;
   const bool fine = top < 0x7F800000u;
-  const int s = max((int)(top >> 23) - 2, 10);               // the block's largest is 4 to 8 times the scale
+  const int s = max((int)((top + 0x100000u) >> 23) - 2, 10);   // the block's largest is 3.75 to 7.5 (the format's own) times the scale
   f32x16 even, odd;                                          // dims 2 i and 2 i + 1, as the conversion takes them
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
@@ -277,7 +289,7 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqIt
   int32_t slots = load_slots();
 
   const uint32_t code_off = (uint32_t)(r16 * kKvqCodes + g * 16), scale_off = (uint32_t)(P * kKvqCodes + r16 * 4 + g);
-  const int64_t page_bytes = (int64_t)P * kKvqRow;
+  const int64_t page_bytes = (int64_t)P * kKvqRow, slot_bytes = a.Hkv * page_bytes;
   auto load_tile = [&](int t, KvqTile& x) __attribute__((always_inline)) {
     if (t * (kKeys / P) - pg0 >= 64) {
       pg0 = t * (kKeys / P);
@@ -286,14 +298,13 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqIt
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb) {
       const int32_t s = __builtin_amdgcn_readlane(slots, t * (kKeys / P) - pg0 + kb * 16 / P);
-      const int64_t at = ((int64_t)s * a.Hkv + it.kvh) * page_bytes;
-      const uint8_t* const kp = s >= 0 ? a.k + at : kvq_zero_page;
-      const uint8_t* const vp = s >= 0 ? a.v + at : kvq_zero_page;
       constexpr int kIn[4] = {0, 16 % P, 32 % P, 48 % P};    // the block's first row in its page
-      x.k[kb] = *(const u32x4*)(kp + code_off + kIn[kb] * kKvqCodes);
-      x.v[kb] = *(const u32x4*)(vp + code_off + kIn[kb] * kKvqCodes);
-      x.ks[kb] = kp[scale_off + kIn[kb] * 4];
-      x.vs[kb] = vp[scale_off + kIn[kb] * 4];
+      const KvqPage k = kvq_page(a.k, s, slot_bytes, it.kvh * page_bytes, page_bytes);
+      const KvqPage v = kvq_page(a.v, s, slot_bytes, it.kvh * page_bytes, page_bytes);
+      x.k[kb] = kvq_load_codes(k, code_off + kIn[kb] * kKvqCodes);
+      x.v[kb] = kvq_load_codes(v, code_off + kIn[kb] * kKvqCodes);
+      x.ks[kb] = kvq_load_scale(k, scale_off + kIn[kb] * 4);
+      x.vs[kb] = kvq_load_scale(v, scale_off + kIn[kb] * 4);
     }
   };
   const int tr_at = (4 * g + (r16 >> 2)) * kKvqVRow + 8 * (r16 & 3);   // this lane's source of a transposed read
@@ -543,14 +554,11 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
     u32x4 codes;
     uint32_t scale;
   };
-  // through a resource of the page, which holds nothing where the slot is -1: zeros then
   const int64_t slot_bytes = a.Hkv * page_bytes;
   auto load = [&](const uint8_t* pool, int32_t s, Staged& x) __attribute__((always_inline)) {
-    const __amdgpu_buffer_rsrc_t page = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint8_t*>(pool + (int64_t)max(s, 0) * slot_bytes + it.kvh * page_bytes), (short)0,
-        s >= 0 ? (int)page_bytes : 0, 0x00020000);
-    x.codes = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(page, code_off, 0, 0));
-    x.scale = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(page, scale_off, 0, 0);
+    const KvqPage page = kvq_page(pool, s, slot_bytes, it.kvh * page_bytes, page_bytes);
+    x.codes = kvq_load_codes(page, code_off);
+    x.scale = kvq_load_scale(page, scale_off);
   };
   auto load_k = [&](int t, Staged& x) __attribute__((always_inline)) {
     load(a.k, __builtin_amdgcn_readlane(slots_k, (t - ts_k) & 63), x);

@@ -466,7 +466,9 @@ def test_attention(i):
 
 
 @pytest.mark.parametrize("heads,page,q,kv,causal", [((8, 2), 16, [1, 1], [40000, 31001], True), ((32, 8), 16, [1], [9000], False),
-                                                    ((2, 1), 32, [40], [20011], True), ((16, 1), 16, [6], [30000], True)])
+                                                    ((2, 1), 32, [40], [20011], True), ((16, 1), 16, [6], [30000], True),
+                                                    ((16, 1), 16, [1, 1], [60000, 1], True), ((4, 4), 32, [1] * 3, [70000, 64, 9000], False),
+                                                    ((16, 4), 32, [2, 30, 1, 7, 14], [9000, 6000, 20000, 77, 12345], True)])
 def test_attention_over_long_caches(heads, page, q, kv, causal):
     check_attn(attn_case(90, heads, page, q, kv, causal), heads, page, q, kv, causal)
 
@@ -583,6 +585,45 @@ def test_attention_gives_the_same_bits_again_and_on_another_stream():
     sa.sa_kvq_attn(ctx, L, 0, qd, k4, v4, *args[2:4], ip, ix, D ** -0.5, again, stream=side)
     side.synchronize()
     assert torch.equal(o, again)
+
+
+def test_two_contexts_at_once_on_two_streams():
+    """Launches that join their own parts, and mixed ones, overlapping from two contexts: each as when alone."""
+    cases = [((32, 8), 16, [1] * 4, [3000, 1000, 4096, 70], True), ((32, 8), 16, [1, 40], [6000, 5000], True)]
+    made = []
+    for i, args in enumerate(cases):
+        L, indptr, indices, k, v, q, o, lse = attn_case(110 + i, *args)
+        made.append((L, args, q.cuda(), torch.from_numpy(k).cuda(), torch.from_numpy(v).cuda(), dev(indptr), dev(indices), o,
+                     [torch.empty_like(o) for _ in range(20)], sa.Context(0), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for n in range(20):
+        for L, args, q, k4, v4, ip, ix, o, outs, ctx, side in made:
+            sa.sa_kvq_attn(ctx, L, 0, q, k4, v4, args[2], args[3], ip, ix, D ** -0.5, outs[n], stream=side)
+    torch.cuda.synchronize()
+    for L, args, q, k4, v4, ip, ix, o, outs, ctx, side in made:
+        sa.sa_sync_check(ctx, side)
+        for out in outs:
+            assert torch.equal(out, o)
+
+
+def test_reserved_contexts_and_timing_events():
+    args = ((32, 8), 16, [1, 1, 33], [5000, 900, 4000], True)
+    L, indptr, indices, k, v, q, o, lse = attn_case(112, *args)
+    k4, v4, qd, ip, ix = torch.from_numpy(k).cuda(), torch.from_numpy(v).cuda(), q.cuda(), dev(indptr), dev(indices)
+    ctx = sa.Context(0)
+    sa.sa_reserve(ctx, 1 << 20, 1 << 24)
+    free = torch.cuda.mem_get_info()[0]
+    start, stop = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    start.record()
+    stop.record()
+    torch.cuda.synchronize()
+    sa.sa_set_kernel_events(ctx, sa.TIMED_ATTN, start.cuda_event, stop.cuda_event)
+    out = torch.empty_like(o)
+    sa.sa_kvq_attn(ctx, L, 0, qd, k4, v4, *args[2:4], ip, ix, D ** -0.5, out)
+    torch.cuda.synchronize()
+    assert 0 < start.elapsed_time(stop) < 50
+    assert torch.cuda.mem_get_info()[0] == free
+    assert torch.equal(out, o)
 
 
 def test_pools_beyond_4_gib():
