@@ -802,8 +802,7 @@ sa_status sa_kvq_unpack(sa_ctx *ctx, const sa_layout *layout, int64_t num_slots4
  * as zeros and is latched for sa_sync_check.  `lse` may be NULL; pages.indices may
  * be NULL where no sequence with queries has keys.  Parts of a launch split by key
  * range (516 bytes of the split-KV partials per query row, head and part) are joined
- * by the launch itself where all sequences have at most 16 query rows on a KV head
- * and a row tile's parts are few, else by a second kernel.  Plans take 52 bytes per
+ * by the launch itself where a row tile has few of them, else by a second kernel.  Plans take 52 bytes per
  * work item and 36 per split row tile.  sa_set_kernel_events times the first kernel
  * (SA_TIMED_ATTN).
  *

@@ -152,37 +152,55 @@ struct KvqTile {
   uint32_t ks[4], vs[4];
 };
 
-// Partial results of a tile's parts and their join by the block that counts itself last.
+// Partial results of a tile's parts and their join by the one that counts itself last.
 // The parts run on different XCDs, whose L2s do not see each other's ordinary stores
 // before the launch ends: they are stored and loaded at device scope, counted once the
-// stores are acknowledged, and nothing waits.  Every thread of the last block has 8
-// dims of a row and every n-th part of it; the order of the sums is the parts', whichever ends last.
-__device__ __forceinline__ void kvq_join(const KvqAttnArgs& a, const KvqItem& it, int rows, int r, int ch, f32x4 o0,
-                                         f32x4 o1, float log2sum, lds_u8* lds) {
+// stores are acknowledged, and nothing waits.  Sums are in the parts' order, whichever
+// ends last.
+struct KvqParts {
+  __amdgpu_buffer_rsrc_t o, lse;             // of all parts: row n of the tile in part s is s * rows + n
+};
+__device__ __forceinline__ KvqParts kvq_parts(const KvqAttnArgs& a, const KvqItem& it, int rows) {
+  return {__builtin_amdgcn_make_buffer_rsrc(a.part_o + (int64_t)it.part0 * kHD, (short)0, it.n_parts * rows * kHD * 4, 0x00020000),
+          __builtin_amdgcn_make_buffer_rsrc(a.part_lse + it.part0, (short)0, it.n_parts * rows * 4, 0x00020000)};
+}
+constexpr uint32_t kKvqNoRow = 0x400000;     // a row beyond the resources: nothing is read
+static_assert(kKvqMostJoin < (int)kKvqNoRow / 2, "rows of a tile's parts");
+
+// Counts at counter c; true for the last of the tile's parts, which puts the counter back.
+__device__ __forceinline__ bool kvq_arrive(const KvqAttnArgs& a, const KvqItem& it, int c) {
+  int32_t* const cnt = a.count + it.counter + c;
+  const bool last = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == it.n_parts - 1;
+  if (last) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return last;
+}
+
+__device__ __forceinline__ int64_t kvq_out_row(const KvqAttnArgs& a, const KvqItem& it, int r) {
+  const int row = it.row0 + r, tok = row / a.G;
+  return (int64_t)(it.q_start + tok) * a.Hq + it.kvh * a.G + (row - tok * a.G);
+}
+
+// Rows first .. first + n - 1 (n up to 16) of a part whose block has them whole: thread (r, ch)
+// has 8 dims of row first + r.  In the block that ends last every thread takes 8 dims of a
+// row and every nsub-th part of it.
+__device__ __forceinline__ void kvq_join(const KvqAttnArgs& a, const KvqItem& it, int rows, int first, int n, int r, int ch,
+                                         f32x4 o0, f32x4 o1, float log2sum, lds_u8* lds) {
   const int tid = threadIdx.x;
-  const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc(a.part_o + (int64_t)it.part0 * kHD, (short)0,
-                                                                     it.n_parts * rows * kHD * 4, 0x00020000);
-  const __amdgpu_buffer_rsrc_t rl =
-      __builtin_amdgcn_make_buffer_rsrc(a.part_lse + it.part0, (short)0, it.n_parts * rows * 4, 0x00020000);
+  const KvqParts parts = kvq_parts(a, it, rows);
   __attribute__((address_space(3))) int32_t* const flag = (__attribute__((address_space(3))) int32_t*)lds;
-  if (r < rows) {
-    const uint32_t at = (uint32_t)(it.part - it.part0 + r);
-    part_st4(ro, at * (kHD * 4) + ch * 32, o0);
-    part_st4(ro, at * (kHD * 4) + ch * 32 + 16, o1);
-    if (ch == 0) part_st1(rl, at * 4, 0, log2sum);
+  if (r < n) {
+    const uint32_t at = (uint32_t)(it.part - it.part0 + first + r);
+    part_st4(parts.o, at * (kHD * 4) + ch * 32, o0);
+    part_st4(parts.o, at * (kHD * 4) + ch * 32 + 16, o1);
+    if (ch == 0) part_st1(parts.lse, at * 4, 0, log2sum);
   }
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(0x0070);                        // vmcnt(0): my stores are acknowledged
   __syncthreads();
-  if (tid == 0) {
-    int32_t* const cnt = a.count + it.counter;
-    const bool last = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == it.n_parts - 1;
-    if (last) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    *flag = last;
-  }
+  if (tid == 0) *flag = kvq_arrive(a, it, first >> 4);
   __syncthreads();
   if (*flag == 0) return;
-  const int nsub = 16 / rows, slot = tid >> 4, sub = slot / rows, row = slot - sub * rows;
+  const int nsub = 16 / n, slot = tid >> 4, sub = slot / n, row = slot - sub * n;
   const bool mine = sub < nsub;
   float top = -INFINITY, den = 0.f;
   f32x4 num[2] = {};
@@ -193,10 +211,10 @@ __device__ __forceinline__ void kvq_join(const KvqAttnArgs& a, const KvqItem& it
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const int s = s0 + k * nsub;
-      const uint32_t at = s < it.n_parts ? (uint32_t)(s * rows + row) : 0x400000u;   // beyond the parts: nothing is read
-      lse[k] = part_ld1(rl, at * 4, 0);
-      x[k][0] = part_ld4(ro, at * (kHD * 4) + ch * 32, 0);
-      x[k][1] = part_ld4(ro, at * (kHD * 4) + ch * 32 + 16, 0);
+      const uint32_t at = s < it.n_parts ? (uint32_t)(s * rows + first + row) : kKvqNoRow;
+      lse[k] = part_ld1(parts.lse, at * 4, 0);
+      x[k][0] = part_ld4(parts.o, at * (kHD * 4) + ch * 32, 0);
+      x[k][1] = part_ld4(parts.o, at * (kHD * 4) + ch * 32 + 16, 0);
     }
     float m = top;
 #pragma unroll
@@ -229,14 +247,14 @@ __device__ __forceinline__ void kvq_join(const KvqAttnArgs& a, const KvqItem& it
     __syncthreads();
     if (sub > 0) return;
     float all = top;
-    for (int k = 1; k < nsub; ++k) all = fmaxf(all, red[((k * rows + row) * 16 + ch) * 10]);
+    for (int k = 1; k < nsub; ++k) all = fmaxf(all, red[((k * n + row) * 16 + ch) * 10]);
     const float off = all == -INFINITY ? 0.f : all;
     float f = exp2f_fast(top - off);
     den *= f;
     num[0] *= f;
     num[1] *= f;
     for (int k = 1; k < nsub; ++k) {
-      const lds_f* const x = red + ((k * rows + row) * 16 + ch) * 10;
+      const lds_f* const x = red + ((k * n + row) * 16 + ch) * 10;
       f = exp2f_fast(x[0] - off);
       den += f * x[1];
 #pragma unroll
@@ -246,8 +264,7 @@ __device__ __forceinline__ void kvq_join(const KvqAttnArgs& a, const KvqItem& it
   }
   if (!mine) return;
   const float inv = den == 0.f ? 0.f : 1.f / den;
-  const int at = it.row0 + row, tok = at / a.G;
-  const int64_t orow = (int64_t)(it.q_start + tok) * a.Hq + it.kvh * a.G + (at - tok * a.G);
+  const int64_t orow = kvq_out_row(a, it, first + row);
   bf16x8 out;
 #pragma unroll
   for (int e = 0; e < 8; ++e) out[e] = (__bf16)(num[e >> 2][e & 3] * inv);
@@ -256,7 +273,7 @@ __device__ __forceinline__ void kvq_join(const KvqAttnArgs& a, const KvqItem& it
     a.lse[orow] = den == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994531f;
 }
 
-template <int P, int kNB, bool kJoin = false>
+template <int P, int kNB>
 __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqItem& it, lds_u8* lds, KvqStats* stats_p) {
   static_assert(P == 16 || P == 32, "page size");
   auto& stats = *stats_p;
@@ -445,7 +462,6 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqIt
     }
     __syncthreads();
     const int r = tid >> 4, ch = tid & 15;                   // row, 8 dims
-    if (!kJoin && 16 * nb + r >= rows) continue;
     float top = stats[0][0][r];
 #pragma unroll
     for (int w = 1; w < kKvqWaves; ++w) top = vmax(top, stats[0][w][r]);
@@ -462,22 +478,19 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqIt
     }
     const float inv = den == 0.f ? 0.f : 1.f / den;
     const float log2sum = den == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(den);
-    if constexpr (kJoin) {
-      if (it.part >= 0) {
-        __syncthreads();                                     // the waves' results have been read
-        kvq_join(a, it, rows, r, ch, num[0] * inv, num[1] * inv, log2sum, lds);
-        return;
-      }
-      if (r >= rows) return;
+    if (it.counter >= 0) {
+      __syncthreads();                                       // the waves' results have been read
+      if (16 * nb < rows) kvq_join(a, it, rows, 16 * nb, min(16, rows - 16 * nb), r, ch, num[0] * inv, num[1] * inv, log2sum, lds);
+      continue;
     }
+    if (16 * nb + r >= rows) continue;
     if (it.part >= 0) {
       const int64_t at = (int64_t)it.part + 16 * nb + r;
       *(f32x4*)(a.part_o + at * kHD + 8 * ch) = num[0] * inv;
       *(f32x4*)(a.part_o + at * kHD + 8 * ch + 4) = num[1] * inv;
       if (ch == 0) a.part_lse[at] = log2sum;
     } else {
-      const int row = it.row0 + 16 * nb + r, tok = row / G;
-      const int64_t at = (int64_t)(it.q_start + tok) * a.Hq + it.kvh * G + (row - tok * G);
+      const int64_t at = kvq_out_row(a, it, 16 * nb + r);
       bf16x8 out;
 #pragma unroll
       for (int e = 0; e < 8; ++e) out[e] = (__bf16)(num[e >> 2][e & 3] * inv);
@@ -785,36 +798,86 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
   }
   if (__ballot(bad) != 0 && lane == 0) atomicOr(a.err, 1);
 
+  // this wave's rows: out, or as a part, which the wave that ends last joins with the others
+  float log2sum[kNB];
+#pragma unroll
+  for (int nb = 0; nb < kNB; ++nb) {
+    const float den = row4_sum(l[nb]);
+    const float inv = den == 0.f ? 0.f : 1.f / den;
+    log2sum[nb] = den == 0.f ? -INFINITY : m[nb] + __builtin_amdgcn_logf(den);
+#pragma unroll
+    for (int db = 0; db < 8; ++db)
+      o[nb][db] = poison[nb] >> (db >> 1) & 1 ? f32x4{NAN, NAN, NAN, NAN} : o[nb][db] * inv;
+  }
+  if (wrow >= rows) return;
+  if (it.counter >= 0) {
+    const KvqParts parts = kvq_parts(a, it, rows);
+#pragma unroll
+    for (int nb = 0; nb < kNB; ++nb) {
+      const int r = wrow + 16 * nb + r16;
+      if (r >= rows) continue;
+      const uint32_t at = (uint32_t)(it.part - it.part0 + r);
+#pragma unroll
+      for (int db = 0; db < 8; ++db) part_st4(parts.o, at * (kHD * 4) + db * 64 + g * 16, o[nb][db]);
+      if (g == 0) part_st1(parts.lse, at * 4, 0, log2sum[nb]);
+    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);                      // vmcnt(0): this wave's stores are acknowledged
+    asm volatile("" ::: "memory");
+    int last = 0;
+    if (lane == 0) last = kvq_arrive(a, it, wave);
+    if (__builtin_amdgcn_readfirstlane(last) == 0) return;
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int nb = 0; nb < kNB; ++nb) {
+      const int r = wrow + 16 * nb + r16;
+      const uint32_t row = r < rows ? (uint32_t)r : kKvqNoRow;
+      float top = -INFINITY, den = 0.f;
+      for (int s = 0; s < it.n_parts; ++s) top = fmaxf(top, part_ld1(parts.lse, (row + s * rows) * 4, 0));
+      const float off = top == -INFINITY ? 0.f : top;
+      f32x4 num[8] = {};
+      for (int s = 0; s < it.n_parts; ++s) {
+        const uint32_t at = row + s * rows;
+        f32x4 x[8];
+#pragma unroll
+        for (int db = 0; db < 8; ++db) x[db] = part_ld4(parts.o, at * (kHD * 4) + db * 64 + g * 16, 0);
+        const float w = exp2f_fast(part_ld1(parts.lse, at * 4, 0) - off);
+        den += w;
+#pragma unroll
+        for (int db = 0; db < 8; ++db) num[db] += w * x[db];
+      }
+      const float inv = den == 0.f ? 0.f : 1.f / den;
+      log2sum[nb] = den == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(den);
+#pragma unroll
+      for (int db = 0; db < 8; ++db) o[nb][db] = num[db] * inv;
+    }
+  }
 #pragma unroll
   for (int nb = 0; nb < kNB; ++nb) {
     const int r = wrow + 16 * nb + r16;
-    const float den = row4_sum(l[nb]);
     if (r >= rows) continue;
-    const float inv = den == 0.f ? 0.f : 1.f / den;
-    const float log2sum = den == 0.f ? -INFINITY : m[nb] + __builtin_amdgcn_logf(den);
-    const int row = it.row0 + r, tok = row / G;
-    const int64_t at = it.part >= 0 ? (int64_t)it.part + r : (int64_t)(it.q_start + tok) * a.Hq + it.kvh * G + (row - tok * G);
+    const bool part = it.part >= 0 && it.counter < 0;
+    const int64_t at = part ? (int64_t)it.part + r : kvq_out_row(a, it, r);
 #pragma unroll
     for (int db = 0; db < 8; ++db) {
-      f32x4 x = o[nb][db] * inv;
-      if (poison[nb] >> (db >> 1) & 1) x = f32x4{NAN, NAN, NAN, NAN};
-      if (it.part >= 0) *(f32x4*)(a.part_o + at * kHD + 16 * db + 4 * g) = x;
+      const f32x4 x = o[nb][db];
+      if (part) *(f32x4*)(a.part_o + at * kHD + 16 * db + 4 * g) = x;
       else st_bf16x4(a.o + at * kHD + 16 * db + 4 * g, x[0], x[1], x[2], x[3]);
     }
     if (g == 0) {
-      if (it.part >= 0) a.part_lse[at] = log2sum;
-      else if (a.lse != nullptr) a.lse[at] = log2sum * 0.69314718055994531f;
+      if (part) a.part_lse[at] = log2sum[nb];
+      else if (a.lse != nullptr) a.lse[at] = log2sum[nb] * 0.69314718055994531f;
     }
   }
 }
 
 // A launch of items of up to 16 rows alone: three blocks on a CU.
-template <int P, bool kJoin>
+template <int P>
 __global__ __launch_bounds__(256, 3) void attn_kvq_few_kernel(KvqAttnArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kKvqWaves * kKvqHalf];
   __shared__ float stats[2][kKvqWaves][16];
   const KvqItem it = ld_uniform(a.items + blockIdx.x);
-  kvq_split_keys<P, 1, kJoin>(a, it, (lds_u8*)lds, (KvqStats*)stats);
+  kvq_split_keys<P, 1>(a, it, (lds_u8*)lds, (KvqStats*)stats);
 }
 
 // Items of every class (kvq_plan.h).

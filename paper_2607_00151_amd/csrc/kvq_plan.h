@@ -20,17 +20,25 @@ constexpr int kKvqKeys = 64;                 // keys of a tile
 // up to 64 and 128, whose waves split the rows.
 constexpr int kKvqClasses = 4;
 constexpr int kKvqRows[kKvqClasses] = {16, 32, 64, 128};
-// What a launch's time is made of, in microseconds, measured with 32/8 heads: a tile of
-// keys where two blocks share every CU; the start and end of an item (of class 0 behind
-// the loads of the CU's other blocks); the launch that joins parts, or the join in the
-// launch itself; each part of a row and each partial row written and read.
+// What a launch's time is made of, in microseconds.  Measured, 32/8 heads: a tile of keys
+// where two blocks share every CU.  Fitted, with the rates in plan_kvq_items, to 70 drawn
+// batches under nine limits each: the start and end of an item, the launch that joins parts,
+// each part of a row and each partial row, and where the launch joins itself, a start, a
+// partial row that a block reads and a part that a wave reads.
 constexpr double kKvqTileUs[kKvqClasses] = {0.8, 0.84, 1.31, 2.0};
-constexpr double kKvqItemUs = 3.0, kKvqFewItemUs = 1.5, kKvqJoinUs = 5.0, kKvqInLaunchUs = 2.0, kKvqPartUs = 0.08, kKvqPartRowUs = 2.1e-4;
-// Parts of a row tile times its rows up to which the block that ends last joins them, in a
-// launch of class 0 alone: its reads are then a trip or two to memory, in place of a launch
-// (four requests of 1K to 4K keys, 8 parts of 4 rows: kKvqJoinUs less of 13 us).
-constexpr int kKvqJoinRows = 128;
-constexpr int64_t kKvqCounters = 16384;
+constexpr double kKvqItemUs = 3.0, kKvqJoinUs = 8.0, kKvqPartUs = 0.08, kKvqPartRowUs = 4e-4;
+constexpr double kKvqInLaunchUs = 1.0, kKvqReadRowUs = 0.03, kKvqReadTileUs = 0.6;
+// Which parts the launch joins itself, and a second one does not have to: of a tile whose
+// waves split the keys up to so many rows (parts times rows), which the block that ends
+// last reads in a trip or two to memory; of one whose waves split the rows up to so many
+// parts, which each wave joins for its own rows.
+constexpr int kKvqJoinRows = 128, kKvqJoinParts = 8;
+constexpr int kKvqMostJoin = kKvqJoinParts * 128 > kKvqJoinRows ? kKvqJoinParts * 128 : kKvqJoinRows;   // rows
+constexpr int kKvqCounted = 4;               // counters of a tile: one for every 16 rows, or for every wave
+constexpr int64_t kKvqCounters = 32768;
+inline bool kvq_joins(int cls, int parts, int rows) {
+  return cls < 2 ? parts * rows <= kKvqJoinRows : parts <= kKvqJoinParts;
+}
 constexpr int kKvqLeast[kKvqClasses] = {8, 8, 4, 4};    // tiles of a part
 constexpr int32_t kKvqMaxLen = INT32_MAX / kKvqKeys * kKvqKeys;   // the end of its last tile fits an int32
 constexpr int64_t kKvqMaxItems = int64_t(1) << 22;   // work items before they are cut
@@ -39,7 +47,7 @@ constexpr int kKvqSimulated = 2048;                  // parts of one KV head who
 // A work item: rows row0 .. (of the class) of a sequence's packed rows of one KV head over
 // keys kv_begin .. kv_end - 1.  part: the first row of its partial among all (-1: the
 // item is whole); of its row tile's parts, part0 is the first one's, n_parts their number
-// and counter the arrivals that they count at.
+// and counter the first of kKvqCounted counters, at which the launch joins them (-1: it does not).
 struct KvqItem {
   int32_t seq, kvh, row0, kv_begin, kv_end, cls;
   int32_t q_start, q_len, kv_len;
@@ -49,9 +57,8 @@ struct KvqItem {
 struct KvqPlan {
   std::vector<KvqItem> items;                // one per workgroup, in launch order
   bool few = false;                          // all of class 0
-  bool joined = false;                       // the launch joins its parts itself (units is empty)
   int64_t counters = 0;
-  std::vector<MergeUnit> units;
+  std::vector<MergeUnit> units;              // the row tiles that a second launch joins
   int64_t part_rows = 0;
   int32_t most_rows = 0, most_parts = 0;     // of a unit
 };
@@ -121,7 +128,7 @@ inline sa_status plan_kvq_items(const sa_layout* layout, int32_t batch, const in
   // How many tile microseconds n blocks do in one.  A block with a CU to itself is quicker
   // than one of two (0.6 of the time; of class 0 half or less, where HBM is what they share),
   // so the end of a launch, when places are empty, does not cost what they would have done.
-  // Over 40 drawn batches the parts chosen so took 1.02 times the best of nine limits' time.
+  // Over the 70 batches the parts chosen so took 1.02 times the best limit's time, at the worst 1.13.
   auto rate = [&](double n) {
     if (out.few) return std::min(2.1 * n, 2.05 * num_cu);
     return n <= num_cu ? 1.67 * n : std::min(2. * num_cu, 1.67 * num_cu + 0.33 * (n - num_cu));
@@ -134,22 +141,23 @@ inline sa_status plan_kvq_items(const sa_layout* layout, int32_t batch, const in
     parts_us.clear();
     double rows = 0, sum = 0;
     int64_t blocks = 0;
-    int most_parts = 0, most_join = 0;
+    double in_launch = 0;
+    int most_parts = 0;
+    bool again = false;
     for (const Tile& t : tiles) {
       const auto [parts, even] = parts_of(t, most);
       blocks += parts;
-      if (parts > 1) {
-        rows += (double)parts * t.rows;
-        most_join = std::max(most_join, parts * t.rows);
-      }
+      if (parts > 1) rows += (double)parts * t.rows;
+      if (parts > 1 && kvq_joins(t.cls, parts, t.rows))
+        in_launch = std::max(in_launch, kKvqInLaunchUs + parts * (t.cls < 2 ? kKvqReadRowUs * t.rows : kKvqReadTileUs));
+      else
+        again = again || parts > 1;
       most_parts = std::max(most_parts, parts);
-      const double us = std::min(even, t.n_tiles) * kKvqTileUs[t.cls] + (out.few ? kKvqFewItemUs : kKvqItemUs);
+      const double us = std::min(even, t.n_tiles) * kKvqTileUs[t.cls] + kKvqItemUs;
       sum += parts * us;
       if (blocks <= kKvqSimulated) parts_us.insert(parts_us.end(), (size_t)parts, us);
     }
-    const double join = rows == 0                                      ? 0.
-                        : out.few && most_join <= kKvqJoinRows ? kKvqInLaunchUs
-                                                                       : kKvqJoinUs + kKvqPartUs * most_parts + Hkv * rows * kKvqPartRowUs;
+    const double join = rows == 0 ? 0. : Hkv * rows * kKvqPartRowUs + (again ? kKvqJoinUs + kKvqPartUs * most_parts : in_launch);
     if (blocks > kKvqSimulated) return Hkv * sum / rate(slots) + join;
     std::sort(parts_us.begin(), parts_us.end(), std::greater<double>());
     // the first blocks go round the CUs: one that has to share its CU from the start does so to its end
@@ -181,23 +189,17 @@ inline sa_status plan_kvq_items(const sa_layout* layout, int32_t batch, const in
       best_us = us;
     }
   }
-  int most_join = 0;
-  int64_t groups = 0;
-  for (const Tile& t : tiles) {
-    const int used = parts_of(t, best).first;
-    if (used == 1) continue;
-    most_join = std::max(most_join, used * t.rows);
-    groups += Hkv;
-  }
-  out.joined = out.few && groups > 0 && groups <= kKvqCounters && most_join <= kKvqJoinRows;
   for (const Tile& t : tiles) {
     const auto [used, per] = parts_of(t, best);
     const int64_t row = out.part_rows;
+    const bool joins = used > 1 && kvq_joins(t.cls, used, t.rows) && out.counters + (int64_t)Hkv * kKvqCounted <= kKvqCounters;
     if (used > 1) {
-      if (!out.joined) out.units.push_back({t.q_start, t.row0, t.rows, (int32_t)row, used, t.rows, 0, 0, 0});
+      if (!joins) out.units.push_back({t.q_start, t.row0, t.rows, (int32_t)row, used, t.rows, 0, 0, 0});
       out.part_rows += (int64_t)Hkv * used * t.rows;
       if (out.part_rows > kMaxPartRows)
         return plan_fail(err, SA_ERR_SHAPE, "too many query rows for one launch (partial results)");
+    }
+    if (used > 1 && !joins) {
       out.most_rows = std::max(out.most_rows, t.rows);
       out.most_parts = std::max(out.most_parts, used);
     }
@@ -207,8 +209,8 @@ inline sa_status plan_kvq_items(const sa_layout* layout, int32_t batch, const in
         out.items.push_back({t.seq, h, t.row0, s * per * kKvqKeys,
                              (int32_t)std::min<int64_t>(t.keys, (int64_t)(s + 1) * per * kKvqKeys), t.cls, t.q_start,
                              h_q_len[t.seq], h_kv_len[t.seq], used > 1 ? (int32_t)(part0 + s * t.rows) : -1,
-                             used > 1 ? (int32_t)part0 : -1, used, out.joined && used > 1 ? (int32_t)out.counters : -1});
-      if (out.joined && used > 1) ++out.counters;
+                             used > 1 ? (int32_t)part0 : -1, used, joins ? (int32_t)out.counters : -1});
+      if (joins) out.counters += kKvqCounted;
     }
   }
   std::stable_sort(out.items.begin(), out.items.end(), [](const KvqItem& x, const KvqItem& y) {

@@ -209,7 +209,7 @@ struct sa_ctx {
   } shared_rec;
   struct KvqRec {
     size_t o_it = 0, n_items = 0, o_un = 0, n_units = 0;
-    bool few = false, joined = false;
+    bool few = false;
     int64_t total_q = 0, total_kv = 0, part_rows = 0, counters = 0;
     int most_rows = 0, block_rows = 8;
   } kvq_rec;
@@ -2046,7 +2046,6 @@ sa_status kvq_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const vo
     if (s != SA_OK) return s;
     PlanImage img;
     rec.few = plan.few;
-    rec.joined = plan.joined;
     rec.counters = plan.counters;
     rec.n_items = plan.items.size();
     rec.o_it = img.add(plan.items.data(), plan.items.size());
@@ -2084,9 +2083,8 @@ sa_status kvq_attn(sa_ctx* ctx, const sa_layout* layout, int32_t layer, const vo
   a.count = ctx->part_count;
   ctx->parts_used = std::max(ctx->parts_used, (rec.counters + sa::kPartCounters - 1) / sa::kPartCounters);
   static_assert(sa::kKvqCounters <= kMaxParts * sa::kPartCounters, "the counters a context owns");
-  auto kernel = layout->page_size == 16
-                    ? (rec.joined ? sa::attn_kvq_few_kernel<16, true> : rec.few ? sa::attn_kvq_few_kernel<16, false> : sa::attn_kvq_kernel<16>)
-                    : (rec.joined ? sa::attn_kvq_few_kernel<32, true> : rec.few ? sa::attn_kvq_few_kernel<32, false> : sa::attn_kvq_kernel<32>);
+  auto kernel = layout->page_size == 16 ? (rec.few ? sa::attn_kvq_few_kernel<16> : sa::attn_kvq_kernel<16>)
+                                        : (rec.few ? sa::attn_kvq_few_kernel<32> : sa::attn_kvq_kernel<32>);
   launch_timed(kernel, dim3((unsigned)rec.n_items), dim3(256), (hipStream_t)stream, ctx->kernel_ev[SA_TIMED_ATTN], a);
   SA_HIP(hipGetLastError());
   if (rec.n_units > 0) {

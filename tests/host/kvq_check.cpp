@@ -44,25 +44,23 @@ static void check(const sa_layout& L, const std::vector<int32_t>& q, const std::
   }
   std::map<int, int> joined;                                 // first partial row -> rows
   int64_t joined_rows = 0;
-  if (plan.joined) {                                         // by the launch itself: every group at a counter of its own
-    CHECK(plan.few && plan.units.empty() && plan.counters > 0 && plan.counters <= sa::kKvqCounters);
-    std::map<int, std::vector<const sa::KvqItem*>> groups;
-    for (const sa::KvqItem& it : plan.items) {
-      CHECK((it.part >= 0) == (it.counter >= 0) && (it.part >= 0) == (it.n_parts > 1));
-      if (it.part >= 0) groups[it.counter].push_back(&it);
+  std::map<int, std::vector<const sa::KvqItem*>> groups;     // joined by the launch itself: every tile at counters of its own
+  for (const sa::KvqItem& it : plan.items) {
+    CHECK((it.part >= 0) == (it.n_parts > 1) && (it.counter < 0 || it.part >= 0));
+    if (it.counter >= 0) groups[it.counter].push_back(&it);
+  }
+  CHECK((int64_t)groups.size() * sa::kKvqCounted == plan.counters && plan.counters <= sa::kKvqCounters);
+  for (auto& [c, items] : groups) {
+    const int rows = std::min(128, items[0]->q_len * G - items[0]->row0);
+    CHECK(c % sa::kKvqCounted == 0 && c < plan.counters && (int)items.size() == items[0]->n_parts);
+    CHECK(sa::kvq_joins(items[0]->cls, items[0]->n_parts, rows) && items[0]->n_parts * rows <= sa::kKvqMostJoin);
+    for (const sa::KvqItem* it : items) {
+      CHECK(it->part0 == items[0]->part0 && it->n_parts == items[0]->n_parts);
+      CHECK(it->part >= it->part0 && it->part + rows <= it->part0 + it->n_parts * rows);
+      CHECK(it->seq == items[0]->seq && it->kvh == items[0]->kvh && it->row0 == items[0]->row0);
+      CHECK(joined.emplace(it->part, rows).second);
     }
-    CHECK((int64_t)groups.size() == plan.counters && groups.begin()->first == 0 && groups.rbegin()->first == plan.counters - 1);
-    for (auto& [c, items] : groups) {
-      const int rows = std::min(128, items[0]->q_len * G - items[0]->row0);
-      CHECK((int)items.size() == items[0]->n_parts && items[0]->n_parts * rows <= sa::kKvqJoinRows);
-      for (const sa::KvqItem* it : items) {
-        CHECK(it->part0 == items[0]->part0 && it->n_parts == items[0]->n_parts);
-        CHECK(it->part >= it->part0 && it->part + rows <= it->part0 + it->n_parts * rows);
-        CHECK(it->seq == items[0]->seq && it->kvh == items[0]->kvh && it->row0 == items[0]->row0);
-        CHECK(joined.emplace(it->part, rows).second);
-      }
-      joined_rows += (int64_t)items.size() * rows;
-    }
+    joined_rows += (int64_t)items.size() * rows;
   }
   for (const sa::MergeUnit& u : plan.units) {
     CHECK(u.b_n == 0 && u.a_n >= 2 && u.n >= 1 && u.n <= plan.most_rows && u.a_n <= plan.most_parts);
