@@ -795,7 +795,7 @@ sa_status sa_kvq_unpack(sa_ctx *ctx, const sa_layout *layout, int64_t num_slots4
  * O = softmax(softmax_scale * q . K^T) V with the values the cache stands for.
  * Scores are the products of the cached keys with the bf16 query rows, held
  * times the scale as three 6-bit floats per value (within 2^-13 of the largest of
- * its 32 dims), summed in fp32; probabilities are rounded to bf16 before the PV product, the rest
+ * its 32 dims, or 2^-129), summed in fp32; probabilities are rounded to bf16 before the PV product, the rest
  * is fp32.  A row that sees a key with a NaN block has a NaN output and a NaN LSE; a
  * NaN block of a value it sees makes those 32 dims of its output NaN.  What a row
  * does not see does not reach it.  A page that is missing or outside the pool reads

@@ -506,6 +506,21 @@ def test_queries_of_all_sizes():
     check_attn(attn_case(93, *args, q_change=q_change, scale=1e-4), *args, scale=1e-4)
 
 
+@pytest.mark.parametrize("power", [100, -100])
+@pytest.mark.parametrize("heads,page,q,kv", [((8, 2), 16, [1, 3, 9], [300, 65, 900]), ((8, 2), 32, [12, 40], [500, 700])])
+def test_scales_far_from_one(heads, page, q, kv, power):
+    """Keys and values times 2^100 or 2^-100, queries by the other: scores are what they were."""
+    def change(k, v, indptr, indices):
+        for pool in (k, v):
+            scales = pool[..., 64 * page:]
+            scales[scales != 255] += np.uint8(power % 256)
+
+    def q_change(x):
+        x.copy_((x.float() * 2.0 ** -power).to(torch.bfloat16))
+    args = (heads, page, q, kv, True)
+    check_attn(attn_case(94, *args, change=change, q_change=q_change), *args)
+
+
 # ---- values that are not finite
 
 def scale_at(pool, layer, slot, head, row, block, P):
