@@ -793,9 +793,10 @@ sa_status sa_kvq_unpack(sa_ctx *ctx, const sa_layout *layout, int64_t num_slots4
  * q_len, kv_len >= 0); where kv_len is 0 the rows are zeros and their LSE is
  * -infinity.  Lengths of keys are at most 2^31 - 64.
  * O = softmax(softmax_scale * q . K^T) V with the values the cache stands for.
- * Scores are the products of the cached keys with the bf16 query rows, held
- * times the scale as three 6-bit floats per value (within 2^-13 of the largest of
- * its 32 dims, or 2^-129), summed in fp32; probabilities are rounded to bf16 before the PV product, the rest
+ * Scores are the products of the cached keys with the bf16 query rows, held as three
+ * 6-bit floats per value (itself from 2^-6 of the largest of its 32 dims on, others
+ * within 2^-14 of that, or 2^-129), summed in fp32 and then scaled; probabilities are
+ * rounded to bf16 before the PV product, the rest
  * is fp32.  A row that sees a key with a NaN block has a NaN output and a NaN LSE; a
  * NaN block of a value it sees makes those 32 dims of its output NaN.  What a row
  * does not see does not reach it.  A page that is missing or outside the pool reads

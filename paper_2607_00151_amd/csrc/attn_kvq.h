@@ -2,17 +2,18 @@
 //
 // Row i of a sequence sees keys j < limit_i (its position, or every key where there
 // is no mask):
-//   s_j = scale q . k_j,  m = max s_j,  O = sum 2^(s_j - m) v_j / l,  l = sum 2^(s_j - m)
-// in the exp2 domain, in one pass with m, l and O carried and rescaled when scores outgrow m.
+//   s_j = c q . k_j,  m = max s_j,  O = sum 2^(s_j - m) v_j / l,  l = sum 2^(s_j - m)
+// with c = scale log2 e, in one pass with m, l and O carried and rescaled when scores outgrow m.
 //
 // Scores come out of the block-scaled matrix instruction (16x16x128), which takes
 // the keys as they lie in the cache: lane l's operand is the 16 code bytes of key
 // l % 16, block l / 16, with that block's scale byte, so a wave's load of 16 keys is
-// one contiguous KB.  The query goes in as three 6-bit floats per value (e2m3, scales
-// 2^e, 2^(e-4), 2^(e-8) per 32 dims, each the rounded rest of the one before), which
-// together are scale times the bf16 value to 2^-13 of the block's largest: against a bf16 product
-// of converted keys the matrix work is 3/4 and the conversion goes, and two 8-bit
-// pieces would cost 4/4 and lose 2^-14 in the instruction's sum (measured).
+// one contiguous KB.  The query goes in as three 6-bit floats per value (e2m3, scales 2^e,
+// 2^(e-4), 2^(e-10) per 32 dims, each the rounded rest of the one before): the bf16 value
+// itself from 2^-6 of the block's largest on, others to 2^-14 of it.  c is multiplied in
+// behind the product, in fp32.  Against a bf16 product of converted keys the matrix work is 3/4
+// and the conversion goes; two 8-bit pieces would cost 4/4 and lose 2^-14 in the instruction's
+// sum (measured).
 // Values have a scale per key and 32 dims, which a sum over keys cannot take in that
 // instruction: they are converted to bf16 (exactly; 2 per v_cvt), laid out in LDS and
 // read back transposed for the 16x16x32 bf16 product.  Probabilities are rounded to
@@ -53,7 +54,7 @@ struct KvqAttnArgs {
   int32_t* err;
   int32_t num_slots, Hq, Hkv, G;
   int32_t causal;
-  float c;                   // softmax scale times log2 e, which goes into the query rows
+  float c;                   // softmax scale times log2 e
 };
 
 // A head's page through a resource, which holds nothing where the slot is -1: zeros then.
@@ -74,11 +75,14 @@ typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x32 __attribute__((ext_vector_type(32)));
 
-// c times 32 dims of a query row as three 6-bit pieces; scales: their bytes (255: the
-// block holds an infinity or a NaN).  The rests are exact.  With S the first piece's
-// scale, they are at most S / 4, S / 128 and in the end S / 4096: half a step each time,
-// of steps S / 2 (values from 4 S), S / 64 (rests from 2 S / 16) and S / 2048.
-__device__ __forceinline__ void kvq_split_q(const uint16_t* p, float c, u32x6 (&piece)[3], int& scales) {
+// 32 dims of a query row as three 6-bit pieces; scales: their bytes (255: the block holds
+// an infinity or a NaN).  The rests are exact.  With S the first piece's scale, the largest
+// dim is 3.75 to 7.5 S, and the first rest is at most S / 4, of a bf16 value with 4 bits
+// behind those taken: two pieces, the second from S / 128 on, hold dims from S on exactly.  The
+// rest of others is at most S / 2^8, 4 of the third piece's units: it comes to S / 2^13 at most
+// (half its largest step), and to nothing from S / 2^5 on.  Without c: c times a bf16 value is
+// none, and three pieces of it leave 20 times as much of normal rows.
+__device__ __forceinline__ void kvq_split_q(const uint16_t* p, u32x6 (&piece)[3], int& scales) {
   u32x4 w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = ld_u32x4(p + 8 * i);
@@ -87,19 +91,19 @@ __device__ __forceinline__ void kvq_split_q(const uint16_t* p, float c, u32x6 (&
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) top = max(top, max(w[i][e] & 0x7FFF0000u, (w[i][e] << 16) & 0x7FFF0000u));
-  top = top < 0x7F800000u ? __float_as_uint(__uint_as_float(top) * c) : top;
   const bool fine = top < 0x7F800000u;
-  const int s = max((int)((top + 0x100000u) >> 23) - 2, 10);   // the block's largest is 3.75 to 7.5 (the format's own) times the scale
+  const int s = max((int)((top + 0x100000u) >> 23) - 2, 11);   // 7.5: the format's largest
   f32x16 even, odd;                                          // dims 2 i and 2 i + 1, as the conversion takes them
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const uint32_t two = fine ? w[i >> 2][i & 3] : 0u;
-    even[i] = __uint_as_float(two << 16) * c;
-    odd[i] = __uint_as_float(two & 0xFFFF0000u) * c;
+    even[i] = __uint_as_float(two << 16);
+    odd[i] = __uint_as_float(two & 0xFFFF0000u);
   }
+  constexpr int kDown[3] = {0, 4, 10};
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
-    const float unit = __uint_as_float((uint32_t)(s - 4 * k) << 23);
+    const float unit = __uint_as_float((uint32_t)(s - kDown[k]) << 23);
     const auto six = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, unit);
     piece[k] = __builtin_bit_cast(u32x6, six);
     if (k == 2) break;
@@ -110,18 +114,18 @@ __device__ __forceinline__ void kvq_split_q(const uint16_t* p, float c, u32x6 (&
       odd[i] -= back[2 * i + 1];
     }
   }
-  scales = fine ? s | (s - 4) << 8 | (s - 8) << 16 : 0xFFFFFF;
+  scales = fine ? s | (s - kDown[1]) << 8 | (s - kDown[2]) << 16 : 0xFFFFFF;
 }
 
-// s plus 16 keys (codes and scale byte kScale of `scales`) times 16 query rows in pieces,
-// the smallest first.
+// 16 keys (codes and scale byte kScale of `scales`) times 16 query rows in pieces, the
+// smallest first.
 template <int kScale>
-__device__ __forceinline__ f32x4 kvq_scores(u32x4 key, uint32_t scales, const u32x6 (&q)[3], int q_scales, f32x4 s) {
+__device__ __forceinline__ f32x4 kvq_scores(u32x4 key, uint32_t scales, const u32x6 (&q)[3], int q_scales) {
   const i32x8 a = {(int)key[0], (int)key[1], (int)key[2], (int)key[3], 0, 0, 0, 0};
   auto piece = [&](const u32x6& w) __attribute__((always_inline)) {
     return i32x8{(int)w[0], (int)w[1], (int)w[2], (int)w[3], (int)w[4], (int)w[5], 0, 0};
   };
-  s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, piece(q[2]), s, 4, 2, kScale, (int)scales, 2, q_scales);
+  f32x4 s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, piece(q[2]), f32x4{}, 4, 2, kScale, (int)scales, 2, q_scales);
   s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, piece(q[1]), s, 4, 2, kScale, (int)scales, 1, q_scales);
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, piece(q[0]), s, 4, 2, kScale, (int)scales, 0, q_scales);
 }
@@ -142,8 +146,10 @@ __device__ __forceinline__ float row4_sum(float x) {
 constexpr int kKvqWaves = 4;
 // How far (log2) scores may outgrow a row's offset before l and O are rescaled: weights
 // then reach 2^8, which their rounding to bf16, relative as it is, does not notice.  Moved
-// at every growth, some row of a wave moves in 45% of the tiles of 8K keys.
-constexpr float kKvqLag = 8.f;
+// at every growth, some row of a wave moves in 45% of the tiles of 8K keys.  Where the
+// waves split the rows no maximum is taken at all as long as a lane's 16 weights of a row
+// come to no more than kKvqMost (sums of values from 2^110 on may overflow then).
+constexpr float kKvqLag = 8.f, kKvqMost = 65536.f;
 // Bytes of a key's bf16 values in LDS: 32 more than they take, so that the 8 keys x 32
 // bytes of half a wave's transposed reads, and the 8 rows' chunks of a quarter's
 // writes, lie in different banks.
@@ -343,7 +349,7 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqIt
     const int tok = rr / G;
     const int head = it.kvh * G + (rr - tok * G);
     limit[nb] = min(it.kv_end, a.causal ? pre + tok + 1 : it.kv_len);
-    kvq_split_q(a.q + ((int64_t)(it.q_start + tok) * a.Hq + head) * kHD + g * 32, a.c, q[nb], qs[nb]);
+    kvq_split_q(a.q + ((int64_t)(it.q_start + tok) * a.Hq + head) * kHD + g * 32, q[nb], qs[nb]);
   }
   // keys below are seen by all rows
   const int all_see = min(it.kv_end, a.causal ? pre + it.row0 / G + 1 : it.kv_len);
@@ -391,9 +397,7 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqIt
     for (int nb = 0; nb < kNB; ++nb) {
       f32x4 s[4];
 #pragma unroll
-      for (int kb = 0; kb < 4; ++kb) {
-        s[kb] = kvq_scores<0>(now.k[kb], now.ks[kb], q[nb], qs[nb], f32x4{});
-      }
+      for (int kb = 0; kb < 4; ++kb) s[kb] = kvq_scores<0>(now.k[kb], now.ks[kb], q[nb], qs[nb]);
       if (masked) {
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb)
@@ -404,7 +408,7 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqIt
       float top = s[0][0];
 #pragma unroll
       for (int j = 1; j < 16; ++j) top = vmax(top, s[j >> 2][j & 3]);
-      const float grown = vmax(m[nb], row4_max(top));
+      const float grown = vmax(m[nb], row4_max(top) * a.c);
       if (__ballot(!(grown <= m[nb] + kKvqLag))) {
         const float f = exp2f_fast(m[nb] - (grown == -INFINITY ? 0.f : grown));
         l[nb] *= f;
@@ -417,7 +421,7 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqIt
       for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float e = exp2f_fast(s[kb][i] - off);
+          const float e = exp2f_fast(__builtin_fmaf(s[kb][i], a.c, -off));
           l[nb] += e;
           p[nb][kb >> 1][4 * (kb & 1) + i] = (__bf16)e;
         }
@@ -509,12 +513,12 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqIt
 // Items of up to 64 kNB rows whose four waves hold 16 kNB rows each and go over the
 // same keys together: the tile's values are converted once, a quarter by each wave.
 //
-// A step makes the scores of tile t + 1 while the probabilities of tile t are taken,
-// and then O += P V of tile t with the row maxima of t + 1: matrix and vector
-// instructions of one wave, each independent of the other's.  Behind the barrier of
-// step t - 1 LDS holds the values of tile t (bf16) and the codes of the keys of t + 1;
-// step t writes the values of t + 1 and the keys of t + 2 from registers, whose
-// loads were issued a step before.
+// A step makes the scores of tile t + 1 while the probabilities of tile t are taken, and
+// then O += P V of tile t while the values of t + 1 are converted: matrix and vector
+// instructions of one wave, each independent of the other's.  Behind the barrier of step
+// t - 1 LDS holds the values of tile t (bf16) and the codes of the keys of t + 1; step t
+// writes the values of t + 1 and the keys of t + 2 from registers, whose loads were issued
+// a step before.
 constexpr int kKvqTile = 64 * kKvqVRow, kKvqKeyBytes = 64 * kKvqCodes;
 struct KvqRowsLds {
   uint8_t v[2][kKvqTile];
@@ -622,25 +626,24 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
     const int tok = rr / G;
     const int head = it.kvh * G + (rr - tok * G);
     limit[nb] = min(it.kv_end, a.causal ? pre + tok + 1 : it.kv_len);
-    kvq_split_q(a.q + ((int64_t)(it.q_start + tok) * a.Hq + head) * kHD + g * 32, a.c, q[nb], qs[nb]);
+    kvq_split_q(a.q + ((int64_t)(it.q_start + tok) * a.Hq + head) * kHD + g * 32, q[nb], qs[nb]);
   }
   const int wave_sees = min(it.kv_end, a.causal ? pre + (it.row0 + min(wrow, rows - 1)) / G + 1 : it.kv_len);
 
   f32x4 o[kNB][8];
-  float m[kNB], l[kNB];
+  float m[kNB], l[kNB], off[kNB], most[kNB];   // off: m, or 0 where the row has met no key
   uint32_t poison[kNB];
 #pragma unroll
   for (int nb = 0; nb < kNB; ++nb) {
     m[nb] = -INFINITY;
     l[nb] = 0.f;
+    off[nb] = 0.f;
+    most[nb] = -1.f;
     poison[nb] = 0;
 #pragma unroll
     for (int db = 0; db < 8; ++db) o[nb][db] = f32x4{};
   }
 
-  f32x4 start[kNB];                            // of the scores: -m, or 0 where the row has met no key
-#pragma unroll
-  for (int nb = 0; nb < kNB; ++nb) start[nb] = f32x4{};
   auto scores = [&](int b, f32x4 (&x)[kNB][4]) __attribute__((always_inline)) {
     const uint32_t scales = lds->ks[b][lane];
     const lds_u8* const k = k0 + b * kKeyBytes + lane * 16;
@@ -649,25 +652,66 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
     for (int kb = 0; kb < 4; ++kb) key[kb] = *(const __attribute__((address_space(3))) u32x4*)(k + kb * 1024);
 #pragma unroll
     for (int nb = 0; nb < kNB; ++nb) {
-      x[nb][0] = kvq_scores<0>(key[0], scales, q[nb], qs[nb], start[nb]);
-      x[nb][1] = kvq_scores<1>(key[1], scales, q[nb], qs[nb], start[nb]);
-      x[nb][2] = kvq_scores<2>(key[2], scales, q[nb], qs[nb], start[nb]);
-      x[nb][3] = kvq_scores<3>(key[3], scales, q[nb], qs[nb], start[nb]);
+      x[nb][0] = kvq_scores<0>(key[0], scales, q[nb], qs[nb]);
+      x[nb][1] = kvq_scores<1>(key[1], scales, q[nb], qs[nb]);
+      x[nb][2] = kvq_scores<2>(key[2], scales, q[nb], qs[nb]);
+      x[nb][3] = kvq_scores<3>(key[3], scales, q[nb], qs[nb]);
     }
   };
-  // P of a tile's scores
-  auto weigh = [&](const f32x4 (&x)[kNB][4], bf16x8 (&p)[kNB][2]) __attribute__((always_inline)) {
+  // m, l and O moved to the maxima of a tile's scores
+  auto settle = [&](const f32x4 (&x)[kNB][4]) __attribute__((always_inline)) {
 #pragma unroll
     for (int nb = 0; nb < kNB; ++nb) {
-      float sum[2] = {0.f, 0.f};
+      float top = x[nb][0][0];
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const float e = exp2f_fast(x[nb][j >> 2][j & 3]);
-        sum[j & 1] += e;
-        p[nb][j >> 3][j & 7] = (__bf16)e;
-      }
-      l[nb] += sum[0] + sum[1];
+      for (int j = 1; j < 16; ++j) top = vmax(top, x[nb][j >> 2][j & 3]);
+      top = vmax(m[nb], row4_max(top) * a.c);
+      const bool met = top != -INFINITY;
+      off[nb] = met ? top : 0.f;
+      most[nb] = met ? kKvqMost : -1.f;
+      const float f = exp2f_fast(m[nb] - off[nb]);
+      l[nb] *= f;
+#pragma unroll
+      for (int db = 0; db < 8; ++db) o[nb][db] *= f;
+      m[nb] = top;
     }
+  };
+  // P of a tile's scores, from the offsets as they are.  Only where a lane's weights come to more than
+  // kKvqMost, or its row has met no key, m, l and O are moved to the maxima and P is taken again: 34
+  // vector instructions less in a step, which pays for c behind the product (246 us for 2048 rows x 4
+  // heads behind 8K keys; 266 with maxima, 250 with c in the query).  ahead: the scores of the next
+  // tile, which the compiler else moves behind the branch, away from the exponentials.
+  auto weigh = [&](const f32x4 (&x)[kNB][4], bf16x8 (&p)[kNB][2], const f32x4 (*ahead)[4]) __attribute__((always_inline)) {
+    float sum[kNB];
+    auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int nb = 0; nb < kNB; ++nb) {
+        float part[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const float e = exp2f_fast(__builtin_fmaf(x[nb][j >> 2][j & 3], a.c, -off[nb]));
+          part[j & 1] += e;
+          p[nb][j >> 3][j & 7] = (__bf16)e;
+        }
+        sum[nb] = part[0] + part[1];
+      }
+    };
+    weights();
+    if (ahead != nullptr) {
+#pragma unroll
+      for (int nb = 0; nb < kNB; ++nb)
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) asm volatile("" ::"v"(ahead[nb][kb]));
+    }
+    bool far = false;
+#pragma unroll
+    for (int nb = 0; nb < kNB; ++nb) far |= !(sum[nb] <= most[nb]);
+    if (__ballot(far)) {
+      settle(x);
+      weights();
+    }
+#pragma unroll
+    for (int nb = 0; nb < kNB; ++nb) l[nb] += sum[nb];
   };
   auto product = [&](int b, const bf16x8 (&p)[kNB][2]) __attribute__((always_inline)) {
     const lds_u8* const vt = v0 + b * kTile + (4 * g + (r16 >> 2)) * kKvqVRow + 8 * (r16 & 3);
@@ -687,35 +731,6 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
           o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[nb][half], o[nb][db], 0, 0, 0);
       }
   };
-  auto maxima = [&](const f32x4 (&x)[kNB][4], float (&top)[kNB]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int nb = 0; nb < kNB; ++nb) {
-      top[nb] = x[nb][0][0];
-#pragma unroll
-      for (int j = 1; j < 16; ++j) top[nb] = vmax(top[nb], x[nb][j >> 2][j & 3]);
-      top[nb] = vmax(m[nb], row4_max(top[nb]) - start[nb][0]);
-    }
-  };
-  // m, l, O and the scores themselves moved to their maxima
-  auto settle = [&](f32x4 (&x)[kNB][4], const float (&top)[kNB]) __attribute__((always_inline)) {
-    bool moves = false;
-#pragma unroll
-    for (int nb = 0; nb < kNB; ++nb) moves |= !(top[nb] <= m[nb] + kKvqLag);
-    if (__ballot(moves)) {
-#pragma unroll
-      for (int nb = 0; nb < kNB; ++nb) {
-        const float to = top[nb] == -INFINITY ? 0.f : top[nb];
-        const float f = exp2f_fast(m[nb] - to);
-        l[nb] *= f;
-#pragma unroll
-        for (int db = 0; db < 8; ++db) o[nb][db] *= f;
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb) x[nb][kb] += -to - start[nb][0];
-        m[nb] = top[nb];
-        start[nb] = f32x4{-to, -to, -to, -to};
-      }
-    }
-  };
   auto mask = [&](int t, f32x4 (&x)[kNB][4]) __attribute__((always_inline)) {
 #pragma unroll
     for (int nb = 0; nb < kNB; ++nb)
@@ -733,9 +748,7 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
     lds_barrier();
     scores(0, s[0]);
     if ((t0 + 1) * kKeys > wave_sees) mask(t0, s[0]);
-    float top[kNB];
-    maxima(s[0], top);
-    settle(s[0], top);
+    settle(s[0]);
     if (t0 + 1 < t1) {
       put_k(1, kx);
       load_v(t0 + 1, vx);
@@ -743,26 +756,23 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
     }
     lds_barrier();
   }
-  // steps whose tile and the next one all rows see, and behind which two more follow: no branch but the
-  // slots' and the rescale's, so that the compiler mixes their instructions
+  // steps whose tile and the next one all rows see: no branch but the slots' and the rescale's, so that the
+  // compiler mixes their instructions; keys and values behind the item's last tile are loaded as zeros
   auto plain = [&](int t, auto buf) __attribute__((always_inline)) {
     constexpr int b = decltype(buf)::value;
     need_slots(t + 3);
     bf16x8 p[kNB][2];
-    float top[kNB];
     scores(b ^ 1, s[b ^ 1]);
-    weigh(s[b], p);
+    weigh(s[b], p, s[b ^ 1]);
     put_v(b ^ 1, vx);
     put_k(b, kx);
     load_v(t + 2, vx);
     load_k(t + 3, kx);
     product(b, p);
-    maxima(s[b ^ 1], top);
-    settle(s[b ^ 1], top);
     lds_barrier();
   };
   int t = t0;
-  for (const int end = min(t1 - 3, all_see / kKeys - 1); t + 1 < end; t += 2) {
+  for (const int end = min(t1, all_see / kKeys) - 1; t + 1 < end; t += 2) {
     plain(t, std::integral_constant<int, 0>{});
     plain(t + 1, std::integral_constant<int, 1>{});
   }
@@ -770,7 +780,7 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
     const int b = (t - t0) & 1;
     bf16x8 p[kNB][2];
     if (t + 1 < t1) scores(b ^ 1, s[1]);
-    weigh(s[0], p);
+    weigh(s[0], p, nullptr);
     product(b, p);
     if ((t + 1) * kKeys > all_see) {
 #pragma unroll
@@ -792,9 +802,6 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
         if (t + 3 < t1) load_k(t + 3, kx);
       }
       if ((t + 2) * kKeys > wave_sees) mask(t + 1, s[1]);
-      float top[kNB];
-      maxima(s[1], top);
-      settle(s[1], top);
     }
 #pragma unroll
     for (int nb = 0; nb < kNB; ++nb)

@@ -59,8 +59,8 @@ def attention(q, k, v, scale, causal):
     """One sequence in float64: q [n][Hq][128]; k, v [Hkv][kv][128].  Returns o, lse, and what each may be off by.
 
     Probabilities are rounded to bf16 (2^-8 of sum p |v| / l = A) and so is the output (2^-8 |o|).  A score is off by
-    e = scale (2^-13 sum over blocks of max |q| sum |k| + 128 2^-23 sum |q k|) at most: the query's pieces (the last of
-    three leaves S / 4096 of a block whose largest value is at least 3.75 S), and the fp32 sum; that moves every weight by a factor within exp(+-2 e).  The fp32 sums over n keys add n 2^-23 A."""
+    e = scale (2^-14 sum over blocks of max |q| sum |k| + 128 2^-23 sum |q k|) at most: the query's pieces (the last of
+    three leaves S / 2^13 of a block whose largest value is at least 3.75 S), and the fp32 sum; that moves every weight by a factor within exp(+-2 e).  The fp32 sums over n keys add n 2^-23 A."""
     n, Hq, kv = q.shape[0], q.shape[1], k.shape[1]
     G = Hq // k.shape[0]
     o, lse = torch.zeros((n, Hq, D), dtype=torch.float64), torch.full((n, Hq), -math.inf, dtype=torch.float64)
@@ -79,7 +79,7 @@ def attention(q, k, v, scale, causal):
         a = w @ vv.abs()
         out = w @ vv
         kb = kk.abs().reshape(kv, 4, 32).sum(-1)
-        e = (q[:, h].abs().reshape(n, 4, 32).amax(-1) @ kb.t() * 2.0 ** -13 + q[:, h].abs() @ kk.abs().t() * 128 * 2.0 ** -23) * scale
+        e = (q[:, h].abs().reshape(n, 4, 32).amax(-1) @ kb.t() * 2.0 ** -14 + q[:, h].abs() @ kk.abs().t() * 128 * 2.0 ** -23) * scale
         e = torch.where(seen, e, 0).amax(1, keepdim=True)
         o[:, h], lse[:, h] = out.cpu(), (top + torch.log(total))[:, 0].cpu()
         tol[:, h] = (2.0 ** -8 * (a + out.abs()) + (4 * e + (kv + 64) * 2.0 ** -23) * a).cpu() + 1e-30

@@ -506,6 +506,24 @@ def test_queries_of_all_sizes():
     check_attn(attn_case(93, *args, q_change=q_change, scale=1e-4), *args, scale=1e-4)
 
 
+@pytest.mark.parametrize("heads,page,q,kv", [((8, 2), 16, [1, 6], [900, 1500]), ((8, 2), 16, [20, 12], [1100, 640]),
+                                             ((32, 4), 32, [30, 7], [3000, 1290])])
+@pytest.mark.parametrize("slope", [0.5, 8.0, -8.0])
+def test_scores_that_rise_or_fall_along_the_keys(heads, page, q, kv, slope):
+    """Offsets that every few tiles outgrow, every one, or none behind the first."""
+    def change(k, v, indptr, indices):
+        for b, n in enumerate(kv):
+            slots = indices[indptr[b]:indptr[b + 1]]
+            x = np.zeros((len(slots), heads[1], page, D))
+            x += (slope * np.arange(len(slots) * page) / 64).reshape(-1, 1, page, 1)
+            k[-1, slots] = page_bytes(x * (1 + 0.25 * np.arange(D) / D))
+
+    def q_change(x):
+        x.copy_((x.float() + 0.5).to(torch.bfloat16))
+    args = (heads, page, q, kv, True)
+    check_attn(attn_case(95, *args, change=change, q_change=q_change, std=0.25), *args)
+
+
 @pytest.mark.parametrize("power", [100, -100])
 @pytest.mark.parametrize("heads,page,q,kv", [((8, 2), 16, [1, 3, 9], [300, 65, 900]), ((8, 2), 32, [12, 40], [500, 700])])
 def test_scales_far_from_one(heads, page, q, kv, power):
