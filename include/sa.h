@@ -745,8 +745,8 @@ sa_status sa_kv_append_rope_axes(sa_ctx *ctx, const sa_layout *layout, int32_t l
  * NULL, h_pos and axes too, and q_stride is not read.  Otherwise the key heads, and
  * the query heads where q and q_out are given (both or neither), are normed and
  * rotated as by sa_kv_append_rope (axes NULL; positions from h_pos, or h_start) or
- * sa_kv_append_rope_axes (h_pos NULL); keys are quantised from the fp32 results,
- * query rows rounded to bf16.  Value rows are quantised as they are.  Rows go to the
+ * sa_kv_append_rope_axes (h_pos NULL); keys are computed in 64 bits and
+ * quantised from that, query rows in fp32 and rounded to bf16.  Value rows are quantised as they are.  Rows go to the
  * positions sa_kv_append would give them; nothing else in the pools changes.
  *
  * Errors: as sa_kv_append_rope and sa_kv_append_rope_axes, for the arguments given;

@@ -28,6 +28,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "common.h"
 #include "kvq_kernels.h"
 #include "kv_kernels.h"
@@ -82,29 +84,33 @@ __device__ __forceinline__ int wave_find_seq(const int32_t* tok_begin, int B, in
   return lo;
 }
 
-// Sine and cosine of a phase in fractions of 2^32 of a turn, to about an fp32 rounding:
-// the nearest quarter turn goes by symmetry, the rest, up to an eighth, by the Taylor
-// series up to the 9th and 10th power (what is left out is below 2^-28).  v_sin and v_cos
-// are off by some 2^-21, which a rounding to bf16 hides but which decides more of the ties
-// between two elements of 4 bits, a whole step apart.
-__device__ __forceinline__ void turn_sincos(uint32_t phase, float& sine, float& cosine) {
-  const uint32_t quarter = (phase + 0x20000000u) >> 30;
-  const float a = (float)(int32_t)(phase - (quarter << 30)) * 1.4629180792671596e-9f;   // 2 pi / 2^32
-  const float x = a * a;
-  float s = __builtin_fmaf(x, 2.7557319e-6f, -1.9841270e-4f);
-  s = __builtin_fmaf(x, s, 8.3333333e-3f);
-  s = __builtin_fmaf(x, s, -1.6666667e-1f);
-  s = __builtin_fmaf(a * x, s, a);
-  float c = __builtin_fmaf(x, -2.7557319e-7f, 2.4801587e-5f);
-  c = __builtin_fmaf(x, c, -1.3888889e-3f);
-  c = __builtin_fmaf(x, c, 4.1666667e-2f);
-  c = __builtin_fmaf(x, c, -0.5f);
-  c = __builtin_fmaf(x, c, 1.f);
+// Sine and cosine of a phase in fractions of 2^64 of a turn, to some 2^-45: the nearest
+// quarter turn goes by symmetry, the rest, up to an eighth, by the Taylor series up to the
+// 13th and 14th power.
+__device__ __forceinline__ void turn_sincos(uint64_t phase, double& sine, double& cosine) {
+  const uint32_t quarter = (uint32_t)((phase + (uint64_t(1) << 61)) >> 62);
+  const double a = (double)(int64_t)(phase - ((uint64_t)quarter << 62)) * 3.4061215800304785e-19;   // 2 pi / 2^64
+  const double x = a * a;
+  double s = __builtin_fma(x, 1. / 6227020800., -1. / 39916800.);
+  s = __builtin_fma(x, s, 1. / 362880.);
+  s = __builtin_fma(x, s, -1. / 5040.);
+  s = __builtin_fma(x, s, 1. / 120.);
+  s = __builtin_fma(x, s, -1. / 6.);
+  s = __builtin_fma(a * x, s, a);
+  double c = __builtin_fma(x, -1. / 87178291200., 1. / 479001600.);
+  c = __builtin_fma(x, c, -1. / 3628800.);
+  c = __builtin_fma(x, c, 1. / 40320.);
+  c = __builtin_fma(x, c, -1. / 720.);
+  c = __builtin_fma(x, c, 1. / 24.);
+  c = __builtin_fma(x, c, -0.5);
+  c = __builtin_fma(x, c, 1.);
   sine = quarter & 1 ? c : s;
   cosine = quarter & 1 ? s : c;
   if (quarter & 2) sine = -sine;
   if ((quarter + 1) & 2) cosine = -cosine;
 }
+
+typedef double f64x2 __attribute__((ext_vector_type(2)));
 
 template <int kCtrl>
 __device__ __forceinline__ float row16(float x) {
@@ -122,6 +128,34 @@ __device__ __forceinline__ float row16_sum(float x) {
   x += row16<0x128>(x);      // 8 lanes on
   return x;
 }
+__device__ __forceinline__ double row16_sum(double x) {
+  auto add = [&](auto ctrl) __attribute__((always_inline)) {
+    const uint64_t w = __builtin_bit_cast(uint64_t, x);
+    const uint64_t lo = row16u<decltype(ctrl)::value>((uint32_t)w), hi = row16u<decltype(ctrl)::value>((uint32_t)(w >> 32));
+    x += __builtin_bit_cast(double, hi << 32 | lo);
+  };
+  add(std::integral_constant<int, 0xB1>{});
+  add(std::integral_constant<int, 0x4E>{});
+  add(std::integral_constant<int, 0x124>{});
+  add(std::integral_constant<int, 0x128>{});
+  return x;
+}
+
+// To fp32 with the last bit set where anything is cut off, so that no later rounding finds
+// a tie that is none.
+__device__ __forceinline__ float rounded_to_odd(double z) {
+  const float f = (float)z;
+  const double rest = z - (double)f;
+  const uint32_t w = __float_as_uint(f);
+  const bool odd = (w & 1) != 0 || rest == 0. || f == 0.f || !(fabsf(f) < INFINITY);
+  return odd ? f : __uint_as_float((rest > 0.) == (f > 0.f) ? w + 1 : w - 1);
+}
+
+// out = r (x own + p other), p the pair's other value
+struct RopeCoef {
+  float own[8], other[8];
+  bool normed;
+};
 
 __device__ __forceinline__ void unpack8(u32x4 w, float (&x)[8]) {
 #pragma unroll
@@ -146,9 +180,13 @@ constexpr int64_t kRopeStreamBytes = int64_t(256) << 20;
 // token's positions are loaded by as many lanes beside the axis numbers, not behind
 // them, and handed round.
 //
-// kKvq: key and value rows go into pages of 4 bits (kvq_kernels.h), keys from the fp32
-// results: a lane's 8 dims are a quarter of a block, so the scale is a maximum over
-// 4 lanes.  With Hq = 0 and nothing to norm or rotate the keys are the input's bits.
+// kKvq: key and value rows go into pages of 4 bits (kvq_kernels.h): a lane's 8 dims are
+// a quarter of a block, so the scale is a maximum over 4 lanes.  Keys are normed and
+// rotated in 64 bits, since a value by a tie between two elements moves by a whole step:
+// of 10 million values of fp32 results about one does.  16 requests of 512 to 4096 new
+// tokens with the pages read back take 220 us so, 200 in fp32; with the coefficients of
+// the keys held in 64 bits 227, and with fewer rounds to a wave 253 and more.  With
+// nothing to norm or rotate the keys are the input's bits.
 template <RopePair kPair, bool kStream, bool kAxes = false, bool kKvq = false>
 __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
   const int lane = threadIdx.x & 63;
@@ -206,6 +244,21 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
   uint32_t pos = 0;
   if constexpr (!kAxes) pos = (uint32_t)(a.pos[b] + step);
   float cs[8], sn[8];
+  f64x2* turns = nullptr;                                   // of this wave: cosine and sine of each pair
+  if constexpr (kKvq) {
+    // lane j works pair j out, and the lanes of its dims read it
+    __shared__ f64x2 lds[4][64];
+    turns = lds[threadIdx.x >> 6];
+    const bool mine = 2 * lane < a.rot;
+    if constexpr (kAxes) pos = (uint32_t)__shfl(token_pos, mine ? a.axis[lane] : 0);
+    if (mine) {
+      double s, co;
+      turn_sincos(a.freq[lane] * (kAxes ? (uint64_t)(int64_t)(int32_t)pos : (uint64_t)pos), s, co);
+      turns[lane] = f64x2{co, s};
+    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+  }
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     if (kPair == kPairInLane && (e & 1)) {
@@ -214,17 +267,19 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
       continue;
     }
     const int j = kPair == kPairInLane ? 4 * c + e / 2 : 8 * (upper ? partner : c) + e;
-    cs[e] = 1.f;
-    sn[e] = 0.f;
-    if constexpr (kAxes) pos = (uint32_t)__shfl(token_pos, rotates ? a.axis[j] : 0);
+    cs[e] = 1;
+    sn[e] = 0;
+    if constexpr (kAxes && !kKvq) pos = (uint32_t)__shfl(token_pos, rotates ? a.axis[j] : 0);
     if (rotates) {
-      const uint64_t f = a.freq[j];
-      uint32_t phase = __umulhi((uint32_t)f, pos) + (uint32_t)(f >> 32) * pos;
-      if constexpr (kAxes) phase -= (int32_t)pos < 0 ? (uint32_t)f : 0u;   // pos stands for pos - 2^32
       float s;
       if constexpr (kKvq) {
-        turn_sincos(phase, s, cs[e]);
+        const f64x2 both = turns[j];
+        cs[e] = (float)both[0];
+        s = (float)both[1];
       } else {
+        const uint64_t f = a.freq[j];
+        uint32_t phase = __umulhi((uint32_t)f, pos) + (uint32_t)(f >> 32) * pos;
+        if constexpr (kAxes) phase -= (int32_t)pos < 0 ? (uint32_t)f : 0u;   // pos stands for pos - 2^32
         const float turns = (float)(int32_t)phase * 2.3283064365386963e-10f;   // 2^-32
         cs[e] = __builtin_amdgcn_cosf(turns);
         s = __builtin_amdgcn_sinf(turns);
@@ -232,13 +287,8 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
       sn[e] = upper ? s : -s;
     }
   }
-  // out = r * (x * own + p * other)
-  struct Coef {
-    float own[8], other[8];
-    bool normed;
-  };
   auto coefs = [&](const uint16_t* wt) __attribute__((always_inline)) {
-    Coef k;
+    RopeCoef k;
     k.normed = wt != nullptr;
     float g[8], h[8];
     if (k.normed) {
@@ -254,9 +304,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
     }
     return k;
   };
-  auto turn = [&](u32x4 raw, const Coef& k, float (&z)[8]) __attribute__((always_inline)) {
-    float y[8], p[8];
-    unpack8(raw, y);
+  auto partners = [&](u32x4 raw, const float (&y)[8], float (&p)[8]) __attribute__((always_inline)) {
     if constexpr (kPair == kPairInLane) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) p[e] = rotates ? y[e ^ 1] : 0.f;
@@ -271,6 +319,11 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
       }
       unpack8(o, p);
     }
+  };
+  auto turn = [&](u32x4 raw, const RopeCoef& k, float (&z)[8]) __attribute__((always_inline)) {
+    float y[8], p[8];
+    unpack8(raw, y);
+    partners(raw, y, p);
     float r = 1.f;
     if (k.normed) {
       float ss[2] = {0.f, 0.f};
@@ -282,6 +335,36 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
     for (int e = 0; e < 8; ++e) {
       z[e] = __builtin_fmaf(y[e], k.own[e], p[e] * k.other[e]);
       if (k.normed) z[e] = r * z[e];
+    }
+  };
+  // the same of a key row in 64 bits, its coefficients made where they are used
+  auto turn_key = [&](u32x4 raw, u32x4 own, u32x4 other, float (&z)[8]) __attribute__((always_inline)) {
+    float y[8], p[8], g[8], h[8];
+    unpack8(raw, y);
+    partners(raw, y, p);
+    unpack8(own, g);
+    unpack8(other, h);
+    double r = 1.;
+    if (a.k_weight != nullptr) {
+      double ss[2] = {0., 0.};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss[e & 1] = __builtin_fma((double)y[e], (double)y[e], ss[e & 1]);
+      const double x = row16_sum(ss[0] + ss[1]) * (1. / kHD) + (double)a.eps;
+      r = __builtin_amdgcn_rsq(x);
+      r = __builtin_fma(0.5 * r, __builtin_fma(-x * r, r, 1.), r);   // a Newton step behind v_rsq's 2^-26
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      double own_e = 1., other_e = 1.;
+      if (a.k_weight != nullptr) {
+        own_e = (double)g[e] + (double)a.offset;
+        other_e = (double)h[kPair == kPairInLane ? e ^ 1 : e] + (double)a.offset;
+      }
+      f64x2 both = {1., 0.};
+      if (rotates) both = turns[kPair == kPairInLane ? 4 * c + e / 2 : 8 * (upper ? partner : c) + e];
+      const bool plus = kPair == kPairInLane ? e & 1 : upper;
+      const double v = __builtin_fma((double)y[e], own_e * both[0], (plus ? (double)p[e] : -(double)p[e]) * (other_e * both[1]));
+      z[e] = rounded_to_odd(r * v);
     }
   };
   auto rounded = [](const float (&z)[8]) __attribute__((always_inline)) {
@@ -304,9 +387,17 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
 
   uint16_t* const q_out = a.q_out + (int64_t)t * a.Hq * kHD + c * 8;
   const int64_t page_at = ((int64_t)slot * a.Hkv * a.P + prow) * kHD + c * 8;
-  Coef cq, ck;
+  RopeCoef cq, ck;
+  u32x4 key_own{}, key_other{};
   if (row_begin < a.Hq) cq = coefs(a.q_weight);
-  if (row_end > a.Hq && row_begin < n_qk) ck = coefs(a.k_weight);
+  if (row_end > a.Hq && row_begin < n_qk) {
+    if constexpr (!kKvq) {
+      ck = coefs(a.k_weight);
+    } else if (a.k_weight != nullptr) {
+      key_own = ld_u32x4(a.k_weight + c * 8);
+      key_other = ld_u32x4(a.k_weight + partner * 8);
+    }
+  }
   for (int row0 = row_begin; row0 < row_end; row0 += kRopeRows) {
     u32x4 next[4];
     load(row0 + kRopeRows, next);
@@ -321,10 +412,10 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a) {
       if constexpr (kKvq) {
         uint32_t codes, scale;
         if (first + 3 >= a.Hq && first < n_qk) {
-          if (a.rot == 0 && !ck.normed) {
+          if (a.rot == 0 && a.k_weight == nullptr) {
             codes = kvq_codes_bf16(x[i], scale);
           } else {
-            turn(x[i], ck, z);
+            turn_key(x[i], key_own, key_other, z);
             codes = kvq_codes(z, scale);
           }
           store4(a.kq_pool, row - a.Hq, codes, scale, row >= a.Hq && row < n_qk && slot >= 0);
