@@ -27,8 +27,8 @@
 //
 // Bound by HBM for one token a sequence: 64 contexts of 4K to 32K keys, 32/8 heads, 1.39 GB
 // in 258 us, 5.4 TB/s; 96 equal ones of 16K 5.7.  From some 64 rows on by the matrix cores
-// and the softmax beside them: 2048 rows x 4 heads behind 8K keys, 309 GFLOP in 268 us (1.15
-// PFLOP/s, matrix cores busy 48% of the time), which the bf16 cache's attention takes 262 to 268 for.
+// and the softmax beside them: 2048 rows x 4 heads behind 8K keys, 309 GFLOP in 246 to 253 us (1.22
+// PFLOP/s, matrix cores busy 49% of the time), which the bf16 cache's attention takes 262 to 268 for.
 #pragma once
 
 #include "attn_pipe.h"

@@ -20,7 +20,7 @@ constexpr int kKvqKeys = 64;                 // keys of a tile
 // up to 64 and 128, whose waves split the rows.
 constexpr int kKvqClasses = 4;
 constexpr int kKvqRows[kKvqClasses] = {16, 32, 64, 128};
-// What a launch's time is made of, in microseconds.  Measured, 32/8 heads: a tile of keys
+// What a launch's time is made of, in microseconds.  Measured to 5%, 32/8 heads: a tile of keys
 // where two blocks share every CU.  Fitted, with the rates in plan_kvq_items, to 70 drawn
 // batches under nine limits each: the start and end of an item, the launch that joins parts,
 // each part of a row and each partial row, and where the launch joins itself, a start, a
@@ -128,7 +128,7 @@ inline sa_status plan_kvq_items(const sa_layout* layout, int32_t batch, const in
   // How many tile microseconds n blocks do in one.  A block with a CU to itself is quicker
   // than one of two (0.6 of the time; of class 0 half or less, where HBM is what they share),
   // so the end of a launch, when places are empty, does not cost what they would have done.
-  // Over the 70 batches the parts chosen so took 1.02 times the best limit's time, at the worst 1.13.
+  // Over the 70 batches the parts chosen so take 1.03 to 1.04 times the best limit's time, at the worst 1.17.
   auto rate = [&](double n) {
     if (out.few) return std::min(2.1 * n, 2.05 * num_cu);
     return n <= num_cu ? 1.67 * n : std::min(2. * num_cu, 1.67 * num_cu + 0.33 * (n - num_cu));
