@@ -793,11 +793,12 @@ sa_status sa_kvq_unpack(sa_ctx *ctx, const sa_layout *layout, int64_t num_slots4
  * q_len, kv_len >= 0); where kv_len is 0 the rows are zeros and their LSE is
  * -infinity.  Lengths of keys are at most 2^31 - 64.
  * O = softmax(softmax_scale * q . K^T) V with the values the cache stands for.
- * Scores are the products of the cached keys with the bf16 query rows, held as three
- * 6-bit floats per value (itself from 2^-6 of the largest of its 32 dims on, others
- * within 2^-14 of that, or 2^-129), summed in fp32 and then scaled; probabilities are
- * rounded to bf16 before the PV product, the rest
- * is fp32.  A row that sees a key with a NaN block has a NaN output and a NaN LSE; a
+ * Scores are the products of the cached keys with the bf16 query rows, summed in fp32
+ * and then scaled.  In work items of more than 32 packed rows (num_q_heads / num_kv_heads
+ * to a token) up to an eighth of the query values in a block of 32 dims are taken to within
+ * 2^-14 of the block's largest (or 2^-129), if they are below 2^-6 of that; where it would be
+ * more, the item's products are exact, as in smaller items.  Probabilities are rounded to
+ * bf16 before the PV product, the rest is fp32.  A row that sees a key with a NaN block has a NaN output and a NaN LSE; a
  * NaN block of a value it sees makes those 32 dims of its output NaN.  What a row
  * does not see does not reach it.  A page that is missing or outside the pool reads
  * as zeros and is latched for sa_sync_check.  `lse` may be NULL; pages.indices may

@@ -5,15 +5,21 @@
 //   s_j = c q . k_j,  m = max s_j,  O = sum 2^(s_j - m) v_j / l,  l = sum 2^(s_j - m)
 // with c = scale log2 e, in one pass with m, l and O carried and rescaled when scores outgrow m.
 //
-// Scores come out of the block-scaled matrix instruction (16x16x128), which takes
+// Up to 32 rows, scores are bf16 products of converted keys (a 4-bit value is a bf16 one) with
+// the query rows, so exact but for the fp32 sum.  They cost nothing there, where HBM bounds:
+// 259 us for 64 contexts of 4K to 32K keys, 257 with the pieces below.
+// More rows take them from the block-scaled matrix instruction (16x16x128), which has
 // the keys as they lie in the cache: lane l's operand is the 16 code bytes of key
-// l % 16, block l / 16, with that block's scale byte, so a wave's load of 16 keys is
-// one contiguous KB.  The query goes in as three 6-bit floats per value (e2m3, scales 2^e,
-// 2^(e-4), 2^(e-10) per 32 dims, each the rounded rest of the one before): the bf16 value
-// itself from 2^-6 of the block's largest on, others to 2^-14 of it.  c is multiplied in
-// behind the product, in fp32.  Against a bf16 product of converted keys the matrix work is 3/4
+// l % 16, block l / 16, with that block's scale byte.  The query goes in as three 6-bit floats
+// per value (e2m3, scales 2^e, 2^(e-4), 2^(e-10) per 32 dims, each the rounded rest of the one
+// before): the bf16 value itself from 2^-6 of the block's largest on, others to 2^-14 of it.  c is
+// multiplied in behind the product, in fp32.  Against a bf16 product the matrix work is 3/4
 // and the conversion goes; two 8-bit pieces would cost 4/4 and lose 2^-14 in the instruction's
-// sum (measured).
+// sum (measured).  In rows whose dims are of one size next to none are inexact (of normal
+// ones 0.2 of 32), but beside an outlier all can be, and what keys of zeros at the outlier
+// leave of a score is then off by as much as it is.  An item with a row where more than an
+// eighth of 32 dims are inexact takes bf16 products (one normal item of 128 rows in 1000): 2048
+// rows x 4 heads behind 8K keys, 254 to 258 us, take 307 with an outlier in every row.
 // Values have a scale per key and 32 dims, which a sum over keys cannot take in that
 // instruction: they are converted to bf16 (exactly; 2 per v_cvt), laid out in LDS and
 // read back transposed for the 16x16x32 bf16 product.  Probabilities are rounded to
@@ -26,8 +32,8 @@
 // share them out and go over the keys together (kvq_split_rows).
 //
 // Bound by HBM for one token a sequence: 64 contexts of 4K to 32K keys, 32/8 heads, 1.39 GB
-// in 258 us, 5.4 TB/s; 96 equal ones of 16K 5.7.  From some 64 rows on by the matrix cores
-// and the softmax beside them: 2048 rows x 4 heads behind 8K keys, 309 GFLOP in 246 to 253 us (1.22
+// in 259 us, 5.4 TB/s; 96 equal ones of 16K 5.7.  From some 64 rows on by the matrix cores
+// and the softmax beside them: 2048 rows x 4 heads behind 8K keys, 309 GFLOP in 254 to 258 us (1.21
 // PFLOP/s, matrix cores busy 49% of the time), which the bf16 cache's attention takes 262 to 268 for.
 #pragma once
 
@@ -76,7 +82,7 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x32 __attribute__((ext_vector_type(32)));
 
 // 32 dims of a query row as three 6-bit pieces; scales: their bytes (255: the block holds
-// an infinity or a NaN).  The rests are exact.  With S the first piece's scale, the largest
+// an infinity or a NaN).  The rests' arithmetic is exact.  With S the first piece's scale, the largest
 // dim is 3.75 to 7.5 S, and the first rest is at most S / 4, of a bf16 value with 4 bits
 // behind those taken: two pieces, the second from S / 128 on, hold dims from S on exactly.  The
 // rest of others is at most S / 2^8, 4 of the third piece's units: it comes to S / 2^13 at most
@@ -117,6 +123,34 @@ __device__ __forceinline__ void kvq_split_q(const uint16_t* p, u32x6 (&piece)[3]
   scales = fine ? s | (s - kDown[1]) << 8 | (s - kDown[2]) << 16 : 0xFFFFFF;
 }
 
+// Whether pieces do for 32 dims of a row: of a scale S, they do not hold those dims that are no multiple
+// of S / 2^13.  Every eighth of the dims that are not zero may be one.  Of blocks of normal
+// values one in half a million has more than 4, one in 20 thousand more than 3; an item of 128
+// rows has 512 blocks.
+__device__ __forceinline__ bool kvq_coarse(const uint16_t* p) {
+  u32x4 w[4];
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    w[i] = ld_u32x4(p + 8 * i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = max(top, max(w[i][e] & 0x7FFF0000u, (w[i][e] << 16) & 0x7FFF0000u));
+  }
+  const int n = 127 + 13 - max((int)((top + 0x100000u) >> 23) - 2, 11);   // x 2^13 / S is x 2^n
+  int zeros = 0, rests = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t two = w[i >> 2][i & 3];
+    const float x[2] = {__uint_as_float(two << 16), __uint_as_float(two & 0xFFFF0000u)};
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      zeros += x[e] == 0.f;
+      rests += __builtin_amdgcn_fractf(__builtin_ldexpf(x[e], n)) != 0.f;
+    }
+  }
+  return top < 0x7F800000u && 8 * rests > 32 - zeros;
+}
+
 // 16 keys (codes and scale byte kScale of `scales`) times 16 query rows in pieces, the
 // smallest first.
 template <int kScale>
@@ -128,6 +162,37 @@ __device__ __forceinline__ f32x4 kvq_scores(u32x4 key, uint32_t scales, const u3
   f32x4 s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, piece(q[2]), f32x4{}, 4, 2, kScale, (int)scales, 2, q_scales);
   s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, piece(q[1]), s, 4, 2, kScale, (int)scales, 1, q_scales);
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, piece(q[0]), s, 4, 2, kScale, (int)scales, 0, q_scales);
+}
+
+// The dims as they are, all NaN where one is an infinity or a NaN: keys of zeros would make a
+// NaN of an infinity, others not.
+__device__ __forceinline__ void kvq_load_q(const uint16_t* p, bf16x8 (&q)[4]) {
+  u32x4 w[4];
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    w[i] = ld_u32x4(p + 8 * i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = max(top, max(w[i][e] & 0x7FFF0000u, (w[i][e] << 16) & 0x7FFF0000u));
+  }
+  const uint32_t spoiled = top < 0x7F800000u ? 0u : 0x7FFF7FFFu;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q[i] = __builtin_bit_cast(bf16x8, w[i] | spoiled);
+}
+
+// 16 keys, converted, times bf16 query rows: exact products.  Element e of a lane's operands of
+// product j is dim 32 (lane / 16) + 8 j + e.
+template <int kNB>
+__device__ __forceinline__ void kvq_scores_bf16(u32x4 codes, uint32_t scale, const bf16x8 (&q)[kNB][4], int kb,
+                                                f32x4 (&x)[kNB][4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t w = codes[j];
+    const bf16x8 key = __builtin_bit_cast(bf16x8, kvq_values(w, scale));
+#pragma unroll
+    for (int nb = 0; nb < kNB; ++nb)
+      x[nb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[nb][j], j == 0 ? f32x4{} : x[nb][kb], 0, 0, 0);
+  }
 }
 
 __device__ __forceinline__ float row4_max(float x) {         // over the lanes that share lane % 16, NaN if any is
@@ -341,15 +406,15 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqIt
   if (t0 < t1) load_tile(t0, now);
 
   // every wave holds the same rows: row r16 of each 16-row block, dims 32 g on
-  u32x6 q[kNB][3];
-  int qs[kNB], limit[kNB];
+  bf16x8 q[kNB][4];
+  int limit[kNB];
 #pragma unroll
   for (int nb = 0; nb < kNB; ++nb) {
     const int rr = it.row0 + min(16 * nb + r16, rows - 1);
     const int tok = rr / G;
     const int head = it.kvh * G + (rr - tok * G);
     limit[nb] = min(it.kv_end, a.causal ? pre + tok + 1 : it.kv_len);
-    kvq_split_q(a.q + ((int64_t)(it.q_start + tok) * a.Hq + head) * kHD + g * 32, q[nb], qs[nb]);
+    kvq_load_q(a.q + ((int64_t)(it.q_start + tok) * a.Hq + head) * kHD + g * 32, q[nb]);
   }
   // keys below are seen by all rows
   const int all_see = min(it.kv_end, a.causal ? pre + it.row0 / G + 1 : it.kv_len);
@@ -393,11 +458,12 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqIt
       }
     }
     bf16x8 p[kNB][2];
+    f32x4 x[kNB][4];
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) kvq_scores_bf16(now.k[kb], now.ks[kb], q, kb, x);
 #pragma unroll
     for (int nb = 0; nb < kNB; ++nb) {
-      f32x4 s[4];
-#pragma unroll
-      for (int kb = 0; kb < 4; ++kb) s[kb] = kvq_scores<0>(now.k[kb], now.ks[kb], q[nb], qs[nb]);
+      f32x4(&s)[4] = x[nb];
       if (masked) {
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb)
@@ -516,22 +582,44 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqIt
 // A step makes the scores of tile t + 1 while the probabilities of tile t are taken, and
 // then O += P V of tile t while the values of t + 1 are converted: matrix and vector
 // instructions of one wave, each independent of the other's.  Behind the barrier of step
-// t - 1 LDS holds the values of tile t (bf16) and the codes of the keys of t + 1; step t
+// t - 1 LDS holds the values of tile t (bf16) and the keys of t + 1 (codes, or bf16); step t
 // writes the values of t + 1 and the keys of t + 2 from registers, whose loads were issued
 // a step before.
-constexpr int kKvqTile = 64 * kKvqVRow, kKvqKeyBytes = 64 * kKvqCodes;
-struct KvqRowsLds {
+constexpr int kKvqTile = 64 * kKvqVRow;
+constexpr int kKvqKRow = kHD * 2 + 16;       // a key's bf16 values: 16 rows' 16-byte chunks in all banks
+template <bool kExact>
+struct KvqRowsLds {                          // kExact: keys converted, for bf16 products; else codes
   uint8_t v[2][kKvqTile];
-  uint8_t k[2][kKvqKeyBytes];
+  uint8_t k[2][64 * (kExact ? kKvqKRow : kKvqCodes)];
   uint64_t nan[2][4];        // masked tiles: bit 16 g + r16 of a 16-key block, a value block that is NaN
-  uint32_t ks[2][64];        // lane (key r16, block g): the scale bytes of the four 16-key blocks
+  uint32_t ks[2][64];        // codes: lane (key r16, block g): the scale bytes of the four 16-key blocks
 };
 
-template <int P, int kNB>
+// Whether the item has a row for which pieces would not do: for all four waves, which share the
+// keys' form in LDS.
+template <int kNB>
+__device__ __forceinline__ bool kvq_any_coarse(const KvqAttnArgs& a, const KvqItem& it,
+                                               __attribute__((address_space(3))) int* votes) {
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, r16 = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rows = min(it.q_len * a.G - it.row0, 64 * kNB);
+  bool coarse = false;
+#pragma unroll
+  for (int nb = 0; nb < kNB; ++nb) {
+    const int rr = it.row0 + min(16 * kNB * wave + 16 * nb + r16, rows - 1), tok = rr / a.G;
+    coarse |= kvq_coarse(a.q + ((int64_t)(it.q_start + tok) * a.Hq + it.kvh * a.G + (rr - tok * a.G)) * kHD + g * 32);
+  }
+  const bool any = __ballot(coarse) != 0;
+  if (lane == 0) votes[wave] = any;
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(votes[0] | votes[1] | votes[2] | votes[3]) != 0;
+}
+
+template <int P, int kNB, bool kExact>
 __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqItem& it,
-                                               __attribute__((address_space(3))) KvqRowsLds* lds) {
+                                               __attribute__((address_space(3))) KvqRowsLds<kExact>* lds) {
   static_assert(P == 16 || P == 32, "page size");
-  constexpr int kTile = kKvqTile, kKeyBytes = kKvqKeyBytes;
+  constexpr int kTile = kKvqTile;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 4, r16 = lane & 15;
@@ -591,15 +679,22 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
   };
   lds_u8* const v0 = (lds_u8*)lds->v;
   lds_u8* const k0 = (lds_u8*)lds->k;
-  auto put_k = [&](int b, const Staged& x) __attribute__((always_inline)) {
-    *(__attribute__((address_space(3))) u32x4*)(k0 + b * kKeyBytes + wave * 1024 + lane * 16) = x.codes;
-    ((lds_u8*)lds->ks)[b * 256 + lane * 4 + wave] = (uint8_t)x.scale;
-  };
-  auto put_v = [&](int b, const Staged& x) __attribute__((always_inline)) {
-    lds_u8* const row = v0 + b * kTile + (16 * wave + r16) * kKvqVRow + 64 * g;
+  auto put = [&](lds_u8* row, const Staged& x) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      *(__attribute__((address_space(3))) u32x4*)(row + 16 * j) = kvq_values(x.codes[j], x.scale);
+      *(__attribute__((address_space(3))) u32x4*)(row + 64 * g + 16 * j) = kvq_values(x.codes[j], x.scale);
+  };
+  auto put_k = [&](int b, const Staged& x) __attribute__((always_inline)) {
+    lds_u8* const k = k0 + b * sizeof(lds->k[0]);
+    if constexpr (kExact) {
+      put(k + (16 * wave + r16) * kKvqKRow, x);
+    } else {
+      *(__attribute__((address_space(3))) u32x4*)(k + wave * 1024 + lane * 16) = x.codes;
+      ((lds_u8*)lds->ks)[b * 256 + lane * 4 + wave] = (uint8_t)x.scale;
+    }
+  };
+  auto put_v = [&](int b, const Staged& x) __attribute__((always_inline)) {
+    put(v0 + b * kTile + (16 * wave + r16) * kKvqVRow, x);
   };
   // of a tile that is masked for some row: values that no row sees are zeros, and NaN
   // blocks, which would reach rows that do not see them, go round the product
@@ -618,15 +713,18 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
 
   // this wave's rows: row r16 of each 16-row block, dims 32 g on
   const int wrow = 16 * kNB * wave;
-  u32x6 q[kNB][3];
-  int qs[kNB], limit[kNB];
+  u32x6 pieces[kNB][3];
+  bf16x8 q[kNB][4];
+  int scales[kNB], limit[kNB];
 #pragma unroll
   for (int nb = 0; nb < kNB; ++nb) {
     const int rr = it.row0 + min(wrow + 16 * nb + r16, rows - 1);
     const int tok = rr / G;
     const int head = it.kvh * G + (rr - tok * G);
     limit[nb] = min(it.kv_end, a.causal ? pre + tok + 1 : it.kv_len);
-    kvq_split_q(a.q + ((int64_t)(it.q_start + tok) * a.Hq + head) * kHD + g * 32, q[nb], qs[nb]);
+    const uint16_t* const row = a.q + ((int64_t)(it.q_start + tok) * a.Hq + head) * kHD + g * 32;
+    if constexpr (kExact) kvq_load_q(row, q[nb]);
+    else kvq_split_q(row, pieces[nb], scales[nb]);
   }
   const int wave_sees = min(it.kv_end, a.causal ? pre + (it.row0 + min(wrow, rows - 1)) / G + 1 : it.kv_len);
 
@@ -645,17 +743,30 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
   }
 
   auto scores = [&](int b, f32x4 (&x)[kNB][4]) __attribute__((always_inline)) {
-    const uint32_t scales = lds->ks[b][lane];
-    const lds_u8* const k = k0 + b * kKeyBytes + lane * 16;
-    u32x4 key[4];
+    if constexpr (kExact) {
+      const lds_u8* const k = k0 + b * sizeof(lds->k[0]) + r16 * kKvqKRow + 64 * g;
 #pragma unroll
-    for (int kb = 0; kb < 4; ++kb) key[kb] = *(const __attribute__((address_space(3))) u32x4*)(k + kb * 1024);
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
-    for (int nb = 0; nb < kNB; ++nb) {
-      x[nb][0] = kvq_scores<0>(key[0], scales, q[nb], qs[nb]);
-      x[nb][1] = kvq_scores<1>(key[1], scales, q[nb], qs[nb]);
-      x[nb][2] = kvq_scores<2>(key[2], scales, q[nb], qs[nb]);
-      x[nb][3] = kvq_scores<3>(key[3], scales, q[nb], qs[nb]);
+        for (int kb = 0; kb < 4; ++kb) {
+          const bf16x8 key = *(const __attribute__((address_space(3))) bf16x8*)(k + 16 * kb * kKvqKRow + 16 * j);
+#pragma unroll
+          for (int nb = 0; nb < kNB; ++nb)
+            x[nb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[nb][j], j == 0 ? f32x4{} : x[nb][kb], 0, 0, 0);
+        }
+    } else {
+      const uint32_t ks = lds->ks[b][lane];
+      const lds_u8* const k = k0 + b * sizeof(lds->k[0]) + lane * 16;
+      u32x4 key[4];
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb) key[kb] = *(const __attribute__((address_space(3))) u32x4*)(k + kb * 1024);
+#pragma unroll
+      for (int nb = 0; nb < kNB; ++nb) {
+        x[nb][0] = kvq_scores<0>(key[0], ks, pieces[nb], scales[nb]);
+        x[nb][1] = kvq_scores<1>(key[1], ks, pieces[nb], scales[nb]);
+        x[nb][2] = kvq_scores<2>(key[2], ks, pieces[nb], scales[nb]);
+        x[nb][3] = kvq_scores<3>(key[3], ks, pieces[nb], scales[nb]);
+      }
     }
   };
   // m, l and O moved to the maxima of a tile's scores
@@ -884,6 +995,16 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
   }
 }
 
+// Asked beforehand: a vote inside the loop's function, or both forms under one loop, cost the
+// pieces' loop registers (64 and 85 spilled; 257 us for 2048 rows x 4 heads so, 415 else).
+template <int P, int kNB>
+__device__ __forceinline__ void kvq_rows(const KvqAttnArgs& a, const KvqItem& it, lds_u8* lds, KvqStats* stats) {
+  if (kvq_any_coarse<kNB>(a, it, (__attribute__((address_space(3))) int*)stats))
+    kvq_split_rows<P, kNB, true>(a, it, (__attribute__((address_space(3))) KvqRowsLds<true>*)lds);
+  else
+    kvq_split_rows<P, kNB, false>(a, it, (__attribute__((address_space(3))) KvqRowsLds<false>*)lds);
+}
+
 // A launch of items of up to 16 rows alone: three blocks on a CU.
 template <int P>
 __global__ __launch_bounds__(256, 3) void attn_kvq_few_kernel(KvqAttnArgs a) {
@@ -896,14 +1017,14 @@ __global__ __launch_bounds__(256, 3) void attn_kvq_few_kernel(KvqAttnArgs a) {
 // Items of every class (kvq_plan.h).
 template <int P>
 __global__ __launch_bounds__(256, 2) void attn_kvq_kernel(KvqAttnArgs a) {
-  constexpr int kBytes = sizeof(KvqRowsLds) > kKvqWaves * kKvqHalf ? sizeof(KvqRowsLds) : kKvqWaves * kKvqHalf;
+  constexpr int kBytes = std::max<int>(std::max(sizeof(KvqRowsLds<false>), sizeof(KvqRowsLds<true>)), kKvqWaves * kKvqHalf);
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kBytes];
   __shared__ float stats[2][kKvqWaves][16];
   const KvqItem it = ld_uniform(a.items + blockIdx.x);
   if (it.cls == 0) kvq_split_keys<P, 1>(a, it, (lds_u8*)lds, (KvqStats*)stats);
   else if (it.cls == 1) kvq_split_keys<P, 2>(a, it, (lds_u8*)lds, (KvqStats*)stats);
-  else if (it.cls == 2) kvq_split_rows<P, 1>(a, it, (__attribute__((address_space(3))) KvqRowsLds*)lds);
-  else kvq_split_rows<P, 2>(a, it, (__attribute__((address_space(3))) KvqRowsLds*)lds);
+  else if (it.cls == 2) kvq_rows<P, 1>(a, it, (lds_u8*)lds, (KvqStats*)stats);
+  else kvq_rows<P, 2>(a, it, (lds_u8*)lds, (KvqStats*)stats);
 }
 
 }  // namespace sa
