@@ -798,8 +798,10 @@ sa_status sa_kvq_unpack(sa_ctx *ctx, const sa_layout *layout, int64_t num_slots4
  * to a token) up to an eighth of the query values in a block of 32 dims are taken to within
  * 2^-14 of the block's largest (or 2^-129), if they are below 2^-6 of that; where it would be
  * more, the item's products are exact, as in smaller items.  Probabilities are rounded to
- * bf16 before the PV product, the rest is fp32.  A row that sees a key with a NaN block has a NaN output and a NaN LSE; a
- * NaN block of a value it sees makes those 32 dims of its output NaN.  What a row
+ * bf16 before the PV product, the rest is fp32.  A row that sees a key
+ * with a NaN block has a NaN output and a NaN LSE; a NaN block of a value it sees makes those
+ * 32 dims of its output NaN, and an infinite element (see sa_kvq_unpack) makes its dim infinite
+ * or NaN; an infinite element of a key may make its row NaN.  What a row
  * does not see does not reach it.  A page that is missing or outside the pool reads
  * as zeros and is latched for sa_sync_check.  `lse` may be NULL; pages.indices may
  * be NULL where no sequence with queries has keys.  Parts of a launch split by key

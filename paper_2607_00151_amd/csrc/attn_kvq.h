@@ -208,6 +208,25 @@ __device__ __forceinline__ float row4_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// Of 8 codes those whose values no bf16 holds (4 and 6 under a scale byte of 253, 2 and more under
+// 254: infinities), others 0.
+__device__ __forceinline__ uint32_t kvq_beyond(uint32_t w, uint32_t scale) {
+  const uint32_t two = w >> 2 & 0x11111111u;
+  return w & (scale == 254 ? two : scale == 253 ? two & w >> 1 : 0u) * 15u;
+}
+// A key's infinities of one block of 32 dims, which stayed out of the product, where the row sees it.
+__device__ __forceinline__ void kvq_add_beyond(f32x4 (&o)[8], bool sees, int block, u32x4 codes, int g) {
+#pragma unroll
+  for (int db = 0; db < 8; ++db) {                           // dims 16 db + 4 g + i
+    if (db >> 1 != block || !sees) continue;
+    const uint32_t lo = codes[2 * (db & 1)], hi = codes[2 * (db & 1) + 1];
+    const uint32_t four = (g & 2 ? hi : lo) >> (16 * (g & 1));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (four >> (4 * i) & 4) o[db][i] += four >> (4 * i) & 8 ? -INFINITY : INFINITY;
+  }
+}
+
 constexpr int kKvqWaves = 4;
 // How far (log2) scores may outgrow a row's offset before l and O are rescaled: weights
 // then reach 2^8, which their rounding to bf16, relative as it is, does not notice.  Moved
@@ -437,7 +456,8 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqIt
     const bool masked = key0 + kKeys > all_see;
     if (masked) {
       // Values that no row sees are zeros; a NaN that some rows see is kept out of the
-      // product, where it would reach the others, and put into those rows at the end.
+      // product, where it would reach the others, and put into those rows at the end, an
+      // infinity added to them here.
 #pragma unroll
       for (int kb = 0; kb < 4; ++kb) {
         const int key = key0 + 16 * kb + r16;
@@ -454,6 +474,21 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqIt
         if (now.vs[kb] == 255) {
           now.v[kb] = u32x4{};
           now.vs[kb] = 127;
+        }
+        if (const uint64_t some = __ballot(now.vs[kb] > 252)) {
+          u32x4 far;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) far[j] = kvq_beyond(now.v[kb][j], now.vs[kb]);
+          now.v[kb] ^= far;
+          for (uint64_t hit = some; hit != 0; hit &= hit - 1) {
+            const int from = __builtin_ctzll(hit);
+            u32x4 codes;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) codes[j] = (uint32_t)__builtin_amdgcn_readlane((int)far[j], from);
+#pragma unroll
+            for (int nb = 0; nb < kNB; ++nb)
+              kvq_add_beyond(o[nb], key0 + 16 * kb + (from & 15) < limit[nb], from >> 4, codes, g);
+          }
         }
       }
     }
@@ -476,7 +511,8 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqIt
       for (int j = 1; j < 16; ++j) top = vmax(top, s[j >> 2][j & 3]);
       const float grown = vmax(m[nb], row4_max(top) * a.c);
       if (__ballot(!(grown <= m[nb] + kKvqLag))) {
-        const float f = exp2f_fast(m[nb] - (grown == -INFINITY ? 0.f : grown));
+        // a row that had met no key has nothing but this tile's infinities
+        const float f = m[nb] == -INFINITY ? 1.f : exp2f_fast(m[nb] - grown);
         l[nb] *= f;
 #pragma unroll
         for (int db = 0; db < 8; ++db) o[nb][db] *= f;
@@ -592,6 +628,8 @@ struct KvqRowsLds {                          // kExact: keys converted, for bf16
   uint8_t v[2][kKvqTile];
   uint8_t k[2][64 * (kExact ? kKvqKRow : kKvqCodes)];
   uint64_t nan[2][4];        // masked tiles: bit 16 g + r16 of a 16-key block, a value block that is NaN
+  uint64_t some[2][4];       // the same, one that may hold infinities, and
+  const uint8_t* page[2][4]; // the pages that those 16 keys lie in
   uint32_t ks[2][64];        // codes: lane (key r16, block g): the scale bytes of the four 16-key blocks
 };
 
@@ -697,12 +735,20 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
     put(v0 + b * kTile + (16 * wave + r16) * kKvqVRow, x);
   };
   // of a tile that is masked for some row: values that no row sees are zeros, and NaN
-  // blocks, which would reach rows that do not see them, go round the product
+  // blocks and infinities, which would reach rows that do not see them, go round the product
   auto filter_v = [&](int t, int b, Staged& x) __attribute__((always_inline)) {
     if (t * kKeys + 16 * wave + r16 >= it.kv_end) x = Staged{u32x4{}, 127};
     const uint64_t hit = __ballot(x.scale == 255);
     if (lane == 0) lds->nan[b][wave] = hit;
     if (x.scale == 255) x = Staged{u32x4{}, 127};
+    const uint64_t some = __ballot(x.scale > 252);
+    if (lane == 0) lds->some[b][wave] = some;
+    if (some != 0) {
+      if (lane == 0)
+        lds->page[b][wave] = a.v + __builtin_amdgcn_readlane(slots_v, (t - ts_v) & 63) * slot_bytes + it.kvh * page_bytes;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x.codes[j] ^= kvq_beyond(x.codes[j], x.scale);
+    }
   };
 
   Staged kx, vx;
@@ -901,6 +947,20 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
 #pragma unroll
           for (int nb = 0; nb < kNB; ++nb)
             if (t * kKeys + 16 * kb + (from & 15) < limit[nb]) poison[nb] |= 1u << (from >> 4);
+        }
+#pragma nounroll
+      for (int kb = 0; kb < 4; ++kb)
+        for (uint64_t hit = lds->some[b][kb]; hit != 0; hit &= hit - 1) {
+          const int from = __builtin_ctzll(hit);
+          const int row = (16 * kb) % P + (from & 15), block = from >> 4;
+          const uint8_t* const page = lds->page[b][kb];
+          const uint32_t scale = page[P * kKvqCodes + row * 4 + block];
+          u32x4 codes = ld_u32x4((const uint16_t*)(page + row * kKvqCodes + block * 16));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) codes[j] = kvq_beyond(codes[j], scale);
+#pragma unroll
+          for (int nb = 0; nb < kNB; ++nb)
+            kvq_add_beyond(o[nb], t * kKeys + 16 * kb + (from & 15) < limit[nb], block, codes, g);
         }
     }
     if (t + 1 < t1) {

@@ -1,4 +1,4 @@
-"""Attention over a 4-bit cache where it can go wrong: queries with outlier dims.
+"""Attention over a 4-bit cache where it can go wrong: queries with outlier dims, values that are infinities.
 
 References and bounds: kvq_bounds.py."""
 import numpy as np
@@ -14,9 +14,10 @@ pytestmark = pytest.mark.gpu
 
 
 class Case:
-    """A cache, queries and page tables of one call; edit(x) changes the float64 rows k and v before they are quantised."""
+    """A cache, queries and page tables of one call; edit(x) changes the float64 rows k and v before they are quantised,
+    patch(case) their bytes."""
 
-    def __init__(self, seed, heads, page, q_len, kv_len, causal=True, scale=D ** -0.5, edit=None, q=None):
+    def __init__(self, seed, heads, page, q_len, kv_len, causal=True, scale=D ** -0.5, edit=None, q=None, patch=None):
         r = np.random.default_rng(seed)
         pages = [-(-n // page) for n in kv_len]
         self.L = lay(heads, page, sum(pages) + 3)
@@ -29,6 +30,8 @@ class Case:
         self.q = rows(r, (sum(q_len), heads[0], D), 0.5)
         if q is not None:
             q(self.q)
+        if patch:
+            patch(self)
         self.on_gpu()
 
     def on_gpu(self):
@@ -102,3 +105,75 @@ def test_one_row_with_an_outlier_among_ordinary_ones():
     def q(x):
         x[77, 3, 5] = 20000.0
     checked(9, (32, 8), 16, [100, 60], [2000, 700], True, edit=edit, q=q)
+
+
+# Codes that stand for more than a bf16 holds, by scale byte: 4 and 6 under 253, 2 and more under 254.
+BEYOND = {253: {6: 1, 7: 1, 14: -1, 15: -1}, 254: {4: 1, 5: 1, 6: 1, 7: 1, 12: -1, 13: -1, 14: -1, 15: -1}}
+
+
+@pytest.mark.parametrize("heads,page,q,kv,at,causal", [
+    ((8, 2), 16, 1, 300, 299, True), ((8, 2), 16, 6, 300, 297, True), ((8, 2), 16, 3, 3, 1, True), ((32, 8), 32, 40, 200, 170, True),
+    ((8, 2), 16, 70, 70, 3, True), ((4, 2), 16, 9, 130, 64, False), ((2, 1), 16, 100, 5000, 4950, True), ((4, 4), 16, 9, 40, 35, True),
+    ((1, 1), 32, 130, 1000, 900, True), ((4, 1), 16, 32, 700, 680, True)])
+@pytest.mark.parametrize("scale", [253, 254])
+@pytest.mark.parametrize("outlier", [False, True])
+def test_an_infinite_value_reaches_the_rows_that_see_it(heads, page, q, kv, at, causal, scale, outlier):
+    """A block under a scale byte that quantising never gives, as another tool may have written it: infinities in some of
+    its dims, finite values or zeros in the others."""
+    signs = np.zeros(32)
+    codes = np.zeros(32, np.uint8)
+    for i, (c, sign) in enumerate(BEYOND[scale].items()):
+        codes[3 * i + 1], signs[3 * i + 1] = c, sign
+    codes[[2, 31]] = 1, 9                                   # half a unit: finite
+
+    def bytes_of(case):
+        p = case.v[0, case.indices[at // page], 0]
+        return p[:64 * page].reshape(page, 64)[at % page, 32:48], p[64 * page:].reshape(page, 4)[at % page]
+
+    def patch(case):
+        b, s = bytes_of(case)
+        b[:], s[2] = codes[0::2] | codes[1::2] << 4, scale
+
+    def big(x):
+        if outlier:
+            x[..., 5] = 5000.0
+    c = Case(31, heads, page, [q], [kv], causal, patch=patch, q=big, edit=lambda x: x["k"].__setitem__((..., 5), 0))
+    ctx = sa.Context(0)
+    o, lse = c.run(ctx)
+    sa.sa_sync_check(ctx)
+    G = heads[0] // heads[1]
+    sees = np.array([not causal or kv - q + i >= at for i in range(q)])
+    got = o.double().cpu().numpy()
+    want = np.zeros_like(got)
+    want[np.ix_(sees, np.arange(G), np.arange(64, 96))] = np.where(signs == 0, 0, np.inf * np.where(signs == 0, 1, signs))
+    np.testing.assert_array_equal(np.where(np.isinf(got) | np.isnan(got), got, 0), want)
+    # everything else is as with zeros in those dims
+    b, s = bytes_of(c)
+    codes[signs != 0] = 0
+    b[:] = codes[0::2] | codes[1::2] << 4
+    k, v = (rows_of(p[0], c.indptr, c.indices, 0, kv, page) for p in (c.k, c.v))
+    ref = attention(c.q, k, v, c.scale, causal)
+    off = ((o.double().cpu() - ref[0]).abs() / ref[2]).numpy()
+    assert (off[want == 0] <= 1).all()
+    assert ((lse.double().cpu() - ref[1]).abs() <= ref[3]).all()
+
+
+@pytest.mark.parametrize("heads,page,q,kv,at", [((8, 2), 16, 6, 300, 297), ((32, 8), 32, 40, 200, 170), ((4, 4), 16, 9, 40, 35)])
+def test_an_infinite_key_stays_out_of_the_rows_that_do_not_see_it(heads, page, q, kv, at):
+    def bytes_of(case):
+        p = case.k[0, case.indices[at // page], 0]
+        return p[:64 * page].reshape(page, 64)[at % page, 32:48], p[64 * page:].reshape(page, 4)[at % page]
+
+    def patch(case):
+        b, s = bytes_of(case)
+        b[:], s[2] = 0x7E, 254
+    c = Case(32, heads, page, [q], [kv], True, patch=patch)
+    ctx = sa.Context(0)
+    o, lse = c.run(ctx)
+    sa.sa_sync_check(ctx)
+    bytes_of(c)[0][:] = 0
+    k, v = (rows_of(p[0], c.indptr, c.indices, 0, kv, page) for p in (c.k, c.v))
+    n = at - (kv - q)                                       # rows before the one at that position
+    part = attention(c.q, k, v, c.scale, True)
+    off = worst(o[:n], lse[:n], [x[:n] for x in part])
+    assert n > 0 and max(off) <= 1.0, off
