@@ -802,7 +802,8 @@ sa_status sa_kvq_unpack(sa_ctx *ctx, const sa_layout *layout, int64_t num_slots4
  * with a NaN block has a NaN output and a NaN LSE; a NaN block of a value it sees makes those
  * 32 dims of its output NaN, and an infinite element (see sa_kvq_unpack) makes its dim infinite
  * or NaN; an infinite element of a key may make its row NaN.  What a row
- * does not see does not reach it.  A page that is missing or outside the pool reads
+ * does not see does not reach it.  Sums of values below 2^110 do not overflow, over however
+ * many keys; of larger ones they may.  A page that is missing or outside the pool reads
  * as zeros and is latched for sa_sync_check.  `lse` may be NULL; pages.indices may
  * be NULL where no sequence with queries has keys.  Parts of a launch split by key
  * range (516 bytes of the split-KV partials per query row, head and part) are joined

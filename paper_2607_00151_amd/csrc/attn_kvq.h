@@ -231,9 +231,15 @@ constexpr int kKvqWaves = 4;
 // How far (log2) scores may outgrow a row's offset before l and O are rescaled: weights
 // then reach 2^8, which their rounding to bf16, relative as it is, does not notice.  Moved
 // at every growth, some row of a wave moves in 45% of the tiles of 8K keys.  Where the
-// waves split the rows no maximum is taken at all as long as a lane's 16 weights of a row
-// come to no more than kKvqMost (sums of values from 2^110 on may overflow then).
-constexpr float kKvqLag = 8.f, kKvqMost = 65536.f;
+// waves split the rows no maximum is taken at all as long as the weights a lane has added up
+// for a row come to no more than kKvqMost; where they split the keys, l and O are rescaled
+// beyond kKvqMostOfKeys too.  A row's weights then never come to 2^18, and values below 2^110 to no
+// infinite sum, over any number of keys.  An offset goes to the maximum, or beyond it by
+// as many powers of two as bring the row's weights below 2^10.
+constexpr float kKvqLag = 8.f, kKvqMostOfKeys = 8192.f, kKvqMost = 32768.f;
+__device__ __forceinline__ float kvq_offset(float m, float top, float l) {
+  return vmax(top, m + (float)max(__builtin_amdgcn_frexp_expf(row4_sum(l)) - 10, 0));
+}
 // Bytes of a key's bf16 values in LDS: 32 more than they take, so that the 8 keys x 32
 // bytes of half a wave's transposed reads, and the 8 rows' chunks of a quarter's
 // writes, lie in different banks.
@@ -509,8 +515,9 @@ __device__ __forceinline__ void kvq_split_keys(const KvqAttnArgs& a, const KvqIt
       float top = s[0][0];
 #pragma unroll
       for (int j = 1; j < 16; ++j) top = vmax(top, s[j >> 2][j & 3]);
-      const float grown = vmax(m[nb], row4_max(top) * a.c);
-      if (__ballot(!(grown <= m[nb] + kKvqLag))) {
+      float grown = vmax(m[nb], row4_max(top) * a.c);
+      if (__ballot(!(grown <= m[nb] + kKvqLag) | !(l[nb] <= kKvqMostOfKeys))) {
+        grown = kvq_offset(m[nb], grown, l[nb]);
         // a row that had met no key has nothing but this tile's infinities
         const float f = m[nb] == -INFINITY ? 1.f : exp2f_fast(m[nb] - grown);
         l[nb] *= f;
@@ -822,7 +829,7 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
       float top = x[nb][0][0];
 #pragma unroll
       for (int j = 1; j < 16; ++j) top = vmax(top, x[nb][j >> 2][j & 3]);
-      top = vmax(m[nb], row4_max(top) * a.c);
+      top = kvq_offset(m[nb], vmax(m[nb], row4_max(top) * a.c), l[nb]);
       const bool met = top != -INFINITY;
       off[nb] = met ? top : 0.f;
       most[nb] = met ? kKvqMost : -1.f;
@@ -862,7 +869,7 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
     }
     bool far = false;
 #pragma unroll
-    for (int nb = 0; nb < kNB; ++nb) far |= !(sum[nb] <= most[nb]);
+    for (int nb = 0; nb < kNB; ++nb) far |= !(l[nb] + sum[nb] <= most[nb]);
     if (__ballot(far)) {
       settle(x);
       weights();

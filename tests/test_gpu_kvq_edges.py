@@ -1,4 +1,5 @@
-"""Attention over a 4-bit cache where it can go wrong: queries with outlier dims, values that are infinities.
+"""Attention over a 4-bit cache where it can go wrong: queries with outlier dims, values that are infinities
+or large, very many keys.
 
 References and bounds: kvq_bounds.py."""
 import numpy as np
@@ -17,17 +18,20 @@ class Case:
     """A cache, queries and page tables of one call; edit(x) changes the float64 rows k and v before they are quantised,
     patch(case) their bytes."""
 
-    def __init__(self, seed, heads, page, q_len, kv_len, causal=True, scale=D ** -0.5, edit=None, q=None, patch=None):
+    def __init__(self, seed, heads, page, q_len, kv_len, causal=True, scale=D ** -0.5, edit=None, q=None, patch=None, copies=1):
         r = np.random.default_rng(seed)
         pages = [-(-n // page) for n in kv_len]
         self.L = lay(heads, page, sum(pages) + 3)
         self.heads, self.page, self.q_len, self.kv_len, self.causal, self.scale = heads, page, q_len, kv_len, causal, scale
         self.indptr, self.indices, _ = tables(r, pages, self.L.num_slots)
+        if copies > 1:                                       # that many sequences over the same pages
+            self.indptr, self.indices = np.arange(copies + 1) * pages[0], np.tile(self.indices, copies)
+            self.q_len, self.kv_len = q_len * copies, kv_len * copies
         self.x = {n: r.standard_normal((1, self.L.num_slots, heads[1], page, D)) * 0.5 for n in "kv"}
         if edit:
             edit(self.x)
         self.k, self.v = (page_bytes(self.x[n]) for n in "kv")
-        self.q = rows(r, (sum(q_len), heads[0], D), 0.5)
+        self.q = rows(r, (sum(self.q_len), heads[0], D), 0.5)
         if q is not None:
             q(self.q)
         if patch:
@@ -45,10 +49,10 @@ class Case:
                        causal=self.causal, stream=stream)
         return o, lse
 
-    def check(self, o, lse):
+    def check(self, o, lse, only=None):
         t = 0
         for b, (n, kv) in enumerate(zip(self.q_len, self.kv_len)):
-            if n:
+            if n and (only is None or b in only):
                 k, v = (rows_of(p[0], self.indptr, self.indices, b, kv, self.page) for p in (self.k, self.v))
                 off = worst(o[t:t + n], lse[t:t + n], attention(self.q[t:t + n], k, v, self.scale, self.causal))
                 assert max(off) <= 1.0, (b, off)
@@ -177,3 +181,49 @@ def test_an_infinite_key_stays_out_of_the_rows_that_do_not_see_it(heads, page, q
     part = attention(c.q, k, v, c.scale, True)
     off = worst(o[:n], lse[:n], [x[:n] for x in part])
     assert n > 0 and max(off) <= 1.0, off
+
+
+# 512 sequences over the same pages: as many items as there are places, whose keys are not cut into many parts
+@pytest.mark.parametrize("q,rise", [([1], 7.5), ([20], 7.5), ([40], 10.5), ([100], 10.5)])
+def test_sums_of_large_values_are_finite(q, rise):
+    """Values just below 2^110, and weights that outgrow a row's first ones by nearly as much as its offset lets them."""
+    kv = 20000
+
+    def edit(x):
+        x["k"][:], x["v"][:] = 0, np.abs(x["v"]) % 0.35 * 2.0 ** 110 + 2.0 ** 109
+
+    def patch(case):                                        # every other 64 keys: ones
+        ones = page_bytes(np.ones((1, 16, D)))
+        for i in range(kv // 16):
+            if i // 4 % 2:
+                case.k[0, case.indices[i]] = ones
+
+    def q_half(x):
+        x[:] = 0.5
+    c = Case(41, (1, 1), 16, q, [kv], False, scale=rise * np.log(2) / 64, edit=edit, patch=patch, q=q_half, copies=512)
+    ctx = sa.Context(0)
+    o, lse = c.run(ctx)
+    sa.sa_sync_check(ctx)
+    c.check(o, lse, only=(0, 511))
+    assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("q", [[1], [6], [20], [40], [100]])
+def test_more_keys_of_one_weight_than_an_offset_keeps(q):
+    """Keys of zeros: the LSE is that of their number, of which one is 6.7e-6; the output their values' mean."""
+    kv = 150001
+
+    def edit(x):
+        x["k"][:] = 0
+    c = Case(42, (1, 1), 16, q, [kv], False, edit=edit, copies=512)
+    ctx = sa.Context(0)
+    o, lse = c.run(ctx)
+    sa.sa_sync_check(ctx)
+    v = rows_of(c.v[0], c.indptr, c.indices, 0, kv, 16)
+    mean, size = (torch.from_numpy(f(v).mean(1)) for f in (np.asarray, np.abs))
+    # log2 of the sum: fp32 additions of whole numbers are exact, v_log's result and the sum's power of two
+    # are off by half a unit of 2^-19 each, the product with ln 2 by half a unit of 2^-20
+    assert (lse.double().cpu() - np.log(kv)).abs().max() <= (2.0 ** -19 * np.log(2) + 2.0 ** -21)
+    # weights are powers of two, so only the output is rounded, and fp32 sums of a sixteenth of the keys at most
+    off = (o.double().cpu() - mean[None]).abs() - 2.0 ** -8 * mean[None].abs() - (kv / 16 + 64) * 2.0 ** -24 * size[None]
+    assert off.max() <= 0
