@@ -53,3 +53,29 @@ def worst(got, got_lse, ref):
     off = got.double().cpu() - o
     return ((off.abs() / tol).max().item(), ((got_lse.double().cpu() - lse).abs() / ltol).max().item(),
             (torch.linalg.vector_norm(off, dim=2) / row).max().item())
+
+
+# ---- caches of known weights: keys of zeros, and values that tell which 64 keys they are of
+
+def coded_values(kv):
+    """[kv][128]: a one in the dim that its 64 keys have."""
+    v = torch.zeros((kv, D), dtype=torch.float64)
+    j = torch.arange(kv)
+    v[j, j // 64 % D] = 1
+    return v
+
+
+def coded_worst(got, got_lse, kv, causal):
+    """How far off the outputs [n][Hq][128] and LSEs of such a cache are, in units of what is allowed.  Row i sees
+    kv - n + i + 1 keys (all, without a mask): its LSE is their number's logarithm, its output their counts by dim over it.
+
+    Up to 2^16 keys a part's log2 is off by v_log's 2^-20 and as much comes back through the weights it gives its
+    sums; the joined sum's log2 is off by 2^-20 and 2^-21, its product with ln 2 by 2^-21: 2.2e-6, twice that is
+    allowed.  Outputs are rounded to bf16 and their parts' weights off as above."""
+    n = got.shape[0]
+    counts = torch.cumsum(coded_values(kv), 0)
+    seen = [kv - n + i + 1 if causal else kv for i in range(n)]
+    o = torch.stack([counts[s - 1] / s for s in seen])[:, None]
+    lse = torch.tensor(seen, dtype=torch.float64).log()[:, None]
+    return (((got.double().cpu() - o).abs() / ((2.0 ** -8 + 1e-5) * o + 1e-30)).max().item(),
+            ((got_lse.double().cpu() - lse).abs() / 4.4e-6).max().item())

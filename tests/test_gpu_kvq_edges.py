@@ -1,5 +1,5 @@
 """Attention over a 4-bit cache where it can go wrong: queries with outlier dims, values that are infinities
-or large, very many keys.
+or large, very many keys; and caches so long that a few lost keys hardly show.
 
 References and bounds: kvq_bounds.py."""
 import numpy as np
@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import paper_2607_00151_amd as sa
-from kvq_bounds import attention, worst
+from kvq_bounds import attention, coded_values, coded_worst, worst
 from kvq_reference import D, page_bytes, rows_of
 from test_gpu_branches import dev, lay, rows, tables
 
@@ -227,3 +227,39 @@ def test_more_keys_of_one_weight_than_an_offset_keeps(q):
     # weights are powers of two, so only the output is rounded, and fp32 sums of a sixteenth of the keys at most
     off = (o.double().cpu() - mean[None]).abs() - 2.0 ** -8 * mean[None].abs() - (kv / 16 + 64) * 2.0 ** -24 * size[None]
     assert off.max() <= 0
+
+
+# ---- long caches
+
+LONG = [((8, 2), 16, [1, 1], [40000, 31001], True), ((32, 8), 16, [1], [9000], False), ((2, 1), 32, [40], [20011], True),
+        ((16, 1), 16, [6], [30000], True), ((16, 1), 16, [1, 1], [60000, 1], True), ((4, 4), 32, [1] * 3, [65000, 64, 9000], False),
+        ((16, 4), 32, [2, 30, 1, 7, 14], [9000, 6000, 20000, 77, 12345], True), ((2, 1), 16, [100], [8000], True),
+        ((32, 8), 16, [1, 40, 1, 1], [5000, 3000, 12000, 65], True), ((4, 1), 32, [200], [30000], False)]
+
+
+@pytest.mark.parametrize("case", LONG)
+def test_long_caches(case):
+    checked(51, *case)
+
+
+@pytest.mark.parametrize("case", LONG)
+def test_every_key_of_a_long_cache_counts_once(case):
+    heads, page, q_len, kv_len, causal = case
+
+    def patch(c):
+        for b, kv in enumerate(kv_len):
+            slots = c.indices[c.indptr[b]:c.indptr[b + 1]]
+            v = coded_values(len(slots) * page).numpy().reshape(len(slots), 1, page, D)
+            c.v[0, slots] = page_bytes(v)
+
+    def edit(x):
+        x["k"][:] = 0
+    c = Case(52, heads, page, q_len, kv_len, causal, edit=edit, patch=patch)
+    ctx = sa.Context(0)
+    o, lse = c.run(ctx)
+    sa.sa_sync_check(ctx)
+    t = 0
+    for n, kv in zip(q_len, kv_len):
+        off = coded_worst(o[t:t + n], lse[t:t + n], kv, causal)
+        assert max(off) <= 1.0, (n, kv, off)
+        t += n
