@@ -813,6 +813,7 @@ def sa_kvq_attn(ctx, layout: Layout, layer: int, q, kq_pool, vq_pool, q_len, kv_
     _check(load_library().sa_kvq_attn(
         _ctx_handle(ctx), ctypes.byref(layout), int(layer), _on(q, "q", "bf16", rows * layout.head_dim, at, T == 0),
         _on(kq_pool, "kq_pool", "u8", n, at), _on(vq_pool, "vq_pool", "u8", n, at), B, _ptr(q_len), _ptr(kv_len),
-        _table_on(pages_indptr, pages_indices, B, at, "page table", max(kv_len.tolist(), default=0) <= 0),
+        _table_on(pages_indptr, pages_indices, B, at, "page table",
+                  pages_indices is None and not ((q_len > 0) & (kv_len > 0)).any()),
         int(bool(causal)), float(softmax_scale), _on(o, "o", "bf16", rows * layout.head_dim, at, T == 0),
         None if lse is None else _on(lse, "lse", "f32", rows, at), _stream_of(ctx, stream)))

@@ -263,3 +263,17 @@ def test_every_key_of_a_long_cache_counts_once(case):
         off = coded_worst(o[t:t + n], lse[t:t + n], kv, causal)
         assert max(off) <= 1.0, (n, kv, off)
         t += n
+
+
+def test_a_page_list_is_needed_only_where_queries_have_keys():
+    L, ctx = lay((4, 2), 16, 4), sa.Context(0)
+    pool = torch.zeros(sa.kvq_pool_shape(L), dtype=torch.uint8, device="cuda")
+    q = torch.ones((2, 4, D), dtype=torch.bfloat16, device="cuda")
+    o, lse = torch.full_like(q, 7.0), torch.full((2, 4), 7.0, device="cuda")
+    sa.sa_kvq_attn(ctx, L, 0, q, pool, pool, [0, 2, 0], [50, 0, 3], dev([0, 0, 0, 0]), None, 1.0, o, lse, causal=False)
+    sa.sa_sync_check(ctx)
+    assert (o == 0).all() and (lse == -np.inf).all()
+    sa.sa_kvq_attn(ctx, L, 0, None, pool, pool, [0], [50], dev([0, 0]), None, 1.0, None)
+    with pytest.raises(ValueError):
+        sa.sa_kvq_attn(ctx, L, 0, q, pool, pool, [0, 2], [50, 3], dev([0, 0, 0]), None, 1.0, o, lse)
+    sa.sa_sync_check(ctx)
