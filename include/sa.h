@@ -170,8 +170,8 @@ sa_status sa_attn_plan_stats(const sa_layout *layout, int32_t batch, const int32
 /* Wait for `stream`, then report SA_ERR_RANGE if any kernel of this context
  * met an out-of-range page id or slot, or a slot's count that does not fit the
  * tables, since the last check (and clear it; the message says which and ends
- * with the flags: 1 an attention, 2 an append, 4 a splice, fork, count or
- * compaction, 8 a count), or
+ * with the flags: 1 an attention, 2 an append, 4 a splice, fork, count,
+ * compaction or conversion, 8 a count), or
  * SA_ERR_OVERLAP if launches split by key range overlapped against the rules
  * above and left the context's arrival counters off (and clear them; only then,
  * or while a launch of the context still runs on another stream, it also waits

@@ -34,7 +34,7 @@
 // Bound by HBM for one token a sequence: 64 contexts of 4K to 32K keys, 32/8 heads, 1.39 GB
 // in 259 us, 5.4 TB/s; 96 equal ones of 16K 5.7.  From some 64 rows on by the matrix cores
 // and the softmax beside them: 2048 rows x 4 heads behind 8K keys, 309 GFLOP in 254 to 258 us (1.21
-// PFLOP/s, matrix cores busy 49% of the time), which the bf16 cache's attention takes 262 to 268 for.
+// PFLOP/s, matrix cores busy 47% of the time), which the bf16 cache's attention takes 262 to 268 for.
 #pragma once
 
 #include "attn_pipe.h"
@@ -842,8 +842,8 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
   };
   // P of a tile's scores, from the offsets as they are.  Only where a lane's weights come to more than
   // kKvqMost, or its row has met no key, m, l and O are moved to the maxima and P is taken again: 34
-  // vector instructions less in a step, which pays for c behind the product (246 us for 2048 rows x 4
-  // heads behind 8K keys; 266 with maxima, 250 with c in the query).  ahead: the scores of the next
+  // vector instructions less in a step, which pays for c behind the product (measured together: 246 us for
+  // 2048 rows x 4 heads behind 8K keys, 266 with maxima, 250 with c in the query).  ahead: the scores of the next
   // tile, which the compiler else moves behind the branch, away from the exponentials.
   auto weigh = [&](const f32x4 (&x)[kNB][4], bf16x8 (&p)[kNB][2], const f32x4 (*ahead)[4]) __attribute__((always_inline)) {
     float sum[kNB];

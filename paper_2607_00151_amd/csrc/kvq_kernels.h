@@ -7,9 +7,9 @@
 // magnitude,
 //   s = exponent of amax rounded half up to one bit behind the point, less 2,
 // so that 3.5 <= amax / 2^(s - 127) < 7 (the last binade's upper end rounds to 6),
-// and elements are rounded to the nearest, ties to the even code.  Rounding amax
-// first rather than taking its exponent keeps amax's own error at 1/7 where 6 would
-// cut off up to a quarter.  Powers of two make every step exact: x / 2^(s - 127) has
+// and elements are rounded to the nearest, ties to the even code.  amax itself is then
+// off by 1/5 at most (5 goes to 4; cutting off at 6 takes up to 1/7); by its exponent alone,
+// without rounding, 6 would cut off up to a quarter.  Powers of two make every step exact: x / 2^(s - 127) has
 // x's bits, so the codes do not depend on who computes them.  s is held to 1 .. 252:
 // below, elements are under 2^-127 anyway; above, 4 times the scale is no bf16 number.
 // A block that holds an infinity or a NaN is 255 with codes of 0: NaN throughout.
@@ -105,9 +105,10 @@ struct KvqConvArgs {
 // 4 (l % 4) + l / 16's: the 16 rows' 64 scale bytes go out in one store.
 //
 // Bound by HBM: 512 pages x 32 layers (1.07 GB of bf16, 0.29 of 4 bits) to 4 bits and back
-// take 468 us, 5.8 TB/s, with the bf16 rows read and written past the caches' use of them
-// and two groups of rows in flight; 506 us with ordinary loads and stores, one group at a
-// time.  One or four groups, and codes transposed to 16 bytes a lane, are within 1.5% of it.
+// take 468 us, 5.8 TB/s (487 where every pass has other pages; 559 seen on another card),
+// with the bf16 rows read and written past the caches' use of them and two groups of rows in
+// flight; 506 us, where it is 468, with ordinary loads and stores, one group at a time.  One
+// or four groups, and codes transposed to 16 bytes a lane, are within 1.5% of it.
 template <bool kPack>
 __global__ __launch_bounds__(256) void kvq_convert_kernel(KvqConvArgs a) {
   const int lane = threadIdx.x & 63, c = lane & 15, sub = lane >> 4;

@@ -277,3 +277,7 @@ def test_a_page_list_is_needed_only_where_queries_have_keys():
     with pytest.raises(ValueError):
         sa.sa_kvq_attn(ctx, L, 0, q, pool, pool, [0, 2], [50, 3], dev([0, 0, 0]), None, 1.0, o, lse)
     sa.sa_sync_check(ctx)
+
+
+def test_rows_without_keys_beside_rows_with_some():
+    checked(81, (32, 8), 16, [40, 1, 100, 6, 20], [0, 0, 500, 0, 77], False)
