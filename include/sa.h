@@ -795,15 +795,15 @@ sa_status sa_kvq_unpack(sa_ctx *ctx, const sa_layout *layout, int64_t num_slots4
  * O = softmax(softmax_scale * q . K^T) V with the values the cache stands for.
  * Scores are the products of the cached keys with the bf16 query rows, summed in fp32
  * and then scaled.  In work items of more than 32 packed rows (num_q_heads / num_kv_heads
- * to a token) up to an eighth of the query values in a block of 32 dims are taken to within
- * 2^-14 of the block's largest (or 2^-129), if they are below 2^-6 of that; where it would be
- * more, the item's products are exact, as in smaller items.  Probabilities are rounded to
- * bf16 before the PV product, the rest is fp32.  A row that sees a key
- * with a NaN block has a NaN output and a NaN LSE; a NaN block of a value it sees makes those
- * 32 dims of its output NaN, and an infinite element (see sa_kvq_unpack) makes its dim infinite
- * or NaN; an infinite element of a key may make its row NaN.  What a row
- * does not see does not reach it.  Sums of values below 2^110 do not overflow, over however
- * many keys; of larger ones they may.  A page that is missing or outside the pool reads
+ * to a token) query values below 2^-6 of the largest of their 32 dims may be off by 2^-14 of
+ * that, if in no block of 32 dims of the item's rows this adds up to more than 2^-14 of the
+ * magnitudes of all its dims but the largest; else, and in smaller items, products are exact.
+ * Probabilities are rounded to bf16 before the PV product, the rest is fp32.  A row that
+ * sees a key with a NaN block has a NaN output and a NaN LSE; a NaN block of a value it sees
+ * makes those 32 dims of its output NaN, and an infinite element (see sa_kvq_unpack) makes its
+ * dim infinite or NaN; an infinite element of a key may make its row NaN.  What a row does
+ * not see does not reach it.  Sums of values below 2^110 do not overflow, over however many
+ * keys; of larger ones they may.  A page that is missing or outside the pool reads
  * as zeros and is latched for sa_sync_check.  `lse` may be NULL; pages.indices may
  * be NULL where no sequence with queries has keys.  Parts of a launch split by key
  * range (516 bytes of the split-KV partials per query row, head and part) are joined

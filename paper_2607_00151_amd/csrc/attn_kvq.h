@@ -17,9 +17,10 @@
 // and the conversion goes; two 8-bit pieces would cost 4/4 and lose 2^-14 in the instruction's
 // sum (measured).  In rows whose dims are of one size next to none are inexact (of normal
 // ones 0.2 of 32), but beside an outlier all can be, and what keys of zeros at the outlier
-// leave of a score is then off by as much as it is.  An item with a row where more than an
-// eighth of 32 dims are inexact takes bf16 products (one normal item of 128 rows in 1000): 2048
-// rows x 4 heads behind 8K keys, 254 to 258 us, take 307 with an outlier in every row.
+// leave of a score is then off by as much as it is.  An item with a row of which pieces would
+// lose more than kvq_coarse allows takes bf16 products (no item of 128 normal rows in some
+// 60 thousand, one in 2000 of rows with two-sided exponential values, of most with a dim 8 times
+// the others): 2048 rows x 4 heads behind 8K keys, 254 to 258 us, take 307 so.
 // Values have a scale per key and 32 dims, which a sum over keys cannot take in that
 // instruction: they are converted to bf16 (exactly; 2 per v_cvt), laid out in LDS and
 // read back transposed for the 16x16x32 bf16 product.  Probabilities are rounded to
@@ -123,10 +124,9 @@ __device__ __forceinline__ void kvq_split_q(const uint16_t* p, u32x6 (&piece)[3]
   scales = fine ? s | (s - kDown[1]) << 8 | (s - kDown[2]) << 16 : 0xFFFFFF;
 }
 
-// Whether pieces do for 32 dims of a row: of a scale S, they do not hold those dims that are no multiple
-// of S / 2^13.  Every eighth of the dims that are not zero may be one.  Of blocks of normal
-// values one in half a million has more than 4, one in 20 thousand more than 3; an item of 128
-// rows has 512 blocks.
+// Whether pieces would not do for 32 dims of a row.  Of a scale S they do not hold those dims that are
+// no multiple of S / 2^13, and each of these is off by that at most; together it may be 2^-14
+// of the magnitudes of all dims but the largest.
 __device__ __forceinline__ bool kvq_coarse(const uint16_t* p) {
   u32x4 w[4];
   uint32_t top = 0;
@@ -137,18 +137,19 @@ __device__ __forceinline__ bool kvq_coarse(const uint16_t* p) {
     for (int e = 0; e < 4; ++e) top = max(top, max(w[i][e] & 0x7FFF0000u, (w[i][e] << 16) & 0x7FFF0000u));
   }
   const int n = 127 + 13 - max((int)((top + 0x100000u) >> 23) - 2, 11);   // x 2^13 / S is x 2^n
-  int zeros = 0, rests = 0;
+  int rests = 0;
+  float sum = -__builtin_ldexpf(__uint_as_float(top), n);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const uint32_t two = w[i >> 2][i & 3];
-    const float x[2] = {__uint_as_float(two << 16), __uint_as_float(two & 0xFFFF0000u)};
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      zeros += x[e] == 0.f;
-      rests += __builtin_amdgcn_fractf(__builtin_ldexpf(x[e], n)) != 0.f;
+      const float x = __builtin_ldexpf(__uint_as_float(e == 0 ? two << 16 & 0x7FFFFFFFu : two & 0x7FFF0000u), n);
+      rests += __builtin_amdgcn_fractf(x) != 0.f;
+      sum += x;
     }
   }
-  return top < 0x7F800000u && 8 * rests > 32 - zeros;
+  return top < 0x7F800000u && (float)(rests << 14) > sum;
 }
 
 // 16 keys (codes and scale byte kScale of `scales`) times 16 query rows in pieces, the

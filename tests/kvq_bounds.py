@@ -8,7 +8,7 @@ D = 128
 DEVICE = "cuda" if torch.cuda.is_available() else "cpu"
 
 
-def attention(q, k, v, scale, causal):
+def attention(q, k, v, scale, causal, inexact=False):
     """One sequence: q [n][Hq][128]; k, v [Hkv][kv][128].  Returns o, lse, the most each element of them may be off, and
     the most each row of o may be off as a vector.
 
@@ -17,7 +17,10 @@ def attention(q, k, v, scale, causal):
     a sixteenth of the keys at most one by one (four waves and, within 64 keys, four lanes share them, or the waves
     share the rows and a lane adds its 16 of a tile to each other first), 2^-24 each, and the joins of waves and parts some 64 times more.  Weights are
     rounded to bf16 and so is the output: 2^-8 of each at most.  As a vector the weights' roundings add up as
-    independent ones, at most sqrt(sum (2^-8 w |v|)^2); twice that is allowed."""
+    independent ones, at most sqrt(sum (2^-8 w |v|)^2); twice that is allowed.
+
+    inexact: what items of more than 32 rows may lose of small query dims, which of a block of 32 adds up to 2^-14 of the
+    magnitudes of all but its largest, times the block's largest key."""
     n, Hq, kv = q.shape[0], q.shape[1], k.shape[1]
     G = Hq // k.shape[0]
     o, lse = torch.zeros((n, Hq, D), dtype=torch.float64), torch.full((n, Hq), -math.inf, dtype=torch.float64)
@@ -37,6 +40,9 @@ def attention(q, k, v, scale, causal):
         norm = torch.linalg.vector_norm(out, dim=1, keepdim=True)
         spread = torch.sqrt((w * w) @ (vv * vv).sum(1, keepdim=True))
         e = scale * 2.0 ** -16 * (q[:, h].abs() @ kk.abs().t()) + 2.0 ** -22 * (s.abs() + 1)
+        if inexact:
+            b = q[:, h].abs().reshape(n, 4, 32)
+            e = e + scale * 2.0 ** -14 * ((b.sum(2) - b.amax(2)) @ kk.abs().reshape(kv, 4, 32).amax(2).t())
         e = torch.where(seen, e, 0).amax(1, keepdim=True) + (kv / 16 + 64) * 2.0 ** -24
         logs = (top + torch.log(total))[:, 0]
         o[:, h], lse[:, h] = out.cpu(), logs.cpu()

@@ -49,12 +49,12 @@ class Case:
                        causal=self.causal, stream=stream)
         return o, lse
 
-    def check(self, o, lse, only=None):
+    def check(self, o, lse, only=None, inexact=False):
         t = 0
         for b, (n, kv) in enumerate(zip(self.q_len, self.kv_len)):
             if n and (only is None or b in only):
                 k, v = (rows_of(p[0], self.indptr, self.indices, b, kv, self.page) for p in (self.k, self.v))
-                off = worst(o[t:t + n], lse[t:t + n], attention(self.q[t:t + n], k, v, self.scale, self.causal))
+                off = worst(o[t:t + n], lse[t:t + n], attention(self.q[t:t + n], k, v, self.scale, self.causal, inexact))
                 assert max(off) <= 1.0, (b, off)
             t += n
 
@@ -99,6 +99,26 @@ def test_a_few_small_dims_beside_an_outlier_and_zeros(size):
         x[..., 3:8], x[..., 9:32] = 0, 0
         x[..., 8] *= 5000
     checked(7, heads, page, q_len, kv_len, causal, edit=edit, q=q)
+
+
+@pytest.mark.parametrize("spread", ["2", "4", "8", "32", "exponential", "lognormal"])
+@pytest.mark.parametrize("heads,page,q,kv", [((32, 8), 16, [40], [60]), ((1, 1), 32, [100, 34], [100, 2000]), ((8, 1), 16, [5] * 9, [5] * 9)])
+def test_what_rows_of_spread_queries_may_lose(heads, page, q, kv, spread):
+    """Rows on both sides of what pieces hold well enough, over few keys and with large scores."""
+    def change(x):
+        r = np.random.default_rng(17)
+        if spread == "lognormal":
+            f = np.exp(1.5 * r.standard_normal(x.shape))
+        elif spread == "exponential":
+            f = np.sqrt(r.exponential(size=x.shape))
+        else:
+            f = np.where(np.arange(D) % 32 == 9, float(spread), 1.0)
+        x.copy_((x.double() * torch.from_numpy(np.broadcast_to(f, x.shape).copy())).to(torch.bfloat16))
+    c = Case(11, heads, page, q, kv, True, scale=0.3, q=change, edit=lambda x: x["k"].__setitem__((..., np.arange(D) % 32 == 9), 0))
+    ctx = sa.Context(0)
+    o, lse = c.run(ctx)
+    sa.sa_sync_check(ctx)
+    c.check(o, lse, inexact=True)
 
 
 def test_one_row_with_an_outlier_among_ordinary_ones():
