@@ -18,9 +18,9 @@
 // sum (measured).  In rows whose dims are of one size next to none are inexact (of normal
 // ones 0.2 of 32), but beside an outlier all can be, and what keys of zeros at the outlier
 // leave of a score is then off by as much as it is.  An item with a row of which pieces would
-// lose more than kvq_coarse allows takes bf16 products (no item of 128 normal rows in some
-// 60 thousand, one in 2000 of rows with two-sided exponential values, of most with a dim 8 times
-// the others): 2048 rows x 4 heads behind 8K keys, 254 to 258 us, take 307 so.
+// lose more than kvq_coarse allows takes bf16 products (none of 16 thousand items of 128 normal
+// rows, one in 2000 of rows with two-sided exponential values, most where a dim is 8 times the
+// others): 2048 rows x 4 heads behind 8K keys, 254 to 258 us, take 305 so.
 // Values have a scale per key and 32 dims, which a sum over keys cannot take in that
 // instruction: they are converted to bf16 (exactly; 2 per v_cvt), laid out in LDS and
 // read back transposed for the 16x16x32 bf16 product.  Probabilities are rounded to
