@@ -797,7 +797,8 @@ sa_status sa_kvq_unpack(sa_ctx *ctx, const sa_layout *layout, int64_t num_slots4
  * and then scaled.  In work items of more than 32 packed rows (num_q_heads / num_kv_heads
  * to a token) query values below 2^-6 of the largest of their 32 dims may be off by 2^-14 of
  * that, if in no block of 32 dims of the item's rows this adds up to more than 2^-14 of the
- * magnitudes of all its dims but the largest; else, and in smaller items, products are exact.
+ * magnitudes of all its dims but the largest; else, in smaller items, and where a part of a
+ * launch is of 512 keys or fewer, products are exact.
  * Probabilities are rounded to bf16 before the PV product, the rest is fp32.  A row that
  * sees a key with a NaN block has a NaN output and a NaN LSE; a NaN block of a value it sees
  * makes those 32 dims of its output NaN, and an infinite element (see sa_kvq_unpack) makes its

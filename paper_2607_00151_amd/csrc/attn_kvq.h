@@ -1063,11 +1063,15 @@ __device__ __forceinline__ void kvq_split_rows(const KvqAttnArgs& a, const KvqIt
   }
 }
 
+// Items of so few keys take bf16 products unasked: the vote's trip to memory is some 2 us.  Over
+// 30 drawn batches with row tiles, against pieces without a vote: every item asked 1.12 times
+// the time (1.27 at the worst), those of more than 256 keys 1.045, 512 1.035, 1024 1.041, 2048 1.05.
+constexpr int kKvqShort = 512;
 // Asked beforehand: a vote inside the loop's function, or both forms under one loop, cost the
 // pieces' loop registers (64 and 85 spilled; 257 us for 2048 rows x 4 heads so, 415 else).
 template <int P, int kNB>
 __device__ __forceinline__ void kvq_rows(const KvqAttnArgs& a, const KvqItem& it, lds_u8* lds, KvqStats* stats) {
-  if (kvq_any_coarse<kNB>(a, it, (__attribute__((address_space(3))) int*)stats))
+  if (it.kv_end - it.kv_begin <= kKvqShort || kvq_any_coarse<kNB>(a, it, (__attribute__((address_space(3))) int*)stats))
     kvq_split_rows<P, kNB, true>(a, it, (__attribute__((address_space(3))) KvqRowsLds<true>*)lds);
   else
     kvq_split_rows<P, kNB, false>(a, it, (__attribute__((address_space(3))) KvqRowsLds<false>*)lds);
